@@ -53,7 +53,7 @@ typedef enum {
     PPS_ERR_SIZE = 5         /* problem larger than the fixed scratch of pps_draft_list_noalloc        */
 } pps_status;
 
-typedef enum { PPS_F32 = 0, PPS_BF16 = 1 } pps_dtype;
+typedef enum { PPS_F32 = 0, PPS_BF16 = 1, PPS_F16 = 2 } pps_dtype; /* PPS_F16: the target-side calls only */
 
 typedef enum {
     PPS_DRAFT_DISTINCT = 0, /* the K smallest first-arrival keys (K distinct tokens)                 */
@@ -71,7 +71,8 @@ typedef struct {
 #define PPS_FLAG_GUARD 1u       /* fp32 streaming filter could not prove a row's candidate set complete */
 #define PPS_FLAG_LOGIT_RANGE 2u /* |logit / T| too large for the fp32 filter's error bound (> 2^16)      */
 #define PPS_FLAG_TREE 4u        /* a sequence's root row (seq_off[s]) lies outside the node rows: nothing emitted */
-#define PPS_FLAG_TIMEOUT 8u     /* an LM-head kernel gave up waiting on its pipeline and returned early         */
+#define PPS_FLAG_TIMEOUT 8u     /* an LM-head or attention kernel gave up waiting on its pipeline and returned early */
+#define PPS_FLAG_INDEX 16u      /* a position, slot, page, length, row or token lies outside its array (target-side calls) */
 
 #define PPS_MAX_K 32
 
@@ -440,6 +441,148 @@ pps_status pps_lmhead_verify_tree(const void* hidden, int64_t ld_hidden, const v
                                   int32_t* out_accept_len, int32_t* out_n_emitted, int32_t* out_emitted,
                                   float* out_score, double* out_score_sum, uint32_t* status, void* ws,
                                   size_t ws_bytes, pps_stream_t stream);
+
+/*
+ * Target side of a step -- what runs between a draft tree and its
+ * verification inside the target model, and the paper's token-level baseline.
+ *
+ * pps_kv_cache: a paged cache of one layer.  Slot s of the cache is token
+ * s % page_size of page s / page_size; element (page, token, head, channel) of
+ * the keys lies at k + page * page_stride + token * tok_stride + head *
+ * head_stride + channel (elements; the values with the same strides at v), so
+ * pages may be laid out token by token or head by head.
+ */
+typedef struct {
+    void* k;
+    void* v;
+    int64_t n_pages;
+    int32_t page_size;  /* tokens per page */
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int64_t page_stride, tok_stride, head_stride;
+} pps_kv_cache;
+
+/* a strided [n_tok, heads, head_dim] tensor, channels contiguous (strides in elements) */
+typedef struct {
+    void* data;
+    int64_t tok_stride, head_stride;
+} pps_heads;
+
+/*
+ * pps_kv_append -- queries and keys of n_tok new tokens are normed per head
+ * (optional) and rotated to the tokens' positions; keys and values are written
+ * to their cache slots.  One pass over the projections' outputs.
+ *
+ *   y = x / sqrt(mean_c x_c^2 + eps) * weight       (where a weight is given)
+ *   rotation of channel pair (a, b) of the first rot channels, angle t:
+ *   (a cos t - b sin t, a sin t + b cos t)
+ *   pair i = channels (i, i + rot/2), or (2i, 2i+1) when `interleaved`
+ * computed in fp32 and rounded once; values are copied.
+ *
+ * dtype        PPS_BF16 or PPS_F16, of q, k, v, the weights, the cache and out_q
+ * q, k, v      [n_tok, n_heads | n_kv_heads | n_kv_heads, head_dim] (e.g. three
+ *              views of one projection's output)
+ * cache        head_dim and n_kv_heads apply to k and v; head_dim a multiple of 8
+ *              up to 256
+ * q_norm, k_norm  nullable [head_dim] norm weights
+ * rope         [max_pos, rot] fp32: cos t of the rot/2 pairs, then sin t; rot
+ *              even, 0 <= rot <= head_dim (0: no rotation, rope nullable)
+ * pos          [n_tok] positions (row of rope), clamped into [0, max_pos)
+ * slot         [n_tok] cache slots; a negative one is not written, one beyond
+ *              the cache neither.  Slots are distinct, or the last write is any.
+ * out_q        [n_tok, n_heads, head_dim] normed and rotated queries; may be q itself
+ * Out-of-range positions and slots raise PPS_FLAG_INDEX.
+ * Any alignment is accepted; 16-byte aligned bases and strides (and rot a
+ * multiple of 16) are moved in 16-byte units.
+ */
+pps_status pps_kv_append(pps_heads q, pps_heads k, pps_heads v, pps_dtype dtype, int64_t n_tok, int32_t n_heads,
+                         pps_kv_cache cache, const void* q_norm, const void* k_norm, float eps, const float* rope,
+                         int64_t max_pos, int32_t rot, int32_t interleaved, const int32_t* pos, const int64_t* slot,
+                         pps_heads out_q, uint32_t* status, pps_stream_t stream);
+
+/*
+ * pps_paged_attention -- attention of the newest tokens of n_seq sequences
+ * over a paged cache that already holds their keys and values: one token each
+ * (decoding), the nodes of a draft tree (the batched target evaluation of
+ * App. B, its contexts sharing their prefix), or a chunk of a prompt.
+ *
+ *   out[t, h] = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale * q[t, h] . k_j)
+ * over the keys j of t's sequence that t sees; head h reads key head
+ * h / (n_heads / n_kv_heads).  Sequence s has tokens q_off[s] .. q_off[s+1]-1
+ * (n of them) and kv_len[s] keys, its tokens' own being the last n: token i of
+ * the sequence sees key j
+ *   causal (mask NULL)  iff j <= kv_len - n + i
+ *   tree                iff j < kv_len - n, or bit b = j - (kv_len - n) of the
+ *                       token's mask is set (word b / 32, bit b % 32; its own
+ *                       bit included)
+ * A token that sees nothing gets zeros.  Keys and values at slots past kv_len
+ * may hold anything.  Products on the tensor cores with fp32 accumulation, the
+ * softmax in fp32, its weights rounded to dtype for the second product.
+ *
+ * dtype        PPS_BF16 or PPS_F16, of q, the cache and out
+ * cache        head_dim a multiple of 8 up to 128, page_size a power of two >= 8;
+ *              bases 16-byte aligned, strides multiples of 8 elements
+ * pages        [n_seq, pages_stride] page of keys p * page_size .. of each
+ *              sequence, max_pages <= pages_stride valid columns.  A page outside
+ *              the cache reads as zeros (PPS_FLAG_INDEX), entries past
+ *              ceil(kv_len / page_size) are not read.
+ * kv_len       [n_seq], 0 .. max_pages * page_size (cut to that, PPS_FLAG_INDEX)
+ * q_off        [n_seq + 1] non-decreasing, within [0, n_tok] (a sequence for
+ *              which it is not is left out, PPS_FLAG_INDEX)
+ * mask         nullable [n_tok, mask_words] tree masks; a token has bits for up
+ *              to 32 * mask_words tokens of its sequence
+ * scale        finite (1 / sqrt(head_dim) as a rule)
+ * out          [n_tok, n_heads, head_dim]
+ * out_lse      nullable [n_tok, n_heads] ln sum_j w_j (-inf where nothing is seen)
+ * ws, ws_bytes pps_attention_workspace_size(n_tok, n_heads, n_kv_heads, head_dim)
+ *              bytes; need not be cleared
+ */
+size_t pps_attention_workspace_size(int64_t n_tok, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+pps_status pps_paged_attention(pps_heads q, pps_dtype dtype, int64_t n_tok, int32_t n_heads, pps_kv_cache cache,
+                               const int32_t* pages, int64_t pages_stride, int32_t max_pages, const int32_t* kv_len,
+                               const int32_t* q_off, int32_t n_seq, const uint32_t* mask, int32_t mask_words,
+                               float scale, pps_heads out, float* out_lse, uint32_t* status, void* ws, size_t ws_bytes,
+                               pps_stream_t stream);
+
+/*
+ * pps_verify_chain -- the token-level maximal coupling (Alg. 1) along drafted
+ * chains, from given random numbers: the unkeyed baseline beside
+ * pps_verify_tree.  With P_c = softmax(p_logits / T) at node c and Q_c =
+ * softmax(q_logits / T) at its draft row, the drafted token x_c is accepted iff
+ * u_c Q_c(x_c) < P_c(x_c); at the first rejection the emitted token is
+ *   argmax_i max(P_c(i) - Q_c(i), 0) / E(i),
+ * a sample of the normalised residual when E(i) are independent Exp(1); past the
+ * chain's end argmax_i P_c(i) / E(i).  Ties go to the smaller token.
+ *
+ * p_logits     [n_nodes, p_stride], q_logits [n_draft, q_stride], both dtype
+ *              (PPS_BF16 or PPS_F32).  NaN counts as -inf; +inf logits share the
+ *              whole mass of their row.
+ * gamma        longest chain, 0 <= gamma <= 64 (a longer one is cut there)
+ * seq_off      [n_seq + 1] sequence s owns nodes seq_off[s] .. seq_off[s+1]-1 in
+ *              chain order (as pps_verify_tree; at least its root)
+ * node_draft_row [n_nodes] draft row of a node's drafted token, -1 at the end of
+ *              the chain; the last node of a sequence never has one
+ * draft_tok, u [n_draft] drafted tokens and their uniforms in [0, 1)
+ * noise        [n_seq, noise_stride] fp32 exponentials E > 0
+ * out_accept_len, out_n_emitted [n_seq], out_emitted [n_seq, gamma + 1] as
+ *              pps_verify_tree (n_emitted = accept_len + 1, -1 past the end, -1
+ *              for a row without a usable logit); a residual that is zero
+ *              everywhere in fp32 is replaced by P
+ * out_accept_prob nullable [n_draft] min(1, P(x) / Q(x)) of every draft row that
+ *              a chain's node names (0 / 0 counts as 0)
+ * A draft row or token out of range is treated as the chain's end or as
+ * rejected, a sequence whose nodes lie outside the rows gets accept_len 0 and
+ * no token; both raise PPS_FLAG_INDEX.
+ * ws, ws_bytes pps_chain_workspace_size(n_nodes, n_draft, n_seq) bytes; need not
+ *              be cleared
+ */
+size_t pps_chain_workspace_size(int64_t n_nodes, int64_t n_draft, int32_t n_seq);
+pps_status pps_verify_chain(const void* p_logits, const void* q_logits, pps_dtype dtype, int64_t n_nodes,
+                            int64_t n_draft, int64_t vocab, int64_t p_stride, int64_t q_stride, float temperature,
+                            int32_t n_seq, int32_t gamma, const int32_t* seq_off, const int32_t* node_draft_row,
+                            const int32_t* draft_tok, const float* u, const float* noise, int64_t noise_stride,
+                            int32_t* out_accept_len, int32_t* out_n_emitted, int32_t* out_emitted,
+                            float* out_accept_prob, uint32_t* status, void* ws, size_t ws_bytes, pps_stream_t stream);
 
 /*
  * pps_draft_list_noalloc -- pps_draft_list for callers that must not

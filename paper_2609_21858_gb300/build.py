@@ -14,6 +14,8 @@ CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "_lib")
 LIB = os.path.join(OUT, "libpps.so")
 SOURCES = ["pps_race.cu", "pps_misc.cu", "pps_api.cu"]
+# sources without the keyed source: compiled once, linked into every variant
+COMMON = ["pps_append.cu", "pps_attention.cu", "pps_chain.cu"]
 HEADERS = ["pps_device.cuh", "pps_internal.h", "pps_trunc.cuh", "pps_lmhead.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
@@ -50,21 +52,21 @@ def build(force: bool = False, verbose: bool = False) -> str:
     def compile_one(job):
         variant, src = job
         s = os.path.join(CSRC, src)
-        d = os.path.join(OUT, "obj" + variant)
+        d = os.path.join(OUT, "obj" + ("_common" if variant is None else variant))
         os.makedirs(d, exist_ok=True)
         o = os.path.join(d, src.replace(".cu", ".o"))
         if force or _stale(o, [s] + hdrs):
-            cmd = [nvcc()] + flags + VARIANTS[variant] + ["-c", s, "-o", o]
+            cmd = [nvcc()] + flags + VARIANTS.get(variant, []) + ["-c", s, "-o", o]
             if verbose:
                 print(" ".join(cmd), flush=True)
             subprocess.run(cmd, check=True)
         return o
 
-    jobs = [(v, src) for v in VARIANTS for src in SOURCES]
+    jobs = [(v, src) for v in VARIANTS for src in SOURCES] + [(None, src) for src in COMMON]
     with ThreadPoolExecutor(max_workers=len(jobs)) as ex:
         objs = list(ex.map(compile_one, jobs))
     for i, v in enumerate(VARIANTS):
-        vobjs = objs[i * len(SOURCES):(i + 1) * len(SOURCES)]
+        vobjs = objs[i * len(SOURCES):(i + 1) * len(SOURCES)] + objs[len(VARIANTS) * len(SOURCES):]
         target = lib_path(v)
         if force or _stale(target, vobjs):
             tmp = target + f".tmp{os.getpid()}"

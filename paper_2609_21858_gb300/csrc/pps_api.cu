@@ -607,6 +607,181 @@ pps_status pps_hetero_block(const int32_t* tokens, pps_row_ids ids, int64_t n, i
     return e == cudaSuccess ? PPS_OK : PPS_ERR_CUDA;
 }
 
+// ---------------------------------------------------------------- target side
+
+static HeadsView heads_view(const pps_heads& h) { return {h.data, h.tok_stride, h.head_stride}; }
+
+// strides hold non-negative offsets that do not pass 63 bits for any index of the array
+static bool strides_ok(int64_t a, int64_t na, int64_t b, int64_t nb, int64_t c = 0, int64_t nc = 1) {
+    const int64_t most = INT64_MAX / 8;
+    if (a < 0 || b < 0 || c < 0) return false;
+    return (na <= 1 || a <= most / na) && (nb <= 1 || b <= most / nb) && (nc <= 1 || c <= most / nc);
+}
+
+static pps_status check_cache(const pps_kv_cache& c) {
+    if (c.n_pages < 0 || c.n_pages > INT32_MAX || c.page_size < 1 || c.n_kv_heads < 1 || c.head_dim < 8)
+        return PPS_ERR_INVALID_ARG;
+    if (c.n_pages > 0 && (!c.k || !c.v)) return PPS_ERR_INVALID_ARG;
+    if (!strides_ok(c.page_stride, c.n_pages, c.tok_stride, c.page_size, c.head_stride, c.n_kv_heads))
+        return PPS_ERR_INVALID_ARG;
+    return PPS_OK;
+}
+
+static CacheView cache_view(const pps_kv_cache& c) {
+    return {c.k, c.v, c.n_pages, c.page_size, c.n_kv_heads, c.head_dim, c.page_stride, c.tok_stride, c.head_stride};
+}
+
+pps_status pps_kv_append(pps_heads q, pps_heads k, pps_heads v, pps_dtype dtype, int64_t n_tok, int32_t n_heads,
+                         pps_kv_cache cache, const void* q_norm, const void* k_norm, float eps, const float* rope,
+                         int64_t max_pos, int32_t rot, int32_t interleaved, const int32_t* pos, const int64_t* slot,
+                         pps_heads out_q, uint32_t* status, pps_stream_t stream) {
+    if (dtype != PPS_BF16 && dtype != PPS_F16) return PPS_ERR_UNSUPPORTED;
+    pps_status st = check_cache(cache);
+    if (st != PPS_OK) return st;
+    if (cache.head_dim % 8 != 0 || cache.head_dim > 256) return PPS_ERR_UNSUPPORTED;
+    if (n_tok < 0 || n_tok > INT32_MAX || n_heads < 1 || n_heads > 65535 || cache.n_kv_heads > 65535)
+        return PPS_ERR_INVALID_ARG;
+    if (rot < 0 || rot % 2 != 0 || rot > cache.head_dim || !(eps >= 0.0f) || !std::isfinite(eps))
+        return PPS_ERR_INVALID_ARG;
+    if (rot > 0 && (!rope || max_pos < 1)) return PPS_ERR_INVALID_ARG;
+    if (!strides_ok(q.tok_stride, n_tok, q.head_stride, n_heads) ||
+        !strides_ok(out_q.tok_stride, n_tok, out_q.head_stride, n_heads) ||
+        !strides_ok(k.tok_stride, n_tok, k.head_stride, cache.n_kv_heads) ||
+        !strides_ok(v.tok_stride, n_tok, v.head_stride, cache.n_kv_heads))
+        return PPS_ERR_INVALID_ARG;
+    if (n_tok == 0) return PPS_OK;
+    if (!q.data || !k.data || !v.data || !out_q.data || !slot || (rot > 0 && !pos)) return PPS_ERR_INVALID_ARG;
+    AppendArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.q = heads_view(q);
+    a.k = heads_view(k);
+    a.v = heads_view(v);
+    a.out = heads_view(out_q);
+    a.c = cache_view(cache);
+    a.n_tok = n_tok;
+    a.max_pos = max_pos;
+    a.n_heads = n_heads;
+    a.rot = rot;
+    a.interleaved = interleaved != 0;
+    a.q_norm = q_norm;
+    a.k_norm = k_norm;
+    a.eps = eps;
+    a.rope = rope;
+    a.pos = pos;
+    a.slot = slot;
+    a.status = status;
+    return launch_kv_append(a, (int)dtype, (cudaStream_t)stream) == cudaSuccess ? PPS_OK : PPS_ERR_CUDA;
+}
+
+size_t pps_attention_workspace_size(int64_t n_tok, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
+    if (n_tok < 0 || n_heads < 1 || n_kv_heads < 1 || head_dim < 1) return 0;
+    return attention_workspace_bytes(n_tok, n_heads, n_kv_heads, head_dim);
+}
+
+pps_status pps_paged_attention(pps_heads q, pps_dtype dtype, int64_t n_tok, int32_t n_heads, pps_kv_cache cache,
+                               const int32_t* pages, int64_t pages_stride, int32_t max_pages, const int32_t* kv_len,
+                               const int32_t* q_off, int32_t n_seq, const uint32_t* mask, int32_t mask_words,
+                               float scale, pps_heads out, float* out_lse, uint32_t* status, void* ws, size_t ws_bytes,
+                               pps_stream_t stream) {
+    if (dtype != PPS_BF16 && dtype != PPS_F16) return PPS_ERR_UNSUPPORTED;
+    pps_status st = check_cache(cache);
+    if (st != PPS_OK) return st;
+    if (cache.head_dim % 8 != 0 || cache.head_dim > 128) return PPS_ERR_UNSUPPORTED;
+    if (cache.page_size < 8 || (cache.page_size & (cache.page_size - 1)) != 0) return PPS_ERR_UNSUPPORTED;
+    if (n_tok < 0 || n_tok > INT32_MAX || n_seq < 0 || n_heads < 1 || n_heads > 65535 ||
+        n_heads % cache.n_kv_heads != 0 || max_pages < 0 || pages_stride < max_pages)
+        return PPS_ERR_INVALID_ARG;
+    if (n_tok * n_heads > INT32_MAX || (int64_t)max_pages * cache.page_size > INT32_MAX) return PPS_ERR_INVALID_ARG;
+    if (!std::isfinite(scale) || mask_words < 0 || (mask && mask_words < 1)) return PPS_ERR_INVALID_ARG;
+    if (!strides_ok(q.tok_stride, n_tok, q.head_stride, n_heads) ||
+        !strides_ok(out.tok_stride, n_tok, out.head_stride, n_heads))
+        return PPS_ERR_INVALID_ARG;
+    // the cache is read by TMA and rows by 16-byte loads: aligned bases and strides
+    auto units = [](int64_t s, int64_t n) { return n <= 1 || s % 8 == 0; };
+    if (!aligned16(cache.k) || !aligned16(cache.v) || !units(cache.page_stride, cache.n_pages) ||
+        !units(cache.tok_stride, cache.page_size) || !units(cache.head_stride, cache.n_kv_heads))
+        return PPS_ERR_INVALID_ARG;
+    if (!aligned16(q.data) || !aligned16(out.data) || !units(q.tok_stride, n_tok) || !units(q.head_stride, n_heads) ||
+        !units(out.tok_stride, n_tok) || !units(out.head_stride, n_heads))
+        return PPS_ERR_INVALID_ARG;
+    if (n_tok == 0 || n_seq == 0) return PPS_OK;
+    if (!q.data || !out.data || !kv_len || !q_off || (max_pages > 0 && !pages)) return PPS_ERR_INVALID_ARG;
+    if (!ws || !aligned16(ws) ||
+        ws_bytes < attention_workspace_bytes(n_tok, n_heads, cache.n_kv_heads, cache.head_dim))
+        return PPS_ERR_WORKSPACE;
+    AttnArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.q = heads_view(q);
+    a.out = heads_view(out);
+    a.c = cache_view(cache);
+    a.n_tok = n_tok;
+    a.pages_stride = pages_stride;
+    a.n_heads = n_heads;
+    a.n_seq = n_seq;
+    a.max_pages = cache.n_pages > 0 ? max_pages : 0;
+    a.mask_words = mask ? mask_words : 0;
+    a.pages = pages;
+    a.kv_len = kv_len;
+    a.q_off = q_off;
+    a.mask = mask;
+    a.scale = scale;
+    a.lse = out_lse;
+    a.status = status;
+    a.ws = ws;
+    return launch_attention(a, (int)dtype, (cudaStream_t)stream) == cudaSuccess ? PPS_OK : PPS_ERR_CUDA;
+}
+
+size_t pps_chain_workspace_size(int64_t n_nodes, int64_t n_draft, int32_t n_seq) {
+    if (n_nodes < 0 || n_draft < 0 || n_seq < 0) return 0;
+    return chain_workspace_bytes(n_nodes, n_draft, n_seq);
+}
+
+pps_status pps_verify_chain(const void* p_logits, const void* q_logits, pps_dtype dtype, int64_t n_nodes,
+                            int64_t n_draft, int64_t vocab, int64_t p_stride, int64_t q_stride, float temperature,
+                            int32_t n_seq, int32_t gamma, const int32_t* seq_off, const int32_t* node_draft_row,
+                            const int32_t* draft_tok, const float* u, const float* noise, int64_t noise_stride,
+                            int32_t* out_accept_len, int32_t* out_n_emitted, int32_t* out_emitted,
+                            float* out_accept_prob, uint32_t* status, void* ws, size_t ws_bytes, pps_stream_t stream) {
+    if (dtype != PPS_F32 && dtype != PPS_BF16) return PPS_ERR_UNSUPPORTED;
+    if (n_nodes < 0 || n_nodes > INT32_MAX || n_draft < 0 || n_draft > INT32_MAX || vocab < 1 || vocab > INT32_MAX)
+        return PPS_ERR_INVALID_ARG;
+    if (p_stride < vocab || q_stride < vocab || noise_stride < vocab) return PPS_ERR_INVALID_ARG;
+    if (!strides_ok(p_stride, n_nodes, q_stride, n_draft, noise_stride, n_seq)) return PPS_ERR_INVALID_ARG;
+    if (!(temperature > 0.0f) || !std::isfinite(temperature)) return PPS_ERR_INVALID_ARG;
+    if (n_seq < 0 || gamma < 0 || gamma > 64) return PPS_ERR_INVALID_ARG;
+    if (n_seq == 0 || n_nodes == 0) return n_seq == 0 && n_nodes == 0 ? PPS_OK : PPS_ERR_INVALID_ARG;
+    if (n_nodes < n_seq) return PPS_ERR_INVALID_ARG;
+    if (!p_logits || !seq_off || !node_draft_row || !noise || !out_accept_len || !out_n_emitted || !out_emitted)
+        return PPS_ERR_INVALID_ARG;
+    if (n_draft > 0 && (!q_logits || !draft_tok || !u)) return PPS_ERR_INVALID_ARG;
+    if (!ws || !aligned16(ws) || ws_bytes < chain_workspace_bytes(n_nodes, n_draft, n_seq)) return PPS_ERR_WORKSPACE;
+    ChainArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.p = p_logits;
+    a.q = q_logits;
+    a.n_nodes = n_nodes;
+    a.n_draft = n_draft;
+    a.V = vocab;
+    a.p_stride = p_stride;
+    a.q_stride = q_stride;
+    a.noise_stride = noise_stride;
+    a.n_seq = n_seq;
+    a.gamma = gamma;
+    a.c = (float)(1.4426950408889634074 / (double)temperature);
+    a.seq_off = seq_off;
+    a.node_draft_row = node_draft_row;
+    a.draft_tok = draft_tok;
+    a.u = u;
+    a.noise = noise;
+    a.out_acc = out_accept_len;
+    a.out_ne = out_n_emitted;
+    a.out_em = out_emitted;
+    a.out_prob = out_accept_prob;
+    a.status = status;
+    a.ws = ws;
+    return launch_chain(a, (int)dtype, (cudaStream_t)stream) == cudaSuccess ? PPS_OK : PPS_ERR_CUDA;
+}
+
 pps_status pps_philox_words(pps_row_ids ids, int64_t n_rows, int64_t vocab, int32_t arrival, uint32_t* out,
                             pps_stream_t stream) {
     if (n_rows < 0 || vocab < 1 || arrival < 1) return PPS_ERR_INVALID_ARG;

@@ -1,0 +1,280 @@
+// pps_append.cu -- norming, rotation and paged-cache append of new tokens' heads.
+//
+// Per head x of a query or key (channels c < D):
+//   y = x / sqrt(mean x^2 + eps) * w                        (where a weight is given)
+//   (a, b) -> (a cos t - b sin t, a sin t + b cos t)        (the first rot channels, in pairs)
+// in fp32, rounded once; values are copied.  Each of the (n_heads + 2 n_kv_heads) D channels of a token
+// is read once and written once, so the pass is bound by HBM; norm and rotation are some ten
+// operations a channel.
+//
+// Layout.  A group of lanes holds one head: lane l has unit l, two vectors of VW channels, the two
+// halves of VW (or, interleaved, 2 x VW / 2) rotation pairs, so that no channel leaves its lane but
+// for the norm's sum (log2(group) shuffles).  A warp keeps one token and walks over its heads, several
+// at a time, four loads ahead; the cosines and sines of the lane's pairs stay in registers for all of them.
+// Few tokens are spread over more warps (wpt per token).
+#include <algorithm>
+#include <cstdint>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "pps.h"
+#include "pps_internal.h"
+
+namespace pps {
+namespace {
+
+constexpr int kAppendWarps = 4;  // per CTA
+constexpr int kAhead = 4;        // heads of a lane group in flight
+
+struct AppendPlan {
+    int lg;          // log2 of the lanes per head
+    int wpt;         // warps per token
+    int units;       // units per head
+    int pair_units;  // of which rotated
+};
+
+template <int VW>
+struct RawVec;
+template <>
+struct RawVec<8> { using type = uint4; };
+template <>
+struct RawVec<4> { using type = uint2; };
+template <>
+struct RawVec<1> { using type = uint16_t; };
+
+__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
+template <typename T>
+__device__ __forceinline__ T from_f(float x);
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <>
+__device__ __forceinline__ __half from_f<__half>(float x) { return __float2half_rn(x); }
+
+template <typename T, int VW>
+union Vec {
+    typename RawVec<VW>::type raw;
+    T e[VW];
+    __device__ Vec() {}
+};
+
+template <typename T, int VW>
+__device__ __forceinline__ void load(Vec<T, VW>& x, const T* p) {
+    x.raw = *reinterpret_cast<const typename RawVec<VW>::type*>(p);
+}
+template <typename T, int VW>
+__device__ __forceinline__ void store(T* p, const Vec<T, VW>& x) {
+    *reinterpret_cast<typename RawVec<VW>::type*>(p) = x.raw;
+}
+
+// NU: units per lane (more than one only for VW = 1)
+template <typename T, int VW, int NU>
+__global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AppendArgs a, const AppendPlan P) {
+    const int lane = threadIdx.x & 31;
+    const int64_t gw = (int64_t)blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
+    const int64_t tok = gw / P.wpt;
+    if (tok >= a.n_tok) return;  // warp-uniform
+    const int part = (int)(gw - tok * P.wpt);
+    const int D = a.c.head_dim, half = a.rot >> 1;
+    const int l = lane & ((1 << P.lg) - 1), hp = 32 >> P.lg;
+    const int n_kv = a.c.n_kv_heads, H = a.n_heads + 2 * n_kv;
+
+    int64_t slot = __ldg(a.slot + tok);
+    bool flag = false;
+    int64_t page = 0;
+    int in_page = 0;
+    if (slot >= 0) {
+        page = slot / a.c.page_size;
+        in_page = (int)(slot - page * a.c.page_size);
+        if (page >= a.c.n_pages) {
+            flag = true;
+            slot = -1;
+        }
+    }
+    const float* table = nullptr;
+    if (half > 0) {
+        int64_t p = __ldg(a.pos + tok);
+        if (p < 0 || p >= a.max_pos) {
+            flag = true;
+            p = p < 0 ? 0 : a.max_pos - 1;
+        }
+        table = a.rope + p * a.rot;
+    }
+    if (flag && part == 0 && lane == 0 && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
+
+    // the lane's units: channel starts of their two vectors, cosines and sines
+    int c0[NU], c1[NU];
+    float cs[NU][VW], sn[NU][VW];
+#pragma unroll
+    for (int n = 0; n < NU; ++n) {
+        const int u = l + (n << P.lg);
+        if (u < P.pair_units) {
+            c0[n] = a.interleaved ? 2 * u * VW : u * VW;
+            c1[n] = a.interleaved ? c0[n] + VW : half + u * VW;
+        } else {
+            c0[n] = u < P.units ? a.rot + (u - P.pair_units) * 2 * VW : D;
+            c1[n] = c0[n] + VW;
+        }
+#pragma unroll
+        for (int e = 0; e < VW; ++e) {
+            cs[n][e] = 1.0f;
+            sn[n][e] = 0.0f;
+        }
+        if (u < P.pair_units) {
+            if constexpr (VW == 1) {
+                cs[n][0] = __ldg(table + u);
+                sn[n][0] = __ldg(table + half + u);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VW; e += 4) {
+                    *reinterpret_cast<float4*>(&cs[n][e]) = __ldg(reinterpret_cast<const float4*>(table + u * VW + e));
+                    *reinterpret_cast<float4*>(&sn[n][e]) = __ldg(reinterpret_cast<const float4*>(table + half + u * VW + e));
+                }
+            }
+        }
+    }
+    const bool any_norm = a.q_norm != nullptr || a.k_norm != nullptr;
+
+    for (int h0 = part * hp + (lane >> P.lg); h0 - (lane >> P.lg) < H; h0 += kAhead * P.wpt * hp) {
+        Vec<T, VW> x[kAhead][NU][2];
+        T* dst[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int h = h0 + j * P.wpt * hp;
+            const T* src = nullptr;
+            dst[j] = nullptr;
+            if (h < a.n_heads) {
+                src = static_cast<const T*>(a.q.p) + tok * a.q.tok + h * a.q.head;
+                dst[j] = static_cast<T*>(a.out.p) + tok * a.out.tok + h * a.out.head;
+            } else if (h < H && slot >= 0) {
+                const bool is_k = h < a.n_heads + n_kv;
+                const int kh = h - a.n_heads - (is_k ? 0 : n_kv);
+                const HeadsView& s = is_k ? a.k : a.v;
+                src = static_cast<const T*>(s.p) + tok * s.tok + kh * s.head;
+                dst[j] = static_cast<T*>(is_k ? a.c.k : a.c.v) + page * a.c.page + in_page * a.c.tok + kh * a.c.head;
+            }
+            if (src != nullptr) {
+#pragma unroll
+                for (int n = 0; n < NU; ++n) {
+                    if (c0[n] < D) load(x[j][n][0], src + c0[n]);
+                    if (c1[n] < D) load(x[j][n][1], src + c1[n]);
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int h = h0 + j * P.wpt * hp;
+            const bool turned = h < a.n_heads + n_kv;  // queries and keys
+            const T* w = static_cast<const T*>(h < a.n_heads ? a.q_norm : a.k_norm);
+            if (!turned || dst[j] == nullptr) w = nullptr;
+            float r = 1.0f;
+            if (any_norm) {  // uniform: every lane takes part in the shuffles
+                float ss = 0.0f;
+                if (w != nullptr) {
+#pragma unroll
+                    for (int n = 0; n < NU; ++n)
+#pragma unroll
+                        for (int v = 0; v < 2; ++v)
+                            if ((v ? c1[n] : c0[n]) < D)
+#pragma unroll
+                                for (int e = 0; e < VW; ++e) {
+                                    const float f = to_f(x[j][n][v].e[e]);
+                                    ss = fmaf(f, f, ss);
+                                }
+                }
+                for (int o = (1 << P.lg) >> 1; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+                r = 1.0f / sqrtf(ss / (float)D + a.eps);
+            }
+            if (dst[j] == nullptr) continue;
+#pragma unroll
+            for (int n = 0; n < NU; ++n) {
+                if (c0[n] >= D) continue;
+                if (turned) {
+                    float f[2][VW];
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) {
+                        const int c = v ? c1[n] : c0[n];
+                        if (c >= D) continue;
+                        if (w != nullptr) {
+                            Vec<T, VW> wv;
+                            load(wv, w + c);
+#pragma unroll
+                            for (int e = 0; e < VW; ++e) f[v][e] = to_f(x[j][n][v].e[e]) * r * to_f(wv.e[e]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < VW; ++e) f[v][e] = to_f(x[j][n][v].e[e]);
+                        }
+                    }
+                    if (c0[n] < a.rot) {
+                        if (VW > 1 && a.interleaved) {
+#pragma unroll
+                            for (int v = 0; v < 2; ++v)
+#pragma unroll
+                                for (int e = 0; e + 1 < VW; e += 2) {
+                                    const float c = cs[n][(v * VW + e) >> 1], s = sn[n][(v * VW + e) >> 1];
+                                    const float p = f[v][e], q = f[v][e + 1];
+                                    f[v][e] = p * c - q * s;
+                                    f[v][e + 1] = p * s + q * c;
+                                }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < VW; ++e) {
+                                const float p = f[0][e], q = f[1][e];
+                                f[0][e] = p * cs[n][e] - q * sn[n][e];
+                                f[1][e] = p * sn[n][e] + q * cs[n][e];
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int v = 0; v < 2; ++v)
+                        if ((v ? c1[n] : c0[n]) < D)
+#pragma unroll
+                            for (int e = 0; e < VW; ++e) x[j][n][v].e[e] = from_f<T>(f[v][e]);
+                }
+                store(dst[j] + c0[n], x[j][n][0]);
+                if (c1[n] < D) store(dst[j] + c1[n], x[j][n][1]);
+            }
+        }
+    }
+}
+
+template <typename T, int VW, int NU>
+cudaError_t launch(const AppendArgs& a, cudaStream_t st) {
+    AppendPlan P;
+    P.pair_units = a.rot / (2 * VW);
+    P.units = P.pair_units + (a.c.head_dim - a.rot + 2 * VW - 1) / (2 * VW);
+    P.lg = 0;
+    while (P.lg < 5 && (1 << P.lg) < P.units) ++P.lg;
+    const int H = a.n_heads + 2 * a.c.n_kv_heads;
+    const int turns = (H + (32 >> P.lg) - 1) / (32 >> P.lg);  // of a warp that has a token to itself
+    const int64_t want = (int64_t)device_sm_count() * 32;
+    P.wpt = (int)std::min<int64_t>(turns, std::max<int64_t>(1, (want + a.n_tok - 1) / a.n_tok));
+    const int64_t blocks = (a.n_tok * P.wpt + kAppendWarps - 1) / kAppendWarps;
+    if (blocks > INT32_MAX) return cudaErrorInvalidValue;
+    append_kernel<T, VW, NU><<<(unsigned)blocks, 32 * kAppendWarps, 0, st>>>(a, P);
+    return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t by_width(const AppendArgs& a, cudaStream_t st) {
+    // the widest vectors that every address and the rotation's halves allow
+    uint64_t bits = 0;  // byte addresses and element strides, doubled to bytes
+    for (const HeadsView* h : {&a.q, &a.k, &a.v, &a.out})
+        bits |= reinterpret_cast<uintptr_t>(h->p) | (uint64_t)h->tok * 2 | (uint64_t)h->head * 2;
+    bits |= reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v);
+    bits |= (uint64_t)(a.c.page | a.c.tok | a.c.head) * 2;
+    bits |= reinterpret_cast<uintptr_t>(a.q_norm) | reinterpret_cast<uintptr_t>(a.k_norm);
+    const bool table = a.rot == 0 || (reinterpret_cast<uintptr_t>(a.rope) & 15) == 0;
+    if (table && bits % 16 == 0 && a.rot % 16 == 0) return launch<T, 8, 1>(a, st);
+    if (table && bits % 8 == 0 && a.rot % 8 == 0) return launch<T, 4, 1>(a, st);
+    return launch<T, 1, 4>(a, st);
+}
+
+}  // namespace
+
+cudaError_t launch_kv_append(const AppendArgs& a, int dtype, cudaStream_t stream) {
+    return dtype == PPS_BF16 ? by_width<__nv_bfloat16>(a, stream) : by_width<__half>(a, stream);
+}
+
+}  // namespace pps

@@ -166,6 +166,72 @@ cudaError_t launch_hetero_expand(int32_t n_seq, int32_t B, int32_t gamma, int32_
                                  uint64_t* node_ctx, uint32_t* node_pos, cudaStream_t stream);
 cudaError_t launch_hetero_block(int64_t n, int32_t B, const int32_t* tok, const uint64_t* key, const uint64_t* ctx,
                                 const uint32_t* pos, int32_t* out, cudaStream_t stream);
+
+// the target side of a step (pps_append.cu, pps_attention.cu, pps_chain.cu); dtype codes are pps_dtype's
+struct HeadsView {  // [n_tok, heads, channels], channels contiguous, strides in elements
+    void* p;
+    int64_t tok, head;
+};
+struct CacheView {
+    void* k;
+    void* v;
+    int64_t n_pages;
+    int page_size, n_kv_heads, head_dim;
+    int64_t page, tok, head;  // strides, elements
+};
+struct AppendArgs {
+    HeadsView q, k, v, out;
+    CacheView c;
+    int64_t n_tok, max_pos;
+    int n_heads, rot, interleaved;
+    const void* q_norm;
+    const void* k_norm;
+    float eps;
+    const float* rope;
+    const int32_t* pos;
+    const int64_t* slot;
+    uint32_t* status;
+};
+cudaError_t launch_kv_append(const AppendArgs& a, int dtype, cudaStream_t stream);
+
+struct AttnArgs {
+    HeadsView q, out;
+    CacheView c;
+    int64_t n_tok, pages_stride;
+    int n_heads, n_seq, max_pages, mask_words;
+    const int32_t* pages;
+    const int32_t* kv_len;
+    const int32_t* q_off;
+    const uint32_t* mask;
+    float scale;
+    float* lse;
+    uint32_t* status;
+    void* ws;
+};
+size_t attention_workspace_bytes(int64_t n_tok, int n_heads, int n_kv_heads, int head_dim);
+cudaError_t launch_attention(const AttnArgs& a, int dtype, cudaStream_t stream);
+
+struct ChainArgs {
+    const void* p;
+    const void* q;
+    int64_t n_nodes, n_draft, V, p_stride, q_stride, noise_stride;
+    int n_seq, gamma;
+    float c;  // log2(e) / T
+    const int32_t* seq_off;
+    const int32_t* node_draft_row;
+    const int32_t* draft_tok;
+    const float* u;
+    const float* noise;
+    int32_t* out_acc;
+    int32_t* out_ne;
+    int32_t* out_em;
+    float* out_prob;
+    uint32_t* status;
+    void* ws;
+};
+size_t chain_workspace_bytes(int64_t n_nodes, int64_t n_draft, int n_seq);
+cudaError_t launch_chain(const ChainArgs& a, int dtype, cudaStream_t stream);
+
 cudaError_t launch_words(const uint64_t* key, const uint64_t* ctx, const uint32_t* pos, int64_t n_rows, int64_t V,
                          int32_t arrival, uint32_t* out, cudaStream_t stream);
 cudaError_t launch_selftest(uint64_t w_begin, uint64_t w_end, float* out, cudaStream_t stream);

@@ -28,9 +28,9 @@ LIB_PATH = library_path(int(os.environ.get("PPS_PHILOX_ROUNDS", "10")))
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_SIZE = 0, 1, 2, 3, 4, 5
 NOALLOC_MAX_ROWS = 4096  # PPS_NOALLOC_MAX_ROWS of include/pps.h (tests/test_abi.py checks the two agree)
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2
 DISTINCT, IID = 0, 1
-FLAG_GUARD, FLAG_LOGIT_RANGE, FLAG_TREE, FLAG_TIMEOUT = 1, 2, 4, 8
+FLAG_GUARD, FLAG_LOGIT_RANGE, FLAG_TREE, FLAG_TIMEOUT, FLAG_INDEX = 1, 2, 4, 8, 16
 MAX_K = 32
 MAX_TOP_K = 64
 MAX_BLOCKS = 32
@@ -42,6 +42,16 @@ _lib = None
 
 class RowIds(ctypes.Structure):
     _fields_ = [("key", ctypes.c_void_p), ("ctx_hash", ctypes.c_void_p), ("pos", ctypes.c_void_p)]
+
+
+class Heads(ctypes.Structure):  # pps_heads
+    _fields_ = [("data", ctypes.c_void_p), ("tok_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class KVCache(ctypes.Structure):  # pps_kv_cache
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_int64),
+                ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_stride", ctypes.c_int64), ("tok_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 class PPSError(RuntimeError):
@@ -130,6 +140,19 @@ def lib():
             L.pps_lmhead_verify_tree.argtypes = [vp, i64, vp, i64, i64, i64, i64, RowIds, f32, i32, i32, vp, vp, i64,
                                                  vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
             L.pps_lmhead_verify_tree.restype = ctypes.c_int
+            L.pps_kv_append.argtypes = [Heads, Heads, Heads, ctypes.c_int, i64, i32, KVCache, vp, vp, f32, vp, i64, i32,
+                                        i32, vp, vp, Heads, vp, vp]
+            L.pps_kv_append.restype = ctypes.c_int
+            L.pps_attention_workspace_size.argtypes = [i64, i32, i32, i32]
+            L.pps_attention_workspace_size.restype = sz
+            L.pps_paged_attention.argtypes = [Heads, ctypes.c_int, i64, i32, KVCache, vp, i64, i32, vp, vp, i32, vp, i32,
+                                              f32, Heads, vp, vp, vp, sz, vp]
+            L.pps_paged_attention.restype = ctypes.c_int
+            L.pps_chain_workspace_size.argtypes = [i64, i64, i32]
+            L.pps_chain_workspace_size.restype = sz
+            L.pps_verify_chain.argtypes = [vp, vp, ctypes.c_int, i64, i64, i64, i64, i64, f32, i32, i32, vp, vp, vp, vp,
+                                           vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
+            L.pps_verify_chain.restype = ctypes.c_int
             L.pps_philox_words.argtypes = [RowIds, i64, i64, i32, vp, vp]
             L.pps_philox_words.restype = ctypes.c_int
             L.pps_selftest_philox_rate.argtypes = [u64, vp, i32, vp]
@@ -632,4 +655,199 @@ def lmhead_verify_tree(hidden, weight, key, ctx, pos, gamma: int, seq_off, node_
                                             _ptr(out["score_sum"]), _ptr(status), _ptr(ws), ws.numel(),
                                             _stream(stream, dev))
     _check("pps_lmhead_verify_tree", code)
+    return out
+
+
+# ---------------------------------------------------------------- target side of a step
+
+_HALVES = {torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _own_memory(stream):
+    """A context for the tensors a call allocates itself: on the stream it is given they come from that
+    stream's pool, so that neither pending nor later work of the current stream shares their memory."""
+    return _HERE_ALREADY if stream is None else torch.cuda.stream(stream)
+
+
+def _heads(name, t, dev, dtype, n=None, heads=None, d=None):
+    """A [n, heads, d] view with contiguous channels, any token and head strides."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != dev.index:
+        raise TypeError(f"{name} must be a CUDA tensor on {dev}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise TypeError(f"{name} must be [tokens, heads, channels] with unit stride along the channels")
+    shape = t.shape
+    if (n is not None and shape[0] != n) or (heads is not None and shape[1] != heads) or (d is not None and shape[2] != d):
+        raise ValueError(f"{name} is {list(shape)}; the call needs {[n, heads, d]}")
+    return Heads(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _cache(k, v, dev, dtype):
+    """The two halves of a paged cache, [pages, page_size, kv heads, channels], of the same strides."""
+    for name, t in (("k_cache", k), ("v_cache", v)):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != dev.index:
+            raise TypeError(f"{name} must be a CUDA tensor on {dev}")
+        if t.dtype is not dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+            raise TypeError(f"{name} must be [pages, page_size, heads, channels] with unit stride along the channels")
+    if k.shape != v.shape or k.stride() != v.stride():
+        raise ValueError("k_cache and v_cache must have the same shape and strides")
+    n, page, heads, d = k.shape
+    sp, st, sh, _ = k.stride()
+    return KVCache(k.data_ptr(), v.data_ptr(), n, page, heads, d, sp, st, sh)
+
+
+def rope_table(max_pos: int, rot: int, base: float = 10000.0, device=None) -> torch.Tensor:
+    """The [max_pos, rot] fp32 table of kv_append: cosines of position * base^(-2i / rot), i < rot / 2, then
+    the sines (formed in 64 bits)."""
+    if rot < 2 or rot % 2:
+        raise ValueError(f"rot must be even and positive, got {rot}")
+    dev = device or "cuda"
+    freq = float(base) ** (-torch.arange(0, rot, 2, device=dev, dtype=torch.float64) / rot)
+    t = torch.arange(max_pos, device=dev, dtype=torch.float64)[:, None] * freq
+    return torch.cat([t.cos(), t.sin()], dim=1).float()
+
+
+def kv_append(q, k, v, pos, slot, k_cache, v_cache, rope, q_norm=None, k_norm=None, eps: float = 1e-6,
+              interleaved: bool = False, out=None, status=None, stream=None):
+    """pps_kv_append: norm (optional) and rotate the queries and keys of new tokens, write keys and values to
+    their cache slots.  Returns the queries (`out`, which may be q).  q [n, heads, d]; k, v [n, kv heads, d];
+    k_cache, v_cache [pages, page_size, kv heads, d]; rope: rope_table or None (no rotation); slot int64, < 0:
+    not written."""
+    dev, dt = q.device, q.dtype
+    if dt not in _HALVES:
+        raise TypeError(f"q must be bfloat16 or float16, got {dt}")
+    hq = _heads("q", q, dev, dt)
+    n, heads, d = q.shape
+    cache = _cache(k_cache, v_cache, dev, dt)
+    hk = _heads("k", k, dev, dt, n, cache.n_kv_heads, d)
+    hv = _heads("v", v, dev, dt, n, cache.n_kv_heads, d)
+    if cache.head_dim != d:
+        raise ValueError(f"the cache has {cache.head_dim} channels a head, q {d}")
+    rot = max_pos = 0
+    if rope is not None:
+        if rope.dim() != 2:
+            raise TypeError("rope must be [max_pos, rot]")
+        max_pos, rot = rope.shape
+        _need("rope", rope, dev, torch.float32)
+        _need("pos", pos, dev, torch.int32, n)
+    _need("slot", slot, dev, torch.int64, n)
+    _need("q_norm", q_norm, dev, dt, d)
+    _need("k_norm", k_norm, dev, dt, d)
+    _need("status", status, dev, torch.int32, 1)
+    with _on(dev):
+        if out is None:
+            with _own_memory(stream):
+                out = torch.empty(n, heads, d, dtype=dt, device=dev)
+        code = lib().pps_kv_append(hq, hk, hv, _HALVES[dt], n, heads, cache, _ptr(q_norm), _ptr(k_norm), eps,
+                                   _ptr(rope), max_pos, rot, 1 if interleaved else 0, _ptr(pos), _ptr(slot),
+                                   _heads("out", out, dev, dt, n, heads, d), _ptr(status), _stream(stream, dev))
+    _check("pps_kv_append", code)
+    return out
+
+
+def attention_workspace(n_tok: int, n_heads: int, n_kv_heads: int, head_dim: int, device=None) -> torch.Tensor:
+    """A workspace for paged_attention calls of up to n_tok tokens (not shared by concurrent calls)."""
+    nb = int(lib().pps_attention_workspace_size(n_tok, n_heads, n_kv_heads, head_dim))
+    return torch.empty(nb, dtype=torch.uint8, device=device or "cuda")
+
+
+def paged_attention(q, k_cache, v_cache, pages, kv_len, q_off, mask=None, scale=None, out=None, lse=None, ws=None,
+                    status=None, stream=None):
+    """pps_paged_attention: the newest tokens of each sequence (q [n, heads, d], those of sequence s in
+    q_off[s] .. q_off[s+1]-1) attend to the paged cache.  pages [n_seq, columns] int32, kv_len [n_seq] int32
+    (the new tokens' own keys included); mask [n, words] int32 tree masks, None: causal; scale None: 1/sqrt(d);
+    lse: an optional [n, heads] float32 output.  Returns out."""
+    dev, dt = q.device, q.dtype
+    if dt not in _HALVES:
+        raise TypeError(f"q must be bfloat16 or float16, got {dt}")
+    hq = _heads("q", q, dev, dt)
+    n, heads, d = q.shape
+    cache = _cache(k_cache, v_cache, dev, dt)
+    if cache.head_dim != d:
+        raise ValueError(f"the cache has {cache.head_dim} channels a head, q {d}")
+    n_seq = kv_len.numel()
+    if pages.dim() != 2 or pages.shape[0] != n_seq or (pages.shape[1] > 1 and pages.stride(1) != 1):
+        raise TypeError("pages must be [n_seq, columns] with unit stride along the columns")
+    columns = pages.shape[1]
+    pages_stride = pages.stride(0) if n_seq > 1 else columns  # a stride below the columns is the library's to refuse
+    _need("pages", pages, dev, torch.int32, 0, False)
+    _need("kv_len", kv_len, dev, torch.int32)
+    _need("q_off", q_off, dev, torch.int32, n_seq + 1)
+    words = 0
+    if mask is not None:
+        if mask.dim() != 2 or mask.shape[0] != n or mask.shape[1] < 1:
+            raise ValueError(f"mask must be [{n}, words]")
+        words = mask.shape[1]
+        _need("mask", mask, dev, torch.int32)
+    _need("lse", lse, dev, torch.float32, n * heads)
+    _need("status", status, dev, torch.int32, 1)
+    _need("ws", ws, dev, torch.uint8)
+    with _on(dev):
+        L = lib()
+        if out is None or ws is None:
+            with _own_memory(stream):
+                if out is None:
+                    out = torch.empty(n, heads, d, dtype=dt, device=dev)
+                if ws is None:
+                    ws = attention_workspace(n, heads, cache.n_kv_heads, d, dev)
+        code = L.pps_paged_attention(hq, _HALVES[dt], n, heads, cache, _ptr(pages), pages_stride, columns, _ptr(kv_len), _ptr(q_off), n_seq, _ptr(mask), words,
+                                     d ** -0.5 if scale is None else scale, _heads("out", out, dev, dt, n, heads, d),
+                                     _ptr(lse), _ptr(status), _ptr(ws), ws.numel(), _stream(stream, dev))
+    _check("pps_paged_attention", code)
+    return out
+
+
+def chain_workspace(n_nodes: int, n_draft: int, n_seq: int, device=None) -> torch.Tensor:
+    """A workspace for verify_chain calls of up to these sizes (not shared by concurrent calls)."""
+    nb = int(lib().pps_chain_workspace_size(n_nodes, n_draft, n_seq))
+    return torch.empty(nb, dtype=torch.uint8, device=device or "cuda")
+
+
+def verify_chain(p_logits, q_logits, gamma: int, seq_off, node_draft_row, draft_tok, u, noise, temperature: float = 1.0,
+                 ws=None, out=None, status=None, stream=None):
+    """pps_verify_chain: the token-level maximal coupling along drafted chains of up to gamma tokens, from the
+    uniforms u [n_draft] and exponentials noise [n_seq, V].  Returns dict(accept_len, n_emitted, emitted,
+    accept_prob); `out` may leave accept_prob out."""
+    n, V, p_stride = _rows(p_logits)
+    n_draft, Vq, q_stride = _rows(q_logits)
+    dev = p_logits.device
+    if Vq != V or q_logits.dtype is not p_logits.dtype or q_logits.device != dev:
+        raise ValueError("p_logits and q_logits must agree in vocabulary, dtype and device")
+    n_seq = seq_off.numel() - 1
+    if noise.dim() != 2 or noise.shape[0] < n_seq or noise.shape[1] < V or noise.stride(1) != 1:
+        raise ValueError(f"noise must be [{n_seq}, >= {V}] with unit stride along the vocabulary")
+    _need("noise", noise, dev, torch.float32, 0, False)
+    for name, t, dt, numel in (("seq_off", seq_off, torch.int32, n_seq + 1),
+                               ("node_draft_row", node_draft_row, torch.int32, n),
+                               ("draft_tok", draft_tok, torch.int32, n_draft), ("u", u, torch.float32, n_draft)):
+        _need(name, t, dev, dt, numel)
+    _need("status", status, dev, torch.int32, 1)
+    _need("ws", ws, dev, torch.uint8)
+    W = gamma + 1
+    with _on(dev):
+        L = lib()
+        if out is None or ws is None:
+            with _own_memory(stream):
+                if out is None:
+                    e = torch.empty
+                    out = dict(accept_len=e(n_seq, dtype=torch.int32, device=dev),
+                               n_emitted=e(n_seq, dtype=torch.int32, device=dev),
+                               emitted=e(n_seq, W, dtype=torch.int32, device=dev),
+                               accept_prob=e(n_draft, dtype=torch.float32, device=dev))
+                if ws is None:
+                    ws = chain_workspace(n, n_draft, n_seq, dev)
+        for name in ("accept_len", "n_emitted", "emitted"):
+            if out.get(name) is None:
+                raise TypeError(f"out[{name!r}] is required")
+        _need_out(out, [("accept_len", torch.int32, n_seq), ("n_emitted", torch.int32, n_seq),
+                        ("emitted", torch.int32, n_seq * W), ("accept_prob", torch.float32, n_draft)], dev)
+        code = L.pps_verify_chain(_ptr(p_logits), _ptr(q_logits), _dtype_code(p_logits), n, n_draft, V, p_stride,
+                                  q_stride, float(temperature), n_seq, int(gamma), _ptr(seq_off), _ptr(node_draft_row),
+                                  _ptr(draft_tok), _ptr(u), _ptr(noise), noise.stride(0), _ptr(out["accept_len"]),
+                                  _ptr(out["n_emitted"]), _ptr(out["emitted"]), _ptr(out.get("accept_prob")),
+                                  _ptr(status), _ptr(ws), ws.numel(), _stream(stream, dev))
+    _check("pps_verify_chain", code)
     return out
