@@ -16,7 +16,7 @@ LIB = os.path.join(OUT, "libpps.so")
 SOURCES = ["pps_race.cu", "pps_misc.cu", "pps_api.cu"]
 # sources without the keyed source: compiled once, linked into every variant
 COMMON = ["pps_append.cu", "pps_attention.cu", "pps_chain.cu"]
-HEADERS = ["pps_device.cuh", "pps_internal.h", "pps_trunc.cuh", "pps_lmhead.cuh"]
+HEADERS = ["pps_device.cuh", "pps_internal.h", "pps_tc.cuh", "pps_trunc.cuh", "pps_lmhead.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -1,87 +1,852 @@
-// pps_attention.cu -- attention of the newest tokens of each sequence over a paged cache.
+// pps_attention.cu -- attention of the newest tokens of each sequence over a paged cache (tcgen05, sm_103a).
 //
-// One warp per (token, head): lane l holds channels 4l .. 4l+3 of the query and of the running output; keys are
-// taken one at a time with the running maximum and sum of an online softmax.
+//   out[i] = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale q_i . k_j)   over the keys j that row i sees,
+//
+// with the running maximum and sum of an online softmax, so that every key and value is read once per row block.
+//
+// Rows.  The tokens of a sequence and the heads that share a key head are packed into rows (token x group + head of
+// the group), so that a decoding step's few rows read their keys once.  A row block is 256 rows in two tiles of
+// 128 (tensor memory's lanes); a block of up to 128 rows is one tile.  Keys are taken 128 at a time.
+//
+// Two streams.  Each of two softmax warpgroups drives one stream: scores S = Q K^T into its own 128 columns of
+// tensor memory, weights P written over them in 16 bits, O += P V into its own accumulator (P is read from tensor
+// memory).  A block of two tiles gives each stream a tile and both the same keys; a block of one tile gives
+// both streams the same rows and every other key tile, and their results are merged at the end.  Either way the tensor
+// cores work for one stream while the other is in its softmax.
+//
+// Softmax.  A thread owns a row.  O is rescaled only when a row's maximum has risen by more than 2^kLazy since the
+// maximum in use (then by its own warpgroup, in place): the weights may pass 1 by that factor, which neither
+// the fp32 sums nor a 16-bit weight feel.  Weights are rounded to the cache's type for the second product
+// (one rounding of 2^-9 or 2^-12 each, of the size of the result's own); their sum is formed before rounding.
+//
+// Work split.  Key tiles of all (sequence, key head, row block) items, plus kFix per item for its start and end, lie
+// on one line that is cut into equal shares, one per SM, whatever the lengths are.  An item cut between CTAs leaves
+// one partial result (maximum, sum, fp32 O) per CTA, at most two per CTA, and a second launch joins them in
+// order: the same call gives the same bits.  Lengths are read on the device; nothing waits for the host.
+//
+// Every wait gives up after tc::kWaitLimit polls and raises PPS_FLAG_TIMEOUT.
+#include <algorithm>
+#include <cfloat>
+#include <climits>
 #include <cstdint>
+#include <cstring>
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include "pps.h"
 #include "pps_internal.h"
+#include "pps_tc.cuh"
 
 namespace pps {
 namespace {
 
-__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
-template <typename T>
-__device__ __forceinline__ T from_f(float x);
-template <>
-__device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-template <>
-__device__ __forceinline__ __half from_f<__half>(float x) { return __float2half_rn(x); }
+using namespace tc;
+
+constexpr int kTileRows = 128, kTileKeys = 128;
+constexpr int kAttnThreads = 384;  // two softmax warpgroups; the loading warp, the issuing warp and two idle ones
+constexpr int kLoadWarp = 8, kMmaWarp = 9;
+constexpr int kMaxCtas = 160;      // shares of the work (one per SM)
+constexpr int kFix = 1;            // key tiles that an item's start and end cost
+constexpr float kLazy = 8.0f;      // log2 of the rise of a maximum that O is not rescaled for
+constexpr uint32_t kColO = 256;    // tensor memory columns: S/P of streams 0, 1; O of streams 0, 1
+
+// what depends on the channels' class DC: 64 (head_dim <= 64) or 128
+template <int DC>
+struct Cfg {
+    static constexpr int kBlock = 128 * 128;                 // 128 rows of 64 channels, 128-byte swizzle
+    static constexpr int kTile = kBlock * (DC / 64);         // 16 or 32 KB: a tile of Q, K or V
+    static constexpr int kStages = (224 * 1024 - 2 * kTile) / kTile;  // 5 (or 12) tiles of K and V in flight
+    static constexpr int kSmem = (2 + kStages) * kTile + 1024 /* alignment */ + 512 /* barriers, plan */;
+    static_assert(8 * (2 * kStages + 8) <= 288, "barriers fit");
+};
+
+// a cut item: nsplit partial results of rows x head_dim, in slot 2 cta + 1 and slots 2 (cta + k), k = 1 .. nsplit - 1
+struct Cut {
+    int32_t nsplit, rows, row0, off, kvh, pad[3];
+};
+
+struct AttnPlan {
+    int group, cap_rows, page_log2;
+    int64_t cap_keys;   // what a row of the page table holds
+    float sc;           // |scale| log2 e
+    uint32_t q_and, q_xor;  // on pairs of query values: a negative scale turns their signs, a zero one clears them
+    Cut* cuts;          // [gridDim.x]
+    float* part_o;      // [2 gridDim.x][cap_rows][DC]
+    float2* part_ml;    // [2 gridDim.x][cap_rows] (maximum, sum)
+};
+
+struct Seq {
+    int off, n, len;  // first token, tokens, keys
+};
+
+__device__ __forceinline__ Seq load_seq(const AttnArgs& a, const AttnPlan& P, int s, bool flag) {
+    Seq q;
+    q.off = __ldg(a.q_off + s);
+    const int end = __ldg(a.q_off + s + 1), len = __ldg(a.kv_len + s);
+    q.n = end - q.off;
+    q.len = (int)min((int64_t)max(len, 0), P.cap_keys);
+    const bool bad = q.off < 0 || end < q.off || end > a.n_tok;
+    if (bad) q.n = 0;
+    if (flag && a.status && (bad || q.len != len)) atomicOr(a.status, PPS_FLAG_INDEX);
+    return q;
+}
+
+// key tiles of row block `blk`: those its last token sees
+__device__ __forceinline__ int block_tiles(const AttnArgs& a, const AttnPlan& P, const Seq& q, int blk) {
+    int vis = q.len;
+    if (a.mask == nullptr) {
+        const int64_t last = min((int64_t)q.n * P.group, (int64_t)(blk + 1) * 2 * kTileRows) - 1;
+        vis = max(0, q.len - q.n + (int)(last / P.group) + 1);
+    }
+    return (vis + kTileKeys - 1) / kTileKeys;
+}
+__device__ __forceinline__ int n_blocks(const AttnPlan& P, const Seq& q) {
+    return (int)(((int64_t)q.n * P.group + 2 * kTileRows - 1) / (2 * kTileRows));
+}
+__device__ __forceinline__ int64_t head_cost(const AttnArgs& a, const AttnPlan& P, const Seq& q) {
+    int64_t c = 0;
+    const int nb = n_blocks(P, q);
+    for (int b = 0; b < nb; ++b) c += block_tiles(a, P, q, b) + kFix;
+    return c;
+}
+
+// A CTA's items in order; every warp walks them by itself.
+struct Walk {
+    int64_t x, x1, base;  // where the walk is, the share's end, the current block's start
+    int s, kvh, blk, nb;
+    Seq q;
+    // the segment: key tiles t0 .. t1 - 1 of T
+    int t0, t1, T, rows;
+
+    __device__ __forceinline__ void start(const AttnArgs& a, const AttnPlan& P, int64_t c0, int64_t c1, int s0, int64_t s_base) {
+        x = c0;
+        x1 = c1;
+        s = s0;
+        kvh = blk = nb = 0;
+        base = c0;
+        if (c0 >= c1) return;
+        q = load_seq(a, P, s, false);
+        nb = n_blocks(P, q);
+        int64_t rem = c0 - s_base;
+        const int64_t per = head_cost(a, P, q);
+        kvh = (int)(rem / per);
+        rem -= kvh * per;
+        for (int c; rem >= (c = block_tiles(a, P, q, blk) + kFix); ++blk) rem -= c;
+        base = c0 - rem;
+    }
+    __device__ __forceinline__ bool next(const AttnArgs& a, const AttnPlan& P) {
+        while (x < x1) {
+            while (blk >= nb) {  // the next key head, or the next sequence with tokens
+                blk = 0;
+                if (nb == 0 || ++kvh == a.c.n_kv_heads) {
+                    kvh = 0;
+                    if (++s >= a.n_seq) return false;
+                    q = load_seq(a, P, s, false);
+                    nb = n_blocks(P, q);
+                }
+            }
+            T = block_tiles(a, P, q, blk);
+            rows = (int)min((int64_t)q.n * P.group - (int64_t)blk * 2 * kTileRows, (int64_t)2 * kTileRows);
+            t0 = (int)(x - base);
+            t1 = (int)min(x1 - base, (int64_t)T);
+            const bool mine = t0 < t1 || (T == 0 && t0 == 0);
+            row0 = blk * 2 * kTileRows;
+            start_ = base;
+            base += T + kFix;
+            x = base;
+            ++blk;
+            if (mine) return true;
+        }
+        return false;
+    }
+    int row0;
+    int64_t start_;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 
 template <typename T>
-__global__ void __launch_bounds__(128) attention_kernel(const AttnArgs a) {
-    const int64_t gw = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31, D = a.c.head_dim;
-    const int64_t tok = gw / a.n_heads;
-    const int h = (int)(gw % a.n_heads), kh = h / (a.n_heads / a.c.n_kv_heads);
-    if (tok >= a.n_tok) return;
-    if (gw == 0 && lane == 0 && a.status)
-        for (int i = 0; i < a.n_seq; ++i)
-            if (a.q_off[i] < 0 || a.q_off[i + 1] > a.n_tok || a.q_off[i + 1] < a.q_off[i]) atomicOr(a.status, PPS_FLAG_INDEX);
-    int s = -1;
-    for (int i = 0; i < a.n_seq; ++i)
-        if (a.q_off[i] >= 0 && a.q_off[i + 1] <= a.n_tok && a.q_off[i] <= tok && tok < a.q_off[i + 1]) s = i;
-    if (s < 0) return;
-    const int n = a.q_off[s + 1] - a.q_off[s], i = (int)tok - a.q_off[s];
-    const int64_t cap = (int64_t)a.max_pages * a.c.page_size;
-    const int64_t L = min((int64_t)max(a.kv_len[s], 0), cap);
-    if (lane == 0 && a.status && L != a.kv_len[s]) atomicOr(a.status, PPS_FLAG_INDEX);
-    const T* qp = static_cast<const T*>(a.q.p) + tok * a.q.tok + h * a.q.head;
-    float q[4], o[4] = {0, 0, 0, 0}, m = -INFINITY, sum = 0.0f;
-    for (int e = 0; e < 4; ++e) q[e] = 4 * lane + e < D ? to_f(qp[4 * lane + e]) * a.scale : 0.0f;
-    for (int64_t j = 0; j < L; ++j) {
-        const int64_t rel = j - (L - n);
-        const bool sees = a.mask ? rel < 0 || (rel < 32 * a.mask_words && (a.mask[tok * a.mask_words + rel / 32] >> (rel % 32) & 1))
-                                 : rel <= i;
-        if (!sees) continue;
-        const int page = a.pages[s * a.pages_stride + j / a.c.page_size];
-        const bool in = page >= 0 && page < a.c.n_pages;
-        if (!in && lane == 0 && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
-        const int64_t at = page * a.c.page + (j % a.c.page_size) * a.c.tok + kh * a.c.head + 4 * lane;
-        float d = 0.0f, v[4] = {0, 0, 0, 0};
-        if (in)
-            for (int e = 0; e < 4; ++e)
-                if (4 * lane + e < D) {
-                    d += q[e] * to_f(static_cast<const T*>(a.c.k)[at + e]);
-                    v[e] = to_f(static_cast<const T*>(a.c.v)[at + e]);
-                }
-        for (int w = 16; w > 0; w >>= 1) d += __shfl_xor_sync(0xffffffffu, d, w);
-        const float M = fmaxf(m, d), r = m == M ? 1.0f : expf(m - M), x = d == M ? 1.0f : expf(d - M);
-        sum = sum * r + x;
-        for (int e = 0; e < 4; ++e) o[e] = o[e] * r + x * v[e];
-        m = M;
+struct Half;
+template <>
+struct Half<__nv_bfloat16> {
+    static constexpr uint32_t kType = 1;    // of an operand in the instruction descriptor
+    static constexpr float kShift = 0.0f;   // log2 of a factor on all weights
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        uint32_t r;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
     }
-    T* op = static_cast<T*>(a.out.p) + tok * a.out.tok + h * a.out.head;
-    for (int e = 0; e < 4; ++e)
-        if (4 * lane + e < D) op[4 * lane + e] = from_f<T>(sum > 0.0f ? o[e] / sum : 0.0f);
-    if (lane == 0 && a.lse) a.lse[tok * a.n_heads + h] = sum > 0.0f ? m + logf(sum) : -INFINITY;
+};
+template <>
+struct Half<__half> {
+    static constexpr uint32_t kType = 0;
+    // weights up to 2^(kLazy + kShift) = 2^14 stay below fp16's largest value, and those down to 2^-20 of the largest
+    // are normal numbers
+    static constexpr float kShift = 6.0f;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        uint32_t r;
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
+    }
+};
+
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort));
+}
+
+// bits c of a tile's 32 columns from key k0 on that a row sees: those below vis, and of its tree's tokens (from key
+// `prefix` on) those of its mask
+__device__ __forceinline__ uint32_t seen_bits(int k0, int vis, int prefix, const uint32_t* mask, int words) {
+    const int n = vis - k0;
+    uint32_t m = n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u;
+    if (mask != nullptr) {
+        const int rel = k0 - prefix;
+        if (rel > -32) {
+            const int w = rel >> 5, sh = rel & 31;
+            const uint32_t lo = w < 0 ? 0xffffffffu : w < words ? __ldg(mask + w) : 0u;
+            const uint32_t hi = w + 1 < words ? __ldg(mask + w + 1) : 0u;
+            m &= __funnelshift_r(lo, hi, sh);
+        }
+    }
+    return m;
+}
+
+template <typename T, int DC>
+__global__ void __launch_bounds__(kAttnThreads, 1)
+    attention_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttnArgs a,
+                     const AttnPlan P) {
+    using C = Cfg<DC>;
+    using H = Half<T>;
+    extern __shared__ uint8_t attn_smem_raw[];
+    const uint32_t raw = smem_u32(attn_smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    uint8_t* gbase = attn_smem_raw + (base - raw);
+    const uint32_t ring = base + 2 * C::kTile;
+    const uint32_t bars = ring + C::kStages * C::kTile;
+    auto full = [&](uint32_t s) { return bars + 8u * s; };
+    auto empty = [&](uint32_t s) { return bars + 8u * (C::kStages + s); };
+    auto sfull = [&](uint32_t w) { return bars + 8u * (2 * C::kStages + w); };
+    auto pready = [&](uint32_t w) { return bars + 8u * (2 * C::kStages + 2 + w); };
+    auto odone = [&](uint32_t w) { return bars + 8u * (2 * C::kStages + 4 + w); };
+    const uint32_t qfull = bars + 8u * (2 * C::kStages + 6), segbar = bars + 8u * (2 * C::kStages + 7);
+    uint8_t* tail = gbase + (2 + C::kStages) * C::kTile + 288;
+    volatile int* abort = reinterpret_cast<volatile int*>(tail);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 4);
+    int* s_seq = reinterpret_cast<int*>(tail + 8);
+    int64_t* s_sum = reinterpret_cast<int64_t*>(tail + 16);   // [12] warp sums, then the sequence's start
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
+    pdl_launch_dependents();
+    if (tid == 0) {
+        for (int s = 0; s < C::kStages; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+        }
+        for (int w = 0; w < 2; ++w) {
+            mbar_init(sfull(w), 1);
+            mbar_init(pready(w), 4);
+            mbar_init(odone(w), 1);
+        }
+        mbar_init(qfull, 8);
+        mbar_init(segbar, 8);
+        *abort = 0;
+        *s_seq = a.n_seq;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        P.cuts[cta].nsplit = 0;
+    }
+    if (warp == kLoadWarp && lane == 0) {
+        tma_prefetch_map(&tmK);
+        tma_prefetch_map(&tmV);
+    }
+
+    // the share: [c0, c1) of the line of costs, and the sequence in which it starts
+    auto cost = [&](int s, bool flag) {
+        const Seq q = load_seq(a, P, s, flag);
+        return q.n > 0 ? head_cost(a, P, q) * a.c.n_kv_heads : (int64_t)0;
+    };
+    auto block_scan = [&](int64_t v, int64_t& total) {  // inclusive
+        int64_t w = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t t = __shfl_up_sync(0xffffffffu, w, o);
+            if (lane >= o) w += t;
+        }
+        __syncthreads();
+        if (lane == 31) s_sum[warp] = w;
+        __syncthreads();
+        total = 0;
+        for (int i = 0; i < kAttnThreads / 32; ++i) {
+            const int64_t t = s_sum[i];
+            if (i < warp) w += t;
+            total += t;
+        }
+        return w;
+    };
+    const int64_t mine = tid < a.n_seq ? cost(tid, cta == 0) : 0;
+    int64_t more = 0;
+    for (int64_t s = tid + kAttnThreads; s < a.n_seq; s += kAttnThreads) more += cost((int)s, cta == 0);
+    int64_t U, U0;
+    int64_t at = block_scan(mine, U0);
+    U = U0;
+    if (a.n_seq > kAttnThreads) {
+        block_scan(more, U);
+        U += U0;
+    }
+    const int64_t share = max((U + gridDim.x - 1) / gridDim.x, (int64_t)1);
+    const int64_t c0 = min(cta * share, U), c1 = min(c0 + share, U);
+    if (c0 < c1) {
+        int64_t before = 0;
+        int64_t v = mine;
+        for (int64_t b = 0;; b += kAttnThreads) {
+            if (c0 >= before + at - v && c0 < before + at) {
+                *s_seq = (int)(b + tid);
+                s_sum[12] = before + at - v;
+            }
+            before += U0;
+            if (before > c0) break;  // CTA-uniform
+            v = b + kAttnThreads + tid < a.n_seq ? cost((int)(b + kAttnThreads + tid), false) : 0;
+            at = block_scan(v, U0);
+        }
+    }
+    if (warp == kMmaWarp && c0 < c1) {
+        tmem_alloc(smem_u32(tmem_slot), 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (c0 >= c1) return;
+    const uint32_t tmem = *tmem_slot;
+    Walk W;
+    W.start(a, P, c0, c1, *s_seq, s_sum[12]);
+    const int D = a.c.head_dim;
+
+    // registers: 384 x 168 at launch = 256 x 208 + 128 x 88
+    if (warp >= kLoadWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == kLoadWarp) {
+        // ---- keys and values: K of the first tile (or two, one per stream), then V_j and the next K in turn
+        uint32_t it = 0;
+        bool ok = true;
+        const int box = min(kTileKeys, a.c.page_size), boxes = kTileKeys / box;
+        while (ok && W.next(a, P)) {
+            const int n = W.t1 - W.t0, ahead = W.rows <= kTileRows ? 2 : 1;
+            const int32_t* table = a.pages + (int64_t)W.s * a.pages_stride;
+            const int len = W.q.len;
+            auto page_of = [&](int j) {  // lane i: the page of tile j's i-th box
+                const int64_t k = (int64_t)(W.t0 + j) * kTileKeys + lane * box;
+                return j < n && lane < boxes && k < len ? __ldg(table + (k >> P.page_log2)) : 0;
+            };
+            auto issue = [&](const CUtensorMap* map, int j, int page) {
+                const uint32_t s = it % C::kStages;
+                if (!wait_warp(empty(s), ((it / C::kStages) & 1u) ^ 1u, abort)) return false;
+                ++it;
+                const int k0 = (W.t0 + j) * kTileKeys, need = (min(kTileKeys, len - k0) + box - 1) / box;
+                const uint32_t dst = ring + s * C::kTile;
+                if (lane == 0) mbar_expect_tx(full(s), (uint32_t)(need * box * 128 * (DC / 64)));
+                __syncwarp();
+                if (lane < need) {
+                    if (page < 0 || page >= a.c.n_pages) {  // reads as zeros past the last page
+                        if (a.status) atomicOr(a.status, PPS_FLAG_INDEX);
+                        page = (int)a.c.n_pages;
+                    }
+                    const int in_page = (k0 + lane * box) & (a.c.page_size - 1);
+#pragma unroll
+                    for (int b = 0; b < DC / 64; ++b)
+                        tma_load_4d(dst + b * C::kBlock + lane * box * 128, map, full(s), b * 64, in_page, W.kvh, page);
+                }
+                return true;
+            };
+            int p0 = page_of(0), p1 = page_of(1), p2 = page_of(2);
+            if (n > 0) ok = issue(&tmK, 0, p0);
+            if (ok && ahead == 2 && n > 1) ok = issue(&tmK, 1, p1);
+            for (int j = 0; j < n && ok; ++j) {
+                const int p3 = page_of(j + 3);
+                ok = issue(&tmV, j, p0);
+                if (ok && j + ahead < n) ok = issue(&tmK, j + ahead, ahead == 2 ? p2 : p1);
+                p0 = p1;
+                p1 = p2;
+                p2 = p3;
+            }
+        }
+        // copies in flight when the CTA gives up: wait (bounded) for each
+        const uint32_t from = it > (uint32_t)C::kStages ? it - C::kStages : 0u;
+        for (uint32_t j = from; j < it && *abort; ++j)
+            for (uint32_t n = 0; n < kWaitLimit && !mbar_try_wait(full(j % C::kStages), (j / C::kStages) & 1u); ++n) {
+            }
+    } else if (warp == kMmaWarp) {
+        // ---- products (one thread): per stream S = Q K^T, then O += P V as its weights arrive
+        if (lane == 0) {
+            const uint32_t dn = (uint32_t)(D + 15) / 16;  // 16-channel steps
+            const uint32_t id_qk = (1u << 4) | (H::kType << 7) | (H::kType << 10) | ((kTileKeys / 8u) << 17) | ((kTileRows / 16u) << 24);
+            const uint32_t id_pv = (1u << 4) | (H::kType << 7) | (H::kType << 10) | (1u << 16) | ((dn * 2u) << 17) | ((kTileRows / 16u) << 24);
+            uint32_t it = 0, np0 = 0, np1 = 0, segs = 0;
+            auto stage = [&](uint32_t i) { return ring + (i % C::kStages) * C::kTile; };
+            auto landed = [&](uint32_t i) {
+                const bool ok = mbar_wait(full(i % C::kStages), (i / C::kStages) & 1u, abort);
+                tc_fence_after();
+                return ok;
+            };
+            auto scores = [&](uint32_t w, uint32_t tile, uint32_t k) {
+                for (uint32_t c = 0; c < dn; ++c) {
+                    const uint32_t o = (c >> 2) * C::kBlock + (c & 3u) * 32u;
+                    tc_mma(tmem + w * 128u, sw128_desc(base + tile * C::kTile + o), sw128_desc(stage(k) + o), id_qk, c != 0);
+                }
+                tc_commit(sfull(w));
+            };
+            auto values = [&](uint32_t w, uint32_t v, bool first) {
+                for (uint32_t c = 0; c < kTileKeys / 16; ++c)
+                    tc_mma_ts(tmem + kColO + w * 128u, tmem + w * 128u + c * 8u,
+                              sw128_desc_mn(stage(v) + c * 2048u, C::kBlock), id_pv, !first || c != 0);
+                tc_commit(odone(w));
+            };
+            bool ok = true;
+            while (ok && W.next(a, P)) {
+                const int n = W.t1 - W.t0;
+                ok = mbar_wait(qfull, segs++ & 1u, abort);
+                if (!ok || n == 0) continue;
+                tc_fence_after();
+                if (W.rows > kTileRows) {  // a tile per stream, the same keys
+                    ok = landed(it);
+                    if (!ok) break;
+                    scores(0, 0, it);
+                    scores(1, 1, it);
+                    tc_commit(empty(it % C::kStages));
+                    ++it;
+                    for (int j = 0; j < n && ok; ++j) {
+                        const uint32_t v = it, k = it + 1;
+                        const bool more_keys = j + 1 < n;
+                        ok = landed(v);
+                        for (uint32_t w = 0; w < 2 && ok; ++w) {
+                            ok = mbar_wait(pready(w), (w ? np1++ : np0++) & 1u, abort);
+                            if (!ok) break;
+                            tc_fence_after();
+                            values(w, v, j == 0);
+                            if (w == 1) tc_commit(empty(v % C::kStages));
+                            if (more_keys) {
+                                if (w == 0) ok = landed(k);
+                                if (!ok) break;
+                                scores(w, w, k);
+                                if (w == 1) tc_commit(empty(k % C::kStages));
+                            }
+                        }
+                        it += more_keys ? 2 : 1;
+                    }
+                } else {  // one tile, every other key tile per stream
+                    for (int j = 0; j < min(n, 2) && ok; ++j) {
+                        ok = landed(it);
+                        if (!ok) break;
+                        scores(j, 0, it);
+                        tc_commit(empty(it % C::kStages));
+                        ++it;
+                    }
+                    for (int j = 0; j < n && ok; ++j) {
+                        const uint32_t w = j & 1;
+                        ok = landed(it) && mbar_wait(pready(w), (w ? np1++ : np0++) & 1u, abort);
+                        if (!ok) break;
+                        tc_fence_after();
+                        values(w, it, j < 2);
+                        tc_commit(empty(it % C::kStages));
+                        ++it;
+                        if (j + 2 < n) {
+                            ok = landed(it);
+                            if (!ok) break;
+                            scores(w, 0, it);
+                            tc_commit(empty(it % C::kStages));
+                            ++it;
+                        }
+                    }
+                }
+            }
+        }
+        __syncwarp();
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        // ---- softmax: warpgroup w drives stream w, thread = row r of its tile
+        const uint32_t w = warp >> 2, q4 = warp & 3;
+        const int r = (int)(q4 * 32) + lane;
+        const uint32_t lanes = (q4 * 32u) << 16;
+        const uint32_t tS = tmem + lanes + w * 128u, tO = tmem + lanes + kColO;
+        uint32_t done = 0, done_other = 0;  // tiles of this stream and of the other one so far
+        uint32_t it = 0, syncs = 0;
+        float2* s_ml = reinterpret_cast<float2*>(gbase + C::kTile);  // [2][128], in the second query tile's place
+        auto seg_sync = [&]() {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(segbar);
+            return wait_warp(segbar, syncs++ & 1u, abort);
+        };
+        bool ok = true;
+        while (ok && W.next(a, P)) {
+            const bool two = W.rows > kTileRows;  // a tile per stream
+            const int n = W.t1 - W.t0;
+            {  // queries: 16-byte chunks, swizzled as TMA would write them
+                constexpr int kChunks = DC / 8, kRp = 32 / kChunks;
+                const int nrow = two ? 32 : 16, r0 = two ? (int)q4 * 32 : (int)(w * 64 + q4 * 16);
+                const int tile = two ? (int)w : 0, chunk = lane % kChunks;
+                const uint32_t dst = base + tile * C::kTile + (chunk >> 3) * C::kBlock;
+#pragma unroll 4
+                for (int p = 0; p < nrow; p += kRp) {
+                    const int row = r0 + p + lane / kChunks, in = tile * kTileRows + row;
+                    if (in < ((W.rows + 31) & ~31)) {  // zeros in the rows past the last one of a warp
+                        const int pr = W.row0 + min(in, W.rows - 1), tok = pr / P.group, h = W.kvh * P.group + (pr - tok * P.group);
+                        uint4 x = make_uint4(0, 0, 0, 0);
+                        if (chunk * 8 < D && in < W.rows)
+                            x = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.q.p) + (int64_t)(W.q.off + tok) * a.q.tok +
+                                                                     h * a.q.head + chunk * 8));
+                        x.x = (x.x & P.q_and) ^ P.q_xor;
+                        x.y = (x.y & P.q_and) ^ P.q_xor;
+                        x.z = (x.z & P.q_and) ^ P.q_xor;
+                        x.w = (x.w & P.q_and) ^ P.q_xor;
+                        const uint32_t at = dst + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w)
+                                     : "memory");
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(qfull);
+            }
+            const int in_block = (two ? (int)w * kTileRows : 0) + r;
+            const bool valid = in_block < W.rows;
+            const bool busy = (two ? (int)w * kTileRows : 0) + (int)q4 * 32 < W.rows;  // warp-uniform
+            const int pr = W.row0 + min(in_block, W.rows - 1), tok = pr / P.group, head = W.kvh * P.group + (pr - tok * P.group);
+            const int prefix = W.q.len - W.q.n;
+            const uint32_t* mask = a.mask ? a.mask + (int64_t)(W.q.off + tok) * a.mask_words : nullptr;
+            const int vis = mask ? W.q.len : prefix + tok + 1;
+            const int plain = mask ? prefix : vis;  // keys below it are seen by the row
+            float m = -INFINITY, l = 0.0f;
+            int i = 0;  // tiles of the stream in this segment
+            for (int j = two ? 0 : (int)w; j < n; j += two ? 1 : 2, ++i) {
+                const int k0 = (W.t0 + j) * kTileKeys;
+                if (!(ok = wait_warp(sfull(w), (done + i) & 1u, abort))) break;
+                tc_fence_after();
+                if (busy) {
+                    uint32_t v[4][32];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, v[c]);
+                    tmem_wait_ld();
+                    if (__any_sync(0xffffffffu, k0 + kTileKeys > plain)) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const uint32_t bits = seen_bits(k0 + 32 * c, vis, prefix, mask, a.mask_words);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!(bits & (1u << e))) v[c][e] = 0xff800000u;  // -inf
+                        }
+                    }
+                    float mx[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        mx[c] = __uint_as_float(v[c][0]);
+#pragma unroll
+                        for (int e = 1; e < 32; ++e) mx[c] = fmaxf(mx[c], __uint_as_float(v[c][e]));
+                    }
+                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                    if (__any_sync(0xffffffffu, (top - m) * P.sc > kLazy)) {
+                        const float M = fmaxf(m, top), f = m == M ? 1.0f : ex2((m - M) * P.sc);
+                        m = M;
+                        l *= f;
+                        if (i > 0) {
+                            if (!(ok = wait_warp(odone(w), (done + i - 1) & 1u, abort))) break;
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int c = 0; c < D; c += 32) {
+                                uint32_t o[32];
+                                tmem_ld32(tO + w * 128u + c, o);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                tmem_st32(tO + w * 128u + c, o);
+                            }
+                        }
+                    }
+                    const float neg = (m == -INFINITY ? 0.0f : -m * P.sc) + H::kShift;
+                    const uint64_t sc2 = pack2(P.sc, P.sc), neg2 = pack2(neg, neg);
+                    uint64_t sum[2] = {0, 0};
+#pragma unroll
+                    for (int c = 0; c < 4; c += 2) {
+                        uint32_t pk[32];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const uint32_t* x = &v[c + (e >> 4)][(e & 15) * 2];
+                            float x0, x1;
+                            unpack2(fma2(pack2(__uint_as_float(x[0]), __uint_as_float(x[1])), sc2, neg2), x0, x1);
+                            x0 = ex2(x0);
+                            x1 = ex2(x1);
+                            sum[e & 1] = add2(sum[e & 1], pack2(x0, x1));
+                            pk[e] = H::pack(x0, x1);
+                        }
+                        tmem_st32(tS + c * 16, pk);
+                    }
+                    float s0, s1;
+                    unpack2(add2(sum[0], sum[1]), s0, s1);
+                    l += s0 + s1;
+                    tmem_wait_st();
+                }
+                // values past the sequence's end (its last tile's): whatever the pages hold there becomes zero
+                if (k0 + kTileKeys > W.q.len && (w == 0 || !two)) {
+                    const uint32_t v = it + 2 * n - 1;  // the segment's last value tile
+                    if (!(ok = wait_warp(full(v % C::kStages), (v / C::kStages) & 1u, abort))) break;
+                    const uint32_t from = ring + (v % C::kStages) * C::kTile + (W.q.len - k0) * 128;
+                    const uint32_t bytes = (k0 + kTileKeys - W.q.len) * 128;
+#pragma unroll
+                    for (int b = 0; b < DC / 64; ++b)
+                        for (uint32_t o = r * 16; o < bytes; o += 128 * 16)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(from + b * C::kBlock + o), "r"(0) : "memory");
+                    fence_async_smem();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(pready(w));
+            }
+            if (!ok) break;
+            // ---- the segment's result
+            const bool whole = W.t0 == 0 && W.t1 == W.T;
+            const int slot = 2 * cta + (W.t0 == 0 ? 1 : 0);
+            if (tid == 0 && W.t0 == 0 && !whole) {
+                Cut c = {};
+                c.nsplit = (int)((W.start_ + W.T - 1) / share) - cta + 1;
+                c.rows = W.rows;
+                c.row0 = W.row0;
+                c.off = W.q.off;
+                c.kvh = W.kvh;
+                P.cuts[cta] = c;
+            }
+            const uint32_t tiles = i, tiles_other = n + (two ? n : 0) - i;
+            if (tiles > 0) ok = wait_warp(odone(w), (done + tiles - 1) & 1u, abort);
+            if (!ok) break;
+            m *= P.sc;  // log2 of the largest weight (-inf stays)
+            float f = 1.0f, f1 = 0.0f;  // factors of the first accumulator (the stream's own) and, of one tile, the second
+            if (!two) {
+                s_ml[w * 128 + r] = make_float2(m, l);
+                if (!(ok = seg_sync())) break;
+                if (tiles_other > 0 && !(ok = wait_warp(odone(w ^ 1u), (done_other + tiles_other - 1) & 1u, abort))) break;
+                const float2 x = s_ml[r], y = s_ml[128 + r];
+                m = fmaxf(x.x, y.x);
+                f = x.x == -INFINITY ? 0.0f : ex2(x.x - m);
+                f1 = y.x == -INFINITY ? 0.0f : ex2(y.x - m);
+                l = x.y * f + y.y * f1;
+            }
+            tc_fence_after();
+            if (busy) {
+                if (whole) {
+                    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+                    f *= inv;
+                    f1 *= inv;
+                }
+                const uint32_t first = two ? w : 0u;
+                const int from = two ? 0 : (int)w * (DC / 2), to = two ? DC : from + DC / 2;
+                T* out = static_cast<T*>(a.out.p) + (int64_t)(W.q.off + tok) * a.out.tok + head * a.out.head;
+                float* part = P.part_o + ((int64_t)slot * P.cap_rows + in_block) * DC;
+                if (valid && (two || w == 0)) {
+                    if (!whole)
+                        P.part_ml[(int64_t)slot * P.cap_rows + in_block] = make_float2(m, l);
+                    else if (a.lse)
+                        a.lse[(int64_t)(W.q.off + tok) * a.n_heads + head] =
+                            l > 0.0f ? (m + log2f(l) - H::kShift) * 0.69314718055994531f : -INFINITY;
+                }
+#pragma unroll 1
+                for (int c = from; c < to && c < D; c += 32) {
+                    uint32_t o[32];
+                    if (n > 0) {
+                        tmem_ld32(tO + first * 128u + c, o);
+                        tmem_wait_ld();
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        o[e] = n > 0 && f != 0.0f ? __float_as_uint(__uint_as_float(o[e]) * f) : 0u;
+                    if (!two && n > 1) {
+                        uint32_t o1[32];
+                        tmem_ld32(tO + 128u + c, o1);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (f1 != 0.0f) o[e] = __float_as_uint(fmaf(__uint_as_float(o1[e]), f1, __uint_as_float(o[e])));
+                    }
+                    if (valid) {
+                        if (whole) {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 8)
+                                if (c + e < D) {
+                                    uint4 x;
+                                    x.x = H::pack(__uint_as_float(o[e]), __uint_as_float(o[e + 1]));
+                                    x.y = H::pack(__uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
+                                    x.z = H::pack(__uint_as_float(o[e + 4]), __uint_as_float(o[e + 5]));
+                                    x.w = H::pack(__uint_as_float(o[e + 6]), __uint_as_float(o[e + 7]));
+                                    *reinterpret_cast<uint4*>(out + c + e) = x;
+                                }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4)
+                                *reinterpret_cast<uint4*>(part + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+            done += tiles;
+            done_other += tiles_other;
+            it += 2 * n;
+            tc_fence_before();
+            ok = seg_sync();  // the accumulators, queries and s_ml are free
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+    if (tid == 0 && *abort && a.status) atomicOr(a.status, PPS_FLAG_TIMEOUT);
+}
+
+// Joins the partial results of the items that are cut between CTAs: a warp per row, its lanes the channels.
+template <typename T, int DC>
+__global__ void __launch_bounds__(256) join_kernel(const AttnArgs a, const AttnPlan P) {
+    using H = Half<T>;
+    constexpr int VW = DC / 32;
+    pdl_wait();
+    const Cut c = P.cuts[blockIdx.x];
+    const int lane = threadIdx.x & 31, D = a.c.head_dim;
+    if (c.nsplit == 0) return;
+    auto slot = [&](int k) { return (int64_t)(k == 0 ? 2 * blockIdx.x + 1 : 2 * (blockIdx.x + k)) * P.cap_rows; };
+    for (int row = blockIdx.y * 8 + (threadIdx.x >> 5); row < c.rows; row += 8 * gridDim.y) {
+        float M = -INFINITY;
+        for (int k = lane; k < c.nsplit; k += 32) M = fmaxf(M, P.part_ml[slot(k) + row].x);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+        float l = 0.0f, o[VW] = {};
+        for (int k0 = 0; k0 < c.nsplit; k0 += 32) {
+            float f = 0.0f;
+            if (k0 + lane < c.nsplit) {
+                const float2 x = P.part_ml[slot(k0 + lane) + row];
+                if (x.x != -INFINITY) f = ex2(x.x - M);
+                l += x.y * f;
+            }
+            const int n = min(32, c.nsplit - k0);
+#pragma unroll 8
+            for (int k = 0; k < n; ++k) {
+                const float g = __shfl_sync(0xffffffffu, f, k);
+                const float* p = P.part_o + (slot(k0 + k) + row) * DC + lane * VW;
+                float x[VW];
+                if constexpr (VW == 4)
+                    *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(p);
+                else
+                    *reinterpret_cast<float2*>(x) = *reinterpret_cast<const float2*>(p);
+#pragma unroll
+                for (int e = 0; e < VW; ++e)
+                    if (g != 0.0f) o[e] = fmaf(x[e], g, o[e]);
+            }
+        }
+#pragma unroll
+        for (int s = 16; s > 0; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        const int pr = c.row0 + row, tok = c.off + pr / P.group, head = c.kvh * P.group + pr % P.group;
+        if (lane * VW < D) {
+            T* out = static_cast<T*>(a.out.p) + (int64_t)tok * a.out.tok + head * a.out.head + lane * VW;
+            if constexpr (VW == 4)
+                *reinterpret_cast<uint2*>(out) = make_uint2(H::pack(o[0] * inv, o[1] * inv), H::pack(o[2] * inv, o[3] * inv));
+            else
+                *reinterpret_cast<uint32_t*>(out) = H::pack(o[0] * inv, o[1] * inv);
+        }
+        if (lane == 0 && a.lse)
+            a.lse[(int64_t)tok * a.n_heads + head] = l > 0.0f ? (M + log2f(l) - H::kShift) * 0.69314718055994531f : -INFINITY;
+    }
+}
+
+// ---------------------------------------------------------------- host side
+
+int cap_rows(int64_t n_tok, int group) {
+    const int64_t r = std::min<int64_t>(n_tok * group, 2 * kTileRows);
+    return (int)((r + 31) / 32 * 32);
+}
+int channel_class(int head_dim) { return head_dim <= 64 ? 64 : 128; }
+size_t cut_bytes() { return sizeof(Cut) * kMaxCtas; }
+size_t ml_bytes(int rows) { return sizeof(float2) * 2 * kMaxCtas * (size_t)rows; }
+
+// one half of the cache as [page, head, token, channel], loaded in boxes of up to 128 tokens x 64 channels
+bool cache_map(CUtensorMap* m, const void* ptr, const CacheView& c, int dtype) {
+    EncodeTiledFn f = encode_fn();
+    if (f == nullptr) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_size, (cuuint64_t)c.n_kv_heads,
+                                (cuuint64_t)std::max<int64_t>(c.n_pages, 1)};
+    // the stride of a dimension of one is never used, but has to be a multiple of 16 bytes
+    const cuuint64_t strides[3] = {(cuuint64_t)c.tok * 2, c.n_kv_heads > 1 ? (cuuint64_t)c.head * 2 : 256,
+                                   c.n_pages > 1 ? (cuuint64_t)c.page * 2 : 256};
+    const cuuint32_t box[4] = {64, (cuuint32_t)std::min(kTileKeys, c.page_size), 1, 1}, es[4] = {1, 1, 1, 1};
+    return f(m, dtype == PPS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+             const_cast<void*>(ptr), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int DC>
+cudaError_t launch(const AttnArgs& a, int dtype, cudaStream_t st) {
+    AttnPlan P;
+    P.group = a.n_heads / a.c.n_kv_heads;
+    P.cap_rows = cap_rows(a.n_tok, P.group);
+    P.page_log2 = 0;
+    while ((1 << P.page_log2) < a.c.page_size) ++P.page_log2;
+    P.cap_keys = (int64_t)a.max_pages * a.c.page_size;
+    const float scale = a.scale;
+    P.sc = scale == 0.0f ? 1.0f : (float)((double)(scale < 0.0f ? -scale : scale) * 1.4426950408889634074);
+    P.q_and = scale == 0.0f ? 0u : 0xffffffffu;
+    P.q_xor = scale < 0.0f ? 0x80008000u : 0u;
+    char* w = static_cast<char*>(a.ws);
+    P.cuts = reinterpret_cast<Cut*>(w);
+    w += cut_bytes();
+    P.part_ml = reinterpret_cast<float2*>(w);
+    w += ml_bytes(P.cap_rows);
+    P.part_o = reinterpret_cast<float*>(w);
+    CUtensorMap tmK, tmV;
+    // an empty cache has nothing to read: any mapped memory will do for its maps
+    if (!cache_map(&tmK, a.c.n_pages > 0 ? a.c.k : a.ws, a.c, dtype) || !cache_map(&tmV, a.c.n_pages > 0 ? a.c.v : a.ws, a.c, dtype))
+        return cudaErrorInvalidValue;
+    cudaError_t e = cudaFuncSetAttribute(attention_kernel<T, DC>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<DC>::kSmem);
+    if (e != cudaSuccess) return e;
+    const int ctas = std::min(device_sm_count(), kMaxCtas);
+    attention_kernel<T, DC><<<ctas, kAttnThreads, Cfg<DC>::kSmem, st>>>(tmK, tmV, a, P);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    return launch_pdl(join_kernel<T, DC>, dim3(ctas, std::min(16, P.cap_rows / 8)), dim3(256), 0, st, a, P);
+}
+
+template <typename T>
+cudaError_t by_channels(const AttnArgs& a, int dtype, cudaStream_t st) {
+    return channel_class(a.c.head_dim) == 64 ? launch<T, 64>(a, dtype, st) : launch<T, 128>(a, dtype, st);
 }
 
 }  // namespace
 
-size_t attention_workspace_bytes(int64_t, int, int, int) { return 256; }
+size_t attention_workspace_bytes(int64_t n_tok, int n_heads, int n_kv_heads, int head_dim) {
+    const int rows = cap_rows(n_tok, (n_heads + n_kv_heads - 1) / n_kv_heads);
+    return cut_bytes() + ml_bytes(rows) + sizeof(float) * 2 * kMaxCtas * (size_t)rows * channel_class(head_dim);
+}
 
 cudaError_t launch_attention(const AttnArgs& a, int dtype, cudaStream_t stream) {
-    const unsigned blocks = (unsigned)((a.n_tok * a.n_heads + 3) / 4);
-    if (dtype == PPS_BF16)
-        attention_kernel<__nv_bfloat16><<<blocks, 128, 0, stream>>>(a);
-    else
-        attention_kernel<__half><<<blocks, 128, 0, stream>>>(a);
-    return cudaGetLastError();
+    return dtype == PPS_BF16 ? by_channels<__nv_bfloat16>(a, dtype, stream) : by_channels<__half>(a, dtype, stream);
 }
 
 }  // namespace pps

@@ -31,6 +31,7 @@
 #include "pps.h"
 #include "pps_device.cuh"
 #include "pps_internal.h"
+#include "pps_tc.cuh"
 
 #ifndef PPS_UNITS
 #define PPS_UNITS 3  // 8-token units per lane per fast-loop iteration (2 Philox blocks each), draft rows
