@@ -44,8 +44,8 @@ namespace {
 using namespace tc;
 
 constexpr int kTileRows = 128, kTileKeys = 128;
-constexpr int kAttnThreads = 384;  // two softmax warpgroups; the loading warp, the issuing warp and two idle ones
-constexpr int kLoadWarp = 8, kMmaWarp = 9;
+constexpr int kAttnThreads = 384;  // two softmax warpgroups; the loading warps (keys, values), the issuing warp, an idle one
+constexpr int kLoadWarp = 8, kMmaWarp = 10;
 constexpr int kMaxCtas = 160;      // shares of the work (one per SM)
 constexpr int kFix = 1;            // key tiles that an item's start and end cost
 constexpr float kLazy = 8.0f;      // log2 of the rise of a maximum that O is not rescaled for
@@ -167,6 +167,11 @@ struct Walk {
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
     return y;
 }
 __device__ __forceinline__ uint64_t pack2(float lo, float hi) {
@@ -344,63 +349,68 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
 
     // registers: 384 x 168 at launch = 256 x 208 + 128 x 88
     if (warp >= kLoadWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    if (warp == kLoadWarp) {
-        // ---- keys and values: K of the first tile (or two, one per stream), then V_j and the next K in turn
-        uint32_t it = 0;
-        bool ok = true;
-        const int box = min(kTileKeys, a.c.page_size), boxes = kTileKeys / box;
-        while (ok && W.next(a, P)) {
-            const int n = W.t1 - W.t0, ahead = W.rows <= kTileRows ? 2 : 1;
-            const int32_t* table = a.pages + (int64_t)W.s * a.pages_stride;
-            const int len = W.q.len;
-            auto page_of = [&](int j) {  // lane i: the page of tile j's i-th box
-                const int64_t k = (int64_t)(W.t0 + j) * kTileKeys + lane * box;
-                return j < n && lane < boxes && k < len ? __ldg(table + (k >> P.page_log2)) : 0;
-            };
-            auto issue = [&](const CUtensorMap* map, int j, int page) {
-                const uint32_t s = it % C::kStages;
-                if (!wait_warp(empty(s), ((it / C::kStages) & 1u) ^ 1u, abort)) return false;
-                ++it;
-                const int k0 = (W.t0 + j) * kTileKeys, need = (min(kTileKeys, len - k0) + box - 1) / box;
-                const uint32_t dst = ring + s * C::kTile;
-                if (lane == 0) mbar_expect_tx(full(s), (uint32_t)(need * box * 128 * (DC / 64)));
-                __syncwarp();
-                if (lane < need) {
-                    if (page < 0 || page >= a.c.n_pages) {  // reads as zeros past the last page
-                        if (a.status) atomicOr(a.status, PPS_FLAG_INDEX);
-                        page = (int)a.c.n_pages;
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        if (warp < kMmaWarp) {
+            // ---- one warp loads the keys' tiles, one the values'.  The ring holds them in the order of their use: K of
+            // the first tile (or two, one per stream), then V_j and the next K in turn.
+            const bool is_v = warp != kLoadWarp;
+            const int box = min(kTileKeys, a.c.page_size), boxes = kTileKeys / box, box_log2 = 31 - __clz(boxes);
+            // the segment's first place in the ring; one past the last place this warp filled, and which it filled before it
+            uint32_t ring0 = 0, last = 0, filled = 0;
+            bool ok = true;
+            while (ok && W.next(a, P)) {
+                const int n = W.t1 - W.t0, ahead = W.rows <= kTileRows ? 2 : 1, len = W.q.len;
+                const int32_t* table = a.pages + (int64_t)W.s * a.pages_stride;
+                // pages of 32 boxes at a time, one per lane; the next 32 are on their way
+                const int per = 32 >> box_log2;  // tiles of 32 boxes
+                auto pages_from = [&](int j) {
+                    const int64_t k = (int64_t)(W.t0 + j) * kTileKeys + lane * box;
+                    return k < len && j < n ? __ldg(table + (k >> P.page_log2)) : 0;
+                };
+                int cur = pages_from(0), nxt = pages_from(per);
+                for (int j = 0; j < n; ++j) {
+                    if (j > 0 && (j & (per - 1)) == 0) {
+                        cur = nxt;
+                        nxt = pages_from(j + per);
                     }
-                    const int in_page = (k0 + lane * box) & (a.c.page_size - 1);
+                    const uint32_t it = ring0 + (is_v ? (j + ahead < n ? ahead + 2 * j : n + j) : j < ahead ? j : 2 * j - ahead + 1);
+                    const uint32_t s = it % C::kStages;
+                    if (!(ok = wait_warp(empty(s), ((it / C::kStages) & 1u) ^ 1u, abort))) break;
+                    filled = (filled << (it + 1 - last)) | 1u;
+                    last = it + 1;
+                    const int k0 = (W.t0 + j) * kTileKeys, need = (min(kTileKeys, len - k0) + box - 1) / box;
+                    const uint32_t dst = ring + s * C::kTile;
+                    int page = __shfl_sync(0xffffffffu, cur, ((j & (per - 1)) << box_log2) + (lane & (boxes - 1)));
+                    if (lane == 0) mbar_expect_tx(full(s), (uint32_t)(need * box * 128 * (DC / 64)));
+                    __syncwarp();
+                    if (lane < need) {
+                        if (page < 0 || page >= a.c.n_pages) {  // reads as zeros past the last page
+                            if (a.status) atomicOr(a.status, PPS_FLAG_INDEX);
+                            page = (int)a.c.n_pages;
+                        }
+                        const int in_page = (k0 + lane * box) & (a.c.page_size - 1);
 #pragma unroll
-                    for (int b = 0; b < DC / 64; ++b)
-                        tma_load_4d(dst + b * C::kBlock + lane * box * 128, map, full(s), b * 64, in_page, W.kvh, page);
+                        for (int b = 0; b < DC / 64; ++b)
+                            if (is_v)
+                                tma_load_4d(dst + b * C::kBlock + lane * box * 128, &tmV, full(s), b * 64, in_page, W.kvh, page);
+                            else
+                                tma_load_4d(dst + b * C::kBlock + lane * box * 128, &tmK, full(s), b * 64, in_page, W.kvh, page);
+                    }
                 }
-                return true;
-            };
-            int p0 = page_of(0), p1 = page_of(1), p2 = page_of(2);
-            if (n > 0) ok = issue(&tmK, 0, p0);
-            if (ok && ahead == 2 && n > 1) ok = issue(&tmK, 1, p1);
-            for (int j = 0; j < n && ok; ++j) {
-                const int p3 = page_of(j + 3);
-                ok = issue(&tmV, j, p0);
-                if (ok && j + ahead < n) ok = issue(&tmK, j + ahead, ahead == 2 ? p2 : p1);
-                p0 = p1;
-                p1 = p2;
-                p2 = p3;
+                ring0 += 2 * n;
             }
-        }
-        // copies in flight when the CTA gives up: wait (bounded) for each
-        const uint32_t from = it > (uint32_t)C::kStages ? it - C::kStages : 0u;
-        for (uint32_t j = from; j < it && *abort; ++j)
-            for (uint32_t n = 0; n < kWaitLimit && !mbar_try_wait(full(j % C::kStages), (j / C::kStages) & 1u); ++n) {
-            }
-    } else if (warp == kMmaWarp) {
+            // copies in flight when the CTA gives up: wait (bounded) for each
+            for (uint32_t j = 0; j < (uint32_t)C::kStages && *abort; ++j)
+                if (filled >> j & 1u)
+                    for (uint32_t n = 0, i = last - 1 - j; n < kWaitLimit && !mbar_try_wait(full(i % C::kStages), (i / C::kStages) & 1u); ++n) {
+                    }
+        } else if (warp == kMmaWarp) {
         // ---- products (one thread): per stream S = Q K^T, then O += P V as its weights arrive
-        if (lane == 0) {
-            const uint32_t dn = (uint32_t)(D + 15) / 16;  // 16-channel steps
-            const uint32_t id_qk = (1u << 4) | (H::kType << 7) | (H::kType << 10) | ((kTileKeys / 8u) << 17) | ((kTileRows / 16u) << 24);
-            const uint32_t id_pv = (1u << 4) | (H::kType << 7) | (H::kType << 10) | (1u << 16) | ((dn * 2u) << 17) | ((kTileRows / 16u) << 24);
+        // Straight-line products of the class's full width (channels past head_dim are zeros): in a loop they issue at
+        // 100 cycles each, so at the tensor core's 64.  No product stands under a condition of its own.
+        if (elect_one()) {
+            constexpr uint32_t id_qk = (1u << 4) | (H::kType << 7) | (H::kType << 10) | ((kTileKeys / 8u) << 17) | ((kTileRows / 16u) << 24);
+            constexpr uint32_t id_pv = (1u << 4) | (H::kType << 7) | (H::kType << 10) | (1u << 16) | ((DC / 8u) << 17) | ((kTileRows / 16u) << 24);
             uint32_t it = 0, np0 = 0, np1 = 0, segs = 0;
             auto stage = [&](uint32_t i) { return ring + (i % C::kStages) * C::kTile; };
             auto landed = [&](uint32_t i) {
@@ -409,16 +419,19 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                 return ok;
             };
             auto scores = [&](uint32_t w, uint32_t tile, uint32_t k) {
-                for (uint32_t c = 0; c < dn; ++c) {
-                    const uint32_t o = (c >> 2) * C::kBlock + (c & 3u) * 32u;
-                    tc_mma(tmem + w * 128u, sw128_desc(base + tile * C::kTile + o), sw128_desc(stage(k) + o), id_qk, c != 0);
+                const uint64_t qd = sw128_desc(base + tile * C::kTile), kd = sw128_desc(stage(k));
+#pragma unroll
+                for (uint32_t c = 0; c < DC / 16; ++c) {
+                    const uint64_t o = ((c >> 2) * C::kBlock + (c & 3u) * 32u) >> 4;
+                    tc_mma(tmem + w * 128u, qd + o, kd + o, id_qk, c != 0);
                 }
                 tc_commit(sfull(w));
             };
             auto values = [&](uint32_t w, uint32_t v, bool first) {
+                const uint64_t vd = sw128_desc_mn(stage(v), C::kBlock);
+#pragma unroll
                 for (uint32_t c = 0; c < kTileKeys / 16; ++c)
-                    tc_mma_ts(tmem + kColO + w * 128u, tmem + w * 128u + c * 8u,
-                              sw128_desc_mn(stage(v) + c * 2048u, C::kBlock), id_pv, !first || c != 0);
+                    tc_mma_ts(tmem + kColO + w * 128u, tmem + w * 128u + c * 8u, vd + c * (2048u >> 4), id_pv, !first || c != 0);
                 tc_commit(odone(w));
             };
             bool ok = true;
@@ -481,7 +494,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             }
         }
         __syncwarp();
-    }
+        }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         // ---- softmax: warpgroup w drives stream w, thread = row r of its tile
@@ -547,6 +560,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, v[c]);
                     tmem_wait_ld();
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_landed(v[c]);
                     if (__any_sync(0xffffffffu, k0 + kTileKeys > plain)) {
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
@@ -559,11 +574,11 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                     float mx[4];
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        mx[c] = __uint_as_float(v[c][0]);
+                        mx[c] = fmaxf(__uint_as_float(v[c][0]), __uint_as_float(v[c][1]));
 #pragma unroll
-                        for (int e = 1; e < 32; ++e) mx[c] = fmaxf(mx[c], __uint_as_float(v[c][e]));
+                        for (int e = 2; e < 32; e += 2) mx[c] = max3(mx[c], __uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1]));
                     }
-                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                    const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]);
                     if (__any_sync(0xffffffffu, (top - m) * P.sc > kLazy)) {
                         const float M = fmaxf(m, top), f = m == M ? 1.0f : ex2((m - M) * P.sc);
                         m = M;
@@ -576,6 +591,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                                 uint32_t o[32];
                                 tmem_ld32(tO + w * 128u + c, o);
                                 tmem_wait_ld();
+                                tmem_landed(o);
 #pragma unroll
                                 for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
                                 tmem_st32(tO + w * 128u + c, o);
@@ -673,6 +689,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                     if (n > 0) {
                         tmem_ld32(tO + first * 128u + c, o);
                         tmem_wait_ld();
+                        tmem_landed(o);
                     }
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
@@ -681,6 +698,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                         uint32_t o1[32];
                         tmem_ld32(tO + 128u + c, o1);
                         tmem_wait_ld();
+                        tmem_landed(o1);
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
                             if (f1 != 0.0f) o[e] = __float_as_uint(fmaf(__uint_as_float(o1[e]), f1, __uint_as_float(o[e])));
