@@ -4,9 +4,10 @@
 //
 // with the running maximum and sum of an online softmax, so that every key and value is read once per row block.
 //
-// Rows.  The tokens of a sequence and the heads that share a key head are packed into rows (token x group + head of
-// the group), so that a decoding step's few rows read their keys once.  A row block is 256 rows in two tiles of
-// 128 (tensor memory's lanes); a block of up to 128 rows is one tile.  Keys are taken 128 at a time.
+// Rows.  The tokens of a sequence and the heads that share a key head (group; taken gs <= 128 at a time) are packed
+// into rows, token after token, so that a decoding step's few rows read their keys once.  A tile is 128 rows (tensor
+// memory's lanes) of which tt gs are used, tt = 128 / gs whole tokens: one TMA box of queries.  A row block is two
+// tiles, or one where its tokens fit into one.  Keys are taken 128 at a time.
 //
 // Two streams.  Each of two softmax warpgroups drives one stream: scores S = Q K^T into its own 128 columns of
 // tensor memory, weights P written over them in 16 bits, O += P V into its own accumulator (P is read from tensor
@@ -44,8 +45,9 @@ namespace {
 using namespace tc;
 
 constexpr int kTileRows = 128, kTileKeys = 128;
-constexpr int kAttnThreads = 384;  // two softmax warpgroups; the loading warps (keys, values), the issuing warp, an idle one
-constexpr int kLoadWarp = 8, kMmaWarp = 10;
+constexpr int kAttnThreads = 384;  // two softmax warpgroups; warps that load keys, values, issue products, load queries
+constexpr int kLoadWarp = 8, kMmaWarp = 10, kQueryWarp = 11;
+static_assert(32 * (kQueryWarp + 1) == kAttnThreads, "the last warp loads the queries");
 constexpr int kMaxCtas = 160;      // shares of the work (one per SM)
 constexpr int kFix = 1;            // key tiles that an item's start and end cost
 constexpr float kLazy = 8.0f;      // log2 of the rise of a maximum that O is not rescaled for
@@ -57,20 +59,23 @@ struct Cfg {
     static constexpr int kBlock = 128 * 128;                 // 128 rows of 64 channels, 128-byte swizzle
     static constexpr int kTile = kBlock * (DC / 64);         // 16 or 32 KB: a tile of Q, K or V
     static constexpr int kStages = (224 * 1024 - 2 * kTile) / kTile;  // 5 (or 12) tiles of K and V in flight
-    static constexpr int kSmem = (2 + kStages) * kTile + 1024 /* alignment */ + 512 /* barriers, plan */;
-    static_assert(8 * (2 * kStages + 8) <= 288, "barriers fit");
+    static constexpr int kBars = 8 * (2 * kStages + 11);
+    static constexpr int kSmem = (2 + kStages) * kTile + 288 /* barriers */ + 224 /* plan */ + 2048 /* maxima and sums */;
+    static_assert(kBars <= 288 && kSmem <= 227 * 1024, "barriers and shared memory fit");
 };
 
-// a cut item: nsplit partial results of rows x head_dim, in slot 2 cta + 1 and slots 2 (cta + k), k = 1 .. nsplit - 1
+// a cut item: nsplit partial results of a block of ntok tokens from tok0 on, in slot 2 cta + 1 and slots 2 (cta + k),
+// k = 1 .. nsplit - 1
 struct Cut {
-    int32_t nsplit, rows, row0, off, kvh, pad[3];
+    int32_t nsplit, ntok, tok0, vh;
 };
 
 struct AttnPlan {
-    int group, cap_rows, page_log2;
+    int group, gs, nsub, tt;  // heads of a key head; those taken at a time, in nsub turns; tokens per tile
+    int cap_rows, page_log2;
     int64_t cap_keys;   // what a row of the page table holds
     float sc;           // |scale| log2 e
-    uint32_t q_and, q_xor;  // on pairs of query values: a negative scale turns their signs, a zero one clears them
+    uint32_t s_and, s_xor;  // on scores: a negative scale turns their signs, a zero one clears them
     Cut* cuts;          // [gridDim.x]
     float* part_o;      // [2 gridDim.x][cap_rows][DC]
     float2* part_ml;    // [2 gridDim.x][cap_rows] (maximum, sum)
@@ -95,73 +100,67 @@ __device__ __forceinline__ Seq load_seq(const AttnArgs& a, const AttnPlan& P, in
 // key tiles of row block `blk`: those its last token sees
 __device__ __forceinline__ int block_tiles(const AttnArgs& a, const AttnPlan& P, const Seq& q, int blk) {
     int vis = q.len;
-    if (a.mask == nullptr) {
-        const int64_t last = min((int64_t)q.n * P.group, (int64_t)(blk + 1) * 2 * kTileRows) - 1;
-        vis = max(0, q.len - q.n + (int)(last / P.group) + 1);
-    }
+    if (a.mask == nullptr) vis = max(0, q.len - q.n + min(q.n, (blk + 1) * 2 * P.tt));
     return (vis + kTileKeys - 1) / kTileKeys;
 }
 __device__ __forceinline__ int n_blocks(const AttnPlan& P, const Seq& q) {
-    return (int)(((int64_t)q.n * P.group + 2 * kTileRows - 1) / (2 * kTileRows));
+    return (int)(((uint32_t)q.n + 2u * P.tt - 1u) / (2u * P.tt));
 }
 __device__ __forceinline__ int64_t head_cost(const AttnArgs& a, const AttnPlan& P, const Seq& q) {
-    int64_t c = 0;
     const int nb = n_blocks(P, q);
+    if (nb == 1 || a.mask != nullptr) return (int64_t)nb * (block_tiles(a, P, q, 0) + kFix);
+    int64_t c = 0;
     for (int b = 0; b < nb; ++b) c += block_tiles(a, P, q, b) + kFix;
     return c;
 }
+__device__ __forceinline__ int64_t divide(int64_t x, int64_t y) {  // of non-negative numbers, most of them small
+    return (x | y) >> 32 ? x / y : (int64_t)((uint32_t)x / (uint32_t)y);
+}
+
+// where a share starts
+struct Start {
+    int64_t base;  // the block's start on the line
+    int s, vh, blk;
+    Seq q;
+};
 
 // A CTA's items in order; every warp walks them by itself.
 struct Walk {
-    int64_t x, x1, base;  // where the walk is, the share's end, the current block's start
-    int s, kvh, blk, nb;
+    int64_t x, x1, base;  // where the walk is, the share's end, the next block's start
+    int s, vh, blk, nb;   // the next block: sequence, turn of a key head (key head x nsub + turn), number; blocks of the sequence
     Seq q;
-    // the segment: key tiles t0 .. t1 - 1 of T
-    int t0, t1, T, rows;
+    // the segment: key tiles t0 .. t1 - 1 of T of a block that starts at `from` on the line, with tokens i0 .. i0 + ntok - 1
+    int64_t from;
+    int t0, t1, T, i0, ntok;
+    int heads;  // the segment's vh
 
-    __device__ __forceinline__ void start(const AttnArgs& a, const AttnPlan& P, int64_t c0, int64_t c1, int s0, int64_t s_base) {
-        x = c0;
-        x1 = c1;
-        s = s0;
-        kvh = blk = nb = 0;
-        base = c0;
-        if (c0 >= c1) return;
-        q = load_seq(a, P, s, false);
-        nb = n_blocks(P, q);
-        int64_t rem = c0 - s_base;
-        const int64_t per = head_cost(a, P, q);
-        kvh = (int)(rem / per);
-        rem -= kvh * per;
-        for (int c; rem >= (c = block_tiles(a, P, q, blk) + kFix); ++blk) rem -= c;
-        base = c0 - rem;
-    }
+    __device__ __forceinline__ Walk(const AttnPlan& P, const Start& st, int64_t c0, int64_t c1)
+        : x(c0), x1(c1), base(st.base), s(st.s), vh(st.vh), blk(st.blk), nb(n_blocks(P, st.q)), q(st.q) {}
     __device__ __forceinline__ bool next(const AttnArgs& a, const AttnPlan& P) {
         while (x < x1) {
-            while (blk >= nb) {  // the next key head, or the next sequence with tokens
+            while (blk >= nb) {  // the next turn of heads, or the next sequence with tokens
                 blk = 0;
-                if (nb == 0 || ++kvh == a.c.n_kv_heads) {
-                    kvh = 0;
+                if (nb == 0 || ++vh == a.c.n_kv_heads * P.nsub) {
+                    vh = 0;
                     if (++s >= a.n_seq) return false;
                     q = load_seq(a, P, s, false);
                     nb = n_blocks(P, q);
                 }
             }
             T = block_tiles(a, P, q, blk);
-            rows = (int)min((int64_t)q.n * P.group - (int64_t)blk * 2 * kTileRows, (int64_t)2 * kTileRows);
+            i0 = blk * 2 * P.tt;
+            ntok = min(q.n - i0, 2 * P.tt);
             t0 = (int)(x - base);
             t1 = (int)min(x1 - base, (int64_t)T);
-            const bool mine = t0 < t1 || (T == 0 && t0 == 0);
-            row0 = blk * 2 * kTileRows;
-            start_ = base;
+            from = base;
+            heads = vh;
             base += T + kFix;
             x = base;
             ++blk;
-            if (mine) return true;
+            if (t0 < t1 || (T == 0 && t0 == 0)) return true;
         }
         return false;
     }
-    int row0;
-    int64_t start_;
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -239,30 +238,41 @@ __device__ __forceinline__ uint32_t seen_bits(int k0, int vis, int prefix, const
 
 template <typename T, int DC>
 __global__ void __launch_bounds__(kAttnThreads, 1)
-    attention_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttnArgs a,
-                     const AttnPlan P) {
+    attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                     const __grid_constant__ CUtensorMap tmV, const AttnArgs a, const AttnPlan P) {
     using C = Cfg<DC>;
     using H = Half<T>;
-    extern __shared__ uint8_t attn_smem_raw[];
-    const uint32_t raw = smem_u32(attn_smem_raw);
-    const uint32_t base = (raw + 1023u) & ~1023u;
-    uint8_t* gbase = attn_smem_raw + (base - raw);
+    extern __shared__ __align__(1024) uint8_t attn_smem[];
+    const uint32_t base = smem_u32(attn_smem);
     const uint32_t ring = base + 2 * C::kTile;
     const uint32_t bars = ring + C::kStages * C::kTile;
-    auto full = [&](uint32_t s) { return bars + 8u * s; };
-    auto empty = [&](uint32_t s) { return bars + 8u * (C::kStages + s); };
-    auto sfull = [&](uint32_t w) { return bars + 8u * (2 * C::kStages + w); };
-    auto pready = [&](uint32_t w) { return bars + 8u * (2 * C::kStages + 2 + w); };
-    auto odone = [&](uint32_t w) { return bars + 8u * (2 * C::kStages + 4 + w); };
-    const uint32_t qfull = bars + 8u * (2 * C::kStages + 6), segbar = bars + 8u * (2 * C::kStages + 7);
-    uint8_t* tail = gbase + (2 + C::kStages) * C::kTile + 288;
+    auto bar = [&](uint32_t i) { return bars + 8u * i; };
+    auto full = [&](uint32_t s) { return bar(s); };
+    auto empty = [&](uint32_t s) { return bar(C::kStages + s); };
+    auto sfull = [&](uint32_t w) { return bar(2 * C::kStages + w); };
+    auto pready = [&](uint32_t w) { return bar(2 * C::kStages + 2 + w); };
+    auto odone = [&](uint32_t w) { return bar(2 * C::kStages + 4 + w); };
+    auto qfull = [&](uint32_t t) { return bar(2 * C::kStages + 6 + t); };
+    auto qfree = [&](uint32_t t) { return bar(2 * C::kStages + 8 + t); };
+    const uint32_t segbar = bar(2 * C::kStages + 10);
+    uint8_t* tail = attn_smem + (2 + C::kStages) * C::kTile + 288;
     volatile int* abort = reinterpret_cast<volatile int*>(tail);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 4);
-    int* s_seq = reinterpret_cast<int*>(tail + 8);
-    int64_t* s_sum = reinterpret_cast<int64_t*>(tail + 16);   // [12] warp sums, then the sequence's start
+    int64_t* s_sum = reinterpret_cast<int64_t*>(tail + 16);          // [12] warp sums
+    Start* s_start = reinterpret_cast<Start*>(tail + 16 + 12 * 8);
+    float2* s_ml = reinterpret_cast<float2*>(tail + 224);            // [2][128]
+    static_assert(16 + 12 * 8 + sizeof(Start) <= 224, "plan fits");
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
     pdl_launch_dependents();
+    // the first sequence of each thread: its loads are on their way while the barriers are set up
+    Seq own = {0, 0, 0};
+    if (tid < a.n_seq) own = load_seq(a, P, tid, cta == 0);
+    if ((base & 1023u) != 0) {  // the swizzled tiles need this alignment
+        if (tid == 0) P.cuts[cta].nsplit = 0;
+        if (tid == 0 && cta == 0 && a.status) atomicOr(a.status, PPS_FLAG_TIMEOUT);
+        return;
+    }
     if (tid == 0) {
         for (int s = 0; s < C::kStages; ++s) {
             mbar_init(full(s), 1);
@@ -273,23 +283,24 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             mbar_init(pready(w), 4);
             mbar_init(odone(w), 1);
         }
-        mbar_init(qfull, 8);
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(qfull(t), 1);
+            mbar_init(qfree(t), 1);
+        }
         mbar_init(segbar, 8);
         *abort = 0;
-        *s_seq = a.n_seq;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         P.cuts[cta].nsplit = 0;
     }
     if (warp == kLoadWarp && lane == 0) {
+        tma_prefetch_map(&tmQ);
         tma_prefetch_map(&tmK);
         tma_prefetch_map(&tmV);
     }
 
-    // the share: [c0, c1) of the line of costs, and the sequence in which it starts
-    auto cost = [&](int s, bool flag) {
-        const Seq q = load_seq(a, P, s, flag);
-        return q.n > 0 ? head_cost(a, P, q) * a.c.n_kv_heads : (int64_t)0;
-    };
+    // the share: [c0, c1) of the line of costs, and where on it the share starts
+    const int n_vh = a.c.n_kv_heads * P.nsub;
+    auto cost = [&](const Seq& q) { return q.n > 0 ? head_cost(a, P, q) * n_vh : (int64_t)0; };
     auto block_scan = [&](int64_t v, int64_t& total) {  // inclusive
         int64_t w = v;
 #pragma unroll
@@ -308,9 +319,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
         }
         return w;
     };
-    const int64_t mine = tid < a.n_seq ? cost(tid, cta == 0) : 0;
+    const int64_t mine = cost(own);
     int64_t more = 0;
-    for (int64_t s = tid + kAttnThreads; s < a.n_seq; s += kAttnThreads) more += cost((int)s, cta == 0);
+    for (int64_t s = tid + kAttnThreads; s < a.n_seq; s += kAttnThreads) more += cost(load_seq(a, P, (int)s, cta == 0));
     int64_t U, U0;
     int64_t at = block_scan(mine, U0);
     U = U0;
@@ -318,19 +329,29 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
         block_scan(more, U);
         U += U0;
     }
-    const int64_t share = max((U + gridDim.x - 1) / gridDim.x, (int64_t)1);
+    const int64_t share = max(divide(U + gridDim.x - 1, gridDim.x), (int64_t)1);
     const int64_t c0 = min(cta * share, U), c1 = min(c0 + share, U);
     if (c0 < c1) {
-        int64_t before = 0;
-        int64_t v = mine;
+        int64_t before = 0, v = mine;
         for (int64_t b = 0;; b += kAttnThreads) {
-            if (c0 >= before + at - v && c0 < before + at) {
-                *s_seq = (int)(b + tid);
-                s_sum[12] = before + at - v;
+            if (c0 >= before + at - v && c0 < before + at) {  // one thread: its sequence holds the start
+                Start st;
+                st.s = (int)(b + tid);
+                st.q = own;
+                const int64_t per = divide(v, n_vh);
+                int64_t rem = c0 - (before + at - v);
+                st.vh = (int)divide(rem, per);
+                rem -= st.vh * per;
+                st.blk = 0;
+                for (int c; rem >= (c = block_tiles(a, P, own, st.blk) + kFix); ++st.blk) rem -= c;
+                st.base = c0 - rem;
+                *s_start = st;
             }
             before += U0;
             if (before > c0) break;  // CTA-uniform
-            v = b + kAttnThreads + tid < a.n_seq ? cost((int)(b + kAttnThreads + tid), false) : 0;
+            own.n = 0;
+            if (b + kAttnThreads + tid < a.n_seq) own = load_seq(a, P, (int)(b + kAttnThreads + tid), false);
+            v = cost(own);
             at = block_scan(v, U0);
         }
     }
@@ -343,8 +364,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
     tc_fence_after();
     if (c0 >= c1) return;
     const uint32_t tmem = *tmem_slot;
-    Walk W;
-    W.start(a, P, c0, c1, *s_seq, s_sum[12]);
+    Walk W(P, *s_start, c0, c1);
     const int D = a.c.head_dim;
 
     // registers: 384 x 168 at launch = 256 x 208 + 128 x 88
@@ -359,7 +379,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             uint32_t ring0 = 0, last = 0, filled = 0;
             bool ok = true;
             while (ok && W.next(a, P)) {
-                const int n = W.t1 - W.t0, ahead = W.rows <= kTileRows ? 2 : 1, len = W.q.len;
+                const int n = W.t1 - W.t0, ahead = W.ntok <= P.tt ? 2 : 1, len = W.q.len, kvh = W.heads / P.nsub;
                 const int32_t* table = a.pages + (int64_t)W.s * a.pages_stride;
                 // pages of 32 boxes at a time, one per lane; the next 32 are on their way
                 const int per = 32 >> box_log2;  // tiles of 32 boxes
@@ -392,9 +412,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
 #pragma unroll
                         for (int b = 0; b < DC / 64; ++b)
                             if (is_v)
-                                tma_load_4d(dst + b * C::kBlock + lane * box * 128, &tmV, full(s), b * 64, in_page, W.kvh, page);
+                                tma_load_4d(dst + b * C::kBlock + lane * box * 128, &tmV, full(s), b * 64, in_page, kvh, page);
                             else
-                                tma_load_4d(dst + b * C::kBlock + lane * box * 128, &tmK, full(s), b * 64, in_page, W.kvh, page);
+                                tma_load_4d(dst + b * C::kBlock + lane * box * 128, &tmK, full(s), b * 64, in_page, kvh, page);
                     }
                 }
                 ring0 += 2 * n;
@@ -411,14 +431,14 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
         if (elect_one()) {
             constexpr uint32_t id_qk = (1u << 4) | (H::kType << 7) | (H::kType << 10) | ((kTileKeys / 8u) << 17) | ((kTileRows / 16u) << 24);
             constexpr uint32_t id_pv = (1u << 4) | (H::kType << 7) | (H::kType << 10) | (1u << 16) | ((DC / 8u) << 17) | ((kTileRows / 16u) << 24);
-            uint32_t it = 0, np0 = 0, np1 = 0, segs = 0;
+            uint32_t it = 0, np0 = 0, np1 = 0, nq0 = 0, nq1 = 0, turn = 0;
             auto stage = [&](uint32_t i) { return ring + (i % C::kStages) * C::kTile; };
             auto landed = [&](uint32_t i) {
                 const bool ok = mbar_wait(full(i % C::kStages), (i / C::kStages) & 1u, abort);
                 tc_fence_after();
                 return ok;
             };
-            auto scores = [&](uint32_t w, uint32_t tile, uint32_t k) {
+            auto scores = [&](uint32_t w, uint32_t tile, uint32_t k, bool last) {  // last: the segment needs the queries no more
                 const uint64_t qd = sw128_desc(base + tile * C::kTile), kd = sw128_desc(stage(k));
 #pragma unroll
                 for (uint32_t c = 0; c < DC / 16; ++c) {
@@ -426,6 +446,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                     tc_mma(tmem + w * 128u, qd + o, kd + o, id_qk, c != 0);
                 }
                 tc_commit(sfull(w));
+                if (last) tc_commit(qfree(tile));
             };
             auto values = [&](uint32_t w, uint32_t v, bool first) {
                 const uint64_t vd = sw128_desc_mn(stage(v), C::kBlock);
@@ -437,14 +458,12 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             bool ok = true;
             while (ok && W.next(a, P)) {
                 const int n = W.t1 - W.t0;
-                ok = mbar_wait(qfull, segs++ & 1u, abort);
-                if (!ok || n == 0) continue;
-                tc_fence_after();
-                if (W.rows > kTileRows) {  // a tile per stream, the same keys
-                    ok = landed(it);
+                if (n == 0) continue;
+                if (W.ntok > P.tt) {  // a tile per stream, the same keys
+                    ok = mbar_wait(qfull(0), nq0++ & 1u, abort) && mbar_wait(qfull(1), nq1++ & 1u, abort) && landed(it);
                     if (!ok) break;
-                    scores(0, 0, it);
-                    scores(1, 1, it);
+                    scores(0, 0, it, n == 1);
+                    scores(1, 1, it, n == 1);
                     tc_commit(empty(it % C::kStages));
                     ++it;
                     for (int j = 0; j < n && ok; ++j) {
@@ -460,17 +479,20 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                             if (more_keys) {
                                 if (w == 0) ok = landed(k);
                                 if (!ok) break;
-                                scores(w, w, k);
+                                scores(w, w, k, j + 2 == n);
                                 if (w == 1) tc_commit(empty(k % C::kStages));
                             }
                         }
                         it += more_keys ? 2 : 1;
                     }
                 } else {  // one tile, every other key tile per stream
+                    const uint32_t tile = turn;
+                    turn ^= 1u;
+                    ok = mbar_wait(qfull(tile), (tile ? nq1++ : nq0++) & 1u, abort);
                     for (int j = 0; j < min(n, 2) && ok; ++j) {
                         ok = landed(it);
                         if (!ok) break;
-                        scores(j, 0, it);
+                        scores(j, tile, it, j + 1 == n);
                         tc_commit(empty(it % C::kStages));
                         ++it;
                     }
@@ -485,7 +507,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                         if (j + 2 < n) {
                             ok = landed(it);
                             if (!ok) break;
-                            scores(w, 0, it);
+                            scores(w, tile, it, j + 3 == n);
                             tc_commit(empty(it % C::kStages));
                             ++it;
                         }
@@ -494,17 +516,47 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             }
         }
         __syncwarp();
+        } else {
+            // ---- queries: both tiles of a block of two, or the tile that the last block of one did not use
+            uint32_t n0 = 0, n1 = 0, turn = 0;
+            bool ok = true;
+            while (ok && W.next(a, P)) {
+                if (W.t0 == W.t1) continue;
+                const bool two = W.ntok > P.tt;
+                const int kvh = W.heads / P.nsub, sub = W.heads - kvh * P.nsub;
+                for (uint32_t i = 0; i < (two ? 2u : 1u) && ok; ++i) {
+                    const uint32_t tile = two ? i : turn;
+                    ok = wait_warp(qfree(tile), ((tile ? n1 : n0) & 1u) ^ 1u, abort);
+                    if (!ok) break;
+                    if (tile) ++n1; else ++n0;
+                    if (lane == 0) {
+                        mbar_expect_tx(qfull(tile), (uint32_t)(P.gs * P.tt * 128 * (DC / 64)));
+#pragma unroll
+                        for (int b = 0; b < DC / 64; ++b)
+                            tma_load_4d(base + tile * C::kTile + b * C::kBlock, &tmQ, qfull(tile), b * 64, sub * P.gs,
+                                        W.q.off + W.i0 + (int)i * P.tt, kvh);
+                    }
+                    __syncwarp();
+                }
+                if (!two) turn ^= 1u;
+            }
+            // copies in flight when the CTA gives up: wait (bounded) for each
+            for (uint32_t tile = 0; tile < 2 && *abort; ++tile) {
+                const uint32_t u = tile ? n1 : n0;
+                for (uint32_t n = 0; u > 0 && n < kWaitLimit && !mbar_try_wait(qfull(tile), (u - 1) & 1u); ++n) {
+                }
+            }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         // ---- softmax: warpgroup w drives stream w, thread = row r of its tile
         const uint32_t w = warp >> 2, q4 = warp & 3;
         const int r = (int)(q4 * 32) + lane;
+        const int row_tok = r / P.gs, row_head = r - row_tok * P.gs;  // the row's token in its tile, its head of the turn
         const uint32_t lanes = (q4 * 32u) << 16;
         const uint32_t tS = tmem + lanes + w * 128u, tO = tmem + lanes + kColO;
         uint32_t done = 0, done_other = 0;  // tiles of this stream and of the other one so far
         uint32_t it = 0, syncs = 0;
-        float2* s_ml = reinterpret_cast<float2*>(gbase + C::kTile);  // [2][128], in the second query tile's place
         auto seg_sync = [&]() {
             __syncwarp();
             if (lane == 0) mbar_arrive(segbar);
@@ -512,39 +564,14 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
         };
         bool ok = true;
         while (ok && W.next(a, P)) {
-            const bool two = W.rows > kTileRows;  // a tile per stream
+            const bool two = W.ntok > P.tt;  // a tile per stream
             const int n = W.t1 - W.t0;
-            {  // queries: 16-byte chunks, swizzled as TMA would write them
-                constexpr int kChunks = DC / 8, kRp = 32 / kChunks;
-                const int nrow = two ? 32 : 16, r0 = two ? (int)q4 * 32 : (int)(w * 64 + q4 * 16);
-                const int tile = two ? (int)w : 0, chunk = lane % kChunks;
-                const uint32_t dst = base + tile * C::kTile + (chunk >> 3) * C::kBlock;
-#pragma unroll 4
-                for (int p = 0; p < nrow; p += kRp) {
-                    const int row = r0 + p + lane / kChunks, in = tile * kTileRows + row;
-                    if (in < ((W.rows + 31) & ~31)) {  // zeros in the rows past the last one of a warp
-                        const int pr = W.row0 + min(in, W.rows - 1), tok = pr / P.group, h = W.kvh * P.group + (pr - tok * P.group);
-                        uint4 x = make_uint4(0, 0, 0, 0);
-                        if (chunk * 8 < D && in < W.rows)
-                            x = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(a.q.p) + (int64_t)(W.q.off + tok) * a.q.tok +
-                                                                     h * a.q.head + chunk * 8));
-                        x.x = (x.x & P.q_and) ^ P.q_xor;
-                        x.y = (x.y & P.q_and) ^ P.q_xor;
-                        x.z = (x.z & P.q_and) ^ P.q_xor;
-                        x.w = (x.w & P.q_and) ^ P.q_xor;
-                        const uint32_t at = dst + row * 128 + (((chunk & 7) ^ (row & 7)) << 4);
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w)
-                                     : "memory");
-                    }
-                }
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(qfull);
-            }
+            const int kvh = W.heads / P.nsub, in_group = (W.heads - kvh * P.nsub) * P.gs + row_head;
+            const int in_tok = (two ? (int)w * P.tt : 0) + row_tok;  // in the block
+            const bool valid = row_tok < P.tt && in_tok < W.ntok && in_group < P.group;
+            const bool busy = __any_sync(0xffffffffu, valid);
+            const int tok = W.i0 + min(in_tok, W.ntok - 1), head = kvh * P.group + in_group;
             const int in_block = (two ? (int)w * kTileRows : 0) + r;
-            const bool valid = in_block < W.rows;
-            const bool busy = (two ? (int)w * kTileRows : 0) + (int)q4 * 32 < W.rows;  // warp-uniform
-            const int pr = W.row0 + min(in_block, W.rows - 1), tok = pr / P.group, head = W.kvh * P.group + (pr - tok * P.group);
             const int prefix = W.q.len - W.q.n;
             const uint32_t* mask = a.mask ? a.mask + (int64_t)(W.q.off + tok) * a.mask_words : nullptr;
             const int vis = mask ? W.q.len : prefix + tok + 1;
@@ -562,6 +589,12 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                     tmem_wait_ld();
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_landed(v[c]);
+                    if (P.s_xor != 0 || P.s_and == 0) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[c][e] = (v[c][e] & P.s_and) ^ P.s_xor;
+                    }
                     if (__any_sync(0xffffffffu, k0 + kTileKeys > plain)) {
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
@@ -579,7 +612,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                         for (int e = 2; e < 32; e += 2) mx[c] = max3(mx[c], __uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1]));
                     }
                     const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]);
-                    if (__any_sync(0xffffffffu, (top - m) * P.sc > kLazy)) {
+                    if (__any_sync(0xffffffffu, valid && (top - m) * P.sc > kLazy)) {
                         const float M = fmaxf(m, top), f = m == M ? 1.0f : ex2((m - M) * P.sc);
                         m = M;
                         l *= f;
@@ -642,12 +675,11 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             const bool whole = W.t0 == 0 && W.t1 == W.T;
             const int slot = 2 * cta + (W.t0 == 0 ? 1 : 0);
             if (tid == 0 && W.t0 == 0 && !whole) {
-                Cut c = {};
-                c.nsplit = (int)((W.start_ + W.T - 1) / share) - cta + 1;
-                c.rows = W.rows;
-                c.row0 = W.row0;
-                c.off = W.q.off;
-                c.kvh = W.kvh;
+                Cut c;
+                c.nsplit = (int)divide(W.from + W.T - 1, share) - cta + 1;
+                c.ntok = W.ntok;
+                c.tok0 = W.q.off + W.i0;
+                c.vh = W.heads;
                 P.cuts[cta] = c;
             }
             const uint32_t tiles = i, tiles_other = n + (two ? n : 0) - i;
@@ -751,7 +783,10 @@ __global__ void __launch_bounds__(256) join_kernel(const AttnArgs a, const AttnP
     const int lane = threadIdx.x & 31, D = a.c.head_dim;
     if (c.nsplit == 0) return;
     auto slot = [&](int k) { return (int64_t)(k == 0 ? 2 * blockIdx.x + 1 : 2 * (blockIdx.x + k)) * P.cap_rows; };
-    for (int row = blockIdx.y * 8 + (threadIdx.x >> 5); row < c.rows; row += 8 * gridDim.y) {
+    const int kvh = c.vh / P.nsub, sub = c.vh - kvh * P.nsub, gs = min(P.gs, P.group - sub * P.gs);
+    for (int i = blockIdx.y * 8 + (threadIdx.x >> 5); i < c.ntok * gs; i += 8 * gridDim.y) {
+        const int t = i / gs, h = i - t * gs;
+        const int row = t < P.tt ? t * P.gs + h : kTileRows + (t - P.tt) * P.gs + h;
         float M = -INFINITY;
         for (int k = lane; k < c.nsplit; k += 32) M = fmaxf(M, P.part_ml[slot(k) + row].x);
 #pragma unroll
@@ -782,7 +817,7 @@ __global__ void __launch_bounds__(256) join_kernel(const AttnArgs a, const AttnP
 #pragma unroll
         for (int s = 16; s > 0; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
         const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-        const int pr = c.row0 + row, tok = c.off + pr / P.group, head = c.kvh * P.group + pr % P.group;
+        const int tok = c.tok0 + t, head = kvh * P.group + sub * P.gs + h;
         if (lane * VW < D) {
             T* out = static_cast<T*>(a.out.p) + (int64_t)tok * a.out.tok + head * a.out.head + lane * VW;
             if constexpr (VW == 4)
@@ -797,10 +832,16 @@ __global__ void __launch_bounds__(256) join_kernel(const AttnArgs a, const AttnP
 
 // ---------------------------------------------------------------- host side
 
-int cap_rows(int64_t n_tok, int group) {
-    const int64_t r = std::min<int64_t>(n_tok * group, 2 * kTileRows);
-    return (int)((r + 31) / 32 * 32);
-}
+// the heads of a key head taken at a time, the tokens of a tile, the rows of a block
+struct Rows {
+    int nsub, gs, tt, cap;
+    Rows(int64_t n_tok, int group) {
+        nsub = (group + kTileRows - 1) / kTileRows;
+        gs = (group + nsub - 1) / nsub;
+        tt = kTileRows / gs;
+        cap = n_tok > tt ? 2 * kTileRows : (int)((n_tok * gs + 31) / 32 * 32);
+    }
+};
 int channel_class(int head_dim) { return head_dim <= 64 ? 64 : 128; }
 size_t cut_bytes() { return sizeof(Cut) * kMaxCtas; }
 size_t ml_bytes(int rows) { return sizeof(float2) * 2 * kMaxCtas * (size_t)rows; }
@@ -820,32 +861,49 @@ bool cache_map(CUtensorMap* m, const void* ptr, const CacheView& c, int dtype) {
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// the queries as [key head, token, head of the group, channel], loaded in boxes of tt tokens x gs heads x 64 channels
+bool query_map(CUtensorMap* m, const AttnArgs& a, const AttnPlan& P, int dtype) {
+    EncodeTiledFn f = encode_fn();
+    if (f == nullptr) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)a.c.head_dim, (cuuint64_t)P.group, (cuuint64_t)a.n_tok, (cuuint64_t)a.c.n_kv_heads};
+    const cuuint64_t strides[3] = {P.group > 1 ? (cuuint64_t)a.q.head * 2 : 256, a.n_tok > 1 ? (cuuint64_t)a.q.tok * 2 : 256,
+                                   a.c.n_kv_heads > 1 ? (cuuint64_t)a.q.head * P.group * 2 : 256};
+    const cuuint32_t box[4] = {64, (cuuint32_t)P.gs, (cuuint32_t)P.tt, 1}, es[4] = {1, 1, 1, 1};
+    return f(m, dtype == PPS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, a.q.p, dims, strides,
+             box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <typename T, int DC>
 cudaError_t launch(const AttnArgs& a, int dtype, cudaStream_t st) {
     AttnPlan P;
     P.group = a.n_heads / a.c.n_kv_heads;
-    P.cap_rows = cap_rows(a.n_tok, P.group);
+    const Rows rows(a.n_tok, P.group);
+    P.nsub = rows.nsub;
+    P.gs = rows.gs;
+    P.tt = rows.tt;
+    P.cap_rows = rows.cap;
     P.page_log2 = 0;
     while ((1 << P.page_log2) < a.c.page_size) ++P.page_log2;
     P.cap_keys = (int64_t)a.max_pages * a.c.page_size;
     const float scale = a.scale;
     P.sc = scale == 0.0f ? 1.0f : (float)((double)(scale < 0.0f ? -scale : scale) * 1.4426950408889634074);
-    P.q_and = scale == 0.0f ? 0u : 0xffffffffu;
-    P.q_xor = scale < 0.0f ? 0x80008000u : 0u;
+    P.s_and = scale == 0.0f ? 0u : 0xffffffffu;
+    P.s_xor = scale < 0.0f ? 0x80000000u : 0u;
     char* w = static_cast<char*>(a.ws);
     P.cuts = reinterpret_cast<Cut*>(w);
     w += cut_bytes();
     P.part_ml = reinterpret_cast<float2*>(w);
     w += ml_bytes(P.cap_rows);
     P.part_o = reinterpret_cast<float*>(w);
-    CUtensorMap tmK, tmV;
+    CUtensorMap tmQ, tmK, tmV;
     // an empty cache has nothing to read: any mapped memory will do for its maps
-    if (!cache_map(&tmK, a.c.n_pages > 0 ? a.c.k : a.ws, a.c, dtype) || !cache_map(&tmV, a.c.n_pages > 0 ? a.c.v : a.ws, a.c, dtype))
+    if (!query_map(&tmQ, a, P, dtype) || !cache_map(&tmK, a.c.n_pages > 0 ? a.c.k : a.ws, a.c, dtype) || !cache_map(&tmV, a.c.n_pages > 0 ? a.c.v : a.ws, a.c, dtype))
         return cudaErrorInvalidValue;
     cudaError_t e = cudaFuncSetAttribute(attention_kernel<T, DC>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<DC>::kSmem);
     if (e != cudaSuccess) return e;
     const int ctas = std::min(device_sm_count(), kMaxCtas);
-    attention_kernel<T, DC><<<ctas, kAttnThreads, Cfg<DC>::kSmem, st>>>(tmK, tmV, a, P);
+    attention_kernel<T, DC><<<ctas, kAttnThreads, Cfg<DC>::kSmem, st>>>(tmQ, tmK, tmV, a, P);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     return launch_pdl(join_kernel<T, DC>, dim3(ctas, std::min(16, P.cap_rows / 8)), dim3(256), 0, st, a, P);
@@ -859,7 +917,7 @@ cudaError_t by_channels(const AttnArgs& a, int dtype, cudaStream_t st) {
 }  // namespace
 
 size_t attention_workspace_bytes(int64_t n_tok, int n_heads, int n_kv_heads, int head_dim) {
-    const int rows = cap_rows(n_tok, (n_heads + n_kv_heads - 1) / n_kv_heads);
+    const int rows = Rows(n_tok, (n_heads + n_kv_heads - 1) / n_kv_heads).cap;
     return cut_bytes() + ml_bytes(rows) + sizeof(float) * 2 * kMaxCtas * (size_t)rows * channel_class(head_dim);
 }
 
