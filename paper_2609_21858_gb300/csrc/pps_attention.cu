@@ -264,15 +264,6 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
     static_assert(16 + 12 * 8 + sizeof(Start) <= 224, "plan fits");
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
-    pdl_launch_dependents();
-    // the first sequence of each thread: its loads are on their way while the barriers are set up
-    Seq own = {0, 0, 0};
-    if (tid < a.n_seq) own = load_seq(a, P, tid, cta == 0);
-    if ((base & 1023u) != 0) {  // the swizzled tiles need this alignment
-        if (tid == 0) P.cuts[cta].nsplit = 0;
-        if (tid == 0 && cta == 0 && a.status) atomicOr(a.status, PPS_FLAG_TIMEOUT);
-        return;
-    }
     if (tid == 0) {
         for (int s = 0; s < C::kStages; ++s) {
             mbar_init(full(s), 1);
@@ -290,13 +281,21 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
         mbar_init(segbar, 8);
         *abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        P.cuts[cta].nsplit = 0;
     }
     if (warp == kLoadWarp && lane == 0) {
         tma_prefetch_map(&tmQ);
         tma_prefetch_map(&tmK);
         tma_prefetch_map(&tmV);
     }
+    if (warp == kMmaWarp) {
+        tmem_alloc(smem_u32(tmem_slot), 512);
+        tmem_relinquish();
+    }
+    pdl_wait();  // what comes before this runs while the stream's last kernel ends
+    pdl_launch_dependents();
+    Seq own = {0, 0, 0};
+    if (tid < a.n_seq) own = load_seq(a, P, tid, cta == 0);
+    if (tid == 0) P.cuts[cta].nsplit = 0;
 
     // the share: [c0, c1) of the line of costs, and where on it the share starts
     const int n_vh = a.c.n_kv_heads * P.nsub;
@@ -355,21 +354,21 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             at = block_scan(v, U0);
         }
     }
-    if (warp == kMmaWarp && c0 < c1) {
-        tmem_alloc(smem_u32(tmem_slot), 512);
-        tmem_relinquish();
-    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (c0 >= c1) return;
     const uint32_t tmem = *tmem_slot;
+    if (c0 >= c1 || (base & 1023u) != 0) {  // no work (or a base that the swizzled tiles cannot have)
+        if (c0 < c1 && tid == 0 && a.status) atomicOr(a.status, PPS_FLAG_TIMEOUT);
+        if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
+        return;
+    }
     Walk W(P, *s_start, c0, c1);
     const int D = a.c.head_dim;
 
     // registers: 384 x 168 at launch = 256 x 208 + 128 x 88
     if (warp >= kLoadWarp) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp < kMmaWarp) {
             // ---- one warp loads the keys' tiles, one the values'.  The ring holds them in the order of their use: K of
             // the first tile (or two, one per stream), then V_j and the next K in turn.
@@ -548,7 +547,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ---- softmax: warpgroup w drives stream w, thread = row r of its tile
         const uint32_t w = warp >> 2, q4 = warp & 3;
         const int r = (int)(q4 * 32) + lane;
@@ -620,14 +619,14 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                             if (!(ok = wait_warp(odone(w), (done + i - 1) & 1u, abort))) break;
                             tc_fence_after();
 #pragma unroll 1
-                            for (int c = 0; c < D; c += 32) {
-                                uint32_t o[32];
-                                tmem_ld32(tO + w * 128u + c, o);
+                            for (int c = 0; c < D; c += 16) {  // few columns: the scores stay in registers
+                                uint32_t o[16];
+                                tmem_ld16(tO + w * 128u + c, o);
                                 tmem_wait_ld();
                                 tmem_landed(o);
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                                tmem_st32(tO + w * 128u + c, o);
+                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                                tmem_st16(tO + w * 128u + c, o);
                             }
                         }
                     }
@@ -773,51 +772,25 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
     if (tid == 0 && *abort && a.status) atomicOr(a.status, PPS_FLAG_TIMEOUT);
 }
 
-// Joins the partial results of the items that are cut between CTAs: a warp per row, its lanes the channels.
+// Joins the partial results of the items that are cut between CTAs.  A row has one warp (its lanes the channels), or up
+// to eight that share its parts where there are many (a long sequence's few rows); four parts are read at a time.
 template <typename T, int DC>
-__global__ void __launch_bounds__(256) join_kernel(const AttnArgs a, const AttnPlan P) {
+__global__ void __launch_bounds__(256, 4) join_kernel(const AttnArgs a, const AttnPlan P) {
     using H = Half<T>;
     constexpr int VW = DC / 32;
+    __shared__ float s_o[8][DC];
+    __shared__ float2 s_x[8];
     pdl_wait();
-    const Cut c = P.cuts[blockIdx.x];
-    const int lane = threadIdx.x & 31, D = a.c.head_dim;
-    if (c.nsplit == 0) return;
-    auto slot = [&](int k) { return (int64_t)(k == 0 ? 2 * blockIdx.x + 1 : 2 * (blockIdx.x + k)) * P.cap_rows; };
-    const int kvh = c.vh / P.nsub, sub = c.vh - kvh * P.nsub, gs = min(P.gs, P.group - sub * P.gs);
-    for (int i = blockIdx.y * 8 + (threadIdx.x >> 5); i < c.ntok * gs; i += 8 * gridDim.y) {
-        const int t = i / gs, h = i - t * gs;
-        const int row = t < P.tt ? t * P.gs + h : kTileRows + (t - P.tt) * P.gs + h;
-        float M = -INFINITY;
-        for (int k = lane; k < c.nsplit; k += 32) M = fmaxf(M, P.part_ml[slot(k) + row].x);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-        float l = 0.0f, o[VW] = {};
-        for (int k0 = 0; k0 < c.nsplit; k0 += 32) {
-            float f = 0.0f;
-            if (k0 + lane < c.nsplit) {
-                const float2 x = P.part_ml[slot(k0 + lane) + row];
-                if (x.x != -INFINITY) f = ex2(x.x - M);
-                l += x.y * f;
-            }
-            const int n = min(32, c.nsplit - k0);
-#pragma unroll 8
-            for (int k = 0; k < n; ++k) {
-                const float g = __shfl_sync(0xffffffffu, f, k);
-                const float* p = P.part_o + (slot(k0 + k) + row) * DC + lane * VW;
-                float x[VW];
-                if constexpr (VW == 4)
-                    *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(p);
-                else
-                    *reinterpret_cast<float2*>(x) = *reinterpret_cast<const float2*>(p);
-#pragma unroll
-                for (int e = 0; e < VW; ++e)
-                    if (g != 0.0f) o[e] = fmaf(x[e], g, o[e]);
-            }
-        }
-#pragma unroll
-        for (int s = 16; s > 0; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+    const int4 cut = __ldcg(reinterpret_cast<const int4*>(P.cuts + blockIdx.x));
+    const int nsplit = cut.x, ntok = cut.y, tok0 = cut.z, vh = cut.w;
+    if (nsplit == 0) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = a.c.head_dim;
+    const int wpr = nsplit <= 4 ? 1 : nsplit <= 8 ? 2 : nsplit <= 16 ? 4 : 8, rpb = 8 / wpr;  // warps per row, rows at a time
+    const int kvh = vh / P.nsub, sub = vh - kvh * P.nsub, gs = min(P.gs, P.group - sub * P.gs);
+    const int64_t first = (int64_t)(2 * blockIdx.x + 1) * P.cap_rows, rest = (int64_t)2 * blockIdx.x * P.cap_rows;
+    auto put = [&](int i, float M, float l, const float (&o)[VW]) {
         const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-        const int tok = c.tok0 + t, head = kvh * P.group + sub * P.gs + h;
+        const int t = i / gs, tok = tok0 + t, head = kvh * P.group + sub * P.gs + (i - t * gs);
         if (lane * VW < D) {
             T* out = static_cast<T*>(a.out.p) + (int64_t)tok * a.out.tok + head * a.out.head + lane * VW;
             if constexpr (VW == 4)
@@ -827,6 +800,72 @@ __global__ void __launch_bounds__(256) join_kernel(const AttnArgs a, const AttnP
         }
         if (lane == 0 && a.lse)
             a.lse[(int64_t)tok * a.n_heads + head] = l > 0.0f ? (M + log2f(l) - H::kShift) * 0.69314718055994531f : -INFINITY;
+    };
+    for (int i0 = blockIdx.y * rpb; i0 < ntok * gs; i0 += rpb * gridDim.y) {
+        const int i = i0 + warp / wpr;
+        float M = -INFINITY, l = 0.0f, o[VW] = {};
+        if (i < ntok * gs) {
+            const int t = i / gs, row = t < P.tt ? t * P.gs + (i - t * gs) : kTileRows + (t - P.tt) * P.gs + (i - t * gs);
+            for (int k0 = warp % wpr; k0 < nsplit; k0 += 4 * wpr) {
+                float2 x[4];
+                float v[4][VW];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int k = k0 + u * wpr;
+                    const int64_t at = (k == 0 ? first : rest + (int64_t)2 * k * P.cap_rows) + row;
+                    x[u] = make_float2(-INFINITY, 0.0f);
+                    if (k < nsplit) {
+                        x[u] = __ldcg(P.part_ml + at);
+                        const float* p = P.part_o + at * DC + lane * VW;
+                        if constexpr (VW == 4)
+                            *reinterpret_cast<float4*>(v[u]) = __ldcg(reinterpret_cast<const float4*>(p));
+                        else
+                            *reinterpret_cast<float2*>(v[u]) = __ldcg(reinterpret_cast<const float2*>(p));
+                    }
+                }
+                const float N = fmaxf(fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x)), M);
+                if (N == -INFINITY) continue;
+                const float g = ex2(M - N);
+                l *= g;
+#pragma unroll
+                for (int e = 0; e < VW; ++e) o[e] *= g;
+                M = N;
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (x[u].x != -INFINITY) {
+                        const float f = ex2(x[u].x - N);
+                        l = fmaf(x[u].y, f, l);
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) o[e] = fmaf(v[u][e], f, o[e]);
+                    }
+            }
+        }
+        if (wpr == 1) {
+            if (i < ntok * gs) put(i, M, l, o);
+            continue;
+        }
+        __syncthreads();  // the last rows are read
+        if (lane == 0) s_x[warp] = make_float2(M, l);
+#pragma unroll
+        for (int e = 0; e < VW; ++e) s_o[warp][lane * VW + e] = o[e];
+        __syncthreads();
+        if (warp % wpr == 0 && i < ntok * gs) {
+            float N = M;
+            for (int k = 1; k < wpr; ++k) N = fmaxf(N, s_x[warp + k].x);
+            const float g = N == -INFINITY ? 0.0f : ex2(M - N);
+            l *= g;
+#pragma unroll
+            for (int e = 0; e < VW; ++e) o[e] *= g;
+            for (int k = 1; k < wpr; ++k) {
+                const float2 x = s_x[warp + k];
+                if (x.x == -INFINITY) continue;
+                const float f = ex2(x.x - N);
+                l = fmaf(x.y, f, l);
+#pragma unroll
+                for (int e = 0; e < VW; ++e) o[e] = fmaf(s_o[warp + k][lane * VW + e], f, o[e]);
+            }
+            put(i, N, l, o);
+        }
     }
 }
 
@@ -903,10 +942,13 @@ cudaError_t launch(const AttnArgs& a, int dtype, cudaStream_t st) {
     cudaError_t e = cudaFuncSetAttribute(attention_kernel<T, DC>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<DC>::kSmem);
     if (e != cudaSuccess) return e;
     const int ctas = std::min(device_sm_count(), kMaxCtas);
-    attention_kernel<T, DC><<<ctas, kAttnThreads, Cfg<DC>::kSmem, st>>>(tmQ, tmK, tmV, a, P);
-    e = cudaGetLastError();
+    e = launch_pdl(attention_kernel<T, DC>, dim3(ctas), dim3(kAttnThreads), Cfg<DC>::kSmem, st, tmQ, tmK, tmV, a, P);
     if (e != cudaSuccess) return e;
-    return launch_pdl(join_kernel<T, DC>, dim3(ctas, std::min(16, P.cap_rows / 8)), dim3(256), 0, st, a, P);
+    // blocks for a cut's mean number of rows (a block takes 8 of them, or one of many parts); 32 for each of the 152 cost
+    // 8 us where most have nothing to do
+    const int64_t mean = (a.n_tok + a.n_seq - 1) / a.n_seq * P.gs;
+    const int per_cut = (int)std::min<int64_t>(std::min<int64_t>(mean, P.cap_rows), 16);
+    return launch_pdl(join_kernel<T, DC>, dim3(ctas, per_cut), dim3(256), 0, st, a, P);
 }
 
 template <typename T>
