@@ -9,9 +9,9 @@
 //
 // Layout.  A group of lanes holds one head: lane l has unit l, two vectors of VW channels, the two
 // halves of VW (or, interleaved, 2 x VW / 2) rotation pairs, so that no channel leaves its lane but
-// for the norm's sum (log2(group) shuffles).  A warp keeps one token and walks over its heads, several
-// at a time, four loads ahead; the cosines and sines of the lane's pairs stay in registers for all of them.
-// Few tokens are spread over more warps (wpt per token).
+// for the norm's sum (log2(group) shuffles).  A warp takes kAhead heads of each lane group, of one token: all its
+// loads of channels are issued before it waits for the token's slot and position and then for the table's row, which
+// stays in registers for all its heads.
 #include <algorithm>
 #include <cstdint>
 
@@ -72,40 +72,16 @@ __device__ __forceinline__ void store(T* p, const Vec<T, VW>& x) {
 template <typename T, int VW, int NU>
 __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AppendArgs a, const AppendPlan P) {
     const int lane = threadIdx.x & 31;
-    const int64_t gw = (int64_t)blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
-    const int64_t tok = gw / P.wpt;
+    const uint32_t gw = blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
+    const int64_t tok = gw / (uint32_t)P.wpt;
     if (tok >= a.n_tok) return;  // warp-uniform
-    const int part = (int)(gw - tok * P.wpt);
+    const int part = (int)(gw - (uint32_t)tok * P.wpt);
     const int D = a.c.head_dim, half = a.rot >> 1;
     const int l = lane & ((1 << P.lg) - 1), hp = 32 >> P.lg;
     const int n_kv = a.c.n_kv_heads, H = a.n_heads + 2 * n_kv;
 
-    int64_t slot = __ldg(a.slot + tok);
-    bool flag = false;
-    int64_t page = 0;
-    int in_page = 0;
-    if (slot >= 0) {
-        page = slot / a.c.page_size;
-        in_page = (int)(slot - page * a.c.page_size);
-        if (page >= a.c.n_pages) {
-            flag = true;
-            slot = -1;
-        }
-    }
-    const float* table = nullptr;
-    if (half > 0) {
-        int64_t p = __ldg(a.pos + tok);
-        if (p < 0 || p >= a.max_pos) {
-            flag = true;
-            p = p < 0 ? 0 : a.max_pos - 1;
-        }
-        table = a.rope + p * a.rot;
-    }
-    if (flag && part == 0 && lane == 0 && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
-
-    // the lane's units: channel starts of their two vectors, cosines and sines
+    // the lane's units: channel starts of their two vectors
     int c0[NU], c1[NU];
-    float cs[NU][VW], sn[NU][VW];
 #pragma unroll
     for (int n = 0; n < NU; ++n) {
         const int u = l + (n << P.lg);
@@ -116,12 +92,49 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AppendA
             c0[n] = u < P.units ? a.rot + (u - P.pair_units) * 2 * VW : D;
             c1[n] = c0[n] + VW;
         }
+    }
+    const int64_t at = __ldg(a.slot + tok);
+    const int pos = half > 0 ? __ldg(a.pos + tok) : 0;
+
+    const int h0 = part * kAhead * hp + (lane >> P.lg);
+    Vec<T, VW> x[kAhead][NU][2];
 #pragma unroll
-        for (int e = 0; e < VW; ++e) {
-            cs[n][e] = 1.0f;
-            sn[n][e] = 0.0f;
+    for (int j = 0; j < kAhead; ++j) {
+        const int h = h0 + j * hp;
+        if (h >= H) break;
+        const bool is_q = h < a.n_heads, is_k = h < a.n_heads + n_kv;
+        const HeadsView& s = is_q ? a.q : is_k ? a.k : a.v;
+        const T* src = static_cast<const T*>(s.p) + tok * s.tok + (h - (is_q ? 0 : is_k ? a.n_heads : a.n_heads + n_kv)) * s.head;
+#pragma unroll
+        for (int n = 0; n < NU; ++n) {
+            if (c0[n] < D) load(x[j][n][0], src + c0[n]);
+            if (c1[n] < D) load(x[j][n][1], src + c1[n]);
         }
-        if (u < P.pair_units) {
+    }
+
+    int64_t page = 0;
+    int in_page = 0;
+    bool flag = false, kept = at >= 0;
+    if (kept) {
+        page = (at >> 32) != 0 ? at / a.c.page_size : (int64_t)((uint32_t)at / (uint32_t)a.c.page_size);
+        in_page = (int)(at - page * a.c.page_size);
+        if (page >= a.c.n_pages) {
+            flag = true;
+            kept = false;
+        }
+    }
+    float cs[NU][VW], sn[NU][VW];
+    if (half > 0) {
+        int64_t p = pos;
+        if (p < 0 || p >= a.max_pos) {
+            flag = true;
+            p = p < 0 ? 0 : a.max_pos - 1;
+        }
+        const float* table = a.rope + p * a.rot;
+#pragma unroll
+        for (int n = 0; n < NU; ++n) {
+            const int u = l + (n << P.lg);
+            if (u >= P.pair_units) continue;
             if constexpr (VW == 1) {
                 cs[n][0] = __ldg(table + u);
                 sn[n][0] = __ldg(table + half + u);
@@ -134,107 +147,88 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AppendA
             }
         }
     }
+    if (flag && part == 0 && lane == 0 && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
     const bool any_norm = a.q_norm != nullptr || a.k_norm != nullptr;
 
-    for (int h0 = part * hp + (lane >> P.lg); h0 - (lane >> P.lg) < H; h0 += kAhead * P.wpt * hp) {
-        Vec<T, VW> x[kAhead][NU][2];
-        T* dst[kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const int h = h0 + j * P.wpt * hp;
-            const T* src = nullptr;
-            dst[j] = nullptr;
-            if (h < a.n_heads) {
-                src = static_cast<const T*>(a.q.p) + tok * a.q.tok + h * a.q.head;
-                dst[j] = static_cast<T*>(a.out.p) + tok * a.out.tok + h * a.out.head;
-            } else if (h < H && slot >= 0) {
-                const bool is_k = h < a.n_heads + n_kv;
-                const int kh = h - a.n_heads - (is_k ? 0 : n_kv);
-                const HeadsView& s = is_k ? a.k : a.v;
-                src = static_cast<const T*>(s.p) + tok * s.tok + kh * s.head;
-                dst[j] = static_cast<T*>(is_k ? a.c.k : a.c.v) + page * a.c.page + in_page * a.c.tok + kh * a.c.head;
-            }
-            if (src != nullptr) {
+    for (int j = 0; j < kAhead; ++j) {
+        if (h0 - (lane >> P.lg) + j * hp >= H) break;  // warp-uniform
+        const int h = h0 + j * hp;
+        const bool is_q = h < a.n_heads, turned = h < a.n_heads + n_kv;  // queries; queries and keys
+        T* dst = nullptr;
+        if (is_q)
+            dst = static_cast<T*>(a.out.p) + tok * a.out.tok + h * a.out.head;
+        else if (h < H && kept)
+            dst = static_cast<T*>(turned ? a.c.k : a.c.v) + page * a.c.page + in_page * a.c.tok +
+                  (h - a.n_heads - (turned ? 0 : n_kv)) * a.c.head;
+        const T* w = static_cast<const T*>(is_q ? a.q_norm : a.k_norm);
+        if (!turned || dst == nullptr) w = nullptr;
+        float r = 1.0f;
+        if (any_norm) {  // uniform: every lane takes part in the shuffles
+            float ss = 0.0f;
+            if (w != nullptr) {
 #pragma unroll
-                for (int n = 0; n < NU; ++n) {
-                    if (c0[n] < D) load(x[j][n][0], src + c0[n]);
-                    if (c1[n] < D) load(x[j][n][1], src + c1[n]);
-                }
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const int h = h0 + j * P.wpt * hp;
-            const bool turned = h < a.n_heads + n_kv;  // queries and keys
-            const T* w = static_cast<const T*>(h < a.n_heads ? a.q_norm : a.k_norm);
-            if (!turned || dst[j] == nullptr) w = nullptr;
-            float r = 1.0f;
-            if (any_norm) {  // uniform: every lane takes part in the shuffles
-                float ss = 0.0f;
-                if (w != nullptr) {
-#pragma unroll
-                    for (int n = 0; n < NU; ++n)
-#pragma unroll
-                        for (int v = 0; v < 2; ++v)
-                            if ((v ? c1[n] : c0[n]) < D)
-#pragma unroll
-                                for (int e = 0; e < VW; ++e) {
-                                    const float f = to_f(x[j][n][v].e[e]);
-                                    ss = fmaf(f, f, ss);
-                                }
-                }
-                for (int o = (1 << P.lg) >> 1; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-                r = 1.0f / sqrtf(ss / (float)D + a.eps);
-            }
-            if (dst[j] == nullptr) continue;
-#pragma unroll
-            for (int n = 0; n < NU; ++n) {
-                if (c0[n] >= D) continue;
-                if (turned) {
-                    float f[2][VW];
-#pragma unroll
-                    for (int v = 0; v < 2; ++v) {
-                        const int c = v ? c1[n] : c0[n];
-                        if (c >= D) continue;
-                        if (w != nullptr) {
-                            Vec<T, VW> wv;
-                            load(wv, w + c);
-#pragma unroll
-                            for (int e = 0; e < VW; ++e) f[v][e] = to_f(x[j][n][v].e[e]) * r * to_f(wv.e[e]);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < VW; ++e) f[v][e] = to_f(x[j][n][v].e[e]);
-                        }
-                    }
-                    if (c0[n] < a.rot) {
-                        if (VW > 1 && a.interleaved) {
-#pragma unroll
-                            for (int v = 0; v < 2; ++v)
-#pragma unroll
-                                for (int e = 0; e + 1 < VW; e += 2) {
-                                    const float c = cs[n][(v * VW + e) >> 1], s = sn[n][(v * VW + e) >> 1];
-                                    const float p = f[v][e], q = f[v][e + 1];
-                                    f[v][e] = p * c - q * s;
-                                    f[v][e + 1] = p * s + q * c;
-                                }
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < VW; ++e) {
-                                const float p = f[0][e], q = f[1][e];
-                                f[0][e] = p * cs[n][e] - q * sn[n][e];
-                                f[1][e] = p * sn[n][e] + q * cs[n][e];
-                            }
-                        }
-                    }
+                for (int n = 0; n < NU; ++n)
 #pragma unroll
                     for (int v = 0; v < 2; ++v)
                         if ((v ? c1[n] : c0[n]) < D)
 #pragma unroll
-                            for (int e = 0; e < VW; ++e) x[j][n][v].e[e] = from_f<T>(f[v][e]);
-                }
-                store(dst[j] + c0[n], x[j][n][0]);
-                if (c1[n] < D) store(dst[j] + c1[n], x[j][n][1]);
+                            for (int e = 0; e < VW; ++e) {
+                                const float f = to_f(x[j][n][v].e[e]);
+                                ss = fmaf(f, f, ss);
+                            }
             }
+            for (int o = (1 << P.lg) >> 1; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            r = 1.0f / sqrtf(ss / (float)D + a.eps);
+        }
+        if (dst == nullptr) continue;
+#pragma unroll
+        for (int n = 0; n < NU; ++n) {
+            if (c0[n] >= D) continue;
+            if (turned) {
+                float f[2][VW];
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    const int c = v ? c1[n] : c0[n];
+                    if (c >= D) continue;
+                    if (w != nullptr) {
+                        Vec<T, VW> wv;
+                        load(wv, w + c);
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) f[v][e] = to_f(x[j][n][v].e[e]) * r * to_f(wv.e[e]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) f[v][e] = to_f(x[j][n][v].e[e]);
+                    }
+                }
+                if (c0[n] < a.rot) {
+                    if (VW > 1 && a.interleaved) {
+#pragma unroll
+                        for (int v = 0; v < 2; ++v)
+#pragma unroll
+                            for (int e = 0; e + 1 < VW; e += 2) {
+                                const float c = cs[n][(v * VW + e) >> 1], s = sn[n][(v * VW + e) >> 1];
+                                const float p = f[v][e], q = f[v][e + 1];
+                                f[v][e] = p * c - q * s;
+                                f[v][e + 1] = p * s + q * c;
+                            }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) {
+                            const float p = f[0][e], q = f[1][e];
+                            f[0][e] = p * cs[n][e] - q * sn[n][e];
+                            f[1][e] = p * sn[n][e] + q * cs[n][e];
+                        }
+                    }
+                }
+#pragma unroll
+                for (int v = 0; v < 2; ++v)
+                    if ((v ? c1[n] : c0[n]) < D)
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) x[j][n][v].e[e] = from_f<T>(f[v][e]);
+            }
+            store(dst + c0[n], x[j][n][0]);
+            if (c1[n] < D) store(dst + c1[n], x[j][n][1]);
         }
     }
 }
@@ -247,11 +241,10 @@ cudaError_t launch(const AppendArgs& a, cudaStream_t st) {
     P.lg = 0;
     while (P.lg < 5 && (1 << P.lg) < P.units) ++P.lg;
     const int H = a.n_heads + 2 * a.c.n_kv_heads;
-    const int turns = (H + (32 >> P.lg) - 1) / (32 >> P.lg);  // of a warp that has a token to itself
-    const int64_t want = (int64_t)device_sm_count() * 32;
-    P.wpt = (int)std::min<int64_t>(turns, std::max<int64_t>(1, (want + a.n_tok - 1) / a.n_tok));
+    const int per_warp = kAhead * (32 >> P.lg);  // heads
+    P.wpt = (H + per_warp - 1) / per_warp;
     const int64_t blocks = (a.n_tok * P.wpt + kAppendWarps - 1) / kAppendWarps;
-    if (blocks > INT32_MAX) return cudaErrorInvalidValue;
+    if (blocks > INT32_MAX / kAppendWarps) return cudaErrorInvalidValue;
     append_kernel<T, VW, NU><<<(unsigned)blocks, 32 * kAppendWarps, 0, st>>>(a, P);
     return cudaGetLastError();
 }

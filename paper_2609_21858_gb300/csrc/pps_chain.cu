@@ -5,12 +5,12 @@
 // the chain argmax_i P(i) / E(i).  exp2 of c (l - max) with c = log2(e) / T stands for exp(l / T) throughout;
 // a logit equal to its row's maximum counts as 1 also where both are infinite.
 //
-// Two launches.  stats_kernel reads every logit once: a CTA takes one slice of one row, each thread up to
-// kVecs 16-byte vectors in registers, their maximum first and then their sum of exponentials, and the
-// CTA leaves (max, sum).  finish_kernel runs slices x sequences: each CTA merges the sums of its chain's rows (a
-// warp a row), finds the first rejection, and races its slice of the one row (pair) that matters; the CTA
-// that arrives last at the sequence's ticket joins the slices in order and writes the outputs.  Both are
-// bound by HBM: all logits once, then one row pair and the noise per sequence.
+// Two launches, both bound by HBM.  stats_kernel reads every logit once: the rows' 16-byte vectors lie on one line
+// that is cut into equal shares, one per CTA, and a CTA leaves (max, sum of exponentials) of each row it meets.  A thread
+// takes kVecs vectors at a time, the next ones on their way: their maximum first, then their exponentials against it.
+// finish_kernel runs slices x sequences: each CTA joins the parts of its chain's rows, finds the first rejection and races
+// its slice of the one row (pair) that matters; the CTA that arrives last at the sequence's ticket joins the slices in
+// order and writes the outputs.
 #include <algorithm>
 #include <climits>
 #include <cstdint>
@@ -23,14 +23,15 @@
 namespace pps {
 namespace {
 
-constexpr int kStatThreads = 256;
-constexpr int kVecs = 8;         // 16-byte vectors per thread of a slice
-constexpr int kMaxSlices = 64;   // of a row
-constexpr int kRaceThreads = 256;
+constexpr int kStatThreads = 256, kStatCtas = 4;  // CTAs per SM
+constexpr int kVecs = 4;         // 16-byte vectors per thread and turn
+constexpr int kRaceThreads = 256, kRaceCtas = 4;
+constexpr int kMaxParts = 1024;  // CTAs of stats_kernel
+constexpr int kMaxSlices = 64;   // of the final row
 constexpr int kMaxChain = 64;    // gamma
 
 struct Stat {
-    float m, s;  // the slice's largest logit (-inf: none) and its sum of exp2(c (l - m))
+    float m, s;  // the largest logit (-inf: none) and the sum of exp2(c (l - m))
 };
 struct Best {
     float v;
@@ -38,13 +39,12 @@ struct Best {
 };
 
 struct ChainPlan {
-    int slices;       // of a row in stats_kernel
-    int vecs;         // 16-byte vectors per slice
-    int race_slices;  // of the final row
-    int race_len;     // its tokens per slice
-    Stat* stats;      // [n_nodes + n_draft][slices]
-    Best* best;       // [n_seq][race_slices]
-    uint32_t* ticket; // [n_seq]
+    int64_t nv, share;  // 16-byte vectors of a row (with room for any alignment), of a CTA's share of rows x nv
+    int race_slices;    // of the final row
+    int race_len;       // its tokens per slice
+    Stat* stats;        // part of row r by CTA c: [r + c]
+    Best* best;         // [n_seq][race_slices]
+    uint32_t* ticket;   // [n_seq]
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -83,86 +83,134 @@ struct Elem<__nv_bfloat16> {
     static __device__ __forceinline__ float get(const __nv_bfloat16* p) { return __bfloat162float(__ldg(p)); }
 };
 
-// (max, sum) of one slice of one row.  The row is seen as the aligned 16-byte vectors that cover it; its first
-// and last one may hold tokens of no concern, and are read token by token.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+// c (x0 - m) and c (x1 - m) at once.  (One product c x - c m would round c m: 6e-6 of the sum at logits of 100.)
+__device__ __forceinline__ void scale2(float& x0, float& x1, float c, float m) {
+    uint64_t x, cc, mm;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(x0), "f"(x1));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(cc) : "f"(c));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(mm) : "f"(-m));
+    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(x) : "l"(mm));
+    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(x) : "l"(cc));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x0), "=f"(x1) : "l"(x));
+}
+
+// one vector of a row seen as the aligned 16-byte vectors that cover it (al: the first one); its first and last one may
+// hold tokens of no concern, and are read token by token
 template <typename T>
-__global__ void __launch_bounds__(kStatThreads) stats_kernel(const ChainArgs a, const ChainPlan P) {
+__device__ __forceinline__ uint4 row_vec(const T* al, int64_t v, int lead, int64_t end) {
     using E = Elem<T>;
     constexpr int VW = E::kVW;
-    __shared__ float sm[kStatThreads / 32], ss[kStatThreads / 32];
-    const int64_t row = blockIdx.x / (unsigned)P.slices;
-    const int slice = (int)(blockIdx.x % (unsigned)P.slices);
+    if (v * VW >= lead && (v + 1) * VW <= end) return __ldg(reinterpret_cast<const uint4*>(al) + v);
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;  // -inf
+#pragma unroll
+    for (int e = 0; e < VW; ++e) {
+        const int64_t t = v * VW + e;
+        if (t >= lead && t < end) {
+            const uint32_t f = __float_as_uint(E::get(al + t));
+            if constexpr (sizeof(T) == 2)
+                w[e >> 1] = (e & 1) ? ((w[e >> 1] & 0xffffu) | (f & 0xffff0000u)) : ((w[e >> 1] & 0xffff0000u) | (f >> 16));
+            else
+                w[e] = f;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// adds the logits of kVecs vectors to a running (max, sum)
+template <typename T>
+__device__ __forceinline__ void add_logits(const uint4 (&x)[kVecs], float& m, float& s, float c) {
+    using E = Elem<T>;
+    float bm = m;
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j)
+#pragma unroll
+        for (int e = 0; e < E::kVW; e += 2) bm = max3(bm, E::at(x[j], e), E::at(x[j], e + 1));  // NaN is passed by
+    if (bm == -INFINITY) return;
+    float bs = 0.0f, b1 = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j)
+#pragma unroll
+        for (int e = 0; e < E::kVW; e += 2) {
+            float x0 = E::at(x[j], e), x1 = E::at(x[j], e + 1);
+            scale2(x0, x1, c, bm);
+            bs += ex2(x0);
+            b1 += ex2(x1);
+        }
+    bs += b1;
+    if (bs != bs) {  // NaN among the logits, or an infinite maximum
+        bs = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kVecs; ++j)
+#pragma unroll
+            for (int e = 0; e < E::kVW; ++e) bs += weight(usable(E::at(x[j], e)), bm, c);
+    }
+    s = fmaf(s, weight(m, bm, c), bs);
+    m = bm;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kStatThreads, kStatCtas) stats_kernel(const ChainArgs a, const ChainPlan P) {
+    constexpr int VW = Elem<T>::kVW;
+    __shared__ Stat sh[2][kStatThreads / 32];
+    pdl_launch_dependents();
     if (blockIdx.x == 0)
         for (int i = threadIdx.x; i < a.n_seq; i += kStatThreads) P.ticket[i] = 0;
-    const T* base = row < a.n_nodes ? static_cast<const T*>(a.p) + row * a.p_stride
-                                    : static_cast<const T*>(a.q) + (row - a.n_nodes) * a.q_stride;
-    const int lead = (int)((reinterpret_cast<uintptr_t>(base) & 15) / sizeof(T));  // tokens of the first vector before the row
-    const T* al = base - lead;
-    const int64_t end = a.V + lead;  // in tokens from al
-    const int64_t v0 = (int64_t)slice * P.vecs, v1 = min(v0 + P.vecs, (end + VW - 1) / VW);
-    float m = -INFINITY, s = 0.0f;
-    for (int64_t b = v0; b < v1; b += kVecs * kStatThreads) {  // one turn, unless the row has more than kMaxSlices full slices
-        uint4 x[kVecs];
+    int64_t x = blockIdx.x * P.share;
+    const int64_t x1 = min(x + P.share, (a.n_nodes + a.n_draft) * P.nv);
+    for (int turn = 0; x < x1; turn ^= 1) {  // one row, or a part of it, at a time
+        const int64_t row = x / P.nv, v0 = x - row * P.nv, v1 = min(v0 + (x1 - x), P.nv);
+        x += v1 - v0;
+        const T* base = row < a.n_nodes ? static_cast<const T*>(a.p) + row * a.p_stride
+                                        : static_cast<const T*>(a.q) + (row - a.n_nodes) * a.q_stride;
+        const int lead = (int)((reinterpret_cast<uintptr_t>(base) & 15) / sizeof(T));  // tokens of the first vector before the row
+        const T* al = base - lead;
+        const int64_t end = a.V + lead;  // in tokens from al
+        const int64_t last = min(v1, (end + VW - 1) / VW);
+        auto fetch = [&](uint4 (&y)[kVecs], int64_t b) {
 #pragma unroll
-        for (int j = 0; j < kVecs; ++j) {
-            const int64_t v = b + threadIdx.x + j * kStatThreads;
-            if (v < v1 && v * VW >= lead && (v + 1) * VW <= end)
-                x[j] = __ldg(reinterpret_cast<const uint4*>(al) + v);
-            else {
-                uint32_t w[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) w[k] = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;  // -inf
-                if (v < v1) {
-#pragma unroll
-                    for (int e = 0; e < VW; ++e) {
-                        const int64_t t = v * VW + e;
-                        if (t >= lead && t < end) {
-                            const uint32_t f = __float_as_uint(E::get(al + t));
-                            if constexpr (sizeof(T) == 2)
-                                w[e >> 1] = (e & 1) ? ((w[e >> 1] & 0xffffu) | (f & 0xffff0000u))
-                                                    : ((w[e >> 1] & 0xffff0000u) | (f >> 16));
-                            else
-                                w[e] = f;
-                        }
-                    }
-                }
-                x[j] = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int j = 0; j < kVecs; ++j) {
+                const int64_t v = b + j * kStatThreads;
+                y[j] = v < last ? row_vec<T>(al, v, lead, end) : make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
+                if (sizeof(T) == 4 && v >= last) y[j] = make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
             }
+        };
+        float m = -INFINITY, s = 0.0f;
+        uint4 cur[kVecs], nxt[kVecs];
+        int64_t b = v0 + threadIdx.x;
+        fetch(cur, b);
+        for (; b < last; b += kVecs * kStatThreads) {
+            fetch(nxt, b + kVecs * kStatThreads);
+            add_logits<T>(cur, m, s, a.c);
+#pragma unroll
+            for (int j = 0; j < kVecs; ++j) cur[j] = nxt[j];
         }
-        float bm = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < kVecs; ++j)
-#pragma unroll
-            for (int e = 0; e < VW; ++e) bm = fmaxf(bm, E::at(x[j], e));  // fmaxf passes NaN by
-        if (bm == -INFINITY) continue;
-        float bs = 0.0f;
-#pragma unroll
-        for (int j = 0; j < kVecs; ++j)
-#pragma unroll
-            for (int e = 0; e < VW; ++e) bs += weight(usable(E::at(x[j], e)), bm, a.c);
-        join(m, s, bm, bs, a.c);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float om = __shfl_xor_sync(0xffffffffu, m, o), os = __shfl_xor_sync(0xffffffffu, s, o);
-        join(m, s, om, os, a.c);
-    }
-    if ((threadIdx.x & 31) == 0) {
-        sm[threadIdx.x >> 5] = m;
-        ss[threadIdx.x >> 5] = s;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kStatThreads / 32; ++w) join(m, s, sm[w], ss[w], a.c);
-        P.stats[row * P.slices + slice] = {m, s};
+        for (int o = 16; o > 0; o >>= 1) {
+            const float om = __shfl_xor_sync(0xffffffffu, m, o), os = __shfl_xor_sync(0xffffffffu, s, o);
+            join(m, s, om, os, a.c);
+        }
+        if ((threadIdx.x & 31) == 0) sh[turn][threadIdx.x >> 5] = {m, s};
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int w = 1; w < kStatThreads / 32; ++w) join(m, s, sh[turn][w].m, sh[turn][w].s, a.c);
+            P.stats[row + blockIdx.x] = {m, s};
+        }
     }
 }
 
 // a row's (max, sum), by one warp, in the same order for every reader
 __device__ __forceinline__ Stat row_stat(const ChainPlan& P, int64_t row, float c, int lane) {
     float m = -INFINITY, s = 0.0f;
-    for (int j = lane; j < P.slices; j += 32) {
-        const Stat t = P.stats[row * P.slices + j];
+    const int64_t from = row * P.nv / P.share, to = ((row + 1) * P.nv - 1) / P.share;
+    for (int64_t j = from + lane; j <= to; j += 32) {
+        const Stat t = P.stats[row + j];
         join(m, s, t.m, t.s, c);
     }
 #pragma unroll
@@ -209,91 +257,112 @@ __device__ __forceinline__ void load8(float (&x)[8], const T* row, int64_t t, in
     }
 }
 
-// the best of tokens [t0, t1) of max(P - Q, 0) / E (q == nullptr: P / E), as this thread's share
+// the best of tokens [t0, t1) of max(P - Q, 0) / E (q == nullptr: P / E), as this thread's share; z: the noise of its first 8
 template <typename T>
-__device__ __forceinline__ Best race(const T* p, const T* q, const float* noise, Stat sp, Stat sq, float c, int64_t t0,
-                                     int64_t t1, int64_t V) {
+__device__ __forceinline__ Best race(const T* p, const T* q, const float* noise, float (&z)[8], Stat sp, Stat sq, float c,
+                                     int64_t t0, int64_t t1, int64_t V) {
     Best b = {0.0f, INT_MAX};  // only positive scores count
     const float ip = sp.s > 0.0f ? 1.0f / sp.s : 0.0f, iq = sq.s > 0.0f ? 1.0f / sq.s : 0.0f;
-    for (int64_t t = t0 + 8 * threadIdx.x; t < t1; t += 8 * kRaceThreads) {
-        float x[8], y[8], z[8];
+    float x[8], y[8];
+    int64_t t = t0 + 8 * threadIdx.x;
+    if (t < t1) {
         load8(x, p, t, V, -INFINITY);
         if (q != nullptr) load8(y, q, t, V, -INFINITY);
-        load8(z, noise, t, V, 1.0f);
+    }
+    while (t < t1) {
+        float xn[8], yn[8], zn[8];
+        const int64_t tn = t + 8 * kRaceThreads;
+        if (tn < t1) {
+            load8(xn, p, tn, V, -INFINITY);
+            if (q != nullptr) load8(yn, q, tn, V, -INFINITY);
+            load8(zn, noise, tn, V, 1.0f);
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             float d = weight(usable(x[e]), sp.m, c) * ip;
             if (q != nullptr) d -= weight(usable(y[e]), sq.m, c) * iq;
             if (t + e < t1 && d > 0.0f) better(b, d / z[e], (int)(t + e));
+            x[e] = xn[e];
+            y[e] = yn[e];
+            z[e] = zn[e];
         }
+        t = tn;
     }
     return b;
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kRaceThreads) finish_kernel(const ChainArgs a, const ChainPlan P) {
+__global__ void __launch_bounds__(kRaceThreads, kRaceCtas) finish_kernel(const ChainArgs a, const ChainPlan P) {
     using E = Elem<T>;
     __shared__ int s_row[kMaxChain], s_tok[kMaxChain], s_ok[kMaxChain];
+    __shared__ Stat s_p[kMaxChain + 1], s_q[kMaxChain];
     __shared__ Best s_best[kRaceThreads / 32];
-    __shared__ Stat s_stat[2];
     __shared__ int s_last;
-    pdl_wait();
     const int seq = (int)(blockIdx.x / (unsigned)P.race_slices), slice = (int)(blockIdx.x % (unsigned)P.race_slices);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = threadIdx.x;
+    const int64_t t0 = (int64_t)slice * P.race_len, t1 = min(t0 + P.race_len, a.V);
+    const float* noise = a.noise + seq * a.noise_stride;
+    // what does not wait for the rows' sums: the slice's first noise, the chain's tokens and their logits
+    float z[8];
+    if (t0 + 8 * j < t1) load8(z, noise, t0 + 8 * j, a.V, 1.0f);
     const int n0 = __ldg(a.seq_off + seq), n1 = __ldg(a.seq_off + seq + 1);
     if (n0 < 0 || n1 <= n0 || n1 > a.n_nodes) {  // CTA-uniform: nothing of the sequence can be read
-        if (slice == 0 && threadIdx.x == 0) {
+        if (slice == 0 && j == 0) {
             a.out_acc[seq] = 0;
             a.out_ne[seq] = 0;
-            for (int j = 0; j <= a.gamma; ++j) a.out_em[(int64_t)seq * (a.gamma + 1) + j] = -1;
+            for (int i = 0; i <= a.gamma; ++i) a.out_em[(int64_t)seq * (a.gamma + 1) + i] = -1;
             if (a.status) atomicOr(a.status, PPS_FLAG_INDEX);
         }
         return;
     }
     const int longest = min(n1 - n0 - 1, a.gamma);
-    for (int j = warp; j < longest; j += kRaceThreads / 32) {
-        const int node = n0 + j, r = __ldg(a.node_draft_row + node);
-        const bool has = r >= 0 && r < a.n_draft;
-        int tok = has ? __ldg(a.draft_tok + r) : -1, ok = 0;
+    int r = -1;
+    float u = 0.0f, lp = -INFINITY, lq = -INFINITY;
+    if (j < longest) {
+        r = __ldg(a.node_draft_row + n0 + j);
         bool bad = r >= a.n_draft;
-        if (has) {
-            const Stat sp = row_stat(P, node, a.c, lane), sq = row_stat(P, a.n_nodes + r, a.c, lane);
-            float px = 0.0f, qx = 0.0f;
+        if (r < 0 || bad) r = -1;
+        int tok = -1;
+        if (r >= 0) {
+            tok = __ldg(a.draft_tok + r);
+            u = __ldg(a.u + r);
             if (tok < 0 || tok >= a.V)
                 bad = true;
             else {
-                const float lp = usable(E::get(static_cast<const T*>(a.p) + node * a.p_stride + tok));
-                const float lq = usable(E::get(static_cast<const T*>(a.q) + r * a.q_stride + tok));
-                if (sp.s > 0.0f) px = weight(lp, sp.m, a.c) / sp.s;
-                if (sq.s > 0.0f) qx = weight(lq, sq.m, a.c) / sq.s;
+                lp = usable(E::get(static_cast<const T*>(a.p) + (n0 + j) * a.p_stride + tok));
+                lq = usable(E::get(static_cast<const T*>(a.q) + r * a.q_stride + tok));
             }
-            ok = __ldg(a.u + r) * qx < px;
-            if (slice == 0 && lane == 0 && a.out_prob)
-                a.out_prob[r] = px > 0.0f ? (px < qx ? px / qx : 1.0f) : 0.0f;
         }
-        if (lane == 0) {
-            s_row[j] = has ? r : -1;
-            s_tok[j] = tok;
-            s_ok[j] = ok;
-            if (bad && slice == 0 && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
-        }
+        s_row[j] = r;
+        s_tok[j] = tok;
+        if (bad && slice == 0 && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
+    }
+    __syncthreads();
+    pdl_wait();
+    for (int i = warp; i < 2 * longest + 1; i += kRaceThreads / 32) {  // the chain's rows, the drafter's after the target's
+        const bool is_q = i > longest;
+        const int64_t row = is_q ? (s_row[i - longest - 1] >= 0 ? a.n_nodes + s_row[i - longest - 1] : -1) : (int64_t)n0 + i;
+        const Stat st = row >= 0 ? row_stat(P, row, a.c, lane) : Stat{-INFINITY, 0.0f};
+        if (lane == 0) (is_q ? s_q[i - longest - 1] : s_p[i]) = st;
+    }
+    __syncthreads();
+    if (j < longest) {
+        // a token out of range has no logit: it counts as impossible under both laws
+        const Stat sp = s_p[j], sq = s_q[j];
+        const float px = lp > -INFINITY && sp.s > 0.0f ? weight(lp, sp.m, a.c) / sp.s : 0.0f;
+        const float qx = lq > -INFINITY && sq.s > 0.0f ? weight(lq, sq.m, a.c) / sq.s : 0.0f;
+        s_ok[j] = r >= 0 && u * qx < px;
+        if (r >= 0 && slice == 0 && a.out_prob) a.out_prob[r] = px > 0.0f ? (px < qx ? px / qx : 1.0f) : 0.0f;
     }
     __syncthreads();
     int acc = 0;
     while (acc < longest && s_ok[acc]) ++acc;
-    const int node = n0 + acc, r = acc < longest ? s_row[acc] : -1;
-    if (warp < 2) {
-        const Stat st = warp == 0 ? row_stat(P, node, a.c, lane) : r >= 0 ? row_stat(P, a.n_nodes + r, a.c, lane) : Stat{0.0f, 0.0f};
-        if (lane == 0) s_stat[warp] = st;
-    }
-    __syncthreads();
-    const Stat sp = s_stat[0], sq = s_stat[1];
+    const int node = n0 + acc, fr = acc < longest ? s_row[acc] : -1;
+    const Stat sp = s_p[acc], sq = fr >= 0 ? s_q[acc] : Stat{0.0f, 0.0f};
     const T* p = static_cast<const T*>(a.p) + node * a.p_stride;
-    const T* q = r >= 0 && sq.s > 0.0f ? static_cast<const T*>(a.q) + r * a.q_stride : nullptr;
-    const float* noise = a.noise + seq * a.noise_stride;
-    const int64_t t0 = (int64_t)slice * P.race_len, t1 = min(t0 + P.race_len, a.V);
+    const T* q = fr >= 0 && sq.s > 0.0f ? static_cast<const T*>(a.q) + fr * a.q_stride : nullptr;
     Best b = {0.0f, INT_MAX};
-    if (sp.s > 0.0f) b = race(p, q, noise, sp, sq, a.c, t0, t1, a.V);
+    if (sp.s > 0.0f) b = race(p, q, noise, z, sp, sq, a.c, t0, t1, a.V);
     b = block_best(b, s_best);
     if (threadIdx.x == 0) {
         __stcg(reinterpret_cast<float2*>(P.best + (int64_t)seq * P.race_slices + slice), make_float2(b.v, __int_as_float(b.i)));
@@ -304,16 +373,18 @@ __global__ void __launch_bounds__(kRaceThreads) finish_kernel(const ChainArgs a,
     if (!s_last) return;
     __threadfence();
     b = {0.0f, INT_MAX};
-    for (int j = threadIdx.x; j < P.race_slices; j += kRaceThreads) {
+    if (j < P.race_slices) {
         const float2 o = __ldcg(reinterpret_cast<const float2*>(P.best + (int64_t)seq * P.race_slices + j));
-        better(b, o.x, __float_as_int(o.y));
+        b = {o.x, __float_as_int(o.y)};
     }
     b = block_best(b, s_best);
-    if (b.i == INT_MAX && q != nullptr && sp.s > 0.0f)  // the residual is zero everywhere (CTA-uniform)
-        b = block_best(race<T>(p, nullptr, noise, sp, sq, a.c, 0, a.V, a.V), s_best);
-    for (int j = threadIdx.x; j <= a.gamma; j += kRaceThreads)
+    if (b.i == INT_MAX && q != nullptr && sp.s > 0.0f) {  // the residual is zero everywhere (CTA-uniform)
+        if (8 * j < a.V) load8(z, noise, 8 * j, a.V, 1.0f);
+        b = block_best(race<T>(p, nullptr, noise, z, sp, sq, a.c, 0, a.V, a.V), s_best);
+    }
+    if (j <= a.gamma)
         a.out_em[(int64_t)seq * (a.gamma + 1) + j] = j < acc ? s_tok[j] : j == acc && b.i != INT_MAX ? b.i : -1;
-    if (threadIdx.x == 0) {
+    if (j == 0) {
         a.out_acc[seq] = acc;
         a.out_ne[seq] = acc + (b.i != INT_MAX);
     }
@@ -324,25 +395,25 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 template <typename T>
 cudaError_t launch(const ChainArgs& a, cudaStream_t st) {
     ChainPlan P;
-    const int64_t rows = a.n_nodes + a.n_draft, nv = (a.V + Elem<T>::kVW - 1) / Elem<T>::kVW + 1;
+    const int64_t rows = a.n_nodes + a.n_draft;
     const int sms = device_sm_count();
-    // slices of at most kVecs vectors a thread (one turn), of fewer where rows alone leave SMs idle
-    const int64_t full = kVecs * kStatThreads;
-    int64_t n = std::max<int64_t>((nv + full - 1) / full, std::min<int64_t>((nv + kStatThreads - 1) / kStatThreads, 4 * sms / rows));
-    P.slices = (int)std::min<int64_t>(std::max<int64_t>(n, 1), kMaxSlices);
-    P.vecs = (int)((nv + P.slices - 1) / P.slices);
-    // the final rows: a turn of 8 tokens a thread at least
-    n = std::min<int64_t>((a.V + 8 * kRaceThreads - 1) / (8 * kRaceThreads), std::max<int64_t>(1, 8 * sms / a.n_seq));
+    P.nv = (a.V + Elem<T>::kVW - 1) / Elem<T>::kVW + 1;
+    // every CTA resident at once, of a vector a thread at least
+    const int64_t most = std::min<int64_t>(kMaxParts, (int64_t)kStatCtas * sms);
+    P.share = std::max<int64_t>((rows * P.nv + most - 1) / most, kStatThreads);
+    const unsigned ctas = (unsigned)((rows * P.nv + P.share - 1) / P.share);
+    // the final rows: every CTA resident at once, of 8 tokens a thread at least
+    const int64_t n = std::min<int64_t>((a.V + 8 * kRaceThreads - 1) / (8 * kRaceThreads), std::max<int64_t>(1, kRaceCtas * sms / a.n_seq));
     P.race_slices = (int)std::min<int64_t>(std::max<int64_t>(n, 1), kMaxSlices);
     P.race_len = (int)(((a.V + P.race_slices - 1) / P.race_slices + 7) / 8 * 8);
     char* w = static_cast<char*>(a.ws);
     P.stats = reinterpret_cast<Stat*>(w);
-    w += align256(sizeof(Stat) * (size_t)rows * kMaxSlices);
+    w += align256(sizeof(Stat) * (size_t)(rows + kMaxParts));
     P.best = reinterpret_cast<Best*>(w);
     w += align256(sizeof(Best) * (size_t)a.n_seq * kMaxSlices);
     P.ticket = reinterpret_cast<uint32_t*>(w);
-    if (rows * P.slices > INT32_MAX || (int64_t)a.n_seq * P.race_slices > INT32_MAX) return cudaErrorInvalidValue;
-    stats_kernel<T><<<(unsigned)(rows * P.slices), kStatThreads, 0, st>>>(a, P);
+    if ((int64_t)a.n_seq * P.race_slices > INT32_MAX) return cudaErrorInvalidValue;
+    stats_kernel<T><<<ctas, kStatThreads, 0, st>>>(a, P);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     return launch_pdl(finish_kernel<T>, dim3((unsigned)(a.n_seq * P.race_slices)), dim3(kRaceThreads), 0, st, a, P);
@@ -351,7 +422,7 @@ cudaError_t launch(const ChainArgs& a, cudaStream_t st) {
 }  // namespace
 
 size_t chain_workspace_bytes(int64_t n_nodes, int64_t n_draft, int n_seq) {
-    return align256(sizeof(Stat) * (size_t)(n_nodes + n_draft) * kMaxSlices) +
+    return align256(sizeof(Stat) * (size_t)(n_nodes + n_draft + kMaxParts)) +
            align256(sizeof(Best) * (size_t)n_seq * kMaxSlices) + align256(sizeof(uint32_t) * (size_t)n_seq);
 }
 
