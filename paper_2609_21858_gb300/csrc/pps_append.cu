@@ -9,9 +9,9 @@
 //
 // Layout.  A group of lanes holds one head: lane l has unit l, two vectors of VW channels, the two
 // halves of VW (or, interleaved, 2 x VW / 2) rotation pairs, so that no channel leaves its lane but
-// for the norm's sum (log2(group) shuffles).  A warp takes kAhead heads of each lane group, of one token: all its
-// loads of channels are issued before it waits for the token's slot and position and then for the table's row, which
-// stays in registers for all its heads.
+// for the norm's sum (log2(group) shuffles).  A warp's item is kAhead heads of each lane group, of one token.  Warps
+// stay and take items in turn, slots and positions two items ahead, channels and the table's row one ahead: a
+// position has to arrive before the row's address is known, and each wait is an item long.
 #include <algorithm>
 #include <cstdint>
 
@@ -25,13 +25,15 @@ namespace pps {
 namespace {
 
 constexpr int kAppendWarps = 4;  // per CTA
-constexpr int kAhead = 4;        // heads of a lane group in flight
+constexpr int kAhead = 2;        // heads of a lane group in an item
+constexpr int kAppendCtas = 4;   // per SM
 
 struct AppendPlan {
     int lg;          // log2 of the lanes per head
-    int wpt;         // warps per token
+    int parts;       // items per token
     int units;       // units per head
     int pair_units;  // of which rotated
+    float inv_d;
 };
 
 template <int VW>
@@ -56,7 +58,12 @@ template <typename T, int VW>
 union Vec {
     typename RawVec<VW>::type raw;
     T e[VW];
-    __device__ Vec() {}
+    __device__ __forceinline__ Vec() {}
+    __device__ __forceinline__ Vec(const Vec& o) : raw(o.raw) {}
+    __device__ __forceinline__ Vec& operator=(const Vec& o) {
+        raw = o.raw;
+        return *this;
+    }
 };
 
 template <typename T, int VW>
@@ -68,17 +75,23 @@ __device__ __forceinline__ void store(T* p, const Vec<T, VW>& x) {
     *reinterpret_cast<typename RawVec<VW>::type*>(p) = x.raw;
 }
 
+// what an item needs from memory
+template <typename T, int VW, int NU>
+struct Item {
+    Vec<T, VW> x[kAhead][NU][2];
+    float cs[NU][VW], sn[NU][VW];
+};
+
 // NU: units per lane (more than one only for VW = 1)
 template <typename T, int VW, int NU>
-__global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AppendArgs a, const AppendPlan P) {
+__global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(const AppendArgs a, const AppendPlan P) {
     const int lane = threadIdx.x & 31;
-    const uint32_t gw = blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
-    const int64_t tok = gw / (uint32_t)P.wpt;
-    if (tok >= a.n_tok) return;  // warp-uniform
-    const int part = (int)(gw - (uint32_t)tok * P.wpt);
     const int D = a.c.head_dim, half = a.rot >> 1;
-    const int l = lane & ((1 << P.lg) - 1), hp = 32 >> P.lg;
-    const int n_kv = a.c.n_kv_heads, H = a.n_heads + 2 * n_kv;
+    const int l = lane & ((1 << P.lg) - 1), hp = 32 >> P.lg, group = lane >> P.lg;
+    const int n_kv = a.c.n_kv_heads, n_qk = a.n_heads + n_kv, H = n_qk + n_kv;
+    const uint32_t items = (uint32_t)a.n_tok * P.parts, stride = gridDim.x * kAppendWarps;
+    uint32_t it = blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
+    if (it >= items) return;  // warp-uniform
 
     // the lane's units: channel starts of their two vectors
     int c0[NU], c1[NU];
@@ -93,143 +106,166 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AppendA
             c1[n] = c0[n] + VW;
         }
     }
-    const int64_t at = __ldg(a.slot + tok);
-    const int pos = half > 0 ? __ldg(a.pos + tok) : 0;
-
-    const int h0 = part * kAhead * hp + (lane >> P.lg);
-    Vec<T, VW> x[kAhead][NU][2];
+    const bool any_norm = a.q_norm != nullptr || a.k_norm != nullptr;
+    auto fetch_x = [&](Item<T, VW, NU>& y, int64_t tok, int part) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-        const int h = h0 + j * hp;
-        if (h >= H) break;
-        const bool is_q = h < a.n_heads, is_k = h < a.n_heads + n_kv;
-        const HeadsView& s = is_q ? a.q : is_k ? a.k : a.v;
-        const T* src = static_cast<const T*>(s.p) + tok * s.tok + (h - (is_q ? 0 : is_k ? a.n_heads : a.n_heads + n_kv)) * s.head;
+        for (int j = 0; j < kAhead; ++j) {
+            const int h = (part * kAhead + j) * hp + group;
+            if (h >= H) break;
+            const bool is_q = h < a.n_heads, is_k = h < n_qk;
+            const HeadsView& s = is_q ? a.q : is_k ? a.k : a.v;
+            const T* src = static_cast<const T*>(s.p) + tok * s.tok + (h - (is_q ? 0 : is_k ? a.n_heads : n_qk)) * s.head;
 #pragma unroll
-        for (int n = 0; n < NU; ++n) {
-            if (c0[n] < D) load(x[j][n][0], src + c0[n]);
-            if (c1[n] < D) load(x[j][n][1], src + c1[n]);
+            for (int n = 0; n < NU; ++n) {
+                if (c0[n] < D) load(y.x[j][n][0], src + c0[n]);
+                if (c1[n] < D) load(y.x[j][n][1], src + c1[n]);
+            }
         }
-    }
-
-    int64_t page = 0;
-    int in_page = 0;
-    bool flag = false, kept = at >= 0;
-    if (kept) {
-        page = (at >> 32) != 0 ? at / a.c.page_size : (int64_t)((uint32_t)at / (uint32_t)a.c.page_size);
-        in_page = (int)(at - page * a.c.page_size);
-        if (page >= a.c.n_pages) {
-            flag = true;
-            kept = false;
-        }
-    }
-    float cs[NU][VW], sn[NU][VW];
-    if (half > 0) {
-        int64_t p = pos;
-        if (p < 0 || p >= a.max_pos) {
-            flag = true;
-            p = p < 0 ? 0 : a.max_pos - 1;
-        }
-        const float* table = a.rope + p * a.rot;
+    };
+    auto fetch_rope = [&](Item<T, VW, NU>& y, int pos) {
+        if (half == 0) return;
+        const float* table = a.rope + min(max((int64_t)pos, (int64_t)0), a.max_pos - 1) * a.rot;
 #pragma unroll
         for (int n = 0; n < NU; ++n) {
             const int u = l + (n << P.lg);
             if (u >= P.pair_units) continue;
             if constexpr (VW == 1) {
-                cs[n][0] = __ldg(table + u);
-                sn[n][0] = __ldg(table + half + u);
+                y.cs[n][0] = __ldg(table + u);
+                y.sn[n][0] = __ldg(table + half + u);
             } else {
 #pragma unroll
                 for (int e = 0; e < VW; e += 4) {
-                    *reinterpret_cast<float4*>(&cs[n][e]) = __ldg(reinterpret_cast<const float4*>(table + u * VW + e));
-                    *reinterpret_cast<float4*>(&sn[n][e]) = __ldg(reinterpret_cast<const float4*>(table + half + u * VW + e));
+                    *reinterpret_cast<float4*>(&y.cs[n][e]) = __ldg(reinterpret_cast<const float4*>(table + u * VW + e));
+                    *reinterpret_cast<float4*>(&y.sn[n][e]) = __ldg(reinterpret_cast<const float4*>(table + half + u * VW + e));
                 }
             }
         }
+    };
+
+    Item<T, VW, NU> cur, nxt;
+    uint32_t tok = it / (uint32_t)P.parts, tok1 = (it + stride) / (uint32_t)P.parts;
+    fetch_x(cur, tok, (int)(it - tok * P.parts));
+    int64_t slot = __ldg(a.slot + tok), slot1 = -1;
+    int pos = half > 0 ? __ldg(a.pos + tok) : 0, pos1 = 0;
+    if (it + stride < items) {
+        slot1 = __ldg(a.slot + tok1);
+        if (half > 0) pos1 = __ldg(a.pos + tok1);
     }
-    if (flag && part == 0 && lane == 0 && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
-    const bool any_norm = a.q_norm != nullptr || a.k_norm != nullptr;
+    fetch_rope(cur, pos);
+    while (true) {
+        const int part = (int)(it - tok * P.parts);
+        const bool more = it + stride < items;
+        const uint32_t tok2 = (it + 2 * stride) / (uint32_t)P.parts;
+        int64_t slot2 = -1;
+        int pos2 = 0;
+        if (more) {
+            fetch_x(nxt, tok1, (int)(it + stride - tok1 * P.parts));
+            if (items - it > 2 * stride) {
+                slot2 = __ldg(a.slot + tok2);
+                if (half > 0) pos2 = __ldg(a.pos + tok2);
+            }
+            fetch_rope(nxt, pos1);
+        }
+
+        int64_t page = 0;
+        int in_page = 0;
+        bool kept = slot >= 0;
+        if (kept) {
+            page = (slot >> 32) != 0 ? slot / a.c.page_size : (int64_t)((uint32_t)slot / (uint32_t)a.c.page_size);
+            in_page = (int)(slot - page * a.c.page_size);
+            kept = page < a.c.n_pages;
+        }
+        if (((slot >= 0 && !kept) || (half > 0 && (pos < 0 || pos >= a.max_pos))) && part == 0 && lane == 0 && a.status)
+            atomicOr(a.status, PPS_FLAG_INDEX);
 
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-        if (h0 - (lane >> P.lg) + j * hp >= H) break;  // warp-uniform
-        const int h = h0 + j * hp;
-        const bool is_q = h < a.n_heads, turned = h < a.n_heads + n_kv;  // queries; queries and keys
-        T* dst = nullptr;
-        if (is_q)
-            dst = static_cast<T*>(a.out.p) + tok * a.out.tok + h * a.out.head;
-        else if (h < H && kept)
-            dst = static_cast<T*>(turned ? a.c.k : a.c.v) + page * a.c.page + in_page * a.c.tok +
-                  (h - a.n_heads - (turned ? 0 : n_kv)) * a.c.head;
-        const T* w = static_cast<const T*>(is_q ? a.q_norm : a.k_norm);
-        if (!turned || dst == nullptr) w = nullptr;
-        float r = 1.0f;
-        if (any_norm) {  // uniform: every lane takes part in the shuffles
-            float ss = 0.0f;
-            if (w != nullptr) {
+        for (int j = 0; j < kAhead; ++j) {
+            if ((part * kAhead + j) * hp >= H) break;  // warp-uniform
+            const int h = (part * kAhead + j) * hp + group;
+            const bool is_q = h < a.n_heads, turned = h < n_qk;  // queries; queries and keys
+            T* dst = nullptr;
+            if (is_q)
+                dst = static_cast<T*>(a.out.p) + tok * a.out.tok + h * a.out.head;
+            else if (h < H && kept)
+                dst = static_cast<T*>(turned ? a.c.k : a.c.v) + page * a.c.page + in_page * a.c.tok +
+                      (h - (turned ? a.n_heads : n_qk)) * a.c.head;
+            const T* w = static_cast<const T*>(is_q ? a.q_norm : a.k_norm);
+            if (!turned || dst == nullptr) w = nullptr;
+            float r = 1.0f;
+            Vec<T, VW> wv[NU][2];
+            if (any_norm) {  // uniform: every lane takes part in the shuffles
+                float ss = 0.0f;
+                if (w != nullptr) {
 #pragma unroll
-                for (int n = 0; n < NU; ++n)
+                    for (int n = 0; n < NU; ++n)
+#pragma unroll
+                        for (int v = 0; v < 2; ++v)
+                            if ((v ? c1[n] : c0[n]) < D) {
+                                load(wv[n][v], w + (v ? c1[n] : c0[n]));
+#pragma unroll
+                                for (int e = 0; e < VW; ++e) {
+                                    const float f = to_f(cur.x[j][n][v].e[e]);
+                                    ss = fmaf(f, f, ss);
+                                }
+                            }
+                }
+                for (int o = (1 << P.lg) >> 1; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+                r = rsqrtf(fmaf(ss, P.inv_d, a.eps));
+            }
+            if (dst == nullptr) continue;
+#pragma unroll
+            for (int n = 0; n < NU; ++n) {
+                if (c0[n] >= D) continue;
+                if (turned) {
+                    float f[2][VW];
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) {
+                        if ((v ? c1[n] : c0[n]) >= D) continue;
+#pragma unroll
+                        for (int e = 0; e < VW; ++e) f[v][e] = to_f(cur.x[j][n][v].e[e]);
+                        if (w != nullptr)
+#pragma unroll
+                            for (int e = 0; e < VW; ++e) f[v][e] *= r * to_f(wv[n][v].e[e]);
+                    }
+                    if (c0[n] < a.rot) {
+                        if (VW > 1 && a.interleaved) {
+#pragma unroll
+                            for (int v = 0; v < 2; ++v)
+#pragma unroll
+                                for (int e = 0; e + 1 < VW; e += 2) {
+                                    const float c = cur.cs[n][(v * VW + e) >> 1], s = cur.sn[n][(v * VW + e) >> 1];
+                                    const float p = f[v][e], q = f[v][e + 1];
+                                    f[v][e] = p * c - q * s;
+                                    f[v][e + 1] = p * s + q * c;
+                                }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < VW; ++e) {
+                                const float p = f[0][e], q = f[1][e];
+                                f[0][e] = p * cur.cs[n][e] - q * cur.sn[n][e];
+                                f[1][e] = p * cur.sn[n][e] + q * cur.cs[n][e];
+                            }
+                        }
+                    }
 #pragma unroll
                     for (int v = 0; v < 2; ++v)
                         if ((v ? c1[n] : c0[n]) < D)
 #pragma unroll
-                            for (int e = 0; e < VW; ++e) {
-                                const float f = to_f(x[j][n][v].e[e]);
-                                ss = fmaf(f, f, ss);
-                            }
-            }
-            for (int o = (1 << P.lg) >> 1; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-            r = 1.0f / sqrtf(ss / (float)D + a.eps);
-        }
-        if (dst == nullptr) continue;
-#pragma unroll
-        for (int n = 0; n < NU; ++n) {
-            if (c0[n] >= D) continue;
-            if (turned) {
-                float f[2][VW];
-#pragma unroll
-                for (int v = 0; v < 2; ++v) {
-                    const int c = v ? c1[n] : c0[n];
-                    if (c >= D) continue;
-                    if (w != nullptr) {
-                        Vec<T, VW> wv;
-                        load(wv, w + c);
-#pragma unroll
-                        for (int e = 0; e < VW; ++e) f[v][e] = to_f(x[j][n][v].e[e]) * r * to_f(wv.e[e]);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < VW; ++e) f[v][e] = to_f(x[j][n][v].e[e]);
-                    }
+                            for (int e = 0; e < VW; ++e) cur.x[j][n][v].e[e] = from_f<T>(f[v][e]);
                 }
-                if (c0[n] < a.rot) {
-                    if (VW > 1 && a.interleaved) {
-#pragma unroll
-                        for (int v = 0; v < 2; ++v)
-#pragma unroll
-                            for (int e = 0; e + 1 < VW; e += 2) {
-                                const float c = cs[n][(v * VW + e) >> 1], s = sn[n][(v * VW + e) >> 1];
-                                const float p = f[v][e], q = f[v][e + 1];
-                                f[v][e] = p * c - q * s;
-                                f[v][e + 1] = p * s + q * c;
-                            }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < VW; ++e) {
-                            const float p = f[0][e], q = f[1][e];
-                            f[0][e] = p * cs[n][e] - q * sn[n][e];
-                            f[1][e] = p * sn[n][e] + q * cs[n][e];
-                        }
-                    }
-                }
-#pragma unroll
-                for (int v = 0; v < 2; ++v)
-                    if ((v ? c1[n] : c0[n]) < D)
-#pragma unroll
-                        for (int e = 0; e < VW; ++e) x[j][n][v].e[e] = from_f<T>(f[v][e]);
+                store(dst + c0[n], cur.x[j][n][0]);
+                if (c1[n] < D) store(dst + c1[n], cur.x[j][n][1]);
             }
-            store(dst + c0[n], x[j][n][0]);
-            if (c1[n] < D) store(dst + c1[n], x[j][n][1]);
         }
+        if (!more) break;
+        it += stride;
+        cur = nxt;
+        tok = tok1;
+        tok1 = tok2;
+        slot = slot1;
+        slot1 = slot2;
+        pos = pos1;
+        pos1 = pos2;
     }
 }
 
@@ -241,10 +277,12 @@ cudaError_t launch(const AppendArgs& a, cudaStream_t st) {
     P.lg = 0;
     while (P.lg < 5 && (1 << P.lg) < P.units) ++P.lg;
     const int H = a.n_heads + 2 * a.c.n_kv_heads;
-    const int per_warp = kAhead * (32 >> P.lg);  // heads
-    P.wpt = (H + per_warp - 1) / per_warp;
-    const int64_t blocks = (a.n_tok * P.wpt + kAppendWarps - 1) / kAppendWarps;
-    if (blocks > INT32_MAX / kAppendWarps) return cudaErrorInvalidValue;
+    const int per_item = kAhead * (32 >> P.lg);  // heads
+    P.parts = (H + per_item - 1) / per_item;
+    P.inv_d = 1.0f / (float)a.c.head_dim;
+    const int64_t items = a.n_tok * P.parts, most = (int64_t)device_sm_count() * kAppendCtas;
+    if (items > INT32_MAX) return cudaErrorInvalidValue;
+    const int64_t blocks = std::min((items + kAppendWarps - 1) / kAppendWarps, most);
     append_kernel<T, VW, NU><<<(unsigned)blocks, 32 * kAppendWarps, 0, st>>>(a, P);
     return cudaGetLastError();
 }

@@ -52,6 +52,12 @@ __device__ __forceinline__ float ex2(float x) {
     asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// the same in one instruction, below 2^-126 zero: for sums, and for races (some token has a probability of 1 / V)
+__device__ __forceinline__ float ex2z(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 // exp2(c (l - m)), 1 at the maximum itself
 __device__ __forceinline__ float weight(float l, float m, float c) { return l == m ? 1.0f : ex2(c * (l - m)); }
 __device__ __forceinline__ float usable(float l) { return l != l ? -INFINITY : l; }
@@ -140,8 +146,8 @@ __device__ __forceinline__ void add_logits(const uint4 (&x)[kVecs], float& m, fl
         for (int e = 0; e < E::kVW; e += 2) {
             float x0 = E::at(x[j], e), x1 = E::at(x[j], e + 1);
             scale2(x0, x1, c, bm);
-            bs += ex2(x0);
-            b1 += ex2(x1);
+            bs += ex2z(x0);
+            b1 += ex2z(x1);
         }
     bs += b1;
     if (bs != bs) {  // NaN among the logits, or an infinite maximum
@@ -263,6 +269,7 @@ __device__ __forceinline__ Best race(const T* p, const T* q, const float* noise,
                                      int64_t t0, int64_t t1, int64_t V) {
     Best b = {0.0f, INT_MAX};  // only positive scores count
     const float ip = sp.s > 0.0f ? 1.0f / sp.s : 0.0f, iq = sq.s > 0.0f ? 1.0f / sq.s : 0.0f;
+    const bool finite = fabsf(sp.m) < INFINITY && (q == nullptr || fabsf(sq.m) < INFINITY);  // CTA-uniform
     float x[8], y[8];
     int64_t t = t0 + 8 * threadIdx.x;
     if (t < t1) {
@@ -270,18 +277,44 @@ __device__ __forceinline__ Best race(const T* p, const T* q, const float* noise,
         if (q != nullptr) load8(y, q, t, V, -INFINITY);
     }
     while (t < t1) {
-        float xn[8], yn[8], zn[8];
+        float xn[8], yn[8], zn[8], d[8];
         const int64_t tn = t + 8 * kRaceThreads;
         if (tn < t1) {
             load8(xn, p, tn, V, -INFINITY);
             if (q != nullptr) load8(yn, q, tn, V, -INFINITY);
             load8(zn, noise, tn, V, 1.0f);
         }
+        if (finite) {
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                scale2(x[e], x[e + 1], c, sp.m);
+                d[e] = ex2z(x[e]) * ip;
+                d[e + 1] = ex2z(x[e + 1]) * ip;
+                if (q != nullptr) {
+                    scale2(y[e], y[e + 1], c, sq.m);
+                    d[e] = fmaf(ex2z(fmaxf(y[e], -INFINITY)), -iq, d[e]);  // a NaN logit of the drafter's counts as -inf
+                    d[e + 1] = fmaf(ex2z(fmaxf(y[e + 1], -INFINITY)), -iq, d[e + 1]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                d[e] = weight(usable(x[e]), sp.m, c) * ip;
+                if (q != nullptr) d[e] -= weight(usable(y[e]), sq.m, c) * iq;
+            }
+        }
+        // a token is looked at closely (the quotient, ties) only if it is not clearly below the best so far
+        const float low = b.v * 0.999999f;
+        uint32_t near = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (d[e] > 0.0f && !(d[e] < low * z[e])) near |= 1u << e;
+        if (near)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if ((near >> e & 1u) && t + e < t1) better(b, d[e] / z[e], (int)(t + e));
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            float d = weight(usable(x[e]), sp.m, c) * ip;
-            if (q != nullptr) d -= weight(usable(y[e]), sq.m, c) * iq;
-            if (t + e < t1 && d > 0.0f) better(b, d / z[e], (int)(t + e));
             x[e] = xn[e];
             y[e] = yn[e];
             z[e] = zn[e];
