@@ -469,6 +469,12 @@ typedef struct {
 } pps_heads;
 
 /*
+ * The three calls below take their arguments in one struct in HOST memory, read
+ * before the call returns; `size` guards against a caller built for another
+ * layout (PPS_ERR_INVALID_ARG).  Pointers in it are device memory as everywhere.
+ */
+
+/*
  * pps_kv_append -- queries and keys of n_tok new tokens are normed per head
  * (optional) and rotated to the tokens' positions; keys and values are written
  * to their cache slots.  One pass over the projections' outputs.
@@ -495,10 +501,22 @@ typedef struct {
  * Any alignment is accepted; 16-byte aligned bases and strides (and rot a
  * multiple of 16) are moved in 16-byte units.
  */
-pps_status pps_kv_append(pps_heads q, pps_heads k, pps_heads v, pps_dtype dtype, int64_t n_tok, int32_t n_heads,
-                         pps_kv_cache cache, const void* q_norm, const void* k_norm, float eps, const float* rope,
-                         int64_t max_pos, int32_t rot, int32_t interleaved, const int32_t* pos, const int64_t* slot,
-                         pps_heads out_q, uint32_t* status, pps_stream_t stream);
+typedef struct {
+    size_t size; /* sizeof(pps_append_args) */
+    pps_heads q, k, v, out_q;
+    pps_kv_cache cache;
+    const void* q_norm;
+    const void* k_norm;
+    const float* rope;
+    const int32_t* pos;
+    const int64_t* slot;
+    uint32_t* status;
+    int64_t n_tok, max_pos;
+    int32_t dtype; /* pps_dtype */
+    int32_t n_heads, rot, interleaved;
+    float eps;
+} pps_append_args;
+pps_status pps_kv_append(const pps_append_args* args, pps_stream_t stream);
 
 /*
  * pps_paged_attention -- attention of the newest tokens of n_seq sequences
@@ -538,11 +556,24 @@ pps_status pps_kv_append(pps_heads q, pps_heads k, pps_heads v, pps_dtype dtype,
  *              bytes; need not be cleared
  */
 size_t pps_attention_workspace_size(int64_t n_tok, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
-pps_status pps_paged_attention(pps_heads q, pps_dtype dtype, int64_t n_tok, int32_t n_heads, pps_kv_cache cache,
-                               const int32_t* pages, int64_t pages_stride, int32_t max_pages, const int32_t* kv_len,
-                               const int32_t* q_off, int32_t n_seq, const uint32_t* mask, int32_t mask_words,
-                               float scale, pps_heads out, float* out_lse, uint32_t* status, void* ws, size_t ws_bytes,
-                               pps_stream_t stream);
+typedef struct {
+    size_t size; /* sizeof(pps_attention_args) */
+    pps_heads q, out;
+    pps_kv_cache cache;
+    const int32_t* pages;
+    const int32_t* kv_len;
+    const int32_t* q_off;
+    const uint32_t* mask;
+    float* out_lse;
+    uint32_t* status;
+    void* ws;
+    size_t ws_bytes;
+    int64_t n_tok, pages_stride;
+    int32_t dtype; /* pps_dtype */
+    int32_t n_heads, max_pages, n_seq, mask_words;
+    float scale;
+} pps_attention_args;
+pps_status pps_paged_attention(const pps_attention_args* args, pps_stream_t stream);
 
 /*
  * pps_verify_chain -- the token-level maximal coupling (Alg. 1) along drafted
@@ -577,12 +608,28 @@ pps_status pps_paged_attention(pps_heads q, pps_dtype dtype, int64_t n_tok, int3
  *              be cleared
  */
 size_t pps_chain_workspace_size(int64_t n_nodes, int64_t n_draft, int32_t n_seq);
-pps_status pps_verify_chain(const void* p_logits, const void* q_logits, pps_dtype dtype, int64_t n_nodes,
-                            int64_t n_draft, int64_t vocab, int64_t p_stride, int64_t q_stride, float temperature,
-                            int32_t n_seq, int32_t gamma, const int32_t* seq_off, const int32_t* node_draft_row,
-                            const int32_t* draft_tok, const float* u, const float* noise, int64_t noise_stride,
-                            int32_t* out_accept_len, int32_t* out_n_emitted, int32_t* out_emitted,
-                            float* out_accept_prob, uint32_t* status, void* ws, size_t ws_bytes, pps_stream_t stream);
+typedef struct {
+    size_t size; /* sizeof(pps_chain_args) */
+    const void* p_logits;
+    const void* q_logits;
+    const int32_t* seq_off;
+    const int32_t* node_draft_row;
+    const int32_t* draft_tok;
+    const float* u;
+    const float* noise;
+    int32_t* out_accept_len;
+    int32_t* out_n_emitted;
+    int32_t* out_emitted;
+    float* out_accept_prob;
+    uint32_t* status;
+    void* ws;
+    size_t ws_bytes;
+    int64_t n_nodes, n_draft, vocab, p_stride, q_stride, noise_stride;
+    int32_t dtype; /* pps_dtype */
+    int32_t n_seq, gamma;
+    float temperature;
+} pps_chain_args;
+pps_status pps_verify_chain(const pps_chain_args* args, pps_stream_t stream);
 
 /*
  * pps_draft_list_noalloc -- pps_draft_list for callers that must not

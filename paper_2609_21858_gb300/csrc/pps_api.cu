@@ -631,10 +631,11 @@ static CacheView cache_view(const pps_kv_cache& c) {
     return {c.k, c.v, c.n_pages, c.page_size, c.n_kv_heads, c.head_dim, c.page_stride, c.tok_stride, c.head_stride};
 }
 
-pps_status pps_kv_append(pps_heads q, pps_heads k, pps_heads v, pps_dtype dtype, int64_t n_tok, int32_t n_heads,
-                         pps_kv_cache cache, const void* q_norm, const void* k_norm, float eps, const float* rope,
-                         int64_t max_pos, int32_t rot, int32_t interleaved, const int32_t* pos, const int64_t* slot,
-                         pps_heads out_q, uint32_t* status, pps_stream_t stream) {
+pps_status pps_kv_append(const pps_append_args* args, pps_stream_t stream) {
+    if (!args || args->size != sizeof(*args)) return PPS_ERR_INVALID_ARG;
+    const auto& [size, q, k, v, out_q, cache, q_norm, k_norm, rope, pos, slot, status, n_tok, max_pos, dtype, n_heads, rot,
+                 interleaved, eps] = *args;
+    (void)size;
     if (dtype != PPS_BF16 && dtype != PPS_F16) return PPS_ERR_UNSUPPORTED;
     pps_status st = check_cache(cache);
     if (st != PPS_OK) return st;
@@ -678,11 +679,11 @@ size_t pps_attention_workspace_size(int64_t n_tok, int32_t n_heads, int32_t n_kv
     return attention_workspace_bytes(n_tok, n_heads, n_kv_heads, head_dim);
 }
 
-pps_status pps_paged_attention(pps_heads q, pps_dtype dtype, int64_t n_tok, int32_t n_heads, pps_kv_cache cache,
-                               const int32_t* pages, int64_t pages_stride, int32_t max_pages, const int32_t* kv_len,
-                               const int32_t* q_off, int32_t n_seq, const uint32_t* mask, int32_t mask_words,
-                               float scale, pps_heads out, float* out_lse, uint32_t* status, void* ws, size_t ws_bytes,
-                               pps_stream_t stream) {
+pps_status pps_paged_attention(const pps_attention_args* args, pps_stream_t stream) {
+    if (!args || args->size != sizeof(*args)) return PPS_ERR_INVALID_ARG;
+    const auto& [size, q, out, cache, pages, kv_len, q_off, mask, out_lse, status, ws, ws_bytes, n_tok, pages_stride, dtype,
+                 n_heads, max_pages, n_seq, mask_words, scale] = *args;
+    (void)size;
     if (dtype != PPS_BF16 && dtype != PPS_F16) return PPS_ERR_UNSUPPORTED;
     pps_status st = check_cache(cache);
     if (st != PPS_OK) return st;
@@ -736,12 +737,12 @@ size_t pps_chain_workspace_size(int64_t n_nodes, int64_t n_draft, int32_t n_seq)
     return chain_workspace_bytes(n_nodes, n_draft, n_seq);
 }
 
-pps_status pps_verify_chain(const void* p_logits, const void* q_logits, pps_dtype dtype, int64_t n_nodes,
-                            int64_t n_draft, int64_t vocab, int64_t p_stride, int64_t q_stride, float temperature,
-                            int32_t n_seq, int32_t gamma, const int32_t* seq_off, const int32_t* node_draft_row,
-                            const int32_t* draft_tok, const float* u, const float* noise, int64_t noise_stride,
-                            int32_t* out_accept_len, int32_t* out_n_emitted, int32_t* out_emitted,
-                            float* out_accept_prob, uint32_t* status, void* ws, size_t ws_bytes, pps_stream_t stream) {
+pps_status pps_verify_chain(const pps_chain_args* args, pps_stream_t stream) {
+    if (!args || args->size != sizeof(*args)) return PPS_ERR_INVALID_ARG;
+    const auto& [size, p_logits, q_logits, seq_off, node_draft_row, draft_tok, u, noise, out_accept_len, out_n_emitted,
+                 out_emitted, out_accept_prob, status, ws, ws_bytes, n_nodes, n_draft, vocab, p_stride, q_stride,
+                 noise_stride, dtype, n_seq, gamma, temperature] = *args;
+    (void)size;
     if (dtype != PPS_F32 && dtype != PPS_BF16) return PPS_ERR_UNSUPPORTED;
     if (n_nodes < 0 || n_nodes > INT32_MAX || n_draft < 0 || n_draft > INT32_MAX || vocab < 1 || vocab > INT32_MAX)
         return PPS_ERR_INVALID_ARG;

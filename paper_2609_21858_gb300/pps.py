@@ -8,6 +8,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import struct
 import threading
 
 import torch
@@ -42,16 +43,6 @@ _lib = None
 
 class RowIds(ctypes.Structure):
     _fields_ = [("key", ctypes.c_void_p), ("ctx_hash", ctypes.c_void_p), ("pos", ctypes.c_void_p)]
-
-
-class Heads(ctypes.Structure):  # pps_heads
-    _fields_ = [("data", ctypes.c_void_p), ("tok_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
-
-
-class KVCache(ctypes.Structure):  # pps_kv_cache
-    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("n_pages", ctypes.c_int64),
-                ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
-                ("page_stride", ctypes.c_int64), ("tok_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 class PPSError(RuntimeError):
@@ -140,19 +131,12 @@ def lib():
             L.pps_lmhead_verify_tree.argtypes = [vp, i64, vp, i64, i64, i64, i64, RowIds, f32, i32, i32, vp, vp, i64,
                                                  vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
             L.pps_lmhead_verify_tree.restype = ctypes.c_int
-            L.pps_kv_append.argtypes = [Heads, Heads, Heads, ctypes.c_int, i64, i32, KVCache, vp, vp, f32, vp, i64, i32,
-                                        i32, vp, vp, Heads, vp, vp]
-            L.pps_kv_append.restype = ctypes.c_int
+            for fn in (L.pps_kv_append, L.pps_paged_attention, L.pps_verify_chain):
+                fn.argtypes, fn.restype = [ctypes.c_char_p, vp], ctypes.c_int
             L.pps_attention_workspace_size.argtypes = [i64, i32, i32, i32]
             L.pps_attention_workspace_size.restype = sz
-            L.pps_paged_attention.argtypes = [Heads, ctypes.c_int, i64, i32, KVCache, vp, i64, i32, vp, vp, i32, vp, i32,
-                                              f32, Heads, vp, vp, vp, sz, vp]
-            L.pps_paged_attention.restype = ctypes.c_int
             L.pps_chain_workspace_size.argtypes = [i64, i64, i32]
             L.pps_chain_workspace_size.restype = sz
-            L.pps_verify_chain.argtypes = [vp, vp, ctypes.c_int, i64, i64, i64, i64, i64, f32, i32, i32, vp, vp, vp, vp,
-                                           vp, i64, vp, vp, vp, vp, vp, vp, sz, vp]
-            L.pps_verify_chain.restype = ctypes.c_int
             L.pps_philox_words.argtypes = [RowIds, i64, i64, i32, vp, vp]
             L.pps_philox_words.restype = ctypes.c_int
             L.pps_selftest_philox_rate.argtypes = [u64, vp, i32, vp]
@@ -659,8 +643,18 @@ def lmhead_verify_tree(hidden, weight, key, ctx, pos, gamma: int, seq_off, node_
 
 
 # ---------------------------------------------------------------- target side of a step
+#
+# Host cost: kv_append of a few tokens runs one launch of 3 us, and took 17 us of Python and ctypes with an object
+# per tensor and an argument each.  The argument structs of these calls are packed by struct.Struct in one go
+# (0.5 us for 40 fields), and the checks go by device index and one shape and stride tuple per tensor.
 
 _HALVES = {torch.bfloat16: BF16, torch.float16: F16}
+
+# the layouts of pps_append_args, pps_attention_args and pps_chain_args ("0q": padded to the struct's alignment)
+_CACHE_FIELDS = "PPqiiiqqq"
+_APPEND_ARGS = struct.Struct("@N" + "Pqq" * 4 + _CACHE_FIELDS + "PPPPPP" + "qq" + "iiiif" + "0q")
+_ATTENTION_ARGS = struct.Struct("@N" + "Pqq" * 2 + _CACHE_FIELDS + "PPPPPPPN" + "qq" + "iiiiif" + "0q")
+_CHAIN_ARGS = struct.Struct("@N" + "P" * 13 + "N" + "q" * 6 + "iiif" + "0q")
 
 
 def _own_memory(stream):
@@ -669,34 +663,63 @@ def _own_memory(stream):
     return _HERE_ALREADY if stream is None else torch.cuda.stream(stream)
 
 
-def _heads(name, t, dev, dtype, n=None, heads=None, d=None):
-    """A [n, heads, d] view with contiguous channels, any token and head strides."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != dev.index:
-        raise TypeError(f"{name} must be a CUDA tensor on {dev}")
-    if t.dtype is not dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise TypeError(f"{name} must be [tokens, heads, channels] with unit stride along the channels")
-    shape = t.shape
-    if (n is not None and shape[0] != n) or (heads is not None and shape[1] != heads) or (d is not None and shape[2] != d):
-        raise ValueError(f"{name} is {list(shape)}; the call needs {[n, heads, d]}")
-    return Heads(t.data_ptr(), t.stride(0), t.stride(1))
+def _handle(stream, di):
+    """The stream's handle; with no stream, the current stream of device di (the tensors')."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(di)
+    if stream.device.index != di:
+        raise ValueError(f"stream is on {stream.device}, the tensors on cuda:{di}")
+    return stream.cuda_stream
 
 
-def _cache(k, v, dev, dtype):
-    """The two halves of a paged cache, [pages, page_size, kv heads, channels], of the same strides."""
-    for name, t in (("k_cache", k), ("v_cache", v)):
-        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != dev.index:
-            raise TypeError(f"{name} must be a CUDA tensor on {dev}")
-        if t.dtype is not dtype:
-            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-        if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
-            raise TypeError(f"{name} must be [pages, page_size, heads, channels] with unit stride along the channels")
-    if k.shape != v.shape or k.stride() != v.stride():
-        raise ValueError("k_cache and v_cache must have the same shape and strides")
-    n, page, heads, d = k.shape
-    sp, st, sh, _ = k.stride()
-    return KVCache(k.data_ptr(), v.data_ptr(), n, page, heads, d, sp, st, sh)
+def _strided(name, t, di, dt, shape, what):
+    """Strides of tensor `t` of dtype `dt` on device di: contiguous along its last dimension, its sizes those of
+    `shape` (None: any)."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != di:
+        raise TypeError(f"{name} must be a CUDA tensor on cuda:{di}")
+    if t.dtype is not dt:
+        raise TypeError(f"{name} must be {dt}, got {t.dtype}")
+    have, st = t.shape, t.stride()
+    if len(have) != len(shape) or (st[-1] != 1 and have[-1] > 1):
+        raise TypeError(f"{name} must be {what} with unit stride along the last dimension")
+    for x, y in zip(have, shape):
+        if y is not None and x != y:
+            raise ValueError(f"{name} is {list(have)}; the call needs {list(shape)} ({what})")
+    return st
+
+
+def _flat(name, t, di, dt, numel):
+    """Address of a contiguous tensor of at least numel elements (0 when it is None)."""
+    if t is None:
+        return 0
+    if isinstance(t, torch.Tensor) and t.get_device() == di and t.dtype is dt and t.is_contiguous() and t.numel() >= numel:
+        return t.data_ptr()
+    _need(name, t, torch.device("cuda", di), dt, numel)
+    return t.data_ptr()
+
+
+def _half_rows(q):
+    """Device index, dtype and dtype code of the queries."""
+    if not isinstance(q, torch.Tensor) or not q.is_cuda:
+        raise TypeError("q must be a CUDA tensor")
+    if q.dtype not in _HALVES:
+        raise TypeError(f"q must be bfloat16 or float16, got {q.dtype}")
+    if q.dim() != 3:
+        raise TypeError("q must be [tokens, heads, channels]")
+    return q.get_device(), q.dtype, _HALVES[q.dtype]
+
+
+_HEADS = "[tokens, heads, channels]"
+_CACHE = "[pages, page_size, heads, channels]"
+
+
+def _cache(k, v, di, dt, d):
+    """The fields of pps_kv_cache of the two halves of a paged cache, which have the same strides."""
+    st = _strided("k_cache", k, di, dt, (None, None, None, d), _CACHE)
+    n, page, heads, _ = shape = k.shape
+    if _strided("v_cache", v, di, dt, shape, _CACHE) != st:
+        raise ValueError("k_cache and v_cache must have the same strides")
+    return k.data_ptr(), v.data_ptr(), n, page, heads, d, st[0], st[1], st[2]
 
 
 def rope_table(max_pos: int, rot: int, base: float = 10000.0, device=None) -> torch.Tensor:
@@ -716,35 +739,38 @@ def kv_append(q, k, v, pos, slot, k_cache, v_cache, rope, q_norm=None, k_norm=No
     their cache slots.  Returns the queries (`out`, which may be q).  q [n, heads, d]; k, v [n, kv heads, d];
     k_cache, v_cache [pages, page_size, kv heads, d]; rope: rope_table or None (no rotation); slot int64, < 0:
     not written."""
-    dev, dt = q.device, q.dtype
-    if dt not in _HALVES:
-        raise TypeError(f"q must be bfloat16 or float16, got {dt}")
-    hq = _heads("q", q, dev, dt)
-    n, heads, d = q.shape
-    cache = _cache(k_cache, v_cache, dev, dt)
-    hk = _heads("k", k, dev, dt, n, cache.n_kv_heads, d)
-    hv = _heads("v", v, dev, dt, n, cache.n_kv_heads, d)
-    if cache.head_dim != d:
-        raise ValueError(f"the cache has {cache.head_dim} channels a head, q {d}")
-    rot = max_pos = 0
+    di, dt, code = _half_rows(q)
+    n, heads, d = shape = q.shape
+    cache = _cache(k_cache, v_cache, di, dt, d)
+    kv_shape = (n, cache[4], d)
+    sq = _strided("q", q, di, dt, shape, _HEADS)
+    sk = _strided("k", k, di, dt, kv_shape, _HEADS)
+    sv = _strided("v", v, di, dt, kv_shape, _HEADS)
+    rot = max_pos = table = at = 0
     if rope is not None:
         if rope.dim() != 2:
             raise TypeError("rope must be [max_pos, rot]")
         max_pos, rot = rope.shape
-        _need("rope", rope, dev, torch.float32)
-        _need("pos", pos, dev, torch.int32, n)
-    _need("slot", slot, dev, torch.int64, n)
-    _need("q_norm", q_norm, dev, dt, d)
-    _need("k_norm", k_norm, dev, dt, d)
-    _need("status", status, dev, torch.int32, 1)
-    with _on(dev):
-        if out is None:
-            with _own_memory(stream):
-                out = torch.empty(n, heads, d, dtype=dt, device=dev)
-        code = lib().pps_kv_append(hq, hk, hv, _HALVES[dt], n, heads, cache, _ptr(q_norm), _ptr(k_norm), eps,
-                                   _ptr(rope), max_pos, rot, 1 if interleaved else 0, _ptr(pos), _ptr(slot),
-                                   _heads("out", out, dev, dt, n, heads, d), _ptr(status), _stream(stream, dev))
-    _check("pps_kv_append", code)
+        table, at = _flat("rope", rope, di, torch.float32, 0), _flat("pos", pos, di, torch.int32, n)
+        if pos is None:
+            raise TypeError("pos is required")
+    if slot is None:
+        raise TypeError("slot is required")
+    slots = _flat("slot", slot, di, torch.int64, n)
+    wq, wk = _flat("q_norm", q_norm, di, dt, d), _flat("k_norm", k_norm, di, dt, d)
+    flags = _flat("status", status, di, torch.int32, 1)
+    if torch._C._cuda_getDevice() != di:
+        with torch.cuda.device(di):
+            return kv_append(q, k, v, pos, slot, k_cache, v_cache, rope, q_norm, k_norm, eps, interleaved, out, status,
+                             stream)
+    if out is None:
+        with _own_memory(stream):
+            out = torch.empty(n, heads, d, dtype=dt, device=q.device)
+    so = _strided("out", out, di, dt, shape, _HEADS)
+    args = _APPEND_ARGS.pack(_APPEND_ARGS.size, q.data_ptr(), sq[0], sq[1], k.data_ptr(), sk[0], sk[1], v.data_ptr(),
+                             sv[0], sv[1], out.data_ptr(), so[0], so[1], *cache, wq, wk, table, at, slots, flags, n,
+                             max_pos, code, heads, rot, 1 if interleaved else 0, eps)
+    _check("pps_kv_append", lib().pps_kv_append(args, _handle(stream, di)))
     return out
 
 
@@ -760,43 +786,42 @@ def paged_attention(q, k_cache, v_cache, pages, kv_len, q_off, mask=None, scale=
     q_off[s] .. q_off[s+1]-1) attend to the paged cache.  pages [n_seq, columns] int32, kv_len [n_seq] int32
     (the new tokens' own keys included); mask [n, words] int32 tree masks, None: causal; scale None: 1/sqrt(d);
     lse: an optional [n, heads] float32 output.  Returns out."""
-    dev, dt = q.device, q.dtype
-    if dt not in _HALVES:
-        raise TypeError(f"q must be bfloat16 or float16, got {dt}")
-    hq = _heads("q", q, dev, dt)
-    n, heads, d = q.shape
-    cache = _cache(k_cache, v_cache, dev, dt)
-    if cache.head_dim != d:
-        raise ValueError(f"the cache has {cache.head_dim} channels a head, q {d}")
+    di, dt, code = _half_rows(q)
+    n, heads, d = shape = q.shape
+    cache = _cache(k_cache, v_cache, di, dt, d)
+    sq = _strided("q", q, di, dt, shape, _HEADS)
+    i32 = torch.int32
     n_seq = kv_len.numel()
-    if pages.dim() != 2 or pages.shape[0] != n_seq or (pages.shape[1] > 1 and pages.stride(1) != 1):
-        raise TypeError("pages must be [n_seq, columns] with unit stride along the columns")
+    sp = _strided("pages", pages, di, i32, (n_seq, None), "[n_seq, columns]")
     columns = pages.shape[1]
-    pages_stride = pages.stride(0) if n_seq > 1 else columns  # a stride below the columns is the library's to refuse
-    _need("pages", pages, dev, torch.int32, 0, False)
-    _need("kv_len", kv_len, dev, torch.int32)
-    _need("q_off", q_off, dev, torch.int32, n_seq + 1)
-    words = 0
+    lens, offs = _flat("kv_len", kv_len, di, i32, 0), _flat("q_off", q_off, di, i32, n_seq + 1)
+    if not lens or not offs:
+        if kv_len is None or q_off is None:
+            raise TypeError("kv_len and q_off are required")
+    words = bits = 0
     if mask is not None:
         if mask.dim() != 2 or mask.shape[0] != n or mask.shape[1] < 1:
             raise ValueError(f"mask must be [{n}, words]")
-        words = mask.shape[1]
-        _need("mask", mask, dev, torch.int32)
-    _need("lse", lse, dev, torch.float32, n * heads)
-    _need("status", status, dev, torch.int32, 1)
-    _need("ws", ws, dev, torch.uint8)
-    with _on(dev):
-        L = lib()
-        if out is None or ws is None:
-            with _own_memory(stream):
-                if out is None:
-                    out = torch.empty(n, heads, d, dtype=dt, device=dev)
-                if ws is None:
-                    ws = attention_workspace(n, heads, cache.n_kv_heads, d, dev)
-        code = L.pps_paged_attention(hq, _HALVES[dt], n, heads, cache, _ptr(pages), pages_stride, columns, _ptr(kv_len), _ptr(q_off), n_seq, _ptr(mask), words,
-                                     d ** -0.5 if scale is None else scale, _heads("out", out, dev, dt, n, heads, d),
-                                     _ptr(lse), _ptr(status), _ptr(ws), ws.numel(), _stream(stream, dev))
-    _check("pps_paged_attention", code)
+        words, bits = mask.shape[1], _flat("mask", mask, di, i32, 0)
+    sums, flags = _flat("lse", lse, di, torch.float32, n * heads), _flat("status", status, di, i32, 1)
+    work = _flat("ws", ws, di, torch.uint8, 0)
+    if torch._C._cuda_getDevice() != di:
+        with torch.cuda.device(di):
+            return paged_attention(q, k_cache, v_cache, pages, kv_len, q_off, mask, scale, out, lse, ws, status, stream)
+    if out is None or ws is None:
+        with _own_memory(stream):
+            if out is None:
+                out = torch.empty(n, heads, d, dtype=dt, device=q.device)
+            if ws is None:
+                ws = attention_workspace(n, heads, cache[4], d, q.device)
+                work = ws.data_ptr()
+    so = _strided("out", out, di, dt, shape, _HEADS)
+    # of one sequence, the table's row stride has no meaning; else one below the columns is the library's to refuse
+    args = _ATTENTION_ARGS.pack(_ATTENTION_ARGS.size, q.data_ptr(), sq[0], sq[1], out.data_ptr(), so[0], so[1], *cache,
+                                pages.data_ptr(), lens, offs, bits, sums, flags, work, ws.numel(), n,
+                                sp[0] if n_seq > 1 else columns, code, heads, columns, n_seq, words,
+                                d ** -0.5 if scale is None else scale)
+    _check("pps_paged_attention", lib().pps_paged_attention(args, _handle(stream, di)))
     return out
 
 
@@ -809,45 +834,52 @@ def chain_workspace(n_nodes: int, n_draft: int, n_seq: int, device=None) -> torc
 def verify_chain(p_logits, q_logits, gamma: int, seq_off, node_draft_row, draft_tok, u, noise, temperature: float = 1.0,
                  ws=None, out=None, status=None, stream=None):
     """pps_verify_chain: the token-level maximal coupling along drafted chains of up to gamma tokens, from the
-    uniforms u [n_draft] and exponentials noise [n_seq, V].  Returns dict(accept_len, n_emitted, emitted,
+    uniforms u [n_draft] and exponentials noise [n_seq, >= V].  Returns dict(accept_len, n_emitted, emitted,
     accept_prob); `out` may leave accept_prob out."""
-    n, V, p_stride = _rows(p_logits)
-    n_draft, Vq, q_stride = _rows(q_logits)
-    dev = p_logits.device
-    if Vq != V or q_logits.dtype is not p_logits.dtype or q_logits.device != dev:
-        raise ValueError("p_logits and q_logits must agree in vocabulary, dtype and device")
+    if not isinstance(p_logits, torch.Tensor) or not p_logits.is_cuda:
+        raise TypeError("p_logits must be a CUDA tensor")
+    di, dt, code = p_logits.get_device(), p_logits.dtype, _dtype_code(p_logits)
+    rows = "[rows, vocabulary]"
+    p_stride = _strided("p_logits", p_logits, di, dt, (None, None), rows)[0]
+    n, V = p_logits.shape
+    q_stride = _strided("q_logits", q_logits, di, q_logits.dtype, (None, V), rows)[0]
+    if q_logits.dtype is not dt:
+        raise ValueError("p_logits and q_logits must have the same dtype")
+    n_draft = q_logits.shape[0]
+    i32, f32 = torch.int32, torch.float32
     n_seq = seq_off.numel() - 1
-    if noise.dim() != 2 or noise.shape[0] < n_seq or noise.shape[1] < V or noise.stride(1) != 1:
-        raise ValueError(f"noise must be [{n_seq}, >= {V}] with unit stride along the vocabulary")
-    _need("noise", noise, dev, torch.float32, 0, False)
-    for name, t, dt, numel in (("seq_off", seq_off, torch.int32, n_seq + 1),
-                               ("node_draft_row", node_draft_row, torch.int32, n),
-                               ("draft_tok", draft_tok, torch.int32, n_draft), ("u", u, torch.float32, n_draft)):
-        _need(name, t, dev, dt, numel)
-    _need("status", status, dev, torch.int32, 1)
-    _need("ws", ws, dev, torch.uint8)
+    noise_stride = _strided("noise", noise, di, f32, (None, None), "[n_seq, >= vocabulary]")[0]
+    if noise.shape[0] < n_seq or noise.shape[1] < V:
+        raise ValueError(f"noise is {list(noise.shape)}; the call needs [{n_seq}, >= {V}]")
+    inputs = [_flat(name, t, di, dtype, numel) for name, t, dtype, numel in (
+        ("seq_off", seq_off, i32, n_seq + 1), ("node_draft_row", node_draft_row, i32, n),
+        ("draft_tok", draft_tok, i32, n_draft), ("u", u, f32, n_draft))]
+    flags, work = _flat("status", status, di, i32, 1), _flat("ws", ws, di, torch.uint8, 0)
+    if torch._C._cuda_getDevice() != di:
+        with torch.cuda.device(di):
+            return verify_chain(p_logits, q_logits, gamma, seq_off, node_draft_row, draft_tok, u, noise, temperature, ws,
+                                out, status, stream)
     W = gamma + 1
-    with _on(dev):
-        L = lib()
-        if out is None or ws is None:
-            with _own_memory(stream):
-                if out is None:
-                    e = torch.empty
-                    out = dict(accept_len=e(n_seq, dtype=torch.int32, device=dev),
-                               n_emitted=e(n_seq, dtype=torch.int32, device=dev),
-                               emitted=e(n_seq, W, dtype=torch.int32, device=dev),
-                               accept_prob=e(n_draft, dtype=torch.float32, device=dev))
-                if ws is None:
-                    ws = chain_workspace(n, n_draft, n_seq, dev)
-        for name in ("accept_len", "n_emitted", "emitted"):
-            if out.get(name) is None:
-                raise TypeError(f"out[{name!r}] is required")
-        _need_out(out, [("accept_len", torch.int32, n_seq), ("n_emitted", torch.int32, n_seq),
-                        ("emitted", torch.int32, n_seq * W), ("accept_prob", torch.float32, n_draft)], dev)
-        code = L.pps_verify_chain(_ptr(p_logits), _ptr(q_logits), _dtype_code(p_logits), n, n_draft, V, p_stride,
-                                  q_stride, float(temperature), n_seq, int(gamma), _ptr(seq_off), _ptr(node_draft_row),
-                                  _ptr(draft_tok), _ptr(u), _ptr(noise), noise.stride(0), _ptr(out["accept_len"]),
-                                  _ptr(out["n_emitted"]), _ptr(out["emitted"]), _ptr(out.get("accept_prob")),
-                                  _ptr(status), _ptr(ws), ws.numel(), _stream(stream, dev))
-    _check("pps_verify_chain", code)
+    if out is None or ws is None:
+        with _own_memory(stream):
+            dev = p_logits.device
+            if out is None:
+                e = torch.empty
+                out = dict(accept_len=e(n_seq, dtype=i32, device=dev), n_emitted=e(n_seq, dtype=i32, device=dev),
+                           emitted=e((n_seq, W), dtype=i32, device=dev), accept_prob=e(n_draft, dtype=f32, device=dev))
+            if ws is None:
+                ws = chain_workspace(n, n_draft, n_seq, dev)
+                work = ws.data_ptr()
+    for name in ("accept_len", "n_emitted", "emitted"):
+        if out.get(name) is None:
+            raise TypeError(f"out[{name!r}] is required")
+    # rows of one sequence or one row have no stride
+    args = _CHAIN_ARGS.pack(_CHAIN_ARGS.size, p_logits.data_ptr(), q_logits.data_ptr(), *inputs, noise.data_ptr(),
+                            _flat("accept_len", out["accept_len"], di, i32, n_seq),
+                            _flat("n_emitted", out["n_emitted"], di, i32, n_seq),
+                            _flat("emitted", out["emitted"], di, i32, n_seq * W),
+                            _flat("accept_prob", out.get("accept_prob"), di, f32, n_draft), flags, work, ws.numel(), n,
+                            n_draft, V, p_stride if n > 1 else V, q_stride if n_draft > 1 else V,
+                            noise_stride if n_seq > 1 else V, code, n_seq, gamma, temperature)
+    _check("pps_verify_chain", lib().pps_verify_chain(args, _handle(stream, di)))
     return out
