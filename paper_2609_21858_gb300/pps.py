@@ -663,6 +663,20 @@ def _own_memory(stream):
     return _HERE_ALREADY if stream is None else torch.cuda.stream(stream)
 
 
+class _Scratch:
+    """`nbytes` of the caching allocator's memory, for the work that is queued on the stream `handle` while it is held:
+    the next to be given it comes later on that stream.  (A tensor for it costs 2 us more.)"""
+
+    def __init__(self, nbytes, handle):
+        self.nbytes = nbytes
+        self.address = torch._C._cuda_cudaCachingAllocator_raw_alloc(max(nbytes, 1), handle)
+
+    def __del__(self):
+        address, self.address = getattr(self, "address", 0), 0
+        if address:
+            torch._C._cuda_cudaCachingAllocator_raw_delete(address)
+
+
 def _handle(stream, di):
     """The stream's handle; with no stream, the current stream of device di (the tensors')."""
     if stream is None:
@@ -675,6 +689,10 @@ def _handle(stream, di):
 def _strided(name, t, di, dt, shape, what):
     """Strides of tensor `t` of dtype `dt` on device di: contiguous along its last dimension, its sizes those of
     `shape` (None: any)."""
+    if isinstance(t, torch.Tensor) and t.get_device() == di and t.dtype is dt and t.shape == shape:
+        st = t.stride()
+        if st[-1] == 1:
+            return st
     if not isinstance(t, torch.Tensor) or t.get_device() != di:
         raise TypeError(f"{name} must be a CUDA tensor on cuda:{di}")
     if t.dtype is not dt:
@@ -808,20 +826,22 @@ def paged_attention(q, k_cache, v_cache, pages, kv_len, q_off, mask=None, scale=
     if torch._C._cuda_getDevice() != di:
         with torch.cuda.device(di):
             return paged_attention(q, k_cache, v_cache, pages, kv_len, q_off, mask, scale, out, lse, ws, status, stream)
-    if out is None or ws is None:
+    if out is None:
         with _own_memory(stream):
-            if out is None:
-                out = torch.empty(n, heads, d, dtype=dt, device=q.device)
-            if ws is None:
-                ws = attention_workspace(n, heads, cache[4], d, q.device)
-                work = ws.data_ptr()
+            out = torch.empty(n, heads, d, dtype=dt, device=q.device)
     so = _strided("out", out, di, dt, shape, _HEADS)
+    L, handle = lib(), _handle(stream, di)
+    if ws is None:
+        scratch = _Scratch(L.pps_attention_workspace_size(n, heads, cache[4], d), handle)
+        work, room = scratch.address, scratch.nbytes
+    else:
+        room = ws.numel()
     # of one sequence, the table's row stride has no meaning; else one below the columns is the library's to refuse
     args = _ATTENTION_ARGS.pack(_ATTENTION_ARGS.size, q.data_ptr(), sq[0], sq[1], out.data_ptr(), so[0], so[1], *cache,
-                                pages.data_ptr(), lens, offs, bits, sums, flags, work, ws.numel(), n,
+                                pages.data_ptr(), lens, offs, bits, sums, flags, work, room, n,
                                 sp[0] if n_seq > 1 else columns, code, heads, columns, n_seq, words,
                                 d ** -0.5 if scale is None else scale)
-    _check("pps_paged_attention", lib().pps_paged_attention(args, _handle(stream, di)))
+    _check("pps_paged_attention", L.pps_paged_attention(args, handle))
     return out
 
 
@@ -860,16 +880,17 @@ def verify_chain(p_logits, q_logits, gamma: int, seq_off, node_draft_row, draft_
             return verify_chain(p_logits, q_logits, gamma, seq_off, node_draft_row, draft_tok, u, noise, temperature, ws,
                                 out, status, stream)
     W = gamma + 1
-    if out is None or ws is None:
+    if out is None:
         with _own_memory(stream):
-            dev = p_logits.device
-            if out is None:
-                e = torch.empty
-                out = dict(accept_len=e(n_seq, dtype=i32, device=dev), n_emitted=e(n_seq, dtype=i32, device=dev),
-                           emitted=e((n_seq, W), dtype=i32, device=dev), accept_prob=e(n_draft, dtype=f32, device=dev))
-            if ws is None:
-                ws = chain_workspace(n, n_draft, n_seq, dev)
-                work = ws.data_ptr()
+            e, dev = torch.empty, p_logits.device
+            out = dict(accept_len=e(n_seq, dtype=i32, device=dev), n_emitted=e(n_seq, dtype=i32, device=dev),
+                       emitted=e((n_seq, W), dtype=i32, device=dev), accept_prob=e(n_draft, dtype=f32, device=dev))
+    L, handle = lib(), _handle(stream, di)
+    if ws is None:
+        scratch = _Scratch(L.pps_chain_workspace_size(n, n_draft, n_seq), handle)
+        work, room = scratch.address, scratch.nbytes
+    else:
+        room = ws.numel()
     for name in ("accept_len", "n_emitted", "emitted"):
         if out.get(name) is None:
             raise TypeError(f"out[{name!r}] is required")
@@ -878,8 +899,8 @@ def verify_chain(p_logits, q_logits, gamma: int, seq_off, node_draft_row, draft_
                             _flat("accept_len", out["accept_len"], di, i32, n_seq),
                             _flat("n_emitted", out["n_emitted"], di, i32, n_seq),
                             _flat("emitted", out["emitted"], di, i32, n_seq * W),
-                            _flat("accept_prob", out.get("accept_prob"), di, f32, n_draft), flags, work, ws.numel(), n,
+                            _flat("accept_prob", out.get("accept_prob"), di, f32, n_draft), flags, work, room, n,
                             n_draft, V, p_stride if n > 1 else V, q_stride if n_draft > 1 else V,
                             noise_stride if n_seq > 1 else V, code, n_seq, gamma, temperature)
-    _check("pps_verify_chain", lib().pps_verify_chain(args, _handle(stream, di)))
+    _check("pps_verify_chain", L.pps_verify_chain(args, handle))
     return out
