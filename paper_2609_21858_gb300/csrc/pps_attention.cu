@@ -21,7 +21,8 @@
 // (one rounding of 2^-9 or 2^-12 each, of the size of the result's own); their sum is formed before rounding.
 //
 // Work split.  Key tiles of all (sequence, key head, row block) items, plus kFix per item for its start and end, lie
-// on one line that is cut into equal shares, one per SM, whatever the lengths are.  An item cut between CTAs leaves
+// on one line that is cut into equal shares, one per SM, whatever the lengths are; a cut that would leave a few tiles
+// of an item alone moves to the item's end.  An item cut between CTAs leaves
 // one partial result (maximum, sum, fp32 O) per CTA, at most two per CTA, and a second launch joins them in
 // order: the same call gives the same bits.  Lengths are read on the device; nothing waits for the host.
 //
@@ -50,7 +51,7 @@ constexpr int kAttnThreads = 384;  // two softmax warpgroups; warps that load ke
 constexpr int kLoadWarp = 8, kMmaWarp = 10, kQueryWarp = 11;
 static_assert(32 * (kQueryWarp + 1) == kAttnThreads, "the last warp loads the queries");
 constexpr int kMaxCtas = 160;      // shares of the work (one per SM)
-constexpr int kFix = 1;            // key tiles that an item's start and end cost
+constexpr int kFix = 4;            // key tiles that an item's start and end cost
 constexpr float kLazy = 8.0f;      // log2 of the rise of a maximum that O is not rescaled for
 constexpr uint32_t kColO = 256;    // tensor memory columns: S/P of streams 0, 1; O of streams 0, 1
 
@@ -60,9 +61,8 @@ struct Cfg {
     static constexpr int kBlock = 128 * 128;                 // 128 rows of 64 channels, 128-byte swizzle
     static constexpr int kTile = kBlock * (DC / 64);         // 16 or 32 KB: a tile of Q, K or V
     static constexpr int kStages = (224 * 1024 - 2 * kTile) / kTile;  // 5 (or 12) tiles of K and V in flight
-    static constexpr int kBars = 8 * (2 * kStages + 11);
-    static constexpr int kSmem = (2 + kStages) * kTile + 288 /* barriers */ + 224 /* plan */ + 2048 /* maxima and sums */;
-    static_assert(kBars <= 288 && kSmem <= 227 * 1024, "barriers and shared memory fit");
+    static constexpr int kSmem = (2 + kStages) * kTile + 320 /* barriers */ + 224 /* plan */ + 2048 /* maxima and sums */;
+    static_assert(8 * (2 * kStages + 13) <= 320 && kSmem <= 227 * 1024, "barriers and shared memory fit");
 };
 
 // a cut item: nsplit partial results of a block of ntok tokens from tok0 on, in slot 2 cta + 1 and slots 2 (cta + k),
@@ -118,6 +118,11 @@ __device__ __forceinline__ int64_t divide(int64_t x, int64_t y) {  // of non-neg
     return (x | y) >> 32 ? x / y : (int64_t)((uint32_t)x / (uint32_t)y);
 }
 
+// key tiles of a block of T before the cut that the line makes after x of them: pieces have `least` tiles or more
+__device__ __forceinline__ int cut_at(int64_t x, int T, int least) {
+    return x < least ? 0 : x > T - least ? T : (int)x;
+}
+
 // where a share starts
 struct Start {
     int64_t base;  // the block's start on the line
@@ -128,6 +133,7 @@ struct Start {
 // A CTA's items in order; every warp walks them by itself.
 struct Walk {
     int64_t x, x1, base;  // where the walk is, the share's end, the next block's start
+    int least;            // key tiles of a cut item's piece
     int s, vh, blk, nb;   // the next block: sequence, turn of a key head (key head x nsub + turn), number; blocks of the sequence
     Seq q;
     // the segment: key tiles t0 .. t1 - 1 of T of a block that starts at `from` on the line, with tokens i0 .. i0 + ntok - 1
@@ -135,8 +141,8 @@ struct Walk {
     int t0, t1, T, i0, ntok;
     int heads;  // the segment's vh
 
-    __device__ __forceinline__ Walk(const AttnPlan& P, const Start& st, int64_t c0, int64_t c1)
-        : x(c0), x1(c1), base(st.base), s(st.s), vh(st.vh), blk(st.blk), nb(n_blocks(P, st.q)), q(st.q) {}
+    __device__ __forceinline__ Walk(const AttnPlan& P, const Start& st, int64_t c0, int64_t c1, int least_)
+        : x(c0), x1(c1), base(st.base), least(least_), s(st.s), vh(st.vh), blk(st.blk), nb(n_blocks(P, st.q)), q(st.q) {}
     __device__ __forceinline__ bool next(const AttnArgs& a, const AttnPlan& P) {
         while (x < x1) {
             while (blk >= nb) {  // the next turn of heads, or the next sequence with tokens
@@ -151,14 +157,15 @@ struct Walk {
             T = block_tiles(a, P, q, blk);
             i0 = blk * 2 * P.tt;
             ntok = min(q.n - i0, 2 * P.tt);
-            t0 = (int)(x - base);
-            t1 = (int)min(x1 - base, (int64_t)T);
+            t0 = cut_at(x - base, T, least);
+            t1 = cut_at(x1 - base, T, least);
+            const bool none = T == 0 && x == base;
             from = base;
             heads = vh;
             base += T + kFix;
             x = base;
             ++blk;
-            if (t0 < t1 || (T == 0 && t0 == 0)) return true;
+            if (t0 < t1 || none) return true;
         }
         return false;
     }
@@ -216,6 +223,31 @@ struct Half<__half> {
     }
 };
 
+// Of each four lanes, lane q gets the q-th 16-byte unit of every lane: u[k] = unit q of lane k.  A warp that holds a row per
+// lane so writes 64 bytes of 8 rows at a time instead of 16 of 32, a quarter of the lines.
+__device__ __forceinline__ uint4 shfl4(const uint4& v, int mask) {
+    return make_uint4(__shfl_xor_sync(0xffffffffu, v.x, mask), __shfl_xor_sync(0xffffffffu, v.y, mask),
+                      __shfl_xor_sync(0xffffffffu, v.z, mask), __shfl_xor_sync(0xffffffffu, v.w, mask));
+}
+__device__ __forceinline__ uint4 pick(bool first, const uint4& a, const uint4& b) {
+    return make_uint4(first ? a.x : b.x, first ? a.y : b.y, first ? a.z : b.z, first ? a.w : b.w);
+}
+__device__ __forceinline__ void quad_transpose(uint4 (&u)[4], int q) {
+    const bool odd = q & 1, high = q & 2;
+#pragma unroll
+    for (int k = 0; k < 4; k += 2) {
+        const uint4 r = shfl4(pick(odd, u[k], u[k + 1]), 1);
+        u[k] = pick(odd, r, u[k]);
+        u[k + 1] = pick(odd, u[k + 1], r);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const uint4 r = shfl4(pick(high, u[k], u[k + 2]), 2);
+        u[k] = pick(high, r, u[k]);
+        u[k + 2] = pick(high, u[k + 2], r);
+    }
+}
+
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort) {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort));
 }
@@ -251,12 +283,12 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
     auto full = [&](uint32_t s) { return bar(s); };
     auto empty = [&](uint32_t s) { return bar(C::kStages + s); };
     auto sfull = [&](uint32_t w) { return bar(2 * C::kStages + w); };
-    auto pready = [&](uint32_t w) { return bar(2 * C::kStages + 2 + w); };
+    auto pready = [&](uint32_t w, uint32_t half) { return bar(2 * C::kStages + (half ? 11 : 2) + w); };  // a barrier per half: no warp may count twice
     auto odone = [&](uint32_t w) { return bar(2 * C::kStages + 4 + w); };
     auto qfull = [&](uint32_t t) { return bar(2 * C::kStages + 6 + t); };
     auto qfree = [&](uint32_t t) { return bar(2 * C::kStages + 8 + t); };
     const uint32_t segbar = bar(2 * C::kStages + 10);
-    uint8_t* tail = attn_smem + (2 + C::kStages) * C::kTile + 288;
+    uint8_t* tail = attn_smem + (2 + C::kStages) * C::kTile + 320;
     volatile int* abort = reinterpret_cast<volatile int*>(tail);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 4);
     int64_t* s_sum = reinterpret_cast<int64_t*>(tail + 16);          // [12] warp sums
@@ -272,7 +304,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
         }
         for (int w = 0; w < 2; ++w) {
             mbar_init(sfull(w), 1);
-            mbar_init(pready(w), 4);
+            mbar_init(pready(w, 0), 4);  // the weights of a tile's first 64 keys
+            mbar_init(pready(w, 1), 4);  // of the others
             mbar_init(odone(w), 1);
         }
         for (int t = 0; t < 2; ++t) {
@@ -364,7 +397,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
         if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
         return;
     }
-    Walk W(P, *s_start, c0, c1);
+    const int least = (int)min(max(share / 8, (int64_t)1), (int64_t)kFix);
+    Walk W(P, *s_start, c0, c1, least);
     const int D = a.c.head_dim;
 
     // registers: 384 x 168 at launch = 256 x 208 + 128 x 88
@@ -448,12 +482,21 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                 tc_commit(sfull(w));
                 if (last) tc_commit(qfree(tile));
             };
+            // O += P V in two halves, each as soon as its weights are there
             auto values = [&](uint32_t w, uint32_t v, bool first) {
                 const uint64_t vd = sw128_desc_mn(stage(v), C::kBlock);
+                const uint32_t o = tmem + kColO + w * 128u, p = tmem + w * 128u, at = w ? np1 : np0;
+                ++(w ? np1 : np0);
+                if (!mbar_wait(pready(w, 0), at & 1u, abort)) return false;
+                tc_fence_after();
 #pragma unroll
-                for (uint32_t c = 0; c < kTileKeys / 16; ++c)
-                    tc_mma_ts(tmem + kColO + w * 128u, tmem + w * 128u + c * 8u, vd + c * (2048u >> 4), id_pv, !first || c != 0);
+                for (uint32_t c = 0; c < kTileKeys / 32; ++c) tc_mma_ts(o, p + c * 8u, vd + c * (2048u >> 4), id_pv, !first || c != 0);
+                if (!mbar_wait(pready(w, 1), at & 1u, abort)) return false;
+                tc_fence_after();
+#pragma unroll
+                for (uint32_t c = kTileKeys / 32; c < kTileKeys / 16; ++c) tc_mma_ts(o, p + c * 8u, vd + c * (2048u >> 4), id_pv, 1u);
                 tc_commit(odone(w));
+                return true;
             };
             bool ok = true;
             while (ok && W.next(a, P)) {
@@ -471,10 +514,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                         const bool more_keys = j + 1 < n;
                         ok = landed(v);
                         for (uint32_t w = 0; w < 2 && ok; ++w) {
-                            ok = mbar_wait(pready(w), (w ? np1++ : np0++) & 1u, abort);
+                            ok = values(w, v, j == 0);
                             if (!ok) break;
-                            tc_fence_after();
-                            values(w, v, j == 0);
                             if (w == 1) tc_commit(empty(v % C::kStages));
                             if (more_keys) {
                                 if (w == 0) ok = landed(k);
@@ -498,10 +539,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                     }
                     for (int j = 0; j < n && ok; ++j) {
                         const uint32_t w = j & 1;
-                        ok = landed(it) && mbar_wait(pready(w), (w ? np1++ : np0++) & 1u, abort);
+                        ok = landed(it) && values(w, it, j < 2);
                         if (!ok) break;
-                        tc_fence_after();
-                        values(w, it, j < 2);
                         tc_commit(empty(it % C::kStages));
                         ++it;
                         if (j + 2 < n) {
@@ -581,6 +620,19 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             for (int j = two ? 0 : (int)w; j < n; j += two ? 1 : 2, ++i) {
                 const int k0 = (W.t0 + j) * kTileKeys;
                 if (!(ok = wait_warp(sfull(w), (done + i) & 1u, abort))) break;
+                // values past the sequence's end (in its last tile): whatever the pages hold there becomes zero before any
+                // weight is handed over
+                if (k0 + kTileKeys > W.q.len && (w == 0 || !two)) {
+                    const uint32_t v = it + 2 * n - 1;  // the segment's last value tile
+                    if (!(ok = wait_warp(full(v % C::kStages), (v / C::kStages) & 1u, abort))) break;
+                    const uint32_t from = ring + (v % C::kStages) * C::kTile + (W.q.len - k0) * 128;
+                    const uint32_t bytes = (k0 + kTileKeys - W.q.len) * 128;
+#pragma unroll
+                    for (int b = 0; b < DC / 64; ++b)
+                        for (uint32_t o = r * 16; o < bytes; o += 128 * 16)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(from + b * C::kBlock + o), "r"(0) : "memory");
+                    fence_async_smem();
+                }
                 tc_fence_after();
                 if (busy) {
                     uint32_t v[4][32];
@@ -648,27 +700,24 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                             pk[e] = H::pack(x0, x1);
                         }
                         tmem_st32(tS + c * 16, pk);
+                        if (c == 0) {
+                            tmem_wait_st();
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(pready(w, 0));
+                        }
                     }
                     float s0, s1;
                     unpack2(add2(sum[0], sum[1]), s0, s1);
                     l += s0 + s1;
                     tmem_wait_st();
-                }
-                // values past the sequence's end (its last tile's): whatever the pages hold there becomes zero
-                if (k0 + kTileKeys > W.q.len && (w == 0 || !two)) {
-                    const uint32_t v = it + 2 * n - 1;  // the segment's last value tile
-                    if (!(ok = wait_warp(full(v % C::kStages), (v / C::kStages) & 1u, abort))) break;
-                    const uint32_t from = ring + (v % C::kStages) * C::kTile + (W.q.len - k0) * 128;
-                    const uint32_t bytes = (k0 + kTileKeys - W.q.len) * 128;
-#pragma unroll
-                    for (int b = 0; b < DC / 64; ++b)
-                        for (uint32_t o = r * 16; o < bytes; o += 128 * 16)
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(from + b * C::kBlock + o), "r"(0) : "memory");
-                    fence_async_smem();
+                } else {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(pready(w, 0));
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(pready(w));
+                if (lane == 0) mbar_arrive(pready(w, 1));
             }
             if (!ok) break;
             // ---- the segment's result
@@ -676,7 +725,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             const int slot = 2 * cta + (W.t0 == 0 ? 1 : 0);
             if (tid == 0 && W.t0 == 0 && !whole) {
                 Cut c;
-                c.nsplit = (int)divide(W.from + W.T - 1, share) - cta + 1;
+                c.nsplit = (int)divide(W.from + W.T - least, share) - cta + 1;  // the cuts that leave `least` tiles on both sides
                 c.ntok = W.ntok;
                 c.tok0 = W.q.off + W.i0;
                 c.vh = W.heads;
@@ -706,7 +755,13 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                 }
                 const uint32_t first = two ? w : 0u;
                 const int from = two ? 0 : (int)w * (DC / 2), to = two ? DC : from + DC / 2;
-                T* out = static_cast<T*>(a.out.p) + (int64_t)(W.q.off + tok) * a.out.tok + head * a.out.head;
+                // the quad's rows: where they go, which of them are there
+                const unsigned long long out = reinterpret_cast<unsigned long long>(
+                    static_cast<T*>(a.out.p) + (int64_t)(W.q.off + tok) * a.out.tok + head * a.out.head);
+                unsigned long long out4[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) out4[k] = __shfl_sync(0xffffffffu, out, (lane & ~3) + k);
+                const uint32_t rows4 = __ballot_sync(0xffffffffu, valid) >> (lane & ~3) & 15u;
                 float* part = P.part_o + ((int64_t)slot * P.cap_rows + in_block) * DC;
                 if (valid && (two || w == 0)) {
                     if (!whole)
@@ -735,22 +790,30 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                         for (int e = 0; e < 32; ++e)
                             if (f1 != 0.0f) o[e] = __float_as_uint(fmaf(__uint_as_float(o1[e]), f1, __uint_as_float(o[e])));
                     }
-                    if (valid) {
-                        if (whole) {
+                    const int q = lane & 3;
+                    if (whole) {
+                        uint4 u[4];
 #pragma unroll
-                            for (int e = 0; e < 32; e += 8)
-                                if (c + e < D) {
-                                    uint4 x;
-                                    x.x = H::pack(__uint_as_float(o[e]), __uint_as_float(o[e + 1]));
-                                    x.y = H::pack(__uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
-                                    x.z = H::pack(__uint_as_float(o[e + 4]), __uint_as_float(o[e + 5]));
-                                    x.w = H::pack(__uint_as_float(o[e + 6]), __uint_as_float(o[e + 7]));
-                                    *reinterpret_cast<uint4*>(out + c + e) = x;
-                                }
-                        } else {
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t* x = o + 8 * e;
+                            u[e] = make_uint4(H::pack(__uint_as_float(x[0]), __uint_as_float(x[1])), H::pack(__uint_as_float(x[2]), __uint_as_float(x[3])),
+                                              H::pack(__uint_as_float(x[4]), __uint_as_float(x[5])), H::pack(__uint_as_float(x[6]), __uint_as_float(x[7])));
+                        }
+                        quad_transpose(u, q);
 #pragma unroll
-                            for (int e = 0; e < 32; e += 4)
-                                *reinterpret_cast<uint4*>(part + c + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                        for (int k = 0; k < 4; ++k)
+                            if ((rows4 >> k & 1u) && c + 8 * q < D)
+                                *reinterpret_cast<uint4*>(reinterpret_cast<T*>(out4[k]) + c + 8 * q) = u[k];
+                    } else {
+#pragma unroll
+                        for (int b = 0; b < 32; b += 16) {
+                            uint4 u[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) u[e] = make_uint4(o[b + 4 * e], o[b + 4 * e + 1], o[b + 4 * e + 2], o[b + 4 * e + 3]);
+                            quad_transpose(u, q);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                if (rows4 >> k & 1u) *reinterpret_cast<uint4*>(part + (k - q) * DC + c + b + 4 * q) = u[k];
                         }
                     }
                     __syncwarp();
@@ -802,6 +865,40 @@ __global__ void __launch_bounds__(256, 4) join_kernel(const AttnArgs a, const At
         if (lane == 0 && a.lse)
             a.lse[(int64_t)tok * a.n_heads + head] = l > 0.0f ? (M + log2f(l) - H::kShift) * 0.69314718055994531f : -INFINITY;
     };
+    if (nsplit == 2) {  // the usual cut of a batch: four rows of two parts in flight
+        const int step = 8 * gridDim.y;
+        for (int i0 = blockIdx.y * 8 + warp; i0 < ntok * gs; i0 += 4 * step) {
+            float2 x[4][2];
+            float v[4][2][VW];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int i = min(i0 + u * step, ntok * gs - 1), t = i / gs;
+                const int row = t < P.tt ? t * P.gs + (i - t * gs) : kTileRows + (t - P.tt) * P.gs + (i - t * gs);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int64_t at = (k == 0 ? first : rest + (int64_t)2 * P.cap_rows) + row;
+                    x[u][k] = __ldcg(P.part_ml + at);
+                    const float* p = P.part_o + at * DC + lane * VW;
+                    if constexpr (VW == 4)
+                        *reinterpret_cast<float4*>(v[u][k]) = __ldcg(reinterpret_cast<const float4*>(p));
+                    else
+                        *reinterpret_cast<float2*>(v[u][k]) = __ldcg(reinterpret_cast<const float2*>(p));
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (i0 + u * step >= ntok * gs) break;
+                const float M = fmaxf(x[u][0].x, x[u][1].x);
+                const float f0 = x[u][0].x == -INFINITY ? 0.0f : ex2(x[u][0].x - M), f1 = x[u][1].x == -INFINITY ? 0.0f : ex2(x[u][1].x - M);
+                float o[VW];
+#pragma unroll
+                for (int e = 0; e < VW; ++e)  // a part without weight may hold anything
+                    o[e] = (f0 != 0.0f ? v[u][0][e] * f0 : 0.0f) + (f1 != 0.0f ? v[u][1][e] * f1 : 0.0f);
+                put(i0 + u * step, M, x[u][0].y * f0 + x[u][1].y * f1, o);
+            }
+        }
+        return;
+    }
     for (int i0 = blockIdx.y * rpb; i0 < ntok * gs; i0 += rpb * gridDim.y) {
         const int i = i0 + warp / wpr;
         float M = -INFINITY, l = 0.0f, o[VW] = {};
