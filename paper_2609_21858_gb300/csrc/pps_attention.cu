@@ -51,7 +51,7 @@ constexpr int kAttnThreads = 384;  // two softmax warpgroups; warps that load ke
 constexpr int kLoadWarp = 8, kMmaWarp = 10, kQueryWarp = 11;
 static_assert(32 * (kQueryWarp + 1) == kAttnThreads, "the last warp loads the queries");
 constexpr int kMaxCtas = 160;      // shares of the work (one per SM)
-constexpr int kFix = 4;            // key tiles that an item's start and end cost
+constexpr int kFix = 6;            // key tiles that an item's start and end cost
 constexpr float kLazy = 8.0f;      // log2 of the rise of a maximum that O is not rescaled for
 constexpr uint32_t kColO = 256;    // tensor memory columns: S/P of streams 0, 1; O of streams 0, 1
 
@@ -636,32 +636,38 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                 tc_fence_after();
                 if (busy) {
                     uint32_t v[4][32];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, v[c]);
+                    tmem_ld32(tS, v[0]);
+                    tmem_ld32(tS + 32, v[1]);
                     tmem_wait_ld();
+                    tmem_landed(v[0]);
+                    tmem_landed(v[1]);
+                    tmem_ld32(tS + 64, v[2]);
+                    tmem_ld32(tS + 96, v[3]);
+                    float mx[4];
+                    auto highest = [&](int c) {
+                        mx[c] = fmaxf(__uint_as_float(v[c][0]), __uint_as_float(v[c][1]));
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_landed(v[c]);
-                    if (P.s_xor != 0 || P.s_and == 0) {
-#pragma unroll
-                        for (int c = 0; c < 4; ++c)
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) v[c][e] = (v[c][e] & P.s_and) ^ P.s_xor;
-                    }
-                    if (__any_sync(0xffffffffu, k0 + kTileKeys > plain)) {
+                        for (int e = 2; e < 32; e += 2) mx[c] = max3(mx[c], __uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1]));
+                    };
+                    highest(0);
+                    highest(1);
+                    tmem_wait_ld();
+                    tmem_landed(v[2]);
+                    tmem_landed(v[3]);
+                    highest(2);
+                    highest(3);
+                    const bool odd_scale = P.s_xor != 0 || P.s_and == 0;
+                    if (odd_scale || __any_sync(0xffffffffu, k0 + kTileKeys > plain)) {  // the tile is not all as it stands
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
                             const uint32_t bits = seen_bits(k0 + 32 * c, vis, prefix, mask, a.mask_words);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e)
+                            for (int e = 0; e < 32; ++e) {
+                                v[c][e] = (v[c][e] & P.s_and) ^ P.s_xor;
                                 if (!(bits & (1u << e))) v[c][e] = 0xff800000u;  // -inf
+                            }
+                            highest(c);
                         }
-                    }
-                    float mx[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        mx[c] = fmaxf(__uint_as_float(v[c][0]), __uint_as_float(v[c][1]));
-#pragma unroll
-                        for (int e = 2; e < 32; e += 2) mx[c] = max3(mx[c], __uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1]));
                     }
                     const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]);
                     if (__any_sync(0xffffffffu, valid && (top - m) * P.sc > kLazy)) {
@@ -686,27 +692,27 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                     const float neg = (m == -INFINITY ? 0.0f : -m * P.sc) + H::kShift;
                     const uint64_t sc2 = pack2(P.sc, P.sc), neg2 = pack2(neg, neg);
                     uint64_t sum[2] = {0, 0};
+                    auto weights = [&](int c) {  // of 32 keys, into tensor memory
+                        uint32_t pk[16];
 #pragma unroll
-                    for (int c = 0; c < 4; c += 2) {
-                        uint32_t pk[32];
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            const uint32_t* x = &v[c + (e >> 4)][(e & 15) * 2];
+                        for (int e = 0; e < 16; ++e) {
                             float x0, x1;
-                            unpack2(fma2(pack2(__uint_as_float(x[0]), __uint_as_float(x[1])), sc2, neg2), x0, x1);
+                            unpack2(fma2(pack2(__uint_as_float(v[c][2 * e]), __uint_as_float(v[c][2 * e + 1])), sc2, neg2), x0, x1);
                             x0 = ex2(x0);
                             x1 = ex2(x1);
                             sum[e & 1] = add2(sum[e & 1], pack2(x0, x1));
                             pk[e] = H::pack(x0, x1);
                         }
-                        tmem_st32(tS + c * 16, pk);
-                        if (c == 0) {
-                            tmem_wait_st();
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(pready(w, 0));
-                        }
-                    }
+                        tmem_st16(tS + c * 16, pk);
+                    };
+                    weights(0);
+                    weights(1);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(pready(w, 0));
+                    weights(2);
+                    weights(3);
                     float s0, s1;
                     unpack2(add2(sum[0], sum[1]), s0, s1);
                     l += s0 + s1;
