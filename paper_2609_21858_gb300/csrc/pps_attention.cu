@@ -602,6 +602,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             return wait_warp(segbar, syncs++ & 1u, abort);
         };
         bool ok = true;
+        const bool odd_scale = P.s_xor != 0 || P.s_and == 0;
         while (ok && W.next(a, P)) {
             const bool two = W.ntok > P.tt;  // a tile per stream
             const int n = W.t1 - W.t0;
@@ -619,6 +620,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             int i = 0;  // tiles of the stream in this segment
             for (int j = two ? 0 : (int)w; j < n; j += two ? 1 : 2, ++i) {
                 const int k0 = (W.t0 + j) * kTileKeys;
+                const bool partly = __any_sync(0xffffffffu, k0 + kTileKeys > plain) || odd_scale;  // not all as it stands
                 if (!(ok = wait_warp(sfull(w), (done + i) & 1u, abort))) break;
                 // values past the sequence's end (in its last tile): whatever the pages hold there becomes zero before any
                 // weight is handed over
@@ -643,11 +645,11 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                     tmem_landed(v[1]);
                     tmem_ld32(tS + 64, v[2]);
                     tmem_ld32(tS + 96, v[3]);
-                    float mx[4];
-                    auto highest = [&](int c) {
-                        mx[c] = fmaxf(__uint_as_float(v[c][0]), __uint_as_float(v[c][1]));
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    auto highest = [&](int c) {  // of 32 scores, in four chains
 #pragma unroll
-                        for (int e = 2; e < 32; e += 2) mx[c] = max3(mx[c], __uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1]));
+                        for (int e = 0; e < 32; e += 2)
+                            mx[(e >> 1) & 3] = max3(mx[(e >> 1) & 3], __uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1]));
                     };
                     highest(0);
                     highest(1);
@@ -656,8 +658,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                     tmem_landed(v[3]);
                     highest(2);
                     highest(3);
-                    const bool odd_scale = P.s_xor != 0 || P.s_and == 0;
-                    if (odd_scale || __any_sync(0xffffffffu, k0 + kTileKeys > plain)) {  // the tile is not all as it stands
+                    if (partly) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) mx[c] = -INFINITY;
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
                             const uint32_t bits = seen_bits(k0 + 32 * c, vis, prefix, mask, a.mask_words);
