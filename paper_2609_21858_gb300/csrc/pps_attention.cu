@@ -1046,16 +1046,9 @@ cudaError_t launch(const AttnArgs& a, int dtype, cudaStream_t st) {
     // an empty cache has nothing to read: any mapped memory will do for its maps
     if (!query_map(&tmQ, a, P, dtype) || !cache_map(&tmK, a.c.n_pages > 0 ? a.c.k : a.ws, a.c, dtype) || !cache_map(&tmV, a.c.n_pages > 0 ? a.c.v : a.ws, a.c, dtype))
         return cudaErrorInvalidValue;
-    static std::atomic<uint64_t> ready{0};  // devices on which the kernel has its shared memory
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    static std::atomic<uint64_t> ready{0};
+    cudaError_t e = allow_smem(ready, (const void*)attention_kernel<T, DC>, Cfg<DC>::kSmem);
     if (e != cudaSuccess) return e;
-    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
-    if ((ready.load(std::memory_order_relaxed) & bit) == 0) {
-        e = cudaFuncSetAttribute(attention_kernel<T, DC>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<DC>::kSmem);
-        if (e != cudaSuccess) return e;
-        ready.fetch_or(bit, std::memory_order_relaxed);
-    }
     const int ctas = std::min(device_sm_count(), kMaxCtas);
     e = launch_pdl(attention_kernel<T, DC>, dim3(ctas), dim3(kAttnThreads), Cfg<DC>::kSmem, st, tmQ, tmK, tmV, a, P);
     if (e != cudaSuccess) return e;
