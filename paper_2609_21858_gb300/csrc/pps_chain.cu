@@ -32,7 +32,7 @@ constexpr int kThreads = 256;    // that compute; a warp more copies
 constexpr int kStatCtas = 2;     // per SM
 constexpr int kVecs = 4;         // 16-byte vectors per thread of a chunk
 constexpr int kStatChunk = kVecs * kThreads * 16;  // bytes
-constexpr int kStatStages = 6;
+constexpr int kStatStages = 3;
 constexpr int kStatSmem = kStatStages * kStatChunk;
 constexpr int kRaceTok = 8;      // tokens per thread of a chunk
 constexpr int kRaceChunk = kRaceTok * kThreads;
@@ -43,6 +43,8 @@ struct RaceSmem {  // a stage: the chunk of the target's row, of the drafter's, 
     static constexpr int kStage = 2 * kRow + kNoise, kBytes = kRaceStages * kStage;
     static constexpr int kCtas = sizeof(T) == 2 ? 3 : 2;  // per SM
 };
+// The first CTA of finish_kernel on an SM fits beside the two of stats_kernel (shared memory, registers): it starts early, and
+// its chain of dependent loads (offsets, rows, tokens, logits) is over when the sums are there.
 constexpr int kMaxParts = 1024;  // CTAs of stats_kernel
 constexpr int kMaxSlices = 64;   // of the final row
 constexpr int kMaxChain = 64;    // gamma
@@ -91,6 +93,11 @@ __device__ __forceinline__ void join(float& m, float& s, float om, float os, flo
     m = M;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
 template <typename T>
 struct Elem;
 template <>
@@ -101,6 +108,15 @@ struct Elem<float> {
     }
     static __device__ __forceinline__ float get(const float* p) { return __ldg(p); }
     static __device__ __forceinline__ float value(float x) { return x; }
+    template <int N>
+    static __device__ __forceinline__ float largest(const uint4 (&x)[N], float m) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            m = max3(m, at(x[j], 0), at(x[j], 1));
+            m = max3(m, at(x[j], 2), at(x[j], 3));
+        }
+        return m;
+    }
 };
 template <>
 struct Elem<__nv_bfloat16> {
@@ -111,13 +127,25 @@ struct Elem<__nv_bfloat16> {
     }
     static __device__ __forceinline__ float get(const __nv_bfloat16* p) { return __bfloat162float(__ldg(p)); }
     static __device__ __forceinline__ float value(__nv_bfloat16 x) { return __bfloat162float(x); }
+    // the largest logit of N vectors, and m; NaN is passed by
+    template <int N>
+    static __device__ __forceinline__ float largest(const uint4 (&x)[N], float m) {
+        uint32_t h[2] = {0xff80ff80u, 0xff80ff80u};  // -inf
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            h[j & 1] = max2(max2(h[j & 1], x[j].x), x[j].y);
+            h[j & 1] = max2(max2(h[j & 1], x[j].z), x[j].w);
+        }
+        h[0] = max2(h[0], h[1]);
+        return max3(m, __uint_as_float(h[0] << 16), __uint_as_float(h[0] & 0xffff0000u));
+    }
+    static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
 };
 
-__device__ __forceinline__ float max3(float a, float b, float c) {
-    float y;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
-    return y;
-}
 __device__ __forceinline__ uint64_t pack2(float a, float b) {
     uint64_t r;
     asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
@@ -145,11 +173,7 @@ __device__ __forceinline__ void weights2(float x0, float x1, uint64_t cc, uint64
 template <typename T>
 __device__ __forceinline__ void add_logits(const uint4 (&x)[kVecs], float& m, float& s, float c) {
     using E = Elem<T>;
-    float bm = m;
-#pragma unroll
-    for (int j = 0; j < kVecs; ++j)
-#pragma unroll
-        for (int e = 0; e < E::kVW; e += 2) bm = max3(bm, E::at(x[j], e), E::at(x[j], e + 1));  // NaN is passed by
+    const float bm = E::largest(x, m);
     if (bm == -INFINITY) return;
     uint64_t sum[2] = {0, 0};
     const uint64_t cc = pack2(c, c), mm = pack2(-bm, -bm);
@@ -199,7 +223,7 @@ struct RowPart {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads + 32, kStatCtas) stats_kernel(const ChainArgs a, const ChainPlan P) {
+__global__ void __launch_bounds__(kThreads + 32, kStatCtas + 1) stats_kernel(const ChainArgs a, const ChainPlan P) {
     using E = Elem<T>;
     constexpr int VW = E::kVW, kChunkVecs = kVecs * kThreads;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -327,6 +351,27 @@ struct Law {
     __device__ __forceinline__ Law(const Stat& sp, const Stat& sq, bool has, float c_)
         : p(sp), q(sq), c(c_), ip(sp.s > 0.0f ? 1.0f / sp.s : 0.0f), iq(sq.s > 0.0f ? 1.0f / sq.s : 0.0f), drafter(has),
           finite(fabsf(sp.m) < INFINITY && (!has || fabsf(sq.m) < INFINITY)) {}
+    // max(P - Q, 0) is the positive part of this
+    __device__ __forceinline__ void excess(float (&x)[kRaceTok], const float (&y)[kRaceTok]) const {
+        if (!finite) {
+#pragma unroll
+            for (int k = 0; k < kRaceTok; ++k) x[k] = excess(x[k], y[k]);
+            return;
+        }
+        const uint64_t cc = pack2(c, c), mp = pack2(-p.m, -p.m), mq = pack2(-q.m, -q.m);
+#pragma unroll
+        for (int k = 0; k < kRaceTok; k += 2) {
+            weights2(x[k], x[k + 1], cc, mp, x[k], x[k + 1]);
+            x[k] *= ip;
+            x[k + 1] *= ip;
+            if (drafter) {
+                float w0, w1;
+                weights2(fmaxf(y[k], -INFINITY), fmaxf(y[k + 1], -INFINITY), cc, mq, w0, w1);
+                x[k] = fmaf(w0, -iq, x[k]);
+                x[k + 1] = fmaf(w1, -iq, x[k + 1]);
+            }
+        }
+    }
     __device__ __forceinline__ float excess(float x, float y) const {
         if (!finite) {
             const float d = weight(usable(x), p.m, c) * ip;
@@ -336,13 +381,23 @@ struct Law {
         return drafter ? fmaf(ex2z((fmaxf(y, -INFINITY) - q.m) * c), -iq, d) : d;
     }
 };
+// 8 consecutive values of a row in shared memory, the j-th 8
+__device__ __forceinline__ void load8(float (&x)[kRaceTok], const uint8_t* row, int j, float) {
+    *reinterpret_cast<float4*>(x) = reinterpret_cast<const float4*>(row)[2 * j];
+    *reinterpret_cast<float4*>(x + 4) = reinterpret_cast<const float4*>(row)[2 * j + 1];
+}
+__device__ __forceinline__ void load8(float (&x)[kRaceTok], const uint8_t* row, int j, __nv_bfloat16) {
+    const uint4 v = reinterpret_cast<const uint4*>(row)[j];
+#pragma unroll
+    for (int k = 0; k < kRaceTok; ++k) x[k] = Elem<__nv_bfloat16>::at(v, k);
+}
 // offers a token: it is looked at closely (the quotient, ties) only if it is not clearly below the best so far
 __device__ __forceinline__ void offer(Best& b, float d, float z, int64_t tok) {
-    if (d > 0.0f && !(d < b.v * 0.999999f * z)) better(b, d / z, (int)tok);
+    if (d > 0.0f && d >= b.v * 0.999999f * z) better(b, d / z, (int)tok);
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads + 32, RaceSmem<T>::kCtas) finish_kernel(const ChainArgs a, const ChainPlan P) {
+__global__ void __launch_bounds__(kThreads + 32) finish_kernel(const ChainArgs a, const ChainPlan P) {
     using E = Elem<T>;
     using S = RaceSmem<T>;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -352,6 +407,7 @@ __global__ void __launch_bounds__(kThreads + 32, RaceSmem<T>::kCtas) finish_kern
     __shared__ int s_last, s_node, s_fr;
     __shared__ __align__(8) uint64_t s_bar[2 * kRaceStages];
     __shared__ volatile int s_abort;
+    __shared__ volatile uint32_t s_high;  // bits of the best score any thread has seen (scores are not negative)
     const uint32_t ring = smem_u32(smem), bars = smem_u32(s_bar);
     auto full = [&](uint32_t s) { return bars + 8u * s; };
     auto empty = [&](uint32_t s) { return bars + 8u * (kRaceStages + s); };
@@ -373,6 +429,7 @@ __global__ void __launch_bounds__(kThreads + 32, RaceSmem<T>::kCtas) finish_kern
             mbar_init(empty(s), kThreads / 32);
         }
         s_abort = 0;
+        s_high = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
@@ -494,10 +551,38 @@ __global__ void __launch_bounds__(kThreads + 32, RaceSmem<T>::kCtas) finish_kern
             const T* ys = reinterpret_cast<const T*>(stage + S::kRow) + skip_q;
             const float* zs = reinterpret_cast<const float*>(stage + 2 * S::kRow) + skip_z;
             if (law.p.s > 0.0f) {
+                // All scores side by side, then one test for any that comes near the CTA's best so far (a thread's own best is
+                // beaten too often: some lane of a warp would divide in every chunk).  Thread j has tokens 8 j .. 8 j + 7 of
+                // an aligned chunk, else j, j + 256 and so on.
+                float x[kRaceTok], y[kRaceTok], z[kRaceTok];
+                const bool wide = P.margin == 0 && n == (uint32_t)kRaceChunk;  // CTA-uniform
+                if (wide) {
+                    load8(x, stage, j, T());
+                    if (law.drafter) load8(y, stage + S::kRow, j, T());
+                    load8(z, stage + 2 * S::kRow, j, 0.0f);
+                } else {
 #pragma unroll
-                for (int k = 0; k < kRaceTok; ++k) {
-                    const uint32_t e = (uint32_t)j + k * kThreads;
-                    if (e < n) offer(b, law.excess(E::value(xs[e]), law.drafter ? E::value(ys[e]) : 0.0f), zs[e], t + e);
+                    for (int k = 0; k < kRaceTok; ++k) {
+                        const uint32_t e = (uint32_t)j + k * kThreads;
+                        x[k] = -INFINITY;
+                        y[k] = z[k] = 0.0f;
+                        if (e < n) {
+                            x[k] = E::value(xs[e]);
+                            if (law.drafter) y[k] = E::value(ys[e]);
+                            z[k] = zs[e];
+                        }
+                    }
+                }
+                law.excess(x, y);
+                const float low = fmaxf(b.v, __uint_as_float(s_high)) * 0.999999f;
+                bool near = false;
+#pragma unroll
+                for (int k = 0; k < kRaceTok; ++k) near = near || x[k] >= low * z[k];
+                if (near) {
+#pragma unroll
+                    for (int k = 0; k < kRaceTok; ++k)
+                        if (x[k] > 0.0f && x[k] >= low * z[k]) better(b, x[k] / z[k], (int)(t + (wide ? kRaceTok * j + k : j + k * kThreads)));
+                    atomicMax(const_cast<uint32_t*>(&s_high), __float_as_uint(b.v));
                 }
             }
             __syncwarp();
@@ -553,7 +638,8 @@ cudaError_t launch(const ChainArgs& a, cudaStream_t st) {
     const int64_t most = std::min<int64_t>(kMaxParts, (int64_t)kStatCtas * sms);
     P.share = std::max<int64_t>((rows * P.nv + most - 1) / most, kThreads);
     const unsigned ctas = (unsigned)((rows * P.nv + P.share - 1) / P.share);
-    // the final rows: every CTA resident at once, of a chunk at least
+    // the final rows: every CTA resident at once, of a chunk at least (64 sequences, V = 128256: 61 us with one CTA per SM, 51
+    // with two, 47.5 with three)
     using S = RaceSmem<T>;
     const int64_t n = std::min<int64_t>((a.V + kRaceChunk - 1) / kRaceChunk, std::max<int64_t>(1, S::kCtas * sms / a.n_seq));
     P.race_slices = (int)std::min<int64_t>(std::max<int64_t>(n, 1), kMaxSlices);
