@@ -39,6 +39,31 @@ def _stale(target: str, deps) -> bool:
 VARIANTS = {"": [], "_r7": ["-DPPS_PHILOX_ROUNDS=7"]}
 
 
+TORCH_EXT = os.path.join(OUT, "pps_torch.so")  # the binding's fast path (host code only)
+
+
+def build_torch_ext(force: bool = False, verbose: bool = False) -> str:
+    import sysconfig
+
+    import torch
+    src, header = os.path.join(CSRC, "pps_torch.cpp"), os.path.join(ROOT, "include", "pps.h")
+    if force or _stale(TORCH_EXT, [src, header, torch.__file__]):
+        os.makedirs(OUT, exist_ok=True)
+        at = os.path.dirname(torch.__file__)
+        cuda = os.path.join(os.path.dirname(os.path.dirname(nvcc())), "include")
+        tmp = TORCH_EXT + f".tmp{os.getpid()}"
+        cmd = ["g++", "-std=c++17", "-O2", "-fPIC", "-shared",
+               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + os.path.join(ROOT, "include"),
+               "-I" + os.path.join(at, "include"), "-I" + os.path.join(at, "include", "torch", "csrc", "api", "include"),
+               "-I" + sysconfig.get_paths()["include"], "-I" + cuda, src, "-o", tmp, "-L" + os.path.join(at, "lib"),
+               "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
+        os.replace(tmp, TORCH_EXT)
+    return TORCH_EXT
+
+
 def lib_path(variant: str = "") -> str:
     return os.path.join(OUT, f"libpps{variant}.so")
 
@@ -63,8 +88,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return o
 
     jobs = [(v, src) for v in VARIANTS for src in SOURCES] + [(None, src) for src in COMMON]
-    with ThreadPoolExecutor(max_workers=len(jobs)) as ex:
+    with ThreadPoolExecutor(max_workers=len(jobs) + 1) as ex:
+        ext = ex.submit(build_torch_ext, force, verbose)
         objs = list(ex.map(compile_one, jobs))
+        ext.result()
     for i, v in enumerate(VARIANTS):
         vobjs = objs[i * len(SOURCES):(i + 1) * len(SOURCES)] + objs[len(VARIANTS) * len(SOURCES):]
         target = lib_path(v)

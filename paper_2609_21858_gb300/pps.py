@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import importlib.util
 import os
 import struct
 import threading
@@ -39,6 +40,7 @@ LMHEAD_MAX_K = 8
 
 _lock = threading.Lock()
 _lib = None
+_fast = None  # pps_torch, bound to the loaded library
 
 
 class RowIds(ctypes.Structure):
@@ -54,10 +56,10 @@ class PPSError(RuntimeError):
 def use_library(rounds: int = 10):
     """Switch the binding to the build for Philox4x32-`rounds` (the next call loads it).
     Device memory (workspaces, outputs) carries over; results follow the new keyed source."""
-    global _lib, LIB_PATH
+    global _lib, _fast, LIB_PATH
     with _lock:
         LIB_PATH = library_path(rounds)
-        _lib = None
+        _lib = _fast = None
 
 
 def philox_rounds() -> int:
@@ -644,9 +646,9 @@ def lmhead_verify_tree(hidden, weight, key, ctx, pos, gamma: int, seq_off, node_
 
 # ---------------------------------------------------------------- target side of a step
 #
-# Host cost: kv_append of a few tokens runs one launch of 3 us, and took 17 us of Python and ctypes with an object
-# per tensor and an argument each.  The argument structs of these calls are packed by struct.Struct in one go
-# (0.5 us for 40 fields), and the checks go by device index and one shape and stride tuple per tensor.
+# Host cost: a model makes these calls once per layer, some of them for a few tokens (kv_append of 8 tokens: one launch of
+# 3 us), and checks and marshalling in Python take 10 to 27 us.  So each call first goes to pps_torch (csrc/pps_torch.cpp),
+# which makes the common call, on the current stream, from C++; what it does not take (None) is checked and made below.
 
 _HALVES = {torch.bfloat16: BF16, torch.float16: F16}
 
@@ -657,10 +659,37 @@ _ATTENTION_ARGS = struct.Struct("@N" + "Pqq" * 2 + _CACHE_FIELDS + "PPPPPPPN" + 
 _CHAIN_ARGS = struct.Struct("@N" + "P" * 13 + "N" + "q" * 6 + "iiif" + "0q")
 
 
+def _load_fast():
+    """The extension that makes the common call (csrc/pps_torch.cpp; raises if it was not built), bound to the library."""
+    global _fast
+    L = lib()
+    with _lock:
+        if _fast is None:
+            path = os.path.join(_HERE, "_lib", "pps_torch.so")
+            if not os.path.exists(path):
+                raise RuntimeError(f"pps_torch.so not found at {path}; build it with "
+                                   "`python -c 'import __graft_entry__ as g; g.build()'`")
+            spec = importlib.util.spec_from_file_location("pps_torch", path)
+            ext = importlib.util.module_from_spec(spec)
+            spec.loader.exec_module(ext)
+            ext.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+                L.pps_kv_append, L.pps_paged_attention, L.pps_verify_chain, L.pps_attention_workspace_size,
+                L.pps_chain_workspace_size)))
+            _fast = ext
+    return _fast
+
+
 def _own_memory(stream):
     """A context for the tensors a call allocates itself: on the stream it is given they come from that
     stream's pool, so that neither pending nor later work of the current stream shares their memory."""
     return _HERE_ALREADY if stream is None else torch.cuda.stream(stream)
+
+
+def _done(fn, x):
+    """What the extension returned: a result, or the status code of a call that the library refused."""
+    if x.__class__ is int:
+        _check(fn, x)
+    return x
 
 
 class _Scratch:
@@ -757,6 +786,11 @@ def kv_append(q, k, v, pos, slot, k_cache, v_cache, rope, q_norm=None, k_norm=No
     their cache slots.  Returns the queries (`out`, which may be q).  q [n, heads, d]; k, v [n, kv heads, d];
     k_cache, v_cache [pages, page_size, kv heads, d]; rope: rope_table or None (no rotation); slot int64, < 0:
     not written."""
+    if stream is None:
+        done = (_fast or _load_fast()).kv_append(q, k, v, pos, slot, k_cache, v_cache, rope, q_norm, k_norm, eps,
+                                                 interleaved, out, status)
+        if done is not None:
+            return _done("pps_kv_append", done)
     di, dt, code = _half_rows(q)
     n, heads, d = shape = q.shape
     cache = _cache(k_cache, v_cache, di, dt, d)
@@ -804,6 +838,11 @@ def paged_attention(q, k_cache, v_cache, pages, kv_len, q_off, mask=None, scale=
     q_off[s] .. q_off[s+1]-1) attend to the paged cache.  pages [n_seq, columns] int32, kv_len [n_seq] int32
     (the new tokens' own keys included); mask [n, words] int32 tree masks, None: causal; scale None: 1/sqrt(d);
     lse: an optional [n, heads] float32 output.  Returns out."""
+    if stream is None:
+        done = (_fast or _load_fast()).paged_attention(q, k_cache, v_cache, pages, kv_len, q_off, mask, scale, out, lse,
+                                                       ws, status)
+        if done is not None:
+            return _done("pps_paged_attention", done)
     di, dt, code = _half_rows(q)
     n, heads, d = shape = q.shape
     cache = _cache(k_cache, v_cache, di, dt, d)
@@ -856,6 +895,11 @@ def verify_chain(p_logits, q_logits, gamma: int, seq_off, node_draft_row, draft_
     """pps_verify_chain: the token-level maximal coupling along drafted chains of up to gamma tokens, from the
     uniforms u [n_draft] and exponentials noise [n_seq, >= V].  Returns dict(accept_len, n_emitted, emitted,
     accept_prob); `out` may leave accept_prob out."""
+    if stream is None and out is None:
+        done = (_fast or _load_fast()).verify_chain(p_logits, q_logits, gamma, seq_off, node_draft_row, draft_tok, u, noise,
+                                                    temperature, ws, status)
+        if done is not None:
+            return _done("pps_verify_chain", done)
     if not isinstance(p_logits, torch.Tensor) or not p_logits.is_cuda:
         raise TypeError("p_logits must be a CUDA tensor")
     di, dt, code = p_logits.get_device(), p_logits.dtype, _dtype_code(p_logits)
