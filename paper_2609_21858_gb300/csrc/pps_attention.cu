@@ -111,6 +111,7 @@ __device__ __forceinline__ int64_t head_cost(const AttnArgs& a, const AttnPlan& 
     const int nb = n_blocks(P, q);
     if (nb == 1 || a.mask != nullptr) return (int64_t)nb * (block_tiles(a, P, q, 0) + kFix);
     int64_t c = 0;
+#pragma unroll 1
     for (int b = 0; b < nb; ++b) c += block_tiles(a, P, q, b) + kFix;
     return c;
 }
@@ -376,6 +377,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                 st.vh = (int)divide(rem, per);
                 rem -= st.vh * per;
                 st.blk = 0;
+#pragma unroll 1
                 for (int c; rem >= (c = block_tiles(a, P, own, st.blk) + kFix); ++st.blk) rem -= c;
                 st.base = c0 - rem;
                 *s_start = st;
@@ -526,26 +528,20 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                         }
                         it += more_keys ? 2 : 1;
                     }
-                } else {  // one tile, every other key tile per stream
+                } else {  // one tile, every other key tile per stream: S of tile j + 2 follows O += P V of tile j
                     const uint32_t tile = turn;
                     turn ^= 1u;
                     ok = mbar_wait(qfull(tile), (tile ? nq1++ : nq0++) & 1u, abort);
-                    for (int j = 0; j < min(n, 2) && ok; ++j) {
-                        ok = landed(it);
-                        if (!ok) break;
-                        scores(j, tile, it, j + 1 == n);
-                        tc_commit(empty(it % C::kStages));
-                        ++it;
-                    }
-                    for (int j = 0; j < n && ok; ++j) {
-                        const uint32_t w = j & 1;
-                        ok = landed(it) && values(w, it, j < 2);
-                        if (!ok) break;
-                        tc_commit(empty(it % C::kStages));
-                        ++it;
+#pragma unroll 1
+                    for (int j = -2; j < n && ok; ++j) {
+                        const uint32_t w = (uint32_t)j & 1u;
+                        if (j >= 0) {
+                            if (!(ok = landed(it) && values(w, it, j < 2))) break;
+                            tc_commit(empty(it % C::kStages));
+                            ++it;
+                        }
                         if (j + 2 < n) {
-                            ok = landed(it);
-                            if (!ok) break;
+                            if (!(ok = landed(it))) break;
                             scores(w, tile, it, j + 3 == n);
                             tc_commit(empty(it % C::kStages));
                             ++it;
@@ -779,8 +775,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                         a.lse[(int64_t)(W.q.off + tok) * a.n_heads + head] =
                             l > 0.0f ? (m + log2f(l) - H::kShift) * 0.69314718055994531f : -INFINITY;
                 }
+                int kind = (whole ? 1 : 0) | (!two && n > 1 ? 2 : 0);
 #pragma unroll 1
                 for (int c = from; c < to && c < D; c += 32) {
+                    asm volatile("" : "+r"(kind));  // one body for all kinds: the compiler would make a loop of each
                     uint32_t o[32];
                     if (n > 0) {
                         tmem_ld32(tO + first * 128u + c, o);
@@ -790,7 +788,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
                         o[e] = n > 0 && f != 0.0f ? __float_as_uint(__uint_as_float(o[e]) * f) : 0u;
-                    if (!two && n > 1) {
+                    if (kind & 2) {
                         uint32_t o1[32];
                         tmem_ld32(tO + 128u + c, o1);
                         tmem_wait_ld();
@@ -800,7 +798,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                             if (f1 != 0.0f) o[e] = __float_as_uint(fmaf(__uint_as_float(o1[e]), f1, __uint_as_float(o[e])));
                     }
                     const int q = lane & 3;
-                    if (whole) {
+                    if (kind & 1) {
                         uint4 u[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {

@@ -48,6 +48,7 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
 // Wait for the phase of parity `parity` to complete; false when the CTA is
 // aborting or the wait gave up (which starts the abort).
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
+#pragma unroll 1
     for (uint32_t n = 0; n < kWaitLimit; ++n) {
         if (mbar_try_wait(bar, parity)) return true;
         if (*abort) return false;
