@@ -52,6 +52,7 @@ constexpr int kLoadWarp = 8, kMmaWarp = 10, kQueryWarp = 11;
 static_assert(32 * (kQueryWarp + 1) == kAttnThreads, "the last warp loads the queries");
 constexpr int kMaxCtas = 160;      // shares of the work (one per SM)
 constexpr int kFix = 6;            // key tiles that an item's start and end cost
+constexpr int kLeast = 3;          // of a cut item's key tiles, at most, for a cut to move to the item's end
 constexpr float kLazy = 8.0f;      // log2 of the rise of a maximum that O is not rescaled for
 constexpr uint32_t kColO = 256;    // tensor memory columns: S/P of streams 0, 1; O of streams 0, 1
 
@@ -399,11 +400,11 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
         if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
         return;
     }
-    const int least = (int)min(max(share / 8, (int64_t)1), (int64_t)kFix);
+    const int least = (int)min(max(share / 8, (int64_t)1), (int64_t)kLeast);
     Walk W(P, *s_start, c0, c1, least);
     const int D = a.c.head_dim;
 
-    // registers: 384 x 168 at launch = 256 x 208 + 128 x 88
+    // registers: 384 x 168 at launch = 256 x 216 + 128 x 72
     if (warp >= kLoadWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp < kMmaWarp) {
