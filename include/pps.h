@@ -534,7 +534,10 @@ pps_status pps_kv_append(const pps_append_args* args, pps_stream_t stream);
  *                       token's mask is set (word b / 32, bit b % 32; its own
  *                       bit included)
  * A token that sees nothing gets zeros.  Keys and values at slots past kv_len
- * may hold anything.  Products on the tensor cores with fp32 accumulation, the
+ * may hold anything; a value within kv_len that is not finite makes every
+ * token computed together with it NaN in that channel, whether the token sees
+ * it or not (a weight of zero times it), as a plain product of weights and
+ * values would.  Products on the tensor cores with fp32 accumulation, the
  * softmax in fp32, its weights rounded to dtype for the second product.
  *
  * dtype        PPS_BF16 or PPS_F16, of q, the cache and out

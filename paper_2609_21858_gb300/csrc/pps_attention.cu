@@ -27,6 +27,24 @@
 // order: the same call gives the same bits.  Lengths are read on the device; nothing waits for the host.
 //
 // Every wait gives up after tc::kWaitLimit polls and raises PPS_FLAG_TIMEOUT.
+//
+// Measured (bf16, 32 heads over 8 key heads of 128 channels unless said; a copy moves 6.78 TB/s, library products run
+// at 1936 TFLOP/s):
+//   64 sequences, a token each, up to 8000 keys      216 us = 6.1 TB/s, 0.91 of the copy's: bound by HBM
+//   one sequence of 130001 keys, 28 over 4 heads      55 us = 4.8 TB/s: one segment per CTA, of which 8 us of start, end, join
+//   64 trees of 41 nodes, up to 4100 keys            180 us = 4.0 TB/s: a key tile takes 3200 clocks (164 rows padded to 256), and
+//                                                    CTAs go through 3.8 segments, 10000 clocks of start and end each
+//   8192 tokens after 8192                          1030 us = 1600 TFLOP/s, 0.83 of the library's rate: a key tile of two row tiles
+//                                                    takes 2880 clocks, 2048 of them tensor work; the rest is the softmax's latency
+//   7 chunks of up to 777 tokens, 14 over 2 x 64      51 us = 380 TFLOP/s: 64 channels halve the products, not the softmax (2650 clocks)
+//   one sequence of 900 keys                          13 us: some 6 us from the launch to the first scores, of which most is
+//                                                    fetching each role's instructions; 4 us for the join
+// Code size is speed here: with the wait loops unrolled by the compiler (198 KB of code, now 110) the long sequence took 66 us.
+//
+// Built and measured slower: P apart from S at 64 channels, so that the next scores need not wait for O += P V (3 to 5 percent: the
+// softmax, not the products' latency, is what a tile takes); the next segment's page table read ahead by the loaders (1 percent);
+// the plan made by every warp for itself (3 to 8 percent: more code at the start); shares of at least 2, 4 or 8 key tiles (short
+// contexts up to 45 percent).
 #include <algorithm>
 #include <atomic>
 #include <cfloat>
@@ -51,7 +69,9 @@ constexpr int kAttnThreads = 384;  // two softmax warpgroups; warps that load ke
 constexpr int kLoadWarp = 8, kMmaWarp = 10, kQueryWarp = 11;
 static_assert(32 * (kQueryWarp + 1) == kAttnThreads, "the last warp loads the queries");
 constexpr int kMaxCtas = 160;      // shares of the work (one per SM)
-constexpr int kFix = 6;            // key tiles that an item's start and end cost
+// Key tiles that an item's start and end cost.  (2, 3, 4: decoding batches and ragged chunks 1 to 3 percent faster, trees 3 to 11
+// and one long sequence 4 to 6 percent slower.)
+constexpr int kFix = 6;
 constexpr int kLeast = 3;          // of a cut item's key tiles, at most, for a cut to move to the item's end
 constexpr float kLazy = 8.0f;      // log2 of the rise of a maximum that O is not rescaled for
 constexpr uint32_t kColO = 256;    // tensor memory columns: S/P of streams 0, 1; O of streams 0, 1
