@@ -43,7 +43,8 @@
 //
 // Built and measured slower: P apart from S at 64 channels, so that the next scores need not wait for O += P V (3 to 5 percent: the
 // softmax, not the products' latency, is what a tile takes); the next segment's page table read ahead by the loaders (1 percent);
-// the plan made by every warp for itself (3 to 8 percent: more code at the start); shares of at least 2, 4 or 8 key tiles (short
+// the plan made by every warp for itself (3 to 8 percent: more code at the start); four softmax warpgroups, half of a row's keys each
+// (28 percent: a vote per tile on the common maximum, 96 registers, so that some scores are read twice); shares of at least 2, 4 or 8 key tiles (short
 // contexts up to 45 percent).
 #include <algorithm>
 #include <atomic>
