@@ -1022,9 +1022,16 @@ bool cache_map(CUtensorMap* m, const void* ptr, const CacheView& c, int dtype) {
     const cuuint64_t strides[3] = {(cuuint64_t)c.tok * 2, c.n_kv_heads > 1 ? (cuuint64_t)c.head * 2 : 256,
                                    c.n_pages > 1 ? (cuuint64_t)c.page * 2 : 256};
     const cuuint32_t box[4] = {64, (cuuint32_t)std::min(kTileKeys, c.page_size), 1, 1}, es[4] = {1, 1, 1, 1};
+    // What a miss brings into L2: no more than the rows fill, since their neighbours are other heads' and are read much later.
+    // 35 sequences decoding over 20 / 4 heads, pages token by token, with 256 -> 64 bytes: 64 channels 133 -> 104 us, 80 203 -> 145,
+    // 96 208 -> 153 (128 bytes: 177); rows that follow one another (pages head by head), of 72 channels: 256 180, 128 145, 64 150;
+    // 128 channels: no difference.
+    const auto fetch = c.head_dim % 128 == 0 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B
+                       : c.tok == c.head_dim    ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B
+                                                : CU_TENSOR_MAP_L2_PROMOTION_L2_64B;
     return f(m, dtype == PPS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
-             const_cast<void*>(ptr), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+             const_cast<void*>(ptr), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, fetch,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // the queries as [key head, token, head of the group, channel], loaded in boxes of tt tokens x gs heads x 64 channels
