@@ -533,7 +533,9 @@ pps_status pps_kv_append(const pps_append_args* args, pps_stream_t stream);
  *   tree                iff j < kv_len - n, or bit b = j - (kv_len - n) of the
  *                       token's mask is set (word b / 32, bit b % 32; its own
  *                       bit included)
- * A token that sees nothing gets zeros.  Keys and values at slots past kv_len
+ * A token that sees nothing gets zeros; one with a score that is NaN or +inf
+ * (its query's, a seen key's) gets NaN, and what keys it does not see hold does
+ * not matter.  Keys and values at slots past kv_len
  * may hold anything; a value within kv_len that is not finite makes every
  * token computed together with it NaN in that channel, whether the token sees
  * it or not (a weight of zero times it), as a plain product of weights and

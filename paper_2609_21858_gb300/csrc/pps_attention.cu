@@ -761,7 +761,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             const uint32_t tiles = i, tiles_other = n + (two ? n : 0) - i;
             if (tiles > 0) ok = wait_warp(odone(w), (done + tiles - 1) & 1u, abort);
             if (!ok) break;
-            m *= P.sc;  // log2 of the largest weight (-inf stays)
+            m = fmaxf(m * P.sc, -INFINITY);  // log2 of the largest weight (-inf stays, whatever the scale)
+            if (l != l) m = INFINITY;  // a score that is not a number, or infinite: so is the row, whatever it is joined with
             float f = 1.0f, f1 = 0.0f;  // factors of the first accumulator (the stream's own) and, of one tile, the second
             if (!two) {
                 s_ml[w * 128 + r] = make_float2(m, l);
@@ -776,7 +777,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             tc_fence_after();
             if (busy) {
                 if (whole) {
-                    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+                    const float inv = l > 0.0f ? 1.0f / l : l;  // (l: zero, or not a number)
                     f *= inv;
                     f1 *= inv;
                 }
@@ -795,7 +796,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                         P.part_ml[(int64_t)slot * P.cap_rows + in_block] = make_float2(m, l);
                     else if (a.lse)
                         a.lse[(int64_t)(W.q.off + tok) * a.n_heads + head] =
-                            l > 0.0f ? (m + log2f(l) - H::kShift) * 0.69314718055994531f : -INFINITY;
+                            l == 0.0f ? -INFINITY : (m + log2f(l) - H::kShift) * 0.69314718055994531f;
                 }
                 int kind = (whole ? 1 : 0) | (!two && n > 1 ? 2 : 0);
 #pragma unroll 1
@@ -882,7 +883,7 @@ __global__ void __launch_bounds__(256, 4) join_kernel(const AttnArgs a, const At
     const int kvh = vh / P.nsub, sub = vh - kvh * P.nsub, gs = min(P.gs, P.group - sub * P.gs);
     const int64_t first = (int64_t)(2 * blockIdx.x + 1) * P.cap_rows, rest = (int64_t)2 * blockIdx.x * P.cap_rows;
     auto put = [&](int i, float M, float l, const float (&o)[VW]) {
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        const float inv = l > 0.0f ? 1.0f / l : l;
         const int t = i / gs, tok = tok0 + t, head = kvh * P.group + sub * P.gs + (i - t * gs);
         if (lane * VW < D) {
             T* out = static_cast<T*>(a.out.p) + (int64_t)tok * a.out.tok + head * a.out.head + lane * VW;
@@ -892,7 +893,7 @@ __global__ void __launch_bounds__(256, 4) join_kernel(const AttnArgs a, const At
                 *reinterpret_cast<uint32_t*>(out) = H::pack(o[0] * inv, o[1] * inv);
         }
         if (lane == 0 && a.lse)
-            a.lse[(int64_t)tok * a.n_heads + head] = l > 0.0f ? (M + log2f(l) - H::kShift) * 0.69314718055994531f : -INFINITY;
+            a.lse[(int64_t)tok * a.n_heads + head] = l == 0.0f ? -INFINITY : (M + log2f(l) - H::kShift) * 0.69314718055994531f;
     };
     if (nsplit == 2) {  // the usual cut of a batch: four rows of two parts in flight
         const int step = 8 * gridDim.y;
