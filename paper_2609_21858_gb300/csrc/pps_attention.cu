@@ -483,96 +483,96 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                     for (uint32_t n = 0, i = last - 1 - j; n < kWaitLimit && !mbar_try_wait(full(i % C::kStages), (i / C::kStages) & 1u); ++n) {
                     }
         } else if (warp == kMmaWarp) {
-        // ---- products (one thread): per stream S = Q K^T, then O += P V as its weights arrive
-        // Straight-line products of the class's full width (channels past head_dim are zeros): in a loop they issue at
-        // 100 cycles each, so at the tensor core's 64.  No product stands under a condition of its own.
-        if (elect_one()) {
-            constexpr uint32_t id_qk = (1u << 4) | (H::kType << 7) | (H::kType << 10) | ((kTileKeys / 8u) << 17) | ((kTileRows / 16u) << 24);
-            constexpr uint32_t id_pv = (1u << 4) | (H::kType << 7) | (H::kType << 10) | (1u << 16) | ((DC / 8u) << 17) | ((kTileRows / 16u) << 24);
-            uint32_t it = 0, np0 = 0, np1 = 0, nq0 = 0, nq1 = 0, turn = 0;
-            auto stage = [&](uint32_t i) { return ring + (i % C::kStages) * C::kTile; };
-            auto landed = [&](uint32_t i) {
-                const bool ok = mbar_wait(full(i % C::kStages), (i / C::kStages) & 1u, abort);
-                tc_fence_after();
-                return ok;
-            };
-            auto scores = [&](uint32_t w, uint32_t tile, uint32_t k, bool last) {  // last: the segment needs the queries no more
-                const uint64_t qd = sw128_desc(base + tile * C::kTile), kd = sw128_desc(stage(k));
+            // ---- products (one thread): per stream S = Q K^T, then O += P V as its weights arrive
+            // Straight-line products of the class's full width (channels past head_dim are zeros): in a loop they issue at
+            // 100 cycles each, so at the tensor core's 64.  No product stands under a condition of its own.
+            if (elect_one()) {
+                constexpr uint32_t id_qk = (1u << 4) | (H::kType << 7) | (H::kType << 10) | ((kTileKeys / 8u) << 17) | ((kTileRows / 16u) << 24);
+                constexpr uint32_t id_pv = (1u << 4) | (H::kType << 7) | (H::kType << 10) | (1u << 16) | ((DC / 8u) << 17) | ((kTileRows / 16u) << 24);
+                uint32_t it = 0, np0 = 0, np1 = 0, nq0 = 0, nq1 = 0, turn = 0;
+                auto stage = [&](uint32_t i) { return ring + (i % C::kStages) * C::kTile; };
+                auto landed = [&](uint32_t i) {
+                    const bool ok = mbar_wait(full(i % C::kStages), (i / C::kStages) & 1u, abort);
+                    tc_fence_after();
+                    return ok;
+                };
+                auto scores = [&](uint32_t w, uint32_t tile, uint32_t k, bool last) {  // last: the segment needs the queries no more
+                    const uint64_t qd = sw128_desc(base + tile * C::kTile), kd = sw128_desc(stage(k));
 #pragma unroll
-                for (uint32_t c = 0; c < DC / 16; ++c) {
-                    const uint64_t o = ((c >> 2) * C::kBlock + (c & 3u) * 32u) >> 4;
-                    tc_mma(tmem + w * 128u, qd + o, kd + o, id_qk, c != 0);
-                }
-                tc_commit(sfull(w));
-                if (last) tc_commit(qfree(tile));
-            };
-            // O += P V in two halves, each as soon as its weights are there
-            auto values = [&](uint32_t w, uint32_t v, bool first) {
-                const uint64_t vd = sw128_desc_mn(stage(v), C::kBlock);
-                const uint32_t o = tmem + kColO + w * 128u, p = tmem + w * 128u, at = w ? np1 : np0;
-                ++(w ? np1 : np0);
-                if (!mbar_wait(pready(w, 0), at & 1u, abort)) return false;
-                tc_fence_after();
-#pragma unroll
-                for (uint32_t c = 0; c < kTileKeys / 32; ++c) tc_mma_ts(o, p + c * 8u, vd + c * (2048u >> 4), id_pv, !first || c != 0);
-                if (!mbar_wait(pready(w, 1), at & 1u, abort)) return false;
-                tc_fence_after();
-#pragma unroll
-                for (uint32_t c = kTileKeys / 32; c < kTileKeys / 16; ++c) tc_mma_ts(o, p + c * 8u, vd + c * (2048u >> 4), id_pv, 1u);
-                tc_commit(odone(w));
-                return true;
-            };
-            bool ok = true;
-            while (ok && W.next(a, P)) {
-                const int n = W.t1 - W.t0;
-                if (n == 0) continue;
-                if (W.ntok > P.tt) {  // a tile per stream, the same keys
-                    ok = mbar_wait(qfull(0), nq0++ & 1u, abort) && mbar_wait(qfull(1), nq1++ & 1u, abort) && landed(it);
-                    if (!ok) break;
-                    scores(0, 0, it, n == 1);
-                    scores(1, 1, it, n == 1);
-                    tc_commit(empty(it % C::kStages));
-                    ++it;
-                    for (int j = 0; j < n && ok; ++j) {
-                        const uint32_t v = it, k = it + 1;
-                        const bool more_keys = j + 1 < n;
-                        ok = landed(v);
-                        for (uint32_t w = 0; w < 2 && ok; ++w) {
-                            ok = values(w, v, j == 0);
-                            if (!ok) break;
-                            if (w == 1) tc_commit(empty(v % C::kStages));
-                            if (more_keys) {
-                                if (w == 0) ok = landed(k);
-                                if (!ok) break;
-                                scores(w, w, k, j + 2 == n);
-                                if (w == 1) tc_commit(empty(k % C::kStages));
-                            }
-                        }
-                        it += more_keys ? 2 : 1;
+                    for (uint32_t c = 0; c < DC / 16; ++c) {
+                        const uint64_t o = ((c >> 2) * C::kBlock + (c & 3u) * 32u) >> 4;
+                        tc_mma(tmem + w * 128u, qd + o, kd + o, id_qk, c != 0);
                     }
-                } else {  // one tile, every other key tile per stream: S of tile j + 2 follows O += P V of tile j
-                    const uint32_t tile = turn;
-                    turn ^= 1u;
-                    ok = mbar_wait(qfull(tile), (tile ? nq1++ : nq0++) & 1u, abort);
-#pragma unroll 1
-                    for (int j = -2; j < n && ok; ++j) {
-                        const uint32_t w = (uint32_t)j & 1u;
-                        if (j >= 0) {
-                            if (!(ok = landed(it) && values(w, it, j < 2))) break;
-                            tc_commit(empty(it % C::kStages));
-                            ++it;
+                    tc_commit(sfull(w));
+                    if (last) tc_commit(qfree(tile));
+                };
+                // O += P V in two halves, each as soon as its weights are there
+                auto values = [&](uint32_t w, uint32_t v, bool first) {
+                    const uint64_t vd = sw128_desc_mn(stage(v), C::kBlock);
+                    const uint32_t o = tmem + kColO + w * 128u, p = tmem + w * 128u, at = w ? np1 : np0;
+                    ++(w ? np1 : np0);
+                    if (!mbar_wait(pready(w, 0), at & 1u, abort)) return false;
+                    tc_fence_after();
+#pragma unroll
+                    for (uint32_t c = 0; c < kTileKeys / 32; ++c) tc_mma_ts(o, p + c * 8u, vd + c * (2048u >> 4), id_pv, !first || c != 0);
+                    if (!mbar_wait(pready(w, 1), at & 1u, abort)) return false;
+                    tc_fence_after();
+#pragma unroll
+                    for (uint32_t c = kTileKeys / 32; c < kTileKeys / 16; ++c) tc_mma_ts(o, p + c * 8u, vd + c * (2048u >> 4), id_pv, 1u);
+                    tc_commit(odone(w));
+                    return true;
+                };
+                bool ok = true;
+                while (ok && W.next(a, P)) {
+                    const int n = W.t1 - W.t0;
+                    if (n == 0) continue;
+                    if (W.ntok > P.tt) {  // a tile per stream, the same keys
+                        ok = mbar_wait(qfull(0), nq0++ & 1u, abort) && mbar_wait(qfull(1), nq1++ & 1u, abort) && landed(it);
+                        if (!ok) break;
+                        scores(0, 0, it, n == 1);
+                        scores(1, 1, it, n == 1);
+                        tc_commit(empty(it % C::kStages));
+                        ++it;
+                        for (int j = 0; j < n && ok; ++j) {
+                            const uint32_t v = it, k = it + 1;
+                            const bool more_keys = j + 1 < n;
+                            ok = landed(v);
+                            for (uint32_t w = 0; w < 2 && ok; ++w) {
+                                ok = values(w, v, j == 0);
+                                if (!ok) break;
+                                if (w == 1) tc_commit(empty(v % C::kStages));
+                                if (more_keys) {
+                                    if (w == 0) ok = landed(k);
+                                    if (!ok) break;
+                                    scores(w, w, k, j + 2 == n);
+                                    if (w == 1) tc_commit(empty(k % C::kStages));
+                                }
+                            }
+                            it += more_keys ? 2 : 1;
                         }
-                        if (j + 2 < n) {
-                            if (!(ok = landed(it))) break;
-                            scores(w, tile, it, j + 3 == n);
-                            tc_commit(empty(it % C::kStages));
-                            ++it;
+                    } else {  // one tile, every other key tile per stream: S of tile j + 2 follows O += P V of tile j
+                        const uint32_t tile = turn;
+                        turn ^= 1u;
+                        ok = mbar_wait(qfull(tile), (tile ? nq1++ : nq0++) & 1u, abort);
+#pragma unroll 1
+                        for (int j = -2; j < n && ok; ++j) {
+                            const uint32_t w = (uint32_t)j & 1u;
+                            if (j >= 0) {
+                                if (!(ok = landed(it) && values(w, it, j < 2))) break;
+                                tc_commit(empty(it % C::kStages));
+                                ++it;
+                            }
+                            if (j + 2 < n) {
+                                if (!(ok = landed(it))) break;
+                                scores(w, tile, it, j + 3 == n);
+                                tc_commit(empty(it % C::kStages));
+                                ++it;
+                            }
                         }
                     }
                 }
             }
-        }
-        __syncwarp();
+            __syncwarp();
         } else {
             // ---- queries: both tiles of a block of two, or the tile that the last block of one did not use
             uint32_t n0 = 0, n1 = 0, turn = 0;
