@@ -379,6 +379,10 @@ __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(
                     f.round(cur.x[j][k]);
                 }
                 put(k);
+                // A vector that is never read (only one of 8 channels can be) stays zero: a norm that is not finite, or a weight,
+                // would make it NaN, and with it the sums of all heads that these lanes take later.
+                if constexpr (NORM && VW == 8)
+                    if (c1[k] >= D) cur.x[j][k][1].raw = typename RawVec<VW>::type{};
             }
         }
         tok += step;
