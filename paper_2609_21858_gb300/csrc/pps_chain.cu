@@ -420,6 +420,7 @@ __global__ void __launch_bounds__(kThreads + 32) finish_kernel(const ChainArgs a
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = threadIdx.x;
     const int n0 = __ldg(a.seq_off + seq), n1 = __ldg(a.seq_off + seq + 1);
     if (n0 < 0 || n1 <= n0 || n1 > a.n_nodes) {  // CTA-uniform: nothing of the sequence can be read
+        pdl_wait();  // a grid without one CTA that waits may end before the statistics do, whose workspace is then another's
         if (slice == 0 && j == 0) {
             a.out_acc[seq] = 0;
             a.out_ne[seq] = 0;
