@@ -605,7 +605,8 @@ pps_status pps_paged_attention(const pps_attention_args* args, pps_stream_t stre
  *              for a row without a usable logit); a residual that is zero
  *              everywhere in fp32 is replaced by P
  * out_accept_prob nullable [n_draft] min(1, P(x) / Q(x)) of every draft row that
- *              a chain's node names (0 / 0 counts as 0)
+ *              one of the first gamma nodes of a sequence names (0 / 0 counts as
+ *              0); 0 for every other row
  * A draft row or token out of range is treated as the chain's end or as
  * rejected, a sequence whose nodes lie outside the rows gets accept_len 0 and
  * no token; both raise PPS_FLAG_INDEX.

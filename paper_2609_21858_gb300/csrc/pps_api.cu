@@ -750,8 +750,12 @@ pps_status pps_verify_chain(const pps_chain_args* args, pps_stream_t stream) {
     if (!strides_ok(p_stride, n_nodes, q_stride, n_draft, noise_stride, n_seq)) return PPS_ERR_INVALID_ARG;
     if (!(temperature > 0.0f) || !std::isfinite(temperature)) return PPS_ERR_INVALID_ARG;
     if (n_seq < 0 || gamma < 0 || gamma > 64) return PPS_ERR_INVALID_ARG;
-    if (n_seq == 0 || n_nodes == 0) return n_seq == 0 && n_nodes == 0 ? PPS_OK : PPS_ERR_INVALID_ARG;
-    if (n_nodes < n_seq) return PPS_ERR_INVALID_ARG;
+    if (n_nodes < n_seq || (n_seq == 0 && n_nodes > 0)) return PPS_ERR_INVALID_ARG;
+    if (n_seq == 0) {  // no chain names a row
+        if (!out_accept_prob || n_draft == 0) return PPS_OK;
+        const cudaError_t e = cudaMemsetAsync(out_accept_prob, 0, sizeof(float) * (size_t)n_draft, (cudaStream_t)stream);
+        return e == cudaSuccess ? PPS_OK : PPS_ERR_CUDA;
+    }
     if (!p_logits || !seq_off || !node_draft_row || !noise || !out_accept_len || !out_n_emitted || !out_emitted)
         return PPS_ERR_INVALID_ARG;
     if (n_draft > 0 && (!q_logits || !draft_tok || !u)) return PPS_ERR_INVALID_ARG;

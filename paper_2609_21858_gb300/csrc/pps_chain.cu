@@ -249,6 +249,9 @@ __global__ void __launch_bounds__(kThreads + 32, kStatCtas + 1) stats_kernel(con
     }
     if (blockIdx.x == 0)
         for (int i = threadIdx.x; i < a.n_seq; i += kThreads + 32) P.ticket[i] = 0;
+    if (a.out_prob)  // for the rows that no chain names; finish_kernel writes the others once this grid has ended
+        for (int64_t i = (int64_t)blockIdx.x * (kThreads + 32) + threadIdx.x; i < a.n_draft; i += (int64_t)gridDim.x * (kThreads + 32))
+            a.out_prob[i] = 0.0f;
     __syncthreads();
     const int64_t x1 = min((blockIdx.x + 1) * P.share, (a.n_nodes + a.n_draft) * P.nv);
     uint32_t it = 0;

@@ -894,7 +894,7 @@ def verify_chain(p_logits, q_logits, gamma: int, seq_off, node_draft_row, draft_
                  ws=None, out=None, status=None, stream=None):
     """pps_verify_chain: the token-level maximal coupling along drafted chains of up to gamma tokens, from the
     uniforms u [n_draft] and exponentials noise [n_seq, >= V].  Returns dict(accept_len, n_emitted, emitted,
-    accept_prob); `out` may leave accept_prob out."""
+    accept_prob [n_draft], 0 for rows that no chain names); `out` may leave accept_prob out."""
     if stream is None and out is None:
         done = (_fast or _load_fast()).verify_chain(p_logits, q_logits, gamma, seq_off, node_draft_row, draft_tok, u, noise,
                                                     temperature, ws, status)
