@@ -2,6 +2,7 @@
 // workspace layout and launches.  Every entry point returns before launching
 // anything when an argument is invalid.
 #include <algorithm>
+#include <cfloat>
 #include <climits>
 #include <cmath>
 #include <cstdint>
@@ -772,7 +773,8 @@ pps_status pps_verify_chain(const pps_chain_args* args, pps_stream_t stream) {
     a.noise_stride = noise_stride;
     a.n_seq = n_seq;
     a.gamma = gamma;
-    a.c = (float)(1.4426950408889634074 / (double)temperature);
+    // finite also at temperatures below 4.3e-39, where the law is its largest logit's: infinity times their difference of zero is NaN
+    a.c = (float)std::min(1.4426950408889634074 / (double)temperature, (double)FLT_MAX);
     a.seq_off = seq_off;
     a.node_draft_row = node_draft_row;
     a.draft_tok = draft_tok;
