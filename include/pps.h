@@ -549,7 +549,8 @@ pps_status pps_kv_append(const pps_append_args* args, pps_stream_t stream);
  *              sequence, max_pages <= pages_stride valid columns.  A page outside
  *              the cache reads as zeros (PPS_FLAG_INDEX), entries past
  *              ceil(kv_len / page_size) are not read.
- * kv_len       [n_seq], 0 .. max_pages * page_size (cut to that, PPS_FLAG_INDEX)
+ * kv_len       [n_seq], 0 .. min(max_pages * page_size, 2^31 - 128) (cut to that,
+ *              PPS_FLAG_INDEX)
  * q_off        [n_seq + 1] non-decreasing, within [0, n_tok] (a sequence for
  *              which it is not is left out, PPS_FLAG_INDEX)
  * mask         nullable [n_tok, mask_words] tree masks; a token has bits for up

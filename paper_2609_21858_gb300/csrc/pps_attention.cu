@@ -96,7 +96,7 @@ struct Cut {
 struct AttnPlan {
     int group, gs, nsub, tt;  // heads of a key head; those taken at a time, in nsub turns; tokens per tile
     int cap_rows, page_log2;
-    int64_t cap_keys;   // what a row of the page table holds
+    int64_t cap_keys;   // what a row of the page table holds, at most whole tiles of an int's range
     float sc;           // |scale| log2 e
     uint32_t s_and, s_xor;  // on scores: a negative scale turns their signs, a zero one clears them
     Cut* cuts;          // [gridDim.x]
@@ -123,7 +123,8 @@ __device__ __forceinline__ Seq load_seq(const AttnArgs& a, const AttnPlan& P, in
 // key tiles of row block `blk`: those its last token sees
 __device__ __forceinline__ int block_tiles(const AttnArgs& a, const AttnPlan& P, const Seq& q, int blk) {
     int vis = q.len;
-    if (a.mask == nullptr) vis = max(0, q.len - q.n + min(q.n, (blk + 1) * 2 * P.tt));
+    const int i0 = blk * 2 * P.tt;
+    if (a.mask == nullptr) vis = max(0, q.len - q.n + i0 + min(q.n - i0, 2 * P.tt));
     return (vis + kTileKeys - 1) / kTileKeys;
 }
 __device__ __forceinline__ int n_blocks(const AttnPlan& P, const Seq& q) {
@@ -1059,7 +1060,7 @@ cudaError_t launch(const AttnArgs& a, int dtype, cudaStream_t st) {
     P.cap_rows = rows.cap;
     P.page_log2 = 0;
     while ((1 << P.page_log2) < a.c.page_size) ++P.page_log2;
-    P.cap_keys = (int64_t)a.max_pages * a.c.page_size;
+    P.cap_keys = std::min<int64_t>((int64_t)a.max_pages * a.c.page_size, INT32_MAX - (kTileKeys - 1));
     const float scale = a.scale;
     P.sc = scale == 0.0f ? 1.0f : (float)((double)(scale < 0.0f ? -scale : scale) * 1.4426950408889634074);
     P.s_and = scale == 0.0f ? 0u : 0xffffffffu;
