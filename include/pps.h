@@ -555,7 +555,7 @@ pps_status pps_kv_append(const pps_append_args* args, pps_stream_t stream);
  *              which it is not is left out, PPS_FLAG_INDEX)
  * mask         nullable [n_tok, mask_words] tree masks; a token has bits for up
  *              to 32 * mask_words tokens of its sequence
- * scale        finite (1 / sqrt(head_dim) as a rule)
+ * scale        scale * log2(e) finite in fp32 (1 / sqrt(head_dim) as a rule)
  * out          [n_tok, n_heads, head_dim]
  * out_lse      nullable [n_tok, n_heads] ln sum_j w_j (-inf where nothing is seen)
  * ws, ws_bytes pps_attention_workspace_size(n_tok, n_heads, n_kv_heads, head_dim)

@@ -694,7 +694,8 @@ pps_status pps_paged_attention(const pps_attention_args* args, pps_stream_t stre
         n_heads % cache.n_kv_heads != 0 || max_pages < 0 || pages_stride < max_pages)
         return PPS_ERR_INVALID_ARG;
     if (n_tok * n_heads > INT32_MAX || (int64_t)max_pages * cache.page_size > INT32_MAX) return PPS_ERR_INVALID_ARG;
-    if (!std::isfinite(scale) || mask_words < 0 || (mask && mask_words < 1)) return PPS_ERR_INVALID_ARG;
+    // (the softmax is formed in powers of two)
+    if (!(std::fabs((double)scale) * 1.4426950408889634074 <= FLT_MAX) || mask_words < 0 || (mask && mask_words < 1)) return PPS_ERR_INVALID_ARG;
     if (!strides_ok(q.tok_stride, n_tok, q.head_stride, n_heads) ||
         !strides_ok(out.tok_stride, n_tok, out.head_stride, n_heads))
         return PPS_ERR_INVALID_ARG;
