@@ -722,8 +722,7 @@ def _strided(name, t, di, dt, shape, what):
         st = t.stride()
         if st[-1] == 1:
             return st
-    if not isinstance(t, torch.Tensor) or t.get_device() != di:
-        raise TypeError(f"{name} must be a CUDA tensor on cuda:{di}")
+    _required(name, t, di)
     if t.dtype is not dt:
         raise TypeError(f"{name} must be {dt}, got {t.dtype}")
     have, st = t.shape, t.stride()
@@ -743,6 +742,13 @@ def _flat(name, t, di, dt, numel):
         return t.data_ptr()
     _need(name, t, torch.device("cuda", di), dt, numel)
     return t.data_ptr()
+
+
+def _required(name, t, di):
+    """Raise unless t is a tensor of device di."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != di:
+        raise TypeError(f"{name} must be a CUDA tensor on cuda:{di}")
+    return t
 
 
 def _half_rows(q):
@@ -800,15 +806,11 @@ def kv_append(q, k, v, pos, slot, k_cache, v_cache, rope, q_norm=None, k_norm=No
     sv = _strided("v", v, di, dt, kv_shape, _HEADS)
     rot = max_pos = table = at = 0
     if rope is not None:
-        if rope.dim() != 2:
+        if _required("rope", rope, di).dim() != 2:
             raise TypeError("rope must be [max_pos, rot]")
         max_pos, rot = rope.shape
-        table, at = _flat("rope", rope, di, torch.float32, 0), _flat("pos", pos, di, torch.int32, n)
-        if pos is None:
-            raise TypeError("pos is required")
-    if slot is None:
-        raise TypeError("slot is required")
-    slots = _flat("slot", slot, di, torch.int64, n)
+        table, at = _flat("rope", rope, di, torch.float32, 0), _flat("pos", _required("pos", pos, di), di, torch.int32, n)
+    slots = _flat("slot", _required("slot", slot, di), di, torch.int64, n)
     wq, wk = _flat("q_norm", q_norm, di, dt, d), _flat("k_norm", k_norm, di, dt, d)
     flags = _flat("status", status, di, torch.int32, 1)
     if torch._C._cuda_getDevice() != di:
@@ -848,16 +850,14 @@ def paged_attention(q, k_cache, v_cache, pages, kv_len, q_off, mask=None, scale=
     cache = _cache(k_cache, v_cache, di, dt, d)
     sq = _strided("q", q, di, dt, shape, _HEADS)
     i32 = torch.int32
-    n_seq = kv_len.numel()
+    n_seq = _required("kv_len", kv_len, di).numel()
     sp = _strided("pages", pages, di, i32, (n_seq, None), "[n_seq, columns]")
     columns = pages.shape[1]
-    lens, offs = _flat("kv_len", kv_len, di, i32, 0), _flat("q_off", q_off, di, i32, n_seq + 1)
-    if not lens or not offs:
-        if kv_len is None or q_off is None:
-            raise TypeError("kv_len and q_off are required")
+    lens = _flat("kv_len", kv_len, di, i32, 0)
+    offs = _flat("q_off", _required("q_off", q_off, di), di, i32, n_seq + 1)
     words = bits = 0
     if mask is not None:
-        if mask.dim() != 2 or mask.shape[0] != n or mask.shape[1] < 1:
+        if _required("mask", mask, di).dim() != 2 or mask.shape[0] != n or mask.shape[1] < 1:
             raise ValueError(f"mask must be [{n}, words]")
         words, bits = mask.shape[1], _flat("mask", mask, di, i32, 0)
     sums, flags = _flat("lse", lse, di, torch.float32, n * heads), _flat("status", status, di, i32, 1)
@@ -906,16 +906,17 @@ def verify_chain(p_logits, q_logits, gamma: int, seq_off, node_draft_row, draft_
     rows = "[rows, vocabulary]"
     p_stride = _strided("p_logits", p_logits, di, dt, (None, None), rows)[0]
     n, V = p_logits.shape
-    q_stride = _strided("q_logits", q_logits, di, q_logits.dtype, (None, V), rows)[0]
+    q_stride = _strided("q_logits", q_logits, di, _required("q_logits", q_logits, di).dtype, (None, V), rows)[0]
     if q_logits.dtype is not dt:
         raise ValueError("p_logits and q_logits must have the same dtype")
     n_draft = q_logits.shape[0]
     i32, f32 = torch.int32, torch.float32
-    n_seq = seq_off.numel() - 1
+    n_seq = _required("seq_off", seq_off, di).numel() - 1
     noise_stride = _strided("noise", noise, di, f32, (None, None), "[n_seq, >= vocabulary]")[0]
     if noise.shape[0] < n_seq or noise.shape[1] < V:
         raise ValueError(f"noise is {list(noise.shape)}; the call needs [{n_seq}, >= {V}]")
-    inputs = [_flat(name, t, di, dtype, numel) for name, t, dtype, numel in (
+    # (a tensor that is not read may be None)
+    inputs = [_flat(name, t if numel == 0 else _required(name, t, di), di, dtype, numel) for name, t, dtype, numel in (
         ("seq_off", seq_off, i32, n_seq + 1), ("node_draft_row", node_draft_row, i32, n),
         ("draft_tok", draft_tok, i32, n_draft), ("u", u, f32, n_draft))]
     flags, work = _flat("status", status, di, i32, 1), _flat("ws", ws, di, torch.uint8, 0)
