@@ -168,7 +168,7 @@ class Session:
             row_k = self.row_k.view(n, -1)[:, lo:hi].flatten().contiguous()
             x = self.model.norm(self.model.embed[tok[:, lo:hi].reshape(-1)])
             y = pps.lmhead_draft_list(x, self.model.head, self.key.repeat_interleave(hi - lo), self.zero[:rows], pos,
-                                      t.K, row_k=row_k, temperature=self.temperature)
+                                      t.K, row_k=row_k, temperature=self.temperature, status=self.status)
             lists[:, lo:hi] = y["tok"].view(n, hi - lo, t.K)
             counts[:, lo:hi] = y["ndist"].view(n, hi - lo)
             b = t.branching[d]
