@@ -489,7 +489,8 @@ typedef struct {
  * q, k, v      [n_tok, n_heads | n_kv_heads | n_kv_heads, head_dim] (e.g. three
  *              views of one projection's output)
  * cache        head_dim and n_kv_heads apply to k and v; head_dim a multiple of 8
- *              up to 256
+ *              up to 256, pages of any size (pps_paged_attention reads caches of
+ *              head_dim up to 128 and pages of a power of two from 8)
  * q_norm, k_norm  nullable [head_dim] norm weights
  * rope         [max_pos, rot] fp32: cos t of the rot/2 pairs, then sin t; rot
  *              even, 0 <= rot <= head_dim (0: no rotation, rope nullable)
@@ -540,7 +541,8 @@ pps_status pps_kv_append(const pps_append_args* args, pps_stream_t stream);
  * token computed together with it NaN in that channel, whether the token sees
  * it or not (a weight of zero times it), as a plain product of weights and
  * values would.  Products on the tensor cores with fp32 accumulation, the
- * softmax in fp32, its weights rounded to dtype for the second product.
+ * softmax in fp32, its weights rounded to dtype for the second product (up to
+ * 2^-8 of each for PPS_BF16, 2^-11 for PPS_F16, beside the result's own rounding).
  *
  * dtype        PPS_BF16 or PPS_F16, of q, the cache and out
  * cache        head_dim a multiple of 8 up to 128, page_size a power of two >= 8;
@@ -556,7 +558,8 @@ pps_status pps_kv_append(const pps_append_args* args, pps_stream_t stream);
  * mask         nullable [n_tok, mask_words] tree masks; a token has bits for up
  *              to 32 * mask_words tokens of its sequence
  * scale        scale * log2(e) finite in fp32 (1 / sqrt(head_dim) as a rule)
- * out          [n_tok, n_heads, head_dim]
+ * out          [n_tok, n_heads, head_dim]; tokens that belong to no sequence are
+ *              not written (nor in out_lse)
  * out_lse      nullable [n_tok, n_heads] ln sum_j w_j (-inf where nothing is seen)
  * ws, ws_bytes pps_attention_workspace_size(n_tok, n_heads, n_kv_heads, head_dim)
  *              bytes; need not be cleared

@@ -17,8 +17,11 @@
 //
 // Softmax.  A thread owns a row.  O is rescaled only when a row's maximum has risen by more than 2^kLazy since the
 // maximum in use (then by its own warpgroup, in place): the weights may pass 1 by that factor, which neither
-// the fp32 sums nor a 16-bit weight feel.  Weights are rounded to the cache's type for the second product
-// (one rounding of 2^-9 or 2^-12 each, of the size of the result's own); their sum is formed before rounding.
+// the fp32 sums nor the 16-bit types' ranges feel.  Weights are rounded to the cache's type for the second product
+// (up to 2^-8 of each in bf16, 2^-11 in fp16, as the result's own rounding); their sum is formed before rounding.  The largest
+// weight of a row is 2^kShift and loses nothing as long as its score is the maximum in use; below a later, larger one (by less than
+// kLazy) it is any number, so a row with one key that matters may be off by one such rounding more.  Against 64 bits the error is 1.4 times
+// that of a result formed in fp32 and rounded once (bf16 2.3e-3 to 1.7e-3, fp16 2.8e-4 to 2.1e-4): weights of 32 bits would double the products.
 //
 // Work split.  Key tiles of all (sequence, key head, row block) items, plus kFix per item for its start and end, lie
 // on one line that is cut into equal shares, one per SM, whatever the lengths are; a cut that would leave a few tiles
@@ -32,10 +35,12 @@
 // at 1936 TFLOP/s):
 //   64 sequences, a token each, up to 8000 keys      216 us = 6.1 TB/s, 0.91 of the copy's: bound by HBM
 //   one sequence of 130001 keys, 28 over 4 heads      55 us = 4.8 TB/s: one segment per CTA, of which 8 us of start, end, join
-//   64 trees of 41 nodes, up to 4100 keys            180 us = 4.0 TB/s: a key tile takes 3200 clocks (164 rows padded to 256), and
+//   64 trees of 41 nodes, up to 4100 keys            180 to 183 us = 4.0 TB/s: a key tile takes 3200 clocks (164 rows padded to 256), and
 //                                                    CTAs go through 3.8 segments, 10000 clocks of start and end each
-//   8192 tokens after 8192                          1030 us = 1600 TFLOP/s, 0.83 of the library's rate: a key tile of two row tiles
-//                                                    takes 2880 clocks, 2048 of them tensor work; the rest is the softmax's latency
+//   8192 tokens after 8192                          1030 to 1050 us = 1600 TFLOP/s, 0.82 of the library's rate: a key tile of two row tiles
+//                                                    takes 2880 clocks, 2048 of them tensor work; the rest is the softmax's latency.
+//                                                    Over seconds 1120 us = 1480 TFLOP/s, 0.86 of the library's sustained rate: the power
+//                                                    limit (1.38 kW) takes the clock from 2070 to 1935 MHz
 //   7 chunks of up to 777 tokens, 14 over 2 x 64      51 us = 380 TFLOP/s: 64 channels halve the products, not the softmax (2650 clocks)
 //   one sequence of 900 keys                          13 us: some 6 us from the launch to the first scores, of which most is
 //                                                    fetching each role's instructions; 4 us for the join

@@ -5,7 +5,7 @@
 // the chain argmax_i P(i) / E(i).  exp2 of c (l - max) with c = log2(e) / T stands for exp(l / T) throughout;
 // a logit equal to its row's maximum counts as 1 also where both are infinite.
 //
-// Two launches, both bound by HBM.  stats_kernel reads every logit once: the rows' 16-byte vectors lie on one line
+// Two launches, both bound by HBM.  stats_kernel (which also writes zeros for the acceptance of all rows) reads every logit once: the rows' 16-byte vectors lie on one line
 // that is cut into equal shares, one per CTA, and a CTA leaves (max, sum of exponentials) of each row it meets.
 // finish_kernel runs slices x sequences: each CTA joins the parts of its chain's rows, finds the first rejection and races
 // its slice of the one row (pair) that matters; the CTA that arrives last at the sequence's ticket joins the slices in
@@ -14,9 +14,9 @@
 // hold enough of them (64 sequences of V = 128256: 66 to 70 us).  The copies take whole 16-byte vectors inside a row;
 // the few tokens at its unaligned ends are read one by one.
 //
-// Measured: 64 chains of 5, V = 128256, bf16: 47.6 us, 4.5 TB/s over both passes (0.66 of a copy's 6.78): the statistics 35 us (2.5
+// Measured (in a graph; launched one by one 1.5 to 2 us more): 64 chains of 5, V = 128256, bf16: 47.5 us, 4.5 TB/s over both passes (0.66 of a copy's 6.78): the statistics 35 us (2.5
 // of 4 issue slots: exponentials and maxima of 8 logits per vector), the race 23 of which a part runs beside them.  16 ragged chains
-// of up to 8, V = 152063, fp32: 31.6 us, 3.2 TB/s.  One chain, V = 32000: 13 us, two launches and their chains of dependent
+// of up to 8, V = 152063, fp32: 31.7 us, 3.2 TB/s.  One chain, V = 32000: 13 to 14 us, two launches and their chains of dependent
 // loads (offsets, rows, tokens, logits; sums, acceptance, the row, the ticket).
 #include <algorithm>
 #include <climits>

@@ -839,7 +839,7 @@ def paged_attention(q, k_cache, v_cache, pages, kv_len, q_off, mask=None, scale=
     """pps_paged_attention: the newest tokens of each sequence (q [n, heads, d], those of sequence s in
     q_off[s] .. q_off[s+1]-1) attend to the paged cache.  pages [n_seq, columns] int32, kv_len [n_seq] int32
     (the new tokens' own keys included); mask [n, words] int32 tree masks, None: causal; scale None: 1/sqrt(d);
-    lse: an optional [n, heads] float32 output.  Returns out."""
+    lse: an optional [n, heads] float32 output.  Returns out (tokens that belong to no sequence are not written)."""
     if stream is None:
         done = (_fast or _load_fast()).paged_attention(q, k_cache, v_cache, pages, kv_len, q_off, mask, scale, out, lse,
                                                        ws, status)
