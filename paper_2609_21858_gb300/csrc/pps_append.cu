@@ -18,7 +18,7 @@
 // issuing them (norm: 24); now 9 and 15.  8192 tokens of (32 + 2 x 8) heads of 128 channels take 35.9 us, 5.7 TB/s (85 percent
 // of a copy's), with norm 43.7; of (14 + 2 x 2) x 64 11.5 and 15.3; of (20 + 2 x 4) x 80, where 5 of 8 lanes have a unit, 19.9 and 28.4
 // (rot 40, 8-byte vectors: 28.1 and 38.8).  With a norm neither the issue slots (1.7 of 4 a clock) nor HBM (20 percent at 2624
-// tokens) are full: the 16 warps of an SM, as many as their 124 registers allow, wait for loads and for one another's results.  A few tokens: 2.5 to 2.8 us
+// tokens) are full: the 16 warps of an SM, as many as their 124 registers allow, wait for loads and for their own last results.  A few tokens: 2.5 to 2.8 us
 // in a graph, 4.1 launched one by one.  Tried: one head
 // ahead and more CTAs, weights held or read before the shuffles (registers, 10 percent slower), one body of the loop
 // that copies the next item's registers (10 percent slower).
