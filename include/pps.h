@@ -73,6 +73,7 @@ typedef struct {
 #define PPS_FLAG_TREE 4u        /* a sequence's root row (seq_off[s]) lies outside the node rows: nothing emitted */
 #define PPS_FLAG_TIMEOUT 8u     /* an LM-head or attention kernel gave up waiting on its pipeline and returned early */
 #define PPS_FLAG_INDEX 16u      /* a position, slot, page, length, row or token lies outside its array (target-side calls) */
+#define PPS_FLAG_POOL 32u       /* the pool has no pages left for a sequence (pps_kv_reserve) */
 
 #define PPS_MAX_K 32
 
@@ -469,7 +470,7 @@ typedef struct {
 } pps_heads;
 
 /*
- * The three calls below take their arguments in one struct in HOST memory, read
+ * The calls from here to pps_adjust_logits take their arguments in one struct in HOST memory, read
  * before the call returns; `size` guards against a caller built for another
  * layout (PPS_ERR_INVALID_ARG).  Pointers in it are device memory as everywhere.
  */
@@ -640,6 +641,233 @@ typedef struct {
     float temperature;
 } pps_chain_args;
 pps_status pps_verify_chain(const pps_chain_args* args, pps_stream_t stream);
+
+/*
+ * A cache held in 4 bits.  Of every head, a block of 16 channels is 16 codes in
+ * the e2m1 format (sign, 0, 0.5, 1, 1.5, 2, 3, 4 or 6), two to a byte with the
+ * even channel in the low half, and a scale in the e4m3 format:
+ *   value = unit[head] * scale * code
+ * held from a block x as  z = x * (1 / unit),  scale = e4m3(min(max |z| / 6, 448)),
+ * code = e2m1(z / scale), in fp32, to nearest with ties to even, at most 6; a
+ * scale that rounds to zero makes the block zeros (of either sign), and a block
+ * with a channel that is not finite is held as NaN throughout.  So a block's channel is off by a
+ * sixth of the block's largest at most (half the step from 4 to 6; a scale's
+ * rounding adds up to 2^-4 of the largest's), and a block whose largest is below
+ * 6 * 2^-10 units is zeros: units (nullable: ones) keep heads of small values in range.
+ * Codes of (page, token, head) are head_dim / 2 bytes at k + page * page_stride +
+ * token * tok_stride + head * head_stride, scales 4 * ceil(head_dim / 64) bytes of which
+ * head_dim / 16 count, at k_scale with strides of their own (all strides in
+ * bytes; codes: bases and strides multiples of 8; scales: of 4).  Pages may be laid out token by
+ * token or head by head; head by head, a page's rows follow one another and
+ * reading wastes nothing of a memory transaction.
+ * head_dim is a multiple of 16 up to 256 (pps_paged_attention_q4: 128).
+ */
+typedef struct {
+    void* k;
+    void* v;
+    void* k_scale;
+    void* v_scale;
+    const float* k_unit; /* nullable [n_kv_heads], positive and finite */
+    const float* v_unit;
+    int64_t n_pages;
+    int32_t page_size, n_kv_heads, head_dim;
+    int64_t page_stride, tok_stride, head_stride;
+    int64_t scale_page_stride, scale_tok_stride, scale_head_stride;
+} pps_kv_cache_q4;
+
+/*
+ * pps_kv_append_q4 -- pps_kv_append into a cache in 4 bits; the arguments of
+ * the same names mean the same.  Keys are held from their norm and rotation in fp32
+ * (no rounding to 16 bits between), values as they are given.
+ */
+typedef struct {
+    size_t size; /* sizeof(pps_append_q4_args) */
+    pps_heads q, k, v, out_q;
+    pps_kv_cache_q4 cache;
+    const void* q_norm;
+    const void* k_norm;
+    const float* rope;
+    const int32_t* pos;
+    const int64_t* slot;
+    uint32_t* status;
+    int64_t n_tok, max_pos;
+    int32_t dtype; /* pps_dtype */
+    int32_t n_heads, rot, interleaved;
+    float eps;
+} pps_append_q4_args;
+pps_status pps_kv_append_q4(const pps_append_q4_args* args, pps_stream_t stream);
+
+/*
+ * pps_kv_read_q4 -- the values of cache slots, back in 16 bits (to move them to
+ * another cache, to hand them on, or to look at them).
+ * slot         [n] cache slots; a negative one reads as zeros, one beyond the
+ *              cache too (PPS_FLAG_INDEX)
+ * k, v         outputs [n, n_kv_heads, head_dim] of dtype (PPS_BF16 or PPS_F16), 16-byte
+ *              aligned, strides multiples of 8 elements; unit * scale * code in
+ *              fp32, rounded once
+ */
+typedef struct {
+    size_t size; /* sizeof(pps_read_q4_args) */
+    pps_heads k, v;
+    pps_kv_cache_q4 cache;
+    const int64_t* slot;
+    uint32_t* status;
+    int64_t n;
+    int32_t dtype; /* pps_dtype */
+} pps_read_q4_args;
+pps_status pps_kv_read_q4(const pps_read_q4_args* args, pps_stream_t stream);
+
+/*
+ * pps_paged_attention_q4 -- pps_paged_attention over a cache in 4 bits; the
+ * arguments of the same names mean the same, and so do masks, lengths, and what is
+ * done about numbers that are not finite.  Codes times scales are exact in fp16, in which both products run
+ * on the tensor cores with fp32 accumulation: queries in bf16 are brought there by a
+ * power of two per row (channels below 2^-31 of a row's largest lose bits), the softmax is in fp32,
+ * its weights are rounded to fp16 for the second product (2^-11 of each).
+ * head_dim is a multiple of 16 up to 128, page_size a power of two >= 8.
+ * ws, ws_bytes pps_attention_q4_workspace_size(n_tok, n_heads, n_kv_heads,
+ *              head_dim) bytes; need not be cleared
+ */
+size_t pps_attention_q4_workspace_size(int64_t n_tok, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+typedef struct {
+    size_t size; /* sizeof(pps_attention_q4_args) */
+    pps_heads q, out;
+    pps_kv_cache_q4 cache;
+    const int32_t* pages;
+    const int32_t* kv_len;
+    const int32_t* q_off;
+    const uint32_t* mask;
+    float* out_lse;
+    uint32_t* status;
+    void* ws;
+    size_t ws_bytes;
+    int64_t n_tok, pages_stride;
+    int32_t dtype; /* pps_dtype */
+    int32_t n_heads, max_pages, n_seq, mask_words;
+    float scale;
+} pps_attention_q4_args;
+pps_status pps_paged_attention_q4(const pps_attention_q4_args* args, pps_stream_t stream);
+
+/*
+ * pps_kv_reserve -- the page tables and the slot map of a step, from the
+ * requests' lengths.  Sequence s holds kv_len[s] tokens in held[s] pages
+ * (columns 0 .. held[s]-1 of its row of `pages`) and brings n_new[s] more: the
+ * pages it lacks for kv_len + n_new tokens come from the pool, a stack of
+ * free_count[0] page numbers.  The k-th page that the call takes, by sequence and
+ * column, is free_list[free_count - 1 - k].
+ * A sequence whose demand, with the demands of those before it, passes the pool
+ * gets nothing (PPS_FLAG_POOL), and neither does any later one that lacks a page;
+ * one that would pass its row's columns gets nothing either and demands nothing
+ * (PPS_FLAG_INDEX).  Such a sequence's tokens have slot -1 and out_kv_len 0, so that nothing is
+ * written for them and they attend to nothing.
+ *
+ * pages        [n_seq, pages_stride] int32, columns <= pages_stride valid (in and out)
+ * held, free_list [free_cap], free_count [1]: in and out (free_list is read)
+ * page_size    tokens per page, any
+ * pos_off      nullable [n_tok]: positions are kv_len[s] + pos_off[t] (e.g. a
+ *              tree node's depth); NULL: + the token's number in its sequence
+ * out_q_off    [n_seq + 1] tokens of sequence s are q_off[s] .. q_off[s+1]-1
+ * out_kv_len   [n_seq] kv_len + n_new (may be kv_len itself)
+ * out_slot     [n_tok] int64, out_pos [n_tok], out_seq nullable [n_tok]: of token
+ *              number i of sequence s, the slot of place kv_len[s] + i.  Places past the last
+ *              token (a batch padded to a fixed size) get slot -1, position 0, sequence -1
+ * Negative lengths count as 0, and more tokens than n_tok are not written; both
+ * raise PPS_FLAG_INDEX.  n_seq <= 8192, else PPS_ERR_UNSUPPORTED.
+ */
+typedef struct {
+    size_t size; /* sizeof(pps_reserve_args) */
+    int32_t* pages;
+    int32_t* held;
+    const int32_t* free_list;
+    int32_t* free_count;
+    const int32_t* kv_len;
+    const int32_t* n_new;
+    const int32_t* pos_off;
+    int32_t* out_q_off;
+    int32_t* out_kv_len;
+    int64_t* out_slot;
+    int32_t* out_pos;
+    int32_t* out_seq;
+    uint32_t* status;
+    int64_t n_tok, pages_stride;
+    int32_t n_seq, columns, page_size, free_cap;
+} pps_reserve_args;
+pps_status pps_kv_reserve(const pps_reserve_args* args, pps_stream_t stream);
+
+/*
+ * pps_kv_trim -- the counterpart, when fewer tokens are kept than were reserved
+ * (or none: the sequence has ended): sequence s keeps the pages of keep[s]
+ * tokens, the others go back to the pool and their columns become -1.  The k-th
+ * of R pages that go back, by sequence and column, becomes free_list[free_count +
+ * R - 1 - k], so that pps_kv_reserve takes them again in that order.
+ * keep[s] is at most what the held pages have room for (more keeps them all and raises
+ * PPS_FLAG_INDEX).  Pages that would pass free_cap are lost (PPS_FLAG_INDEX).
+ */
+typedef struct {
+    size_t size; /* sizeof(pps_trim_args) */
+    int32_t* pages;
+    int32_t* held;
+    int32_t* free_list;
+    int32_t* free_count;
+    const int32_t* keep;
+    uint32_t* status;
+    int64_t pages_stride;
+    int32_t n_seq, columns, page_size, free_cap;
+} pps_trim_args;
+pps_status pps_kv_trim(const pps_trim_args* args, pps_stream_t stream);
+
+/*
+ * pps_adjust_logits -- penalties for repeated tokens, biases and grammar masks,
+ * between the LM head and the race or the verification.  With c how often token
+ * i stands in the output part of the sequence's text and on the row's path, and
+ * said: c > 0, or i stands in the text's first prompt_len tokens,
+ *   y = said ? (x > 0 ? x / repetition : x * repetition) : x
+ *   y = y - frequency * c - presence * [c > 0] + bias,  -inf where not allowed
+ * each operation in fp32, the result rounded once.
+ *
+ * logits       [n_rows, in_stride], out [n_rows, out_stride], both dtype (PPS_BF16
+ *              or PPS_F32); out may be logits itself, else they do not overlap
+ * seq_off      [n_seq + 1] sequence s owns rows seq_off[s] .. seq_off[s+1]-1 (as
+ *              pps_verify_tree).  Rows of no sequence are not written; a sequence whose rows
+ *              lie outside them is left out (PPS_FLAG_INDEX)
+ * text         nullable [n_seq, text_stride], text_len [n_seq] its tokens (at
+ *              most text_cap <= text_stride), prompt_len nullable [n_seq] (NULL: none of them is prompt)
+ * node_tok     nullable [n_rows]: the token that each row's node stands for; the
+ *              row's path is its own and its ancestors' (they count as output):
+ * node_mask    nullable [n_rows, mask_words] bit b: the b-th row of the sequence lies on the path
+ *              (the tree mask of pps_paged_attention); NULL: the rows of a
+ *              sequence are a chain.  A path of more than 64 counts its first 64
+ *              (PPS_FLAG_INDEX)
+ * repetition (> 0), frequency, presence  nullable [n_seq], finite; they need text or node_tok
+ * bias_off     nullable [n_seq + 1]: entries bias_off[s] .. bias_off[s+1]-1 of
+ *              bias_tok, bias_val [n_bias] are added in sequence s; of several for a token the last counts
+ * allowed      nullable [n_rows, allowed_stride] words, bit i % 32 of word i / 32:
+ *              token i may follow (allowed_stride >= ceil(vocab / 32))
+ * Tokens outside the vocabulary are left out (PPS_FLAG_INDEX).
+ */
+typedef struct {
+    size_t size; /* sizeof(pps_adjust_args) */
+    const void* logits;
+    void* out;
+    const int32_t* seq_off;
+    const int32_t* text;
+    const int32_t* text_len;
+    const int32_t* prompt_len;
+    const int32_t* node_tok;
+    const uint32_t* node_mask;
+    const float* repetition;
+    const float* frequency;
+    const float* presence;
+    const int32_t* bias_off;
+    const int32_t* bias_tok;
+    const float* bias_val;
+    const uint32_t* allowed;
+    uint32_t* status;
+    int64_t n_rows, vocab, in_stride, out_stride, text_stride, allowed_stride;
+    int32_t dtype; /* pps_dtype */
+    int32_t n_seq, text_cap, mask_words, n_bias;
+} pps_adjust_args;
+pps_status pps_adjust_logits(const pps_adjust_args* args, pps_stream_t stream);
 
 /*
  * pps_draft_list_noalloc -- pps_draft_list for callers that must not

@@ -790,6 +790,264 @@ pps_status pps_verify_chain(const pps_chain_args* args, pps_stream_t stream) {
     return launch_chain(a, (int)dtype, (cudaStream_t)stream) == cudaSuccess ? PPS_OK : PPS_ERR_CUDA;
 }
 
+// ---- a cache in 4 bits
+
+static bool multiple(const void* p, int64_t m) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)m == 0; }
+
+static pps_status check_cache_q4(const pps_kv_cache_q4& c) {
+    if (c.n_pages < 0 || c.n_pages > INT32_MAX || c.page_size < 1 || c.n_kv_heads < 1 || c.n_kv_heads > 65535 || c.head_dim < 1)
+        return PPS_ERR_INVALID_ARG;
+    if (c.head_dim % 16 != 0 || c.head_dim > 256) return PPS_ERR_UNSUPPORTED;
+    if (c.n_pages > 0 && (!c.k || !c.v || !c.k_scale || !c.v_scale)) return PPS_ERR_INVALID_ARG;
+    if (!strides_ok(c.page_stride, c.n_pages, c.tok_stride, c.page_size, c.head_stride, c.n_kv_heads) ||
+        !strides_ok(c.scale_page_stride, c.n_pages, c.scale_tok_stride, c.page_size, c.scale_head_stride, c.n_kv_heads))
+        return PPS_ERR_INVALID_ARG;
+    auto units = [](int64_t s, int64_t n, int64_t m) { return n <= 1 || s % m == 0; };
+    if (!multiple(c.k, 8) || !multiple(c.v, 8) || !multiple(c.k_scale, 4) || !multiple(c.v_scale, 4) ||
+        !units(c.page_stride, c.n_pages, 8) || !units(c.tok_stride, c.page_size, 8) || !units(c.head_stride, c.n_kv_heads, 8) ||
+        !units(c.scale_page_stride, c.n_pages, 4) || !units(c.scale_tok_stride, c.page_size, 4) ||
+        !units(c.scale_head_stride, c.n_kv_heads, 4))
+        return PPS_ERR_INVALID_ARG;
+    return PPS_OK;
+}
+static CacheView codes_view(const pps_kv_cache_q4& c) {
+    return {c.k, c.v, c.n_pages, c.page_size, c.n_kv_heads, c.head_dim, c.page_stride, c.tok_stride, c.head_stride};
+}
+// an empty cache has no scales: any address that is not null, never used, tells the kernels that there are 4 bits
+static Q4View q4_view(const pps_kv_cache_q4& c) {
+    uint8_t* none = reinterpret_cast<uint8_t*>(8);
+    return {c.n_pages > 0 ? static_cast<uint8_t*>(c.k_scale) : none, c.n_pages > 0 ? static_cast<uint8_t*>(c.v_scale) : none,
+            c.scale_page_stride, c.scale_tok_stride, c.scale_head_stride, c.k_unit, c.v_unit};
+}
+
+pps_status pps_kv_append_q4(const pps_append_q4_args* args, pps_stream_t stream) {
+    if (!args || args->size != sizeof(*args)) return PPS_ERR_INVALID_ARG;
+    const auto& [size, q, k, v, out_q, cache, q_norm, k_norm, rope, pos, slot, status, n_tok, max_pos, dtype, n_heads, rot,
+                 interleaved, eps] = *args;
+    (void)size;
+    if (dtype != PPS_BF16 && dtype != PPS_F16) return PPS_ERR_UNSUPPORTED;
+    pps_status st = check_cache_q4(cache);
+    if (st != PPS_OK) return st;
+    if (n_tok < 0 || n_tok > INT32_MAX || n_heads < 1 || n_heads > 65535) return PPS_ERR_INVALID_ARG;
+    if (rot < 0 || rot % 2 != 0 || rot > cache.head_dim || !(eps >= 0.0f) || !std::isfinite(eps)) return PPS_ERR_INVALID_ARG;
+    if (rot > 0 && (!rope || max_pos < 1)) return PPS_ERR_INVALID_ARG;
+    if (!strides_ok(q.tok_stride, n_tok, q.head_stride, n_heads) ||
+        !strides_ok(out_q.tok_stride, n_tok, out_q.head_stride, n_heads) ||
+        !strides_ok(k.tok_stride, n_tok, k.head_stride, cache.n_kv_heads) ||
+        !strides_ok(v.tok_stride, n_tok, v.head_stride, cache.n_kv_heads))
+        return PPS_ERR_INVALID_ARG;
+    if (n_tok == 0) return PPS_OK;
+    if (!q.data || !k.data || !v.data || !out_q.data || !slot || (rot > 0 && !pos)) return PPS_ERR_INVALID_ARG;
+    AppendArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.q = heads_view(q);
+    a.k = heads_view(k);
+    a.v = heads_view(v);
+    a.out = heads_view(out_q);
+    a.c = codes_view(cache);
+    a.q4 = q4_view(cache);
+    a.n_tok = n_tok;
+    a.max_pos = max_pos;
+    a.n_heads = n_heads;
+    a.rot = rot;
+    a.interleaved = interleaved != 0;
+    a.q_norm = q_norm;
+    a.k_norm = k_norm;
+    a.eps = eps;
+    a.rope = rope;
+    a.pos = pos;
+    a.slot = slot;
+    a.status = status;
+    return launch_kv_append(a, (int)dtype, (cudaStream_t)stream) == cudaSuccess ? PPS_OK : PPS_ERR_CUDA;
+}
+
+pps_status pps_kv_read_q4(const pps_read_q4_args* args, pps_stream_t stream) {
+    if (!args || args->size != sizeof(*args)) return PPS_ERR_INVALID_ARG;
+    const auto& [size, k, v, cache, slot, status, n, dtype] = *args;
+    (void)size;
+    if (dtype != PPS_BF16 && dtype != PPS_F16) return PPS_ERR_UNSUPPORTED;
+    pps_status st = check_cache_q4(cache);
+    if (st != PPS_OK) return st;
+    if (n < 0 || !strides_ok(k.tok_stride, n, k.head_stride, cache.n_kv_heads) ||
+        !strides_ok(v.tok_stride, n, v.head_stride, cache.n_kv_heads))
+        return PPS_ERR_INVALID_ARG;
+    auto units = [](int64_t s, int64_t m) { return m <= 1 || s % 8 == 0; };
+    for (const pps_heads* h : {&k, &v})
+        if (!aligned16(h->data) || !units(h->tok_stride, n) || !units(h->head_stride, cache.n_kv_heads)) return PPS_ERR_INVALID_ARG;
+    if (n == 0) return PPS_OK;
+    if (!k.data || !v.data || !slot) return PPS_ERR_INVALID_ARG;
+    const ReadArgs a = {heads_view(k), heads_view(v), codes_view(cache), q4_view(cache), n, slot, status};
+    return launch_kv_read(a, (int)dtype, (cudaStream_t)stream) == cudaSuccess ? PPS_OK : PPS_ERR_CUDA;
+}
+
+size_t pps_attention_q4_workspace_size(int64_t n_tok, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
+    if (n_tok < 0 || n_heads < 1 || n_kv_heads < 1 || head_dim < 1) return 0;
+    return attention_q4_workspace_bytes(n_tok, n_heads, n_kv_heads, head_dim);
+}
+
+pps_status pps_paged_attention_q4(const pps_attention_q4_args* args, pps_stream_t stream) {
+    if (!args || args->size != sizeof(*args)) return PPS_ERR_INVALID_ARG;
+    const auto& [size, q, out, cache, pages, kv_len, q_off, mask, out_lse, status, ws, ws_bytes, n_tok, pages_stride, dtype,
+                 n_heads, max_pages, n_seq, mask_words, scale] = *args;
+    (void)size;
+    if (dtype != PPS_BF16 && dtype != PPS_F16) return PPS_ERR_UNSUPPORTED;
+    pps_status st = check_cache_q4(cache);
+    if (st != PPS_OK) return st;
+    if (cache.head_dim > 128) return PPS_ERR_UNSUPPORTED;
+    if (cache.page_size < 8 || (cache.page_size & (cache.page_size - 1)) != 0) return PPS_ERR_UNSUPPORTED;
+    if (n_tok < 0 || n_tok > INT32_MAX || n_seq < 0 || n_heads < 1 || n_heads > 65535 ||
+        n_heads % cache.n_kv_heads != 0 || max_pages < 0 || pages_stride < max_pages)
+        return PPS_ERR_INVALID_ARG;
+    if (n_tok * n_heads > INT32_MAX || (int64_t)max_pages * cache.page_size > INT32_MAX) return PPS_ERR_INVALID_ARG;
+    if (!(std::fabs((double)scale) * 1.4426950408889634074 <= FLT_MAX) || mask_words < 0 || (mask && mask_words < 1)) return PPS_ERR_INVALID_ARG;
+    if (!strides_ok(q.tok_stride, n_tok, q.head_stride, n_heads) ||
+        !strides_ok(out.tok_stride, n_tok, out.head_stride, n_heads))
+        return PPS_ERR_INVALID_ARG;
+    auto units = [](int64_t s, int64_t n) { return n <= 1 || s % 8 == 0; };
+    if (!aligned16(q.data) || !aligned16(out.data) || !units(q.tok_stride, n_tok) || !units(q.head_stride, n_heads) ||
+        !units(out.tok_stride, n_tok) || !units(out.head_stride, n_heads))
+        return PPS_ERR_INVALID_ARG;
+    if (n_tok == 0 || n_seq == 0) return PPS_OK;
+    if (!q.data || !out.data || !kv_len || !q_off || (max_pages > 0 && !pages)) return PPS_ERR_INVALID_ARG;
+    if (!ws || !aligned16(ws) ||
+        ws_bytes < attention_q4_workspace_bytes(n_tok, n_heads, cache.n_kv_heads, cache.head_dim))
+        return PPS_ERR_WORKSPACE;
+    AttnArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.q = heads_view(q);
+    a.out = heads_view(out);
+    a.c = codes_view(cache);
+    a.n_tok = n_tok;
+    a.pages_stride = pages_stride;
+    a.n_heads = n_heads;
+    a.n_seq = n_seq;
+    a.max_pages = cache.n_pages > 0 ? max_pages : 0;
+    a.mask_words = mask ? mask_words : 0;
+    a.pages = pages;
+    a.kv_len = kv_len;
+    a.q_off = q_off;
+    a.mask = mask;
+    a.scale = scale;
+    a.lse = out_lse;
+    a.status = status;
+    a.ws = ws;
+    return launch_attention_q4(a, q4_view(cache), (int)dtype, (cudaStream_t)stream) == cudaSuccess ? PPS_OK : PPS_ERR_CUDA;
+}
+
+// ---- page tables and slot maps
+
+pps_status pps_kv_reserve(const pps_reserve_args* args, pps_stream_t stream) {
+    if (!args || args->size != sizeof(*args)) return PPS_ERR_INVALID_ARG;
+    const auto& [size, pages, held, free_list, free_count, kv_len, n_new, pos_off, out_q_off, out_kv_len, out_slot, out_pos,
+                 out_seq, status, n_tok, pages_stride, n_seq, columns, page_size, free_cap] = *args;
+    (void)size;
+    if (n_tok < 0 || n_tok > INT32_MAX || n_seq < 0 || columns < 0 || pages_stride < columns || page_size < 1 || free_cap < 0)
+        return PPS_ERR_INVALID_ARG;
+    if (!strides_ok(pages_stride, n_seq, 0, 0)) return PPS_ERR_INVALID_ARG;
+    if (n_seq > kMaxPageSeqs) return PPS_ERR_UNSUPPORTED;
+    if (!free_count || !out_q_off || (free_cap > 0 && !free_list) || (n_tok > 0 && (!out_slot || !out_pos))) return PPS_ERR_INVALID_ARG;
+    if (n_seq > 0 && (!held || !kv_len || !n_new || !out_kv_len || (columns > 0 && !pages))) return PPS_ERR_INVALID_ARG;
+    ReserveArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.pages = pages;
+    a.pages_stride = pages_stride;
+    a.columns = columns;
+    a.n_seq = n_seq;
+    a.page_size = page_size;
+    a.free_cap = free_cap;
+    a.held = held;
+    a.free_list = const_cast<int32_t*>(free_list);
+    a.free_count = free_count;
+    a.kv_len = kv_len;
+    a.n_new = n_new;
+    a.pos_off = pos_off;
+    a.n_tok = n_tok;
+    a.out_q_off = out_q_off;
+    a.out_len = out_kv_len;
+    a.out_slot = out_slot;
+    a.out_pos = out_pos;
+    a.out_seq = out_seq;
+    a.status = status;
+    return launch_kv_reserve(a, (cudaStream_t)stream) == cudaSuccess ? PPS_OK : PPS_ERR_CUDA;
+}
+
+pps_status pps_kv_trim(const pps_trim_args* args, pps_stream_t stream) {
+    if (!args || args->size != sizeof(*args)) return PPS_ERR_INVALID_ARG;
+    const auto& [size, pages, held, free_list, free_count, keep, status, pages_stride, n_seq, columns, page_size, free_cap] = *args;
+    (void)size;
+    if (n_seq < 0 || columns < 0 || pages_stride < columns || page_size < 1 || free_cap < 0 || !strides_ok(pages_stride, n_seq, 0, 0))
+        return PPS_ERR_INVALID_ARG;
+    if (n_seq > kMaxPageSeqs) return PPS_ERR_UNSUPPORTED;
+    if (n_seq == 0) return PPS_OK;
+    if (!held || !keep || !free_count || (free_cap > 0 && !free_list) || (columns > 0 && !pages)) return PPS_ERR_INVALID_ARG;
+    ReserveArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.pages = pages;
+    a.pages_stride = pages_stride;
+    a.columns = columns;
+    a.n_seq = n_seq;
+    a.page_size = page_size;
+    a.free_cap = free_cap;
+    a.held = held;
+    a.free_list = free_list;
+    a.free_count = free_count;
+    a.kv_len = keep;
+    a.status = status;
+    return launch_kv_trim(a, (cudaStream_t)stream) == cudaSuccess ? PPS_OK : PPS_ERR_CUDA;
+}
+
+// ---- logits
+
+pps_status pps_adjust_logits(const pps_adjust_args* args, pps_stream_t stream) {
+    if (!args || args->size != sizeof(*args)) return PPS_ERR_INVALID_ARG;
+    const auto& [size, logits, out, seq_off, text, text_len, prompt_len, node_tok, node_mask, repetition, frequency, presence,
+                 bias_off, bias_tok, bias_val, allowed, status, n_rows, vocab, in_stride, out_stride, text_stride, allowed_stride,
+                 dtype, n_seq, text_cap, mask_words, n_bias] = *args;
+    (void)size;
+    if (dtype != PPS_F32 && dtype != PPS_BF16) return PPS_ERR_UNSUPPORTED;
+    if (n_rows < 0 || n_rows > INT32_MAX || vocab < 1 || vocab > INT32_MAX - 65536 || n_seq < 0 || text_cap < 0 || mask_words < 0 || n_bias < 0)
+        return PPS_ERR_INVALID_ARG;
+    if (in_stride < vocab || out_stride < vocab || !strides_ok(in_stride, n_rows, out_stride, n_rows)) return PPS_ERR_INVALID_ARG;
+    if (logits == out && in_stride != out_stride && n_rows > 1) return PPS_ERR_INVALID_ARG;
+    if (!multiple(logits, dtype == PPS_F32 ? 4 : 2) || !multiple(out, dtype == PPS_F32 ? 4 : 2)) return PPS_ERR_INVALID_ARG;
+    if (text && (!text_len || text_stride < text_cap || !strides_ok(text_stride, n_seq, 0, 0))) return PPS_ERR_INVALID_ARG;
+    if (node_mask && (!node_tok || mask_words < 1)) return PPS_ERR_INVALID_ARG;
+    if ((repetition || frequency || presence) && !text && !node_tok) return PPS_ERR_INVALID_ARG;
+    if (bias_off && n_bias > 0 && (!bias_tok || !bias_val)) return PPS_ERR_INVALID_ARG;
+    if (allowed && (allowed_stride < (vocab + 31) / 32 || !strides_ok(allowed_stride, n_rows, 0, 0))) return PPS_ERR_INVALID_ARG;
+    if (n_rows == 0 || n_seq == 0) return PPS_OK;
+    if (!logits || !out || !seq_off) return PPS_ERR_INVALID_ARG;
+    AdjustArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.x = logits;
+    a.out = out;
+    a.n_rows = n_rows;
+    a.V = vocab;
+    a.x_stride = in_stride;
+    a.out_stride = out_stride;
+    a.text_stride = text_stride;
+    a.allowed_stride = allowed_stride;
+    a.n_seq = n_seq;
+    a.text_cap = text_cap;
+    a.mask_words = node_mask ? mask_words : 0;
+    a.n_bias = n_bias;
+    a.seq_off = seq_off;
+    a.text = text;
+    a.text_len = text_len;
+    a.prompt_len = prompt_len;
+    a.node_tok = node_tok;
+    a.node_mask = node_mask;
+    a.rep = repetition;
+    a.freq = frequency;
+    a.pres = presence;
+    a.bias_off = n_bias > 0 ? bias_off : nullptr;
+    a.bias_tok = bias_off && n_bias > 0 ? bias_tok : nullptr;
+    a.bias_val = bias_val;
+    a.allowed = allowed;
+    a.status = status;
+    return launch_adjust(a, (int)dtype, (cudaStream_t)stream) == cudaSuccess ? PPS_OK : PPS_ERR_CUDA;
+}
+
 pps_status pps_philox_words(pps_row_ids ids, int64_t n_rows, int64_t vocab, int32_t arrival, uint32_t* out,
                             pps_stream_t stream) {
     if (n_rows < 0 || vocab < 1 || arrival < 1) return PPS_ERR_INVALID_ARG;

@@ -31,6 +31,7 @@
 
 #include "pps.h"
 #include "pps_internal.h"
+#include "pps_q4.cuh"
 
 namespace pps {
 namespace {
@@ -38,6 +39,8 @@ namespace {
 constexpr int kAppendWarps = 4;  // per CTA
 constexpr int kAhead = 2;        // heads of a lane group in an item
 constexpr int kAppendCtas = 4;   // per SM
+// a block's 16 channels in shared memory, 80 bytes apart: eight lanes' 16-byte reads touch all banks
+constexpr int kBlockFloats = 20;
 
 struct AppendPlan {
     int lg;          // log2 of the lanes per head
@@ -187,6 +190,9 @@ struct Wide {
 #pragma unroll
             for (int i = 0; i < kN; ++i) f[v][i] = mul2(f[v][i], mul2(rr, y.f[v][i]));
     }
+    // FUSED: a product's rounding is left out of each second sum (never of what becomes 4 bits: there the values are those of
+    // the formula's own operations in 32 bits, whatever computes them)
+    template <bool FUSED>
     __device__ __forceinline__ void rotate(bool interleaved, const float (&cs)[VW], const float (&sn)[VW]) {
         if (VW > 1 && interleaved) {
 #pragma unroll
@@ -196,7 +202,8 @@ struct Wide {
                     const float c = cs[(v * kN + i) % VW], s = sn[(v * kN + i) % VW];
                     float p, q;
                     unpack2(f[v][i], p, q);
-                    f[v][i] = pack2(p * c - q * s, p * s + q * c);
+                    f[v][i] = FUSED ? pack2(p * c - q * s, p * s + q * c)
+                                    : pack2(__fsub_rn(__fmul_rn(p, c), __fmul_rn(q, s)), __fadd_rn(__fmul_rn(p, s), __fmul_rn(q, c)));
                 }
         } else {
 #pragma unroll
@@ -204,8 +211,25 @@ struct Wide {
                 const uint64_t c = pack2(cs[2 * i], cs[(2 * i + 1) % VW]), s = pack2(sn[2 * i], sn[(2 * i + 1) % VW]);
                 const uint64_t p = f[0][i], q = f[1][i];
                 f[0][i] = sub2(mul2(p, c), mul2(q, s));
-                f[1][i] = fma2(p, s, mul2(q, c));
+                f[1][i] = FUSED ? fma2(p, s, mul2(q, c)) : add2(mul2(p, s), mul2(q, c));
             }
+        }
+    }
+    // in 32 bits to a head's blocks of 16 in shared memory, from channel c0 and channel c1 on
+    __device__ __forceinline__ void spread(float* head, int c0, int c1, bool both) const {
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+            if (v == 1 && !both) break;
+            const int c = v ? c1 : c0;
+            float* to = head + (c >> 4) * kBlockFloats + (c & 15);
+            float x[VW > 1 ? VW : 2];
+#pragma unroll
+            for (int i = 0; i < kN; ++i) unpack2(f[v][i], x[2 * i], x[2 * i + 1]);
+            if constexpr (VW == 1)
+                *to = x[0];
+            else
+#pragma unroll
+                for (int i = 0; i < VW; i += 4) *reinterpret_cast<float4*>(to + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
         }
     }
     __device__ __forceinline__ void round(Vec<T, VW> (&x)[2]) const {
@@ -226,8 +250,12 @@ struct Wide {
 
 // NU: units per lane (more than one only for VW = 1).  NORM: whether queries or keys have a norm (its sums and weights in the
 // loop, although skipped, cost a pass without norm 4 to 17 percent: 8192 tokens of (32 + 2 x 8) x 128 37.6 -> 35.8 us)
-template <typename T, int VW, int NU, bool NORM>
+// Q4: keys and values go to a cache in 4 bits.  An item's keys and values pass through shared memory in 32 bits, whatever the
+// rotation's pairs are, and lanes then have a block of 16 channels each: its scale, its codes, an 8-byte store of codes.
+template <typename T, int VW, int NU, bool NORM, bool Q4>
 __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(const AppendArgs a, const AppendPlan P) {
+    constexpr int kBlocks = 64;  // of an item: 32 lanes x 16 channels x kAhead
+    __shared__ __align__(16) float s_x[Q4 ? kAppendWarps : 1][Q4 ? kBlocks * kBlockFloats : 4];
     const int lane = threadIdx.x & 31;
     const int D = a.c.head_dim, half = a.rot >> 1;
     const int l = lane & ((1 << P.lg) - 1), hp = 32 >> P.lg, group = lane >> P.lg;
@@ -267,6 +295,25 @@ __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(
         src_step[j] = step * s.tok;
         dst[j] = is_q[j] ? static_cast<T*>(a.out.p) + h * a.out.head
                          : static_cast<T*>(turned[j] ? a.c.k : a.c.v) + in_kind * a.c.head;
+    }
+    // the lane's blocks of an item's keys and values: where their codes and scales go but for the slot's offset
+    const int n_blk = Q4 ? D / 16 : 0;
+    uint8_t *codes[2] = {}, *scales[2] = {};
+    float inv[2] = {};
+    float* const mine = s_x[Q4 ? threadIdx.x >> 5 : 0];
+    const bool holds = Q4 && (part + 1) * kAhead * hp > a.n_heads;  // warp-uniform: keys or values among the item's heads
+    if constexpr (Q4) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int b = lane + 32 * i, hs = b / n_blk, h = part * kAhead * hp + hs;
+            if (hs >= kAhead * hp || h < a.n_heads || h >= H) continue;
+            const bool key = h < n_qk;
+            const int in_kind = h - (key ? a.n_heads : n_qk), blk = b - hs * n_blk;
+            codes[i] = static_cast<uint8_t*>(key ? a.c.k : a.c.v) + in_kind * a.c.head + 8 * blk;
+            scales[i] = (key ? a.q4.ks : a.q4.vs) + in_kind * a.q4.head + blk;
+            const float* unit = key ? a.q4.k_unit : a.q4.v_unit;
+            inv[i] = unit ? __frcp_rn(__ldg(unit + in_kind)) : 1.0f;
+        }
     }
     auto fetch_x = [&](Item<T, VW, NU>& y) {
 #pragma unroll
@@ -329,13 +376,17 @@ __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(
             fetch_rope(nxt, pos1);
         }
 
-        int64_t in_cache = 0;
+        int64_t in_cache = 0, in_scales = 0;
         bool kept = slot >= 0;
         if (kept) {
             const int64_t page = P.page_log2 >= 0 ? slot >> P.page_log2
                                  : (slot >> 32) != 0 ? slot / a.c.page_size : (int64_t)((uint32_t)slot / (uint32_t)a.c.page_size);
             kept = page < a.c.n_pages;
-            if (kept) in_cache = page * a.c.page + (int)(slot - page * a.c.page_size) * a.c.tok;
+            if (kept) {
+                const int in_page = (int)(slot - page * a.c.page_size);
+                in_cache = page * a.c.page + in_page * a.c.tok;
+                if constexpr (Q4) in_scales = page * a.q4.page + in_page * a.q4.tok;
+            }
         }
         if (((slot >= 0 && !kept) || (half > 0 && (pos < 0 || pos >= a.max_pos))) && part == 0 && lane == 0 && a.status)
             atomicOr(a.status, PPS_FLAG_INDEX);
@@ -353,7 +404,12 @@ __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(
             if ((part * kAhead + j) * hp >= n_qk) {  // values only: copied
 #pragma unroll
                 for (int k = 0; k < NU; ++k)
-                    if (goes && c0[k] < D) put(k);
+                    if (goes && c0[k] < D) {
+                        if constexpr (Q4)
+                            Wide<T, VW>(cur.x[j][k]).spread(mine + (j * hp + group) * n_blk * kBlockFloats, c0[k], c1[k], c1[k] < D);
+                        else
+                            put(k);
+                    }
                 continue;
             }
             const T* w = static_cast<const T*>(is_q[j] ? a.q_norm : a.k_norm);
@@ -378,14 +434,38 @@ __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(
                         load(wv[1], w + (c1[k] < D ? c1[k] : c0[k]));
                         f.scale(r, wv);
                     }
-                    if (c0[k] < a.rot) f.rotate(a.interleaved != 0, cur.cs[k], cur.sn[k]);
-                    f.round(cur.x[j][k]);
-                }
-                put(k);
+                    if (c0[k] < a.rot) f.template rotate<!Q4>(a.interleaved != 0, cur.cs[k], cur.sn[k]);
+                    if (!Q4 || is_q[j])
+                        f.round(cur.x[j][k]);
+                    else
+                        f.spread(mine + (j * hp + group) * n_blk * kBlockFloats, c0[k], c1[k], c1[k] < D);
+                } else if constexpr (Q4)
+                    Wide<T, VW>(cur.x[j][k]).spread(mine + (j * hp + group) * n_blk * kBlockFloats, c0[k], c1[k], c1[k] < D);
+                if (!Q4 || is_q[j]) put(k);
                 // A vector that is never read (only one of 8 channels can be) stays zero: a norm that is not finite, or a weight,
                 // would make it NaN, and with it the sums of all heads that these lanes take later.
                 if constexpr (NORM && VW == 8)
                     if (c1[k] >= D) cur.x[j][k][1].raw = typename RawVec<VW>::type{};
+            }
+        }
+        if constexpr (Q4) {
+            if (holds) {
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (kept && codes[i] != nullptr) {
+                        const float* x = mine + (lane + 32 * i) * kBlockFloats;
+                        float z[16];
+#pragma unroll
+                        for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(z + e) = *reinterpret_cast<const float4*>(x + e);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) z[e] *= inv[i];
+                        uint32_t scale;
+                        const uint2 c = q4::quantise(z, scale);
+                        *reinterpret_cast<uint2*>(codes[i] + in_cache) = c;
+                        scales[i][in_scales] = (uint8_t)scale;
+                    }
+                __syncwarp();
             }
         }
         tok += step;
@@ -417,10 +497,10 @@ cudaError_t launch(const AppendArgs& a, cudaStream_t st) {
     if (items > INT32_MAX) return cudaErrorInvalidValue;
     P.tok_step = (int)std::max<int64_t>(std::min(items, most) / P.parts, 1);
     const int64_t blocks = ((int64_t)P.tok_step * P.parts + kAppendWarps - 1) / kAppendWarps;
-    if (a.q_norm != nullptr || a.k_norm != nullptr)
-        append_kernel<T, VW, NU, true><<<(unsigned)blocks, 32 * kAppendWarps, 0, st>>>(a, P);
-    else
-        append_kernel<T, VW, NU, false><<<(unsigned)blocks, 32 * kAppendWarps, 0, st>>>(a, P);
+    const bool norm = a.q_norm != nullptr || a.k_norm != nullptr, bits4 = a.q4.ks != nullptr;
+    auto kernel = bits4 ? (norm ? append_kernel<T, VW, NU, true, true> : append_kernel<T, VW, NU, false, true>)
+                        : (norm ? append_kernel<T, VW, NU, true, false> : append_kernel<T, VW, NU, false, false>);
+    kernel<<<(unsigned)blocks, 32 * kAppendWarps, 0, st>>>(a, P);
     return cudaGetLastError();
 }
 
@@ -430,8 +510,10 @@ cudaError_t by_width(const AppendArgs& a, cudaStream_t st) {
     uint64_t bits = 0;  // byte addresses and element strides, doubled to bytes
     for (const HeadsView* h : {&a.q, &a.k, &a.v, &a.out})
         bits |= reinterpret_cast<uintptr_t>(h->p) | (uint64_t)h->tok * 2 | (uint64_t)h->head * 2;
-    bits |= reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v);
-    bits |= (uint64_t)(a.c.page | a.c.tok | a.c.head) * 2;
+    if (a.q4.ks == nullptr) {
+        bits |= reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v);
+        bits |= (uint64_t)(a.c.page | a.c.tok | a.c.head) * 2;
+    }
     bits |= reinterpret_cast<uintptr_t>(a.q_norm) | reinterpret_cast<uintptr_t>(a.k_norm);
     const bool table = a.rot == 0 || (reinterpret_cast<uintptr_t>(a.rope) & 15) == 0;
     if (table && bits % 16 == 0 && a.rot % 16 == 0) return launch<T, 8, 1>(a, st);
@@ -439,7 +521,65 @@ cudaError_t by_width(const AppendArgs& a, cudaStream_t st) {
     return launch<T, 1, 4>(a, st);
 }
 
+// Values of cache slots: a thread has a block of 16 channels of a head, of keys and of values, in every step-th slot.
+template <typename T>
+__global__ void __launch_bounds__(256) read_kernel(const ReadArgs a, int per_slot, int step) {
+    const int n_blk = a.c.head_dim / 16;
+    const int in_cta = 256 / per_slot, sl = threadIdx.x / per_slot, task = threadIdx.x - sl * per_slot;
+    // per_slot: blocks of a slot that a CTA takes at a time; blockIdx.y: which of them
+    const int b = blockIdx.y * per_slot + task, head = b / n_blk, blk = b - head * n_blk;
+    if (sl >= in_cta || head >= a.c.n_kv_heads) return;
+    const float ku = a.q4.k_unit ? __ldg(a.q4.k_unit + head) : 1.0f, vu = a.q4.v_unit ? __ldg(a.q4.v_unit + head) : 1.0f;
+    for (int64_t i = (int64_t)blockIdx.x * in_cta + sl; i < a.n; i += step) {
+        const int64_t slot = __ldg(a.slot + i), page = slot < 0 ? -1 : slot / a.c.page_size;
+        const bool there = page >= 0 && page < a.c.n_pages;
+        if (page >= a.c.n_pages && b == 0 && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
+        const int in_page = there ? (int)(slot - page * a.c.page_size) : 0;
+        const int64_t at = page * a.c.page + in_page * a.c.tok + head * a.c.head + 8 * blk;
+        const int64_t st = page * a.q4.page + in_page * a.q4.tok + head * a.q4.head + blk;
+        uint2 c[2] = {};
+        uint32_t s[2] = {};
+        if (there) {
+            c[0] = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.c.k) + at);
+            c[1] = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.c.v) + at);
+            s[0] = a.q4.ks[st];
+            s[1] = a.q4.vs[st];
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float su = q4::scale_float(s[h]) * (h ? vu : ku);
+            const uint64_t su2 = pack2(su, su);
+            uint32_t w[8], o[8];
+            uint32_t(&w0)[4] = *reinterpret_cast<uint32_t(*)[4]>(w);
+            uint32_t(&w1)[4] = *reinterpret_cast<uint32_t(*)[4]>(w + 4);
+            q4::widen8(c[h].x, w0);
+            q4::widen8(c[h].y, w1);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = narrow<T>(mul2(widen<__half>(w[e]), su2));
+            const HeadsView& out = h ? a.v : a.k;
+            uint4* to = reinterpret_cast<uint4*>(static_cast<T*>(out.p) + i * out.tok + head * out.head + 16 * blk);
+            to[0] = make_uint4(o[0], o[1], o[2], o[3]);
+            to[1] = make_uint4(o[4], o[5], o[6], o[7]);
+        }
+    }
+}
+
 }  // namespace
+
+cudaError_t launch_kv_read(const ReadArgs& a, int dtype, cudaStream_t stream) {
+    const int64_t blocks = (int64_t)a.c.n_kv_heads * (a.c.head_dim / 16);
+    const int per_slot = (int)std::min<int64_t>(blocks, 256), in_cta = 256 / per_slot;
+    const int64_t rounds = (blocks + per_slot - 1) / per_slot;
+    if (rounds > 65535) return cudaErrorInvalidValue;
+    const int64_t ctas = std::min<int64_t>((a.n + in_cta - 1) / in_cta, std::max<int64_t>((int64_t)device_sm_count() * 8 / rounds, 1));
+    const dim3 grid((unsigned)ctas, (unsigned)rounds);
+    const int step = (int)(ctas * in_cta);
+    if (dtype == PPS_BF16)
+        read_kernel<__nv_bfloat16><<<grid, 256, 0, stream>>>(a, per_slot, step);
+    else
+        read_kernel<__half><<<grid, 256, 0, stream>>>(a, per_slot, step);
+    return cudaGetLastError();
+}
 
 cudaError_t launch_kv_append(const AppendArgs& a, int dtype, cudaStream_t stream) {
     return dtype == PPS_BF16 ? by_width<__nv_bfloat16>(a, stream) : by_width<__half>(a, stream);

@@ -1,0 +1,457 @@
+// pps_attention_q4.cu -- attention of the newest tokens of each sequence over a paged cache held in 4 bits (pps_q4.cuh), sm_103a.
+//
+//   out[i] = v_unit sum_j w_j v_j / sum_j w_j,   w_j = exp(scale k_unit q_i . k_j)   over the keys j that row i sees
+//
+// Rows.  The tokens of a sequence and the heads that share a key head are packed into rows, token after token; a row block has
+// R = 8 NT of them.
+//
+// Few rows.  A key's 128 channels are 72 bytes, and what a decoding step has to do per byte of them is to widen it: both
+// products run on registers, without a way through shared memory.  A warp takes 32 keys at a time, keys of a quad side by side:
+//   S^T = K Q^T  (m16n8k16, m: keys, n: rows).  Lane (g, t) of the warp loads a quarter of key g's codes, t-th from the left, and
+//                takes them as the operand's elements whatever channels these are: the queries are read in the same order;
+//   O^T += V^T P^T (m: channels, n: rows, k: keys).  Lane (g, t) loads the g-th eighth of the codes of keys 2t, 2t + 1; nibbles of
+//                two keys are put together into bytes, which become pairs of halves along the keys; a transposing move turns S^T into
+//                the operand P^T.
+// Codes times scales are exact halves.  Queries in bf16 are brought to halves by a power of two per row, exactly but for
+// channels below 2^-31 of the row's largest.  Weights are rounded to halves (2^-11 of each); sums are formed before rounding,
+// in 32 bits, and the softmax is the running one with the rescaling left out while a maximum rises by less than 2^kLazy.
+//
+// Work split.  The line of pps_attn.cuh; a CTA's warps take the 32-key units of a segment in turn and join at its end.
+#include <atomic>
+#include <cstring>
+
+#include "pps_attn.cuh"
+#include "pps_q4.cuh"
+
+namespace pps {
+namespace {
+
+constexpr int kWarps4 = 8, kThreads4 = 32 * kWarps4;
+constexpr int kUnit = 32;         // keys that a warp takes at a time
+constexpr int kPerSm4 = 2;        // CTAs
+constexpr int kMaxCtas4 = 320;
+constexpr int kFix4 = 2;          // key tiles that an item's start and end cost
+constexpr int kLeast4 = 1;
+constexpr float kLazy4 = 8.0f;    // log2 of the rise of a maximum that nothing is rescaled for
+constexpr float kShift4 = 6.0f;   // log2 of a factor on all weights: 2^(8 + 6) is below fp16's largest number
+constexpr int kQBits = 14;        // a bf16 row's largest channel lies in [2^14, 2^15) as a half
+
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+// what a lane holds of 32 keys: eighth e has keys 8e .. 8e + 7
+template <int DC>
+struct Held {
+    static constexpr int kW = DC / 32;  // words of a quarter of a key's codes (4 or 2)
+    static constexpr int kVW = DC / 64; // words of an eighth (2 or 1)
+    uint32_t k[4][kW], v[8][kVW];       // key 8e + g; keys 8e + 2t, 8e + 2t + 1
+    uint32_t ks[4], vs[8];              // scale bytes
+};
+
+template <typename T, int DC, int NT>
+__global__ void __launch_bounds__(kThreads4, kPerSm4) few_rows_kernel(const AttnArgs a, const Q4View z, const AttnPlan P) {
+    using H = Held<DC>;
+    constexpr int R = 8 * NT, RS = DC + 4;  // a row's floats in shared memory: 4 modulo 16, so that lanes (g, t) touch all banks
+    __shared__ int64_t s_sum[kWarps4];
+    __shared__ Start s_start;
+    __shared__ float2 s_ml[kWarps4][R];
+    __shared__ float2 s_tot[R];
+    extern __shared__ __align__(16) float s_o[];  // [kWarps4][R][RS]
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x, g = lane >> 2, t = lane & 3;
+    pdl_wait();
+    pdl_launch_dependents();
+    int64_t c0, c1;
+    const int64_t share = find_share<kThreads4>(a, P, s_sum, &s_start, c0, c1);
+    __syncthreads();
+    if (c0 >= c1) return;
+    const int least = (int)min(max(share / 8, (int64_t)1), (int64_t)kLeast4);
+    Walk W(P, s_start, c0, c1, least);
+    const int D = a.c.head_dim;
+    const bool k_there = t * (DC / 4) < D, v_there = g * (DC / 8) < D;
+    const bool k_whole = (t + 1) * (DC / 4) <= D;  // (else, of 128: half of the quarter)
+
+    while (W.next(a, P)) {
+        const int kvh = W.heads / P.nsub, sub = W.heads - kvh * P.nsub;
+        const int gs = min(P.gs, P.group - sub * P.gs);
+        const int head0 = kvh * P.group + sub * P.gs;
+        const int len = W.q.len, prefix = len - W.q.n;
+        const float ku = z.k_unit ? __ldg(z.k_unit + kvh) : 1.0f, vu = z.v_unit ? __ldg(z.v_unit + kvh) : 1.0f;
+        // ---- queries: row 8 nt + g, the channels of quarter t, as halves
+        uint32_t qf[NT][DC / 8];
+        float row_sc[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = 8 * nt + g, tok = row / P.gs, h = row - tok * P.gs;
+            const bool valid = tok < W.ntok && h < gs;
+            const T* src = static_cast<const T*>(a.q.p) + (int64_t)(W.q.off + W.i0 + tok) * a.q.tok + (head0 + h) * a.q.head + t * (DC / 4);
+            uint4 raw[DC / 32];
+#pragma unroll
+            for (int i = 0; i < DC / 32; ++i) {
+                raw[i] = make_uint4(0, 0, 0, 0);
+                if (valid && t * (DC / 4) + 8 * i < D) raw[i] = __ldg(reinterpret_cast<const uint4*>(src) + i);
+            }
+            const uint32_t* x = reinterpret_cast<const uint32_t*>(raw);
+            row_sc[nt] = P.sc * ku;
+            if constexpr (sizeof(T) == 2 && Half<T>::kType == 0) {
+#pragma unroll
+                for (int i = 0; i < DC / 8; ++i) qf[nt][i] = x[i];
+            } else {
+                uint32_t top = 0;  // the largest finite magnitude
+#pragma unroll
+                for (int i = 0; i < DC / 8; ++i) {
+                    const uint32_t lo = x[i] & 0x7fffu, hi = x[i] >> 16 & 0x7fffu;
+                    top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+                }
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                const int e = (int)(top >> 7);  // exponent field
+                const int k = top == 0 ? 0 : min(kQBits + 127 - e, 126);
+                const float f = __uint_as_float((uint32_t)(127 + k) << 23);
+                row_sc[nt] = min(row_sc[nt] * __uint_as_float((uint32_t)(127 - k) << 23), FLT_MAX);
+#pragma unroll
+                for (int i = 0; i < DC / 8; ++i)
+                    qf[nt][i] = Half<__half>::pack(__uint_as_float(x[i] << 16) * f, __uint_as_float(x[i] & 0xffff0000u) * f);
+            }
+        }
+        // of the lane's rows 8 nt + 2t, + 1 (an odd index: the second)
+        float sc[2 * NT], m[2 * NT], l[2 * NT];
+        int vis[2 * NT];
+        const uint32_t* mask[2 * NT];
+#pragma unroll
+        for (int r = 0; r < 2 * NT; ++r) {
+            sc[r] = __shfl_sync(0xffffffffu, row_sc[r >> 1], 4 * (2 * t + (r & 1)));
+            const int row = 8 * (r >> 1) + 2 * t + (r & 1), tok = W.i0 + min(row / P.gs, W.ntok - 1);
+            mask[r] = a.mask ? a.mask + (int64_t)(W.q.off + tok) * a.mask_words : nullptr;
+            vis[r] = a.mask ? len : prefix + tok + 1;
+            m[r] = -INFINITY;
+            l[r] = 0.0f;
+        }
+        const int plain = a.mask ? prefix : prefix + W.i0 + 1;  // keys below it are seen by every row
+        const int end = a.mask ? len : prefix + W.i0 + W.ntok;  // keys from it on by none
+        float o[NT][DC / 16][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < DC / 16; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.0f;
+
+        const int32_t* table = a.pages + (int64_t)W.s * a.pages_stride;
+        const int first = W.t0 * kTileKeys, last = min(W.t1 * kTileKeys, end);
+        auto page_of = [&](int k0) {  // lanes 0 to 3: of the eighths of the unit from key k0 on
+            const int k = k0 + 8 * (lane & 3);
+            int p = -1;
+            if (k < last && k < len) {
+                p = __ldg(table + (k >> P.page_log2));
+                if (p < 0 || p >= a.c.n_pages) {  // reads as zeros
+                    if (a.status && lane < 4) atomicOr(a.status, PPS_FLAG_INDEX);
+                    p = -1;
+                }
+            }
+            return p;
+        };
+        auto fetch = [&](H& x, int k0, int pages) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int p = __shfl_sync(0xffffffffu, pages, e), in_page = (k0 + 8 * e) & (a.c.page_size - 1);
+                const int64_t at = p * a.c.page + in_page * a.c.tok + kvh * a.c.head;
+                const int64_t st = p * z.page + in_page * z.tok + kvh * z.head;
+                const int left = p >= 0 ? last - k0 - 8 * e : 0;  // keys of the eighth that are there
+#pragma unroll
+                for (int i = 0; i < H::kW; ++i) x.k[e][i] = 0;
+                x.ks[e] = 0;
+                if (g < left && k_there) {
+                    const uint8_t* src = static_cast<const uint8_t*>(a.c.k) + at + g * a.c.tok + t * (DC / 8);
+#pragma unroll
+                    for (int i = 0; i < H::kW; i += 2)
+                        if (i == 0 || k_whole) {
+                            const uint2 w = __ldg(reinterpret_cast<const uint2*>(src) + i / 2);
+                            x.k[e][i] = w.x;
+                            x.k[e][i + 1] = w.y;
+                        }
+                    const uint8_t* sp = z.ks + st + g * z.tok + t * (DC / 64);
+                    if (DC == 128 && k_whole)
+                        x.ks[e] = __ldg(reinterpret_cast<const uint16_t*>(sp));
+                    else
+                        x.ks[e] = __ldg(sp);
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                    for (int i = 0; i < H::kVW; ++i) x.v[2 * e + j][i] = 0;
+                    x.vs[2 * e + j] = 0;
+                    if (2 * t + j < left && v_there) {
+                        const uint8_t* src = static_cast<const uint8_t*>(a.c.v) + at + (2 * t + j) * a.c.tok + g * (DC / 16);
+                        if constexpr (DC == 128) {
+                            const uint2 w = __ldg(reinterpret_cast<const uint2*>(src));
+                            x.v[2 * e + j][0] = w.x;
+                            x.v[2 * e + j][H::kVW - 1] = w.y;
+                        } else
+                            x.v[2 * e + j][0] = __ldg(reinterpret_cast<const uint32_t*>(src));
+                        x.vs[2 * e + j] = __ldg(z.vs + st + (2 * t + j) * z.tok + (DC == 128 ? g : g >> 1));
+                    }
+                }
+            }
+        };
+        auto work = [&](const H& x, int k0) {
+            float s[NT][2][4];
+#pragma unroll
+            for (int G = 0; G < 2; ++G) {
+                uint32_t h[2][DC / 8];  // the quarter of keys 16 G + g and 16 G + 8 + g
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int e = 2 * G + j;
+                    const uint32_t s2 = q4::scales2(x.ks[e]);
+                    const uint32_t lo = __byte_perm(s2, 0, 0x1010), hi = __byte_perm(s2, 0, 0x3232);
+#pragma unroll
+                    for (int i = 0; i < H::kW; ++i) {
+                        uint32_t w[4];
+                        q4::widen8(x.k[e][i], w);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) h[j][4 * i + c] = q4::mul_halves(w[c], i < 2 ? lo : hi);
+                    }
+                }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    s[nt][G][0] = s[nt][G][1] = s[nt][G][2] = s[nt][G][3] = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < DC / 16; ++i) {
+                        const uint32_t A[4] = {h[0][2 * i], h[1][2 * i], h[0][2 * i + 1], h[1][2 * i + 1]};
+                        mma16816(s[nt][G], A, qf[nt][2 * i], qf[nt][2 * i + 1]);
+                    }
+                }
+            }
+            // scores of the lane: keys 16 G + 8 (e >> 1) + g, rows 8 nt + 2t + (e & 1)
+            const bool odd_scale = P.s_xor != 0 || P.s_and == 0;
+            if (k0 + kUnit > plain || odd_scale) {
+#pragma unroll
+                for (int r = 0; r < 2 * NT; ++r) {
+                    const uint32_t bits = seen_bits(k0, vis[r], prefix, mask[r], a.mask_words) >> g;
+#pragma unroll
+                    for (int G = 0; G < 2; ++G)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            float& y = s[r >> 1][G][2 * j + (r & 1)];
+                            y = bits >> (16 * G + 8 * j) & 1u ? __uint_as_float((__float_as_uint(y) & P.s_and) ^ P.s_xor) : -INFINITY;
+                        }
+                }
+            }
+            float top[2 * NT];
+            bool rises = false;
+#pragma unroll
+            for (int r = 0; r < 2 * NT; ++r) {
+                const float(&y)[2][4] = s[r >> 1];
+                top[r] = fmaxf(fmaxf(y[0][r & 1], y[0][2 + (r & 1)]), fmaxf(y[1][r & 1], y[1][2 + (r & 1)]));
+                rises |= (top[r] - m[r]) * sc[r] > kLazy4;
+            }
+            if (__any_sync(0xffffffffu, rises)) {
+#pragma unroll
+                for (int r = 0; r < 2 * NT; ++r) {
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], d));
+                    const float M = fmaxf(m[r], top[r]), f = m[r] == M ? 1.0f : ex2((m[r] - M) * sc[r]);
+                    m[r] = M;
+                    l[r] *= f;
+#pragma unroll
+                    for (int i = 0; i < DC / 16; ++i) {
+                        o[r >> 1][i][r & 1] *= f;
+                        o[r >> 1][i][2 + (r & 1)] *= f;
+                    }
+                }
+            }
+            uint32_t p[NT][4];  // the operand P^T: rows 8 nt + g, keys 8 e + 2t, + 1
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float neg[2];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) neg[r] = (m[2 * nt + r] == -INFINITY ? 0.0f : -m[2 * nt + r] * sc[2 * nt + r]) + kShift4;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x0 = ex2(fmaf(s[nt][e >> 1][2 * (e & 1)], sc[2 * nt], neg[0]));
+                    const float x1 = ex2(fmaf(s[nt][e >> 1][2 * (e & 1) + 1], sc[2 * nt + 1], neg[1]));
+                    l[2 * nt] += x0;
+                    l[2 * nt + 1] += x1;
+                    p[nt][e] = transpose8x8(Half<__half>::pack(x0, x1));
+                }
+            }
+#pragma unroll
+            for (int G = 0; G < 2; ++G) {
+                uint32_t s2[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) s2[j] = q4::scales2(x.vs[4 * G + 2 * j] | x.vs[4 * G + 2 * j + 1] << 8);
+#pragma unroll
+                for (int w = 0; w < H::kVW; ++w) {
+                    uint32_t lo[2][4], hi[2][4];  // the word's even and odd channels of two keys
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint32_t x0 = x.v[4 * G + 2 * j][w], x1 = x.v[4 * G + 2 * j + 1][w];
+                        q4::widen8((x0 & 0x0f0f0f0fu) | (x1 << 4 & 0xf0f0f0f0u), lo[j]);
+                        q4::widen8((x0 >> 4 & 0x0f0f0f0fu) | (x1 & 0xf0f0f0f0u), hi[j]);
+                    }
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t A[4] = {q4::mul_halves(lo[0][c], s2[0]), q4::mul_halves(hi[0][c], s2[0]),
+                                               q4::mul_halves(lo[1][c], s2[1]), q4::mul_halves(hi[1][c], s2[1])};
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w + c], A, p[nt][2 * G], p[nt][2 * G + 1]);
+                    }
+                }
+            }
+        };
+        H even, odd;
+        constexpr int kStep = kUnit * kWarps4;
+        int k0 = first + warp * kUnit;
+        if (k0 < last) {
+            fetch(even, k0, page_of(k0));
+            int pages = page_of(k0 + kStep);
+            auto turn = [&](H& cur, H& nxt) {
+                const int k = k0;
+                k0 += kStep;
+                if (k0 < last) {
+                    fetch(nxt, k0, pages);
+                    pages = page_of(k0 + kStep);
+                }
+                work(cur, k);
+                return k0 < last;
+            };
+            while (turn(even, odd) && turn(odd, even)) {
+            }
+        }
+
+        // ---- the segment's result: the warps' parts, joined
+        const bool whole = W.t0 == 0 && W.t1 == W.T;
+        const int slot = 2 * cta + (W.t0 == 0 ? 1 : 0);
+        if (tid == 0 && W.t0 == 0 && !whole) {
+            Cut c;
+            c.nsplit = (int)divide(W.from + W.T - least, share) - cta + 1;  // the cuts that leave `least` tiles on both sides
+            c.ntok = W.ntok;
+            c.tok0 = W.q.off + W.i0;
+            c.vh = W.heads;
+            P.cuts[cta] = c;
+        }
+#pragma unroll
+        for (int r = 0; r < 2 * NT; ++r) {
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+            m[r] = m[r] == -INFINITY ? -INFINITY : m[r] * sc[r];  // log2 of the largest weight
+            if (l[r] != l[r]) m[r] = INFINITY;  // a score that is not a number, or infinite: so is the row, whatever it is joined with
+            if (g == 0) s_ml[warp][8 * (r >> 1) + 2 * t + (r & 1)] = make_float2(m[r], l[r]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 2 * NT; ++r) {
+            const int row = 8 * (r >> 1) + 2 * t + (r & 1);
+            float M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kWarps4; ++w) M = fmaxf(M, s_ml[w][row].x);
+            const float f = m[r] == -INFINITY ? 0.0f : ex2(m[r] - M);
+            float* to = s_o + ((size_t)warp * R + row) * RS + 2 * g;
+#pragma unroll
+            for (int i = 0; i < DC / 16; ++i) {  // channels g DC / 8 + 2i, + 1 (a part without weight may hold anything)
+                const float x = o[r >> 1][i][r & 1], y = o[r >> 1][i][2 + (r & 1)];
+                *reinterpret_cast<float2*>(to + 16 * i) = f != 0.0f ? make_float2(x * f, y * f) : make_float2(0.0f, 0.0f);
+            }
+        }
+        if (tid < R) {
+            float M = -INFINITY, L = 0.0f;
+            for (int w = 0; w < kWarps4; ++w) M = fmaxf(M, s_ml[w][tid].x);
+            for (int w = 0; w < kWarps4; ++w)
+                if (s_ml[w][tid].x != -INFINITY) L = fmaf(s_ml[w][tid].y, ex2(s_ml[w][tid].x - M), L);
+            s_tot[tid] = make_float2(M, L);
+        }
+        __syncthreads();
+        for (int i = tid; i < R * (DC / 2); i += kThreads4) {
+            const int row = i / (DC / 2), at = i - row * (DC / 2);  // pair `at` of the row: pair at / 8 of the eighth at % 8
+            const int tok = row / P.gs, h = row - tok * P.gs, c = (at & 7) * (DC / 8) + 2 * (at >> 3);
+            if (tok >= W.ntok || h >= gs || c >= D) continue;
+            float2 x = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int w = 0; w < kWarps4; ++w) {
+                const float2 y = *reinterpret_cast<const float2*>(s_o + ((size_t)w * R + row) * RS + 2 * at);
+                x.x += y.x;
+                x.y += y.y;
+            }
+            const float2 ml = s_tot[row];
+            const int token = W.q.off + W.i0 + tok, head = head0 + h;
+            if (whole) {
+                const float inv = (ml.y > 0.0f ? 1.0f / ml.y : ml.y) * vu;  // (the sum: zero, or not a number)
+                *reinterpret_cast<uint32_t*>(static_cast<T*>(a.out.p) + (int64_t)token * a.out.tok + head * a.out.head + c) =
+                    Half<T>::pack(x.x * inv, x.y * inv);
+                if (at == 0 && a.lse)
+                    a.lse[(int64_t)token * a.n_heads + head] = ml.y == 0.0f ? -INFINITY : (ml.x + log2f(ml.y) - kShift4) * 0.69314718055994531f;
+            } else {
+                const int64_t to = (int64_t)slot * P.cap_rows + row;
+                *reinterpret_cast<float2*>(P.part_o + to * DC + c) = make_float2(x.x * vu, x.y * vu);
+                if (at == 0) P.part_ml[to] = ml;
+            }
+        }
+        __syncthreads();  // s_ml, s_o and s_tot are free
+    }
+}
+
+// the rows of a block, the heads taken at a time, the tokens of a block: by the mean number of tokens of a sequence
+struct Rows4 {
+    int nt, nsub, gs, tt;
+    Rows4(int64_t n_tok, int64_t n_seq, int group) {
+        const int64_t mean = n_seq > 0 ? (n_tok + n_seq - 1) / n_seq : n_tok;
+        nt = mean * group <= 8 ? 1 : 2;
+        nsub = (group + 8 * nt - 1) / (8 * nt);
+        gs = (group + nsub - 1) / nsub;
+        tt = 8 * nt / gs;
+    }
+};
+
+template <typename T, int DC, int NT>
+cudaError_t launch_few(const AttnArgs& a, const Q4View& z, const Rows4& rows, cudaStream_t st) {
+    AttnPlan P;
+    std::memset(&P, 0, sizeof(P));
+    P.group = a.n_heads / a.c.n_kv_heads;
+    P.nsub = rows.nsub;
+    P.gs = rows.gs;
+    P.tt = P.bt = rows.tt;
+    P.fix = kFix4;
+    P.cap_rows = 8 * NT;
+    P.shift = kShift4;
+    plan_common(P, a);
+    carve(P, a.ws, kMaxCtas4);
+    constexpr int kSmem = kWarps4 * 8 * NT * (DC + 4) * 4;
+    static std::atomic<uint64_t> ready{0};
+    cudaError_t e = allow_smem(ready, (const void*)few_rows_kernel<T, DC, NT>, kSmem);
+    if (e != cudaSuccess) return e;
+    const int ctas = std::min(device_sm_count() * kPerSm4, kMaxCtas4);
+    e = launch_pdl(few_rows_kernel<T, DC, NT>, dim3(ctas), dim3(kThreads4), kSmem, st, a, z, P);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(join_kernel<T, DC>, dim3(ctas, join_blocks(a, P)), dim3(256), 0, st, a, P);
+}
+
+template <typename T, int DC>
+cudaError_t by_rows(const AttnArgs& a, const Q4View& z, cudaStream_t st) {
+    const Rows4 rows(a.n_tok, a.n_seq, a.n_heads / a.c.n_kv_heads);
+    return rows.nt == 1 ? launch_few<T, DC, 1>(a, z, rows, st) : launch_few<T, DC, 2>(a, z, rows, st);
+}
+
+template <typename T>
+cudaError_t by_channels4(const AttnArgs& a, const Q4View& z, cudaStream_t st) {
+    return channel_class(a.c.head_dim) == 64 ? by_rows<T, 64>(a, z, st) : by_rows<T, 128>(a, z, st);
+}
+
+}  // namespace
+
+size_t attention_q4_workspace_bytes(int64_t n_tok, int n_heads, int n_kv_heads, int head_dim) {
+    (void)n_tok, (void)n_heads, (void)n_kv_heads;
+    return part_bytes(kMaxCtas4, 16, head_dim);
+}
+
+cudaError_t launch_attention_q4(const AttnArgs& a, const Q4View& z, int dtype, cudaStream_t stream) {
+    return dtype == PPS_BF16 ? by_channels4<__nv_bfloat16>(a, z, stream) : by_channels4<__half>(a, z, stream);
+}
+
+}  // namespace pps

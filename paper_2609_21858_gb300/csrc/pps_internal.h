@@ -192,9 +192,18 @@ struct CacheView {
     int page_size, n_kv_heads, head_dim;
     int64_t page, tok, head;  // strides, elements
 };
+// what a cache in 4 bits has beside a CacheView of its codes (strides in bytes there): scales, one a block of 16 channels, and units
+struct Q4View {
+    uint8_t* ks;
+    uint8_t* vs;
+    int64_t page, tok, head;  // strides of the scales, bytes
+    const float* k_unit;      // [n_kv_heads], null: ones
+    const float* v_unit;
+};
 struct AppendArgs {
     HeadsView q, k, v, out;
     CacheView c;
+    Q4View q4;  // ks null: a cache of dtype
     int64_t n_tok, max_pos;
     int n_heads, rot, interleaved;
     const void* q_norm;
@@ -206,6 +215,17 @@ struct AppendArgs {
     uint32_t* status;
 };
 cudaError_t launch_kv_append(const AppendArgs& a, int dtype, cudaStream_t stream);
+
+// values of cache slots, back in 16 bits (pps_append.cu)
+struct ReadArgs {
+    HeadsView k, v;
+    CacheView c;
+    Q4View q4;
+    int64_t n;
+    const int64_t* slot;
+    uint32_t* status;
+};
+cudaError_t launch_kv_read(const ReadArgs& a, int dtype, cudaStream_t stream);
 
 struct AttnArgs {
     HeadsView q, out;
@@ -223,6 +243,55 @@ struct AttnArgs {
 };
 size_t attention_workspace_bytes(int64_t n_tok, int n_heads, int n_kv_heads, int head_dim);
 cudaError_t launch_attention(const AttnArgs& a, int dtype, cudaStream_t stream);
+// over a cache in 4 bits (pps_attention_q4.cu); a.c has the codes, strides in bytes
+size_t attention_q4_workspace_bytes(int64_t n_tok, int n_heads, int n_kv_heads, int head_dim);
+cudaError_t launch_attention_q4(const AttnArgs& a, const Q4View& z, int dtype, cudaStream_t stream);
+
+// page tables and slot maps (pps_pages.cu)
+constexpr int kMaxPageSeqs = 8192;  // sequences of a call: their offsets lie in shared memory
+struct ReserveArgs {
+    int32_t* pages;
+    int64_t pages_stride;
+    int columns, n_seq, page_size, free_cap;
+    int32_t* held;
+    int32_t* free_list;
+    int32_t* free_count;
+    const int32_t* kv_len;
+    const int32_t* n_new;    // reserve; null: trim, to kv_len tokens
+    const int32_t* pos_off;
+    int64_t n_tok;
+    int32_t* out_q_off;
+    int32_t* out_len;
+    int64_t* out_slot;
+    int32_t* out_pos;
+    int32_t* out_seq;
+    uint32_t* status;
+};
+cudaError_t launch_kv_reserve(const ReserveArgs& a, cudaStream_t stream);
+cudaError_t launch_kv_trim(const ReserveArgs& a, cudaStream_t stream);
+
+// penalties, biases and masks on logits (pps_adjust.cu)
+struct AdjustArgs {
+    const void* x;
+    void* out;
+    int64_t n_rows, V, x_stride, out_stride, text_stride, allowed_stride;
+    int n_seq, text_cap, mask_words, n_bias;
+    const int32_t* seq_off;
+    const int32_t* text;
+    const int32_t* text_len;
+    const int32_t* prompt_len;
+    const int32_t* node_tok;
+    const uint32_t* node_mask;
+    const float* rep;
+    const float* freq;
+    const float* pres;
+    const int32_t* bias_off;
+    const int32_t* bias_tok;
+    const float* bias_val;
+    const uint32_t* allowed;
+    uint32_t* status;
+};
+cudaError_t launch_adjust(const AdjustArgs& a, int dtype, cudaStream_t stream);
 
 struct ChainArgs {
     const void* p;

@@ -11,6 +11,7 @@ import importlib.util
 import os
 import struct
 import threading
+import typing
 
 import torch
 
@@ -32,7 +33,7 @@ OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_SIZE = 0, 1, 
 NOALLOC_MAX_ROWS = 4096  # PPS_NOALLOC_MAX_ROWS of include/pps.h (tests/test_abi.py checks the two agree)
 F32, BF16, F16 = 0, 1, 2
 DISTINCT, IID = 0, 1
-FLAG_GUARD, FLAG_LOGIT_RANGE, FLAG_TREE, FLAG_TIMEOUT, FLAG_INDEX = 1, 2, 4, 8, 16
+FLAG_GUARD, FLAG_LOGIT_RANGE, FLAG_TREE, FLAG_TIMEOUT, FLAG_INDEX, FLAG_POOL = 1, 2, 4, 8, 16, 32
 MAX_K = 32
 MAX_TOP_K = 64
 MAX_BLOCKS = 32
@@ -133,8 +134,11 @@ def lib():
             L.pps_lmhead_verify_tree.argtypes = [vp, i64, vp, i64, i64, i64, i64, RowIds, f32, i32, i32, vp, vp, i64,
                                                  vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
             L.pps_lmhead_verify_tree.restype = ctypes.c_int
-            for fn in (L.pps_kv_append, L.pps_paged_attention, L.pps_verify_chain):
+            for fn in (L.pps_kv_append, L.pps_paged_attention, L.pps_verify_chain, L.pps_kv_append_q4, L.pps_kv_read_q4,
+                       L.pps_paged_attention_q4, L.pps_kv_reserve, L.pps_kv_trim, L.pps_adjust_logits):
                 fn.argtypes, fn.restype = [ctypes.c_char_p, vp], ctypes.c_int
+            L.pps_attention_q4_workspace_size.argtypes = [i64, i32, i32, i32]
+            L.pps_attention_q4_workspace_size.restype = sz
             L.pps_attention_workspace_size.argtypes = [i64, i32, i32, i32]
             L.pps_attention_workspace_size.restype = sz
             L.pps_chain_workspace_size.argtypes = [i64, i64, i32]
@@ -948,4 +952,291 @@ def verify_chain(p_logits, q_logits, gamma: int, seq_off, node_draft_row, draft_
                             n_draft, V, p_stride if n > 1 else V, q_stride if n_draft > 1 else V,
                             noise_stride if n_seq > 1 else V, code, n_seq, gamma, temperature)
     _check("pps_verify_chain", L.pps_verify_chain(args, handle))
+    return out
+
+
+# ---------------------------------------------------------------- a cache in 4 bits
+
+_CACHE_Q4_FIELDS = "PPPPPPqiiiqqqqqq"
+_APPEND_Q4_ARGS = struct.Struct("@N" + "Pqq" * 4 + _CACHE_Q4_FIELDS + "PPPPPP" + "qq" + "iiiif" + "0q")
+_READ_Q4_ARGS = struct.Struct("@N" + "Pqq" * 2 + _CACHE_Q4_FIELDS + "PP" + "q" + "i" + "0q")
+_ATTENTION_Q4_ARGS = struct.Struct("@N" + "Pqq" * 2 + _CACHE_Q4_FIELDS + "PPPPPPPN" + "qq" + "iiiiif" + "0q")
+_RESERVE_ARGS = struct.Struct("@N" + "P" * 13 + "qq" + "iiii" + "0q")
+_TRIM_ARGS = struct.Struct("@N" + "P" * 6 + "q" + "iiii" + "0q")
+_ADJUST_ARGS = struct.Struct("@N" + "P" * 16 + "q" * 6 + "iiiii" + "0q")
+
+_SCALES = "[pages, page_size, heads, scale bytes]"
+
+
+class CacheQ4(typing.NamedTuple):
+    """A paged cache in 4 bits (pps_kv_cache_q4): codes k, v [pages, page_size, kv heads, d / 2] uint8, scales k_scale,
+    v_scale [pages, page_size, kv heads, 4 * ceil(d / 64)] uint8 or float8_e4m3fn, units k_unit, v_unit [kv heads] float32 or
+    None (ones)."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    k_unit: typing.Optional[torch.Tensor] = None
+    v_unit: typing.Optional[torch.Tensor] = None
+
+
+def q4_scale_bytes(head_dim: int) -> int:
+    """Bytes of a head's scales: one for 16 channels, filled up to four."""
+    return 4 * -(-head_dim // 64)
+
+
+def cache_q4(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, k_unit=None, v_unit=None, device=None) -> CacheQ4:
+    """An empty (zero) cache in 4 bits, each page laid out head by head in memory."""
+    if head_dim % 16 or not 16 <= head_dim <= 256:
+        raise ValueError(f"head_dim must be a multiple of 16 up to 256, got {head_dim}")
+    made = [torch.zeros(n_pages, n_kv_heads, page_size, n, dtype=torch.uint8, device=device or "cuda").transpose(1, 2)
+            for n in (head_dim // 2, head_dim // 2, q4_scale_bytes(head_dim), q4_scale_bytes(head_dim))]
+    return CacheQ4(*made, k_unit, v_unit)
+
+
+def _bytes4(name, t, di, shape, what):
+    """Strides of a tensor of one-byte elements, checked as _strided does."""
+    if isinstance(t, torch.Tensor) and t.dtype is torch.float8_e4m3fn:
+        t = t.view(torch.uint8)
+    return _strided(name, t, di, torch.uint8, shape, what)
+
+
+def _cache_q4(cache, di, d):
+    """The fields of pps_kv_cache_q4; d None: as the codes say."""
+    if not isinstance(cache, CacheQ4):
+        raise TypeError(f"cache must be a CacheQ4, got {type(cache).__name__}")
+    k, v, ks, vs, ku, vu = cache
+    st = _strided("cache.k", k, di, torch.uint8, (None, None, None, None if d is None else d // 2), _CACHE)
+    n, page, heads, half = shape = k.shape
+    if d is not None and d % 2:
+        raise ValueError(f"a cache in 4 bits has an even number of channels, got {d}")
+    d = 2 * half
+    if _strided("cache.v", v, di, torch.uint8, shape, _CACHE) != st:
+        raise ValueError("cache.k and cache.v must have the same strides")
+    scales = (n, page, heads, q4_scale_bytes(d))
+    ss = _bytes4("cache.k_scale", ks, di, scales, _SCALES)
+    if _bytes4("cache.v_scale", vs, di, scales, _SCALES) != ss:
+        raise ValueError("cache.k_scale and cache.v_scale must have the same strides")
+    units = [_flat(name, t, di, torch.float32, heads) for name, t in (("cache.k_unit", ku), ("cache.v_unit", vu))]
+    return (k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), *units, n, page, heads, d, st[0], st[1], st[2],
+            ss[0], ss[1], ss[2])
+
+
+def kv_append_q4(q, k, v, pos, slot, cache, rope, q_norm=None, k_norm=None, eps: float = 1e-6, interleaved: bool = False,
+                 out=None, status=None, stream=None):
+    """pps_kv_append_q4: kv_append into a cache in 4 bits (CacheQ4).  Returns the queries (`out`, which may be q)."""
+    di, dt, code = _half_rows(q)
+    n, heads, d = shape = q.shape
+    held = _cache_q4(cache, di, d)
+    kv_shape = (n, held[8], d)
+    sq = _strided("q", q, di, dt, shape, _HEADS)
+    sk = _strided("k", k, di, dt, kv_shape, _HEADS)
+    sv = _strided("v", v, di, dt, kv_shape, _HEADS)
+    rot = max_pos = table = at = 0
+    if rope is not None:
+        if _required("rope", rope, di).dim() != 2:
+            raise TypeError("rope must be [max_pos, rot]")
+        max_pos, rot = rope.shape
+        table, at = _flat("rope", rope, di, torch.float32, 0), _flat("pos", _required("pos", pos, di), di, torch.int32, n)
+    slots = _flat("slot", _required("slot", slot, di), di, torch.int64, n)
+    wq, wk = _flat("q_norm", q_norm, di, dt, d), _flat("k_norm", k_norm, di, dt, d)
+    flags = _flat("status", status, di, torch.int32, 1)
+    if torch._C._cuda_getDevice() != di:
+        with torch.cuda.device(di):
+            return kv_append_q4(q, k, v, pos, slot, cache, rope, q_norm, k_norm, eps, interleaved, out, status, stream)
+    if out is None:
+        with _own_memory(stream):
+            out = torch.empty(n, heads, d, dtype=dt, device=q.device)
+    so = _strided("out", out, di, dt, shape, _HEADS)
+    args = _APPEND_Q4_ARGS.pack(_APPEND_Q4_ARGS.size, q.data_ptr(), sq[0], sq[1], k.data_ptr(), sk[0], sk[1], v.data_ptr(),
+                                sv[0], sv[1], out.data_ptr(), so[0], so[1], *held, wq, wk, table, at, slots, flags, n,
+                                max_pos, code, heads, rot, 1 if interleaved else 0, eps)
+    _check("pps_kv_append_q4", lib().pps_kv_append_q4(args, _handle(stream, di)))
+    return out
+
+
+def kv_read_q4(cache, slot, dtype=torch.bfloat16, out=None, status=None, stream=None):
+    """pps_kv_read_q4: the values of cache slots (int64, < 0: zeros).  Returns (k, v) [n, kv heads, d] of dtype, written
+    to the two tensors of `out` where it is given."""
+    if not isinstance(slot, torch.Tensor) or not slot.is_cuda:
+        raise TypeError("slot must be a CUDA tensor")
+    if dtype not in _HALVES:
+        raise TypeError(f"dtype must be bfloat16 or float16, got {dtype}")
+    di, n = slot.get_device(), slot.numel()
+    held = _cache_q4(cache, di, None)
+    slots, flags = _flat("slot", slot, di, torch.int64, n), _flat("status", status, di, torch.int32, 1)
+    if torch._C._cuda_getDevice() != di:
+        with torch.cuda.device(di):
+            return kv_read_q4(cache, slot, dtype, out, status, stream)
+    shape = (n, held[8], held[9])
+    if out is None:
+        with _own_memory(stream):
+            out = tuple(torch.empty(shape, dtype=dtype, device=slot.device) for _ in range(2))
+    k, v = out
+    sk, sv = _strided("out[0]", k, di, dtype, shape, _HEADS), _strided("out[1]", v, di, dtype, shape, _HEADS)
+    args = _READ_Q4_ARGS.pack(_READ_Q4_ARGS.size, k.data_ptr(), sk[0], sk[1], v.data_ptr(), sv[0], sv[1], *held, slots, flags,
+                              n, _HALVES[dtype])
+    _check("pps_kv_read_q4", lib().pps_kv_read_q4(args, _handle(stream, di)))
+    return k, v
+
+
+def attention_q4_workspace(n_tok: int, n_heads: int, n_kv_heads: int, head_dim: int, device=None) -> torch.Tensor:
+    """A workspace for paged_attention_q4 calls of up to n_tok tokens (not shared by concurrent calls)."""
+    nb = int(lib().pps_attention_q4_workspace_size(n_tok, n_heads, n_kv_heads, head_dim))
+    return torch.empty(nb, dtype=torch.uint8, device=device or "cuda")
+
+
+def paged_attention_q4(q, cache, pages, kv_len, q_off, mask=None, scale=None, out=None, lse=None, ws=None, status=None,
+                       stream=None):
+    """pps_paged_attention_q4: paged_attention over a cache in 4 bits (CacheQ4)."""
+    di, dt, code = _half_rows(q)
+    n, heads, d = shape = q.shape
+    held = _cache_q4(cache, di, d)
+    sq = _strided("q", q, di, dt, shape, _HEADS)
+    i32 = torch.int32
+    n_seq = _required("kv_len", kv_len, di).numel()
+    sp = _strided("pages", pages, di, i32, (n_seq, None), "[n_seq, columns]")
+    columns = pages.shape[1]
+    lens = _flat("kv_len", kv_len, di, i32, 0)
+    offs = _flat("q_off", _required("q_off", q_off, di), di, i32, n_seq + 1)
+    words = bits = 0
+    if mask is not None:
+        if _required("mask", mask, di).dim() != 2 or mask.shape[0] != n or mask.shape[1] < 1:
+            raise ValueError(f"mask must be [{n}, words]")
+        words, bits = mask.shape[1], _flat("mask", mask, di, i32, 0)
+    sums, flags = _flat("lse", lse, di, torch.float32, n * heads), _flat("status", status, di, i32, 1)
+    work = _flat("ws", ws, di, torch.uint8, 0)
+    if torch._C._cuda_getDevice() != di:
+        with torch.cuda.device(di):
+            return paged_attention_q4(q, cache, pages, kv_len, q_off, mask, scale, out, lse, ws, status, stream)
+    if out is None:
+        with _own_memory(stream):
+            out = torch.empty(n, heads, d, dtype=dt, device=q.device)
+    so = _strided("out", out, di, dt, shape, _HEADS)
+    L, handle = lib(), _handle(stream, di)
+    if ws is None:
+        scratch = _Scratch(L.pps_attention_q4_workspace_size(n, heads, held[8], d), handle)
+        work, room = scratch.address, scratch.nbytes
+    else:
+        room = ws.numel()
+    # of one sequence, the table's row stride has no meaning
+    args = _ATTENTION_Q4_ARGS.pack(_ATTENTION_Q4_ARGS.size, q.data_ptr(), sq[0], sq[1], out.data_ptr(), so[0], so[1], *held,
+                                   pages.data_ptr(), lens, offs, bits, sums, flags, work, room, n,
+                                   sp[0] if n_seq > 1 else columns, code, heads, columns, n_seq, words,
+                                   d ** -0.5 if scale is None else scale)
+    _check("pps_paged_attention_q4", L.pps_paged_attention_q4(args, handle))
+    return out
+
+
+# ---------------------------------------------------------------- page tables and slot maps
+
+def _pool(pages, held, free_list, free_count):
+    """Device index, (n_seq, columns, row stride) of a page table, and the addresses of it and its pool."""
+    if not isinstance(pages, torch.Tensor) or not pages.is_cuda:
+        raise TypeError("pages must be a CUDA tensor")
+    di, i32 = pages.get_device(), torch.int32
+    st = _strided("pages", pages, di, i32, (None, None), "[n_seq, columns]")
+    n_seq, columns = pages.shape
+    at = [pages.data_ptr()] + [_flat(name, _required(name, t, di), di, i32, m) for name, t, m in (
+        ("held", held, n_seq), ("free_list", free_list, 0), ("free_count", free_count, 1))]
+    return di, n_seq, columns, st[0] if n_seq > 1 else columns, at
+
+
+def kv_reserve(pages, held, free_list, free_count, kv_len, n_new, page_size: int, n_tok: int, pos_off=None, out=None,
+               status=None, stream=None):
+    """pps_kv_reserve: pages for n_new [n_seq] more tokens of every sequence from the pool (free_list, its first
+    free_count[0] entries), and where the tokens go.  pages [n_seq, columns], held [n_seq], free_count [1] are updated in place,
+    all int32.  n_tok: how many tokens the outputs are for (as many as n_new says, or a padded batch).  Returns dict(q_off [n_seq + 1],
+    kv_len [n_seq], slot [n_tok] int64, pos [n_tok], seq [n_tok]); `out` may leave seq out."""
+    di, n_seq, columns, stride, at = _pool(pages, held, free_list, free_count)
+    i32 = torch.int32
+    lens, new = (_flat(name, _required(name, t, di), di, i32, n_seq) for name, t in (("kv_len", kv_len), ("n_new", n_new)))
+    off, flags = _flat("pos_off", pos_off, di, i32, n_tok), _flat("status", status, di, i32, 1)
+    if torch._C._cuda_getDevice() != di:
+        with torch.cuda.device(di):
+            return kv_reserve(pages, held, free_list, free_count, kv_len, n_new, page_size, n_tok, pos_off, out, status, stream)
+    if out is None:
+        with _own_memory(stream):
+            e, dev = torch.empty, pages.device
+            out = dict(q_off=e(n_seq + 1, dtype=i32, device=dev), kv_len=e(n_seq, dtype=i32, device=dev),
+                       slot=e(n_tok, dtype=torch.int64, device=dev), pos=e(n_tok, dtype=i32, device=dev),
+                       seq=e(n_tok, dtype=i32, device=dev))
+    for name in ("q_off", "kv_len", "slot", "pos"):
+        if out.get(name) is None:
+            raise TypeError(f"out[{name!r}] is required")
+    outs = [_flat(name, out.get(name), di, dt, m) for name, dt, m in (
+        ("q_off", i32, n_seq + 1), ("kv_len", i32, n_seq), ("slot", torch.int64, n_tok), ("pos", i32, n_tok), ("seq", i32, n_tok))]
+    args = _RESERVE_ARGS.pack(_RESERVE_ARGS.size, *at, lens, new, off, *outs, flags, n_tok, stride, n_seq, columns, page_size,
+                              free_list.numel())
+    _check("pps_kv_reserve", lib().pps_kv_reserve(args, _handle(stream, di)))
+    return out
+
+
+def kv_trim(pages, held, free_list, free_count, keep, page_size: int, status=None, stream=None):
+    """pps_kv_trim: pages behind the first keep [n_seq] tokens of every sequence go back to the pool (0: all of them)."""
+    di, n_seq, columns, stride, at = _pool(pages, held, free_list, free_count)
+    kept = _flat("keep", _required("keep", keep, di), di, torch.int32, n_seq)
+    flags = _flat("status", status, di, torch.int32, 1)
+    with _on(pages.device):
+        args = _TRIM_ARGS.pack(_TRIM_ARGS.size, *at, kept, flags, stride, n_seq, columns, page_size, free_list.numel())
+        _check("pps_kv_trim", lib().pps_kv_trim(args, _handle(stream, di)))
+
+
+# ---------------------------------------------------------------- logits
+
+def adjust_logits(logits, seq_off, text=None, text_len=None, prompt_len=None, node_tok=None, node_mask=None, repetition=None,
+                  frequency=None, presence=None, bias_off=None, bias_tok=None, bias_val=None, allowed=None, out=None,
+                  status=None, stream=None):
+    """pps_adjust_logits: penalties for tokens of the sequences' texts (text [n_seq, most], text_len, prompt_len [n_seq]) and
+    of the rows' paths (node_tok [n_rows], node_mask [n_rows, words] or None: chains), biases (bias_tok, bias_val [entries],
+    those of sequence s from bias_off[s] to bias_off[s + 1]) and masks (allowed [n_rows, words] int32).  repetition, frequency,
+    presence [n_seq] float32.  Returns out (which may be logits)."""
+    if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
+        raise TypeError("logits must be a CUDA tensor")
+    di, dt, code, i32, f32 = logits.get_device(), logits.dtype, _dtype_code(logits), torch.int32, torch.float32
+    rows = "[rows, vocabulary]"
+    stride = _strided("logits", logits, di, dt, (None, None), rows)[0]
+    n, V = logits.shape
+    offs = _flat("seq_off", _required("seq_off", seq_off, di), di, i32, 1)
+    n_seq = seq_off.numel() - 1
+    texts = lens = text_stride = cap = words = nodes = 0
+    if text is not None:
+        text_stride = _strided("text", text, di, i32, (n_seq, None), "[n_seq, tokens]")[0]
+        texts, cap = text.data_ptr(), text.shape[1]
+        text_stride = text_stride if n_seq > 1 else cap
+        lens = _flat("text_len", _required("text_len", text_len, di), di, i32, n_seq)
+    prompt = _flat("prompt_len", prompt_len, di, i32, n_seq)
+    toks = _flat("node_tok", node_tok, di, i32, n)
+    if node_mask is not None:
+        if _required("node_mask", node_mask, di).dim() != 2 or node_mask.shape[0] != n or node_mask.shape[1] < 1:
+            raise ValueError(f"node_mask must be [{n}, words]")
+        words, nodes = node_mask.shape[1], _flat("node_mask", node_mask, di, i32, 0)
+    laws = [_flat(name, t, di, f32, n_seq) for name, t in (("repetition", repetition), ("frequency", frequency),
+                                                           ("presence", presence))]
+    entries = [0, 0, 0]
+    n_bias = 0
+    if bias_off is not None:
+        n_bias = _required("bias_tok", bias_tok, di).numel()
+        entries = [_flat("bias_off", bias_off, di, i32, n_seq + 1), _flat("bias_tok", bias_tok, di, i32, 0),
+                   _flat("bias_val", _required("bias_val", bias_val, di), di, f32, n_bias)]
+    bits = bits_stride = 0
+    if allowed is not None:
+        bits_stride = _strided("allowed", allowed, di, i32, (n, None), "[rows, words]")[0]
+        if allowed.shape[1] < -(-V // 32):
+            raise ValueError(f"allowed has {allowed.shape[1]} words a row; the call needs {-(-V // 32)}")
+        bits, bits_stride = allowed.data_ptr(), bits_stride if n > 1 else allowed.shape[1]
+    flags = _flat("status", status, di, i32, 1)
+    if torch._C._cuda_getDevice() != di:
+        with torch.cuda.device(di):
+            return adjust_logits(logits, seq_off, text, text_len, prompt_len, node_tok, node_mask, repetition, frequency,
+                                 presence, bias_off, bias_tok, bias_val, allowed, out, status, stream)
+    if out is None:
+        with _own_memory(stream):
+            out = torch.empty(n, V, dtype=dt, device=logits.device)
+    out_stride = _strided("out", out, di, dt, (n, V), rows)[0]
+    # a single row has no stride
+    args = _ADJUST_ARGS.pack(_ADJUST_ARGS.size, logits.data_ptr(), out.data_ptr(), offs, texts, lens, prompt, toks, nodes, *laws,
+                             *entries, bits, flags, n, V, stride if n > 1 else V, out_stride if n > 1 else V, text_stride,
+                             bits_stride, code, n_seq, cap, words, n_bias)
+    _check("pps_adjust_logits", lib().pps_adjust_logits(args, _handle(stream, di)))
     return out
