@@ -16,7 +16,7 @@ LIB = os.path.join(OUT, "libpps.so")
 SOURCES = ["pps_race.cu", "pps_misc.cu", "pps_api.cu"]
 # sources without the keyed source: compiled once, linked into every variant
 COMMON = ["pps_append.cu", "pps_attention.cu", "pps_attention_q4.cu", "pps_chain.cu", "pps_pages.cu", "pps_adjust.cu"]
-HEADERS = ["pps_device.cuh", "pps_internal.h", "pps_tc.cuh", "pps_trunc.cuh", "pps_lmhead.cuh", "pps_attn.cuh", "pps_q4.cuh"]
+HEADERS = ["pps_device.cuh", "pps_internal.h", "pps_tc.cuh", "pps_trunc.cuh", "pps_lmhead.cuh", "pps_attn.cuh", "pps_attn_tiles.cuh", "pps_q4.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -16,12 +16,17 @@
 // channels below 2^-31 of the row's largest.  Weights are rounded to halves (2^-11 of each); sums are formed before rounding,
 // in 32 bits, and the softmax is the running one with the rescaling left out while a maximum rises by less than 2^kLazy.
 //
-// Work split.  The line of pps_attn.cuh; a CTA's warps take the 32-key units of a segment in turn and join at its end.
+// A CTA's warps take the 32-key units of a segment in turn and join at its end.
+//
+// Many rows (trees, chunks).  The 128-row tiles of pps_attn_tiles.cuh on the 5th-generation tensor cores: the warps that load keys and
+// values copy a tile's codes and scales into shared memory two tiles ahead, widen them (64 conversions and as many multiplications
+// a lane for 32 keys of 128 channels) and write the halves where TMA would have put them.  Queries in bf16 become halves in a launch before it.
+//
+// Work split.  The line of pps_attn.cuh.
 #include <atomic>
 #include <cstring>
 
-#include "pps_attn.cuh"
-#include "pps_q4.cuh"
+#include "pps_attn_tiles.cuh"
 
 namespace pps {
 namespace {
@@ -35,6 +40,11 @@ constexpr int kLeast4 = 1;
 constexpr float kLazy4 = 8.0f;    // log2 of the rise of a maximum that nothing is rescaled for
 constexpr float kShift4 = 6.0f;   // log2 of a factor on all weights: 2^(8 + 6) is below fp16's largest number
 constexpr int kQBits = 14;        // a bf16 row's largest channel lies in [2^14, 2^15) as a half
+constexpr int kFewRows = 16;      // of a sequence and key head, on average, up to which the kernel of few rows takes a call
+
+// The power of two that brings a row in bf16 whose largest finite magnitude has the bits `top` to halves.
+__device__ __forceinline__ int halving(uint32_t top) { return top == 0 ? 0 : min(kQBits + 127 - (int)(top >> 7), 126); }
+__device__ __forceinline__ float power_of_two(int k) { return __uint_as_float((uint32_t)(127 + k) << 23); }
 
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -112,10 +122,9 @@ __global__ void __launch_bounds__(kThreads4, kPerSm4) few_rows_kernel(const Attn
                 }
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                const int e = (int)(top >> 7);  // exponent field
-                const int k = top == 0 ? 0 : min(kQBits + 127 - e, 126);
-                const float f = __uint_as_float((uint32_t)(127 + k) << 23);
-                row_sc[nt] = min(row_sc[nt] * __uint_as_float((uint32_t)(127 - k) << 23), FLT_MAX);
+                const int k = halving(top);
+                const float f = power_of_two(k);
+                row_sc[nt] = fminf(row_sc[nt] * power_of_two(-k), FLT_MAX);
 #pragma unroll
                 for (int i = 0; i < DC / 8; ++i)
                     qf[nt][i] = Half<__half>::pack(__uint_as_float(x[i] << 16) * f, __uint_as_float(x[i] & 0xffff0000u) * f);
@@ -432,9 +441,85 @@ cudaError_t launch_few(const AttnArgs& a, const Q4View& z, const Rows4& rows, cu
     return launch_pdl(join_kernel<T, DC>, dim3(ctas, join_blocks(a, P)), dim3(256), 0, st, a, P);
 }
 
+// Queries in bf16 as halves, rows side by side, and the factor that a row's scores get for it.  A warp has a row; four channels a lane.
+__global__ void __launch_bounds__(256) halve_kernel(const AttnArgs a, __half* out, float* row_scale) {
+    pdl_wait();
+    pdl_launch_dependents();
+    const int64_t rows = a.n_tok * a.n_heads;
+    const int lane = threadIdx.x & 31, D = a.c.head_dim;
+    for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < rows; i += (int64_t)gridDim.x * 8) {
+        const int64_t tok = i / a.n_heads;
+        const int head = (int)(i - tok * a.n_heads);
+        uint2 x = make_uint2(0, 0);
+        if (4 * lane < D) x = __ldg(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(a.q.p) + tok * a.q.tok + head * a.q.head) + lane);
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t v = ((e & 2) ? x.y : x.x) >> (16 * (e & 1)) & 0x7fffu;
+            top = max(top, v < 0x7f80u ? v : 0u);
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        const int k = halving(top);
+        const float f = power_of_two(k);
+        if (4 * lane < D) {
+            const uint2 y = make_uint2(Half<__half>::pack(__uint_as_float(x.x << 16) * f, __uint_as_float(x.x & 0xffff0000u) * f),
+                                       Half<__half>::pack(__uint_as_float(x.y << 16) * f, __uint_as_float(x.y & 0xffff0000u) * f));
+            *reinterpret_cast<uint2*>(out + i * D + 4 * lane) = y;
+        }
+        if (lane == 0) row_scale[i] = power_of_two(-k);
+    }
+}
+
+size_t parts4_bytes(int64_t n_tok, int group, int head_dim) {
+    const size_t x = std::max(part_bytes(kMaxCtas4, 16, head_dim), part_bytes(kMaxCtas, Rows(n_tok, group).cap, head_dim));
+    return (x + 255) / 256 * 256;
+}
+size_t halves_bytes(int64_t n_tok, int n_heads, int head_dim) { return ((size_t)n_tok * n_heads * head_dim * 2 + 255) / 256 * 256; }
+
+template <typename T, int DC>
+cudaError_t launch_tiles(const AttnArgs& given, const Q4View& z, cudaStream_t st) {
+    AttnArgs a = given;
+    AttnPlan P;
+    std::memset(&P, 0, sizeof(P));
+    P.group = a.n_heads / a.c.n_kv_heads;
+    const Rows rows(a.n_tok, P.group);
+    P.nsub = rows.nsub;
+    P.gs = rows.gs;
+    P.tt = rows.tt;
+    P.bt = 2 * rows.tt;
+    P.fix = kFix;
+    P.cap_rows = rows.cap;
+    P.shift = Half<__half>::kShift;
+    plan_common(P, a);
+    carve(P, a.ws, kMaxCtas);
+    const int ctas = std::min(device_sm_count(), kMaxCtas);
+    Q4Rows r4 = {z, nullptr};
+    if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+        char* w = static_cast<char*>(a.ws) + parts4_bytes(a.n_tok, P.group, a.c.head_dim);
+        __half* halves = reinterpret_cast<__half*>(w);
+        float* factors = reinterpret_cast<float*>(w + halves_bytes(a.n_tok, a.n_heads, a.c.head_dim));
+        const int64_t blocks = std::min<int64_t>((a.n_tok * a.n_heads + 7) / 8, (int64_t)ctas * 8);
+        const cudaError_t e = launch_pdl(halve_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a, halves, factors);
+        if (e != cudaSuccess) return e;
+        a.q = {halves, (int64_t)a.n_heads * a.c.head_dim, a.c.head_dim};
+        r4.row_scale = factors;
+    }
+    CUtensorMap tmQ;
+    if (!query_map(&tmQ, a, P, PPS_F16)) return cudaErrorInvalidValue;
+    constexpr int kSmem = Cfg<DC, true>::kSmem;
+    static std::atomic<uint64_t> ready{0};
+    cudaError_t e = allow_smem(ready, (const void*)attention_kernel<T, DC, true>, kSmem);
+    if (e != cudaSuccess) return e;
+    e = launch_pdl(attention_kernel<T, DC, true>, dim3(ctas), dim3(kAttnThreads), kSmem, st, tmQ, tmQ, tmQ, a, P, r4);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(join_kernel<T, DC>, dim3(ctas, join_blocks(a, P)), dim3(256), 0, st, a, P);
+}
+
 template <typename T, int DC>
 cudaError_t by_rows(const AttnArgs& a, const Q4View& z, cudaStream_t st) {
-    const Rows4 rows(a.n_tok, a.n_seq, a.n_heads / a.c.n_kv_heads);
+    const int group = a.n_heads / a.c.n_kv_heads;
+    if ((a.n_tok + a.n_seq - 1) / a.n_seq * group > kFewRows) return launch_tiles<T, DC>(a, z, st);
+    const Rows4 rows(a.n_tok, a.n_seq, group);
     return rows.nt == 1 ? launch_few<T, DC, 1>(a, z, rows, st) : launch_few<T, DC, 2>(a, z, rows, st);
 }
 
@@ -446,8 +531,8 @@ cudaError_t by_channels4(const AttnArgs& a, const Q4View& z, cudaStream_t st) {
 }  // namespace
 
 size_t attention_q4_workspace_bytes(int64_t n_tok, int n_heads, int n_kv_heads, int head_dim) {
-    (void)n_tok, (void)n_heads, (void)n_kv_heads;
-    return part_bytes(kMaxCtas4, 16, head_dim);
+    return parts4_bytes(n_tok, (n_heads + n_kv_heads - 1) / n_kv_heads, head_dim) + halves_bytes(n_tok, n_heads, head_dim) +
+           sizeof(float) * (size_t)n_tok * n_heads;
 }
 
 cudaError_t launch_attention_q4(const AttnArgs& a, const Q4View& z, int dtype, cudaStream_t stream) {
