@@ -31,10 +31,10 @@
 namespace pps {
 namespace {
 
-constexpr int kWarps4 = 8, kThreads4 = 32 * kWarps4;
+constexpr int kWarps4 = 4, kThreads4 = 32 * kWarps4;
 constexpr int kUnit = 32;         // keys that a warp takes at a time
-constexpr int kPerSm4 = 2;        // CTAs
-constexpr int kMaxCtas4 = 320;
+constexpr int few_ctas(int nt) { return nt == 1 ? 3 : 2; }  // per SM: 168 or 255 registers
+constexpr int kMaxCtas4 = 480;
 constexpr int kFix4 = 2;          // key tiles that an item's start and end cost
 constexpr int kLeast4 = 1;
 constexpr float kLazy4 = 8.0f;    // log2 of the rise of a maximum that nothing is rescaled for
@@ -59,16 +59,24 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 
 // what a lane holds of 32 keys: eighth e has keys 8e .. 8e + 7
 template <int DC>
-struct Held {
+struct HeldK {
     static constexpr int kW = DC / 32;  // words of a quarter of a key's codes (4 or 2)
-    static constexpr int kVW = DC / 64; // words of an eighth (2 or 1)
-    uint32_t k[4][kW], v[8][kVW];       // key 8e + g; keys 8e + 2t, 8e + 2t + 1
-    uint32_t ks[4], vs[8];              // scale bytes
+    uint32_t c[4][kW], s[4];            // key 8e + g: codes, scale bytes
+};
+template <int DC>
+struct HeldV {
+    static constexpr int kW = DC / 64;  // words of an eighth (2 or 1)
+    uint32_t c[8][kW], s[8];            // keys 8e + 2t, 8e + 2t + 1
+};
+// where the four eighths of a unit's keys start (bytes from a head's first row), and whether all 32 keys are there
+struct Places {
+    int64_t codes[4], scales[4];
+    bool whole;
 };
 
-template <typename T, int DC, int NT>
-__global__ void __launch_bounds__(kThreads4, kPerSm4) few_rows_kernel(const AttnArgs a, const Q4View z, const AttnPlan P) {
-    using H = Held<DC>;
+// EVEN: all DC channels are there, rows start on 16-byte boundaries, and 16 keys in a row share their page
+template <typename T, int DC, int NT, bool EVEN>
+__global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const AttnArgs a, const Q4View z, const AttnPlan P) {
     constexpr int R = 8 * NT, RS = DC + 4;  // a row's floats in shared memory: 4 modulo 16, so that lanes (g, t) touch all banks
     __shared__ int64_t s_sum[kWarps4];
     __shared__ Start s_start;
@@ -84,9 +92,12 @@ __global__ void __launch_bounds__(kThreads4, kPerSm4) few_rows_kernel(const Attn
     if (c0 >= c1) return;
     const int least = (int)min(max(share / 8, (int64_t)1), (int64_t)kLeast4);
     Walk W(P, s_start, c0, c1, least);
-    const int D = a.c.head_dim;
-    const bool k_there = t * (DC / 4) < D, v_there = g * (DC / 8) < D;
-    const bool k_whole = (t + 1) * (DC / 4) <= D;  // (else, of 128: half of the quarter)
+    const int D = EVEN ? DC : a.c.head_dim;
+    // the lane's place in a row of codes and of scales, for keys and for values; what of its scales' bytes counts
+    const bool k_there = EVEN || t * (DC / 4) < D, k_half = EVEN || t * (DC / 4) + 16 < D, v_there = EVEN || g * (DC / 8) < D;
+    const int64_t k_at = g * a.c.tok + (k_there ? t * (DC / 8) : 0), v_at = 2 * t * a.c.tok + (v_there ? g * (DC / 16) : 0);
+    const int64_t ks_at = g * z.tok + (k_there ? t * (DC / 64) : 0), vs_at = 2 * t * z.tok + (v_there ? (DC == 128 ? g : g >> 1) : 0);
+    const uint32_t k_mask = (k_there ? 0xffu : 0u) | (DC == 128 && k_half ? 0xff00u : 0u), v_mask = v_there ? 0xffu : 0u;
 
     while (W.next(a, P)) {
         const int kvh = W.heads / P.nsub, sub = W.heads - kvh * P.nsub;
@@ -94,6 +105,105 @@ __global__ void __launch_bounds__(kThreads4, kPerSm4) few_rows_kernel(const Attn
         const int head0 = kvh * P.group + sub * P.gs;
         const int len = W.q.len, prefix = len - W.q.n;
         const float ku = z.k_unit ? __ldg(z.k_unit + kvh) : 1.0f, vu = z.v_unit ? __ldg(z.v_unit + kvh) : 1.0f;
+        const int plain = a.mask ? prefix : prefix + W.i0 + 1;  // keys below it are seen by every row
+        const int end = a.mask ? len : prefix + W.i0 + W.ntok;  // keys from it on by none
+        const int first = W.t0 * kTileKeys, last = min(W.t1 * kTileKeys, end);
+        const int32_t* table = a.pages + (int64_t)W.s * a.pages_stride;
+        const uint8_t* const kp = static_cast<const uint8_t*>(a.c.k) + kvh * a.c.head + k_at;
+        const uint8_t* const vp = static_cast<const uint8_t*>(a.c.v) + kvh * a.c.head + v_at;
+        const uint8_t* const ksp = z.ks + kvh * z.head + ks_at;
+        const uint8_t* const vsp = z.vs + kvh * z.head + vs_at;
+
+        // pages of the eighths of the unit from key k0 on, in lanes 0 to 3 (and again in the others)
+        auto pages_of = [&](int k0) {
+            const int k = k0 + 8 * t;
+            return k < last ? __ldg(table + (k >> P.page_log2)) : 0;
+        };
+        auto places_of = [&](Places& x, int k0, int page) {
+            const bool key = k0 + 8 * t < last, good = !key || (page >= 0 && page < a.c.n_pages);
+            if (!good) {  // reads as zeros
+                if (a.status) atomicOr(a.status, PPS_FLAG_INDEX);
+                page = -1;
+            }
+            x.whole = __all_sync(0xffffffffu, good) && k0 + kUnit <= last;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (EVEN && (e & 1)) {
+                    x.codes[e] = x.codes[e - 1] + 8 * a.c.tok;
+                    x.scales[e] = x.scales[e - 1] + 8 * z.tok;
+                } else {
+                    const int p = __shfl_sync(0xffffffffu, page, e), in_page = (k0 + 8 * e) & (a.c.page_size - 1);
+                    x.codes[e] = p < 0 ? -1 : p * a.c.page + in_page * a.c.tok;
+                    x.scales[e] = p * z.page + in_page * z.tok;
+                }
+            }
+        };
+        // (keys past the last, and those of a missing page: codes of anything, scales of zero)
+        auto fetch_k = [&](HeldK<DC>& x, const Places& at, int k0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool there = at.whole || (k0 + 8 * e + g < last && at.codes[EVEN ? e & 2 : e] >= 0);
+                x.s[e] = 0;
+#pragma unroll
+                for (int i = 0; i < HeldK<DC>::kW; ++i) x.c[e][i] = 0;
+                if (there) {
+                    const uint8_t* src = kp + at.codes[e];
+                    if constexpr (EVEN && DC == 128) {
+                        const uint4 w = __ldg(reinterpret_cast<const uint4*>(src));
+                        x.c[e][0] = w.x;
+                        x.c[e][1] = w.y;
+                        x.c[e][HeldK<DC>::kW - 2] = w.z;
+                        x.c[e][HeldK<DC>::kW - 1] = w.w;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < HeldK<DC>::kW; i += 2) {
+                            const uint2 w = __ldg(reinterpret_cast<const uint2*>(src) + (k_half ? i / 2 : 0));
+                            x.c[e][i] = w.x;
+                            x.c[e][i + 1] = w.y;
+                        }
+                    }
+                    if constexpr (DC == 128)
+                        x.s[e] = __ldg(reinterpret_cast<const uint16_t*>(ksp + at.scales[e])) & k_mask;
+                    else
+                        x.s[e] = __ldg(ksp + at.scales[e]) & k_mask;
+                }
+            }
+        };
+        auto fetch_v = [&](HeldV<DC>& x, const Places& at, int k0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const bool there = at.whole || (k0 + 8 * e + 2 * t + j < last && at.codes[EVEN ? e & 2 : e] >= 0);
+                    x.s[2 * e + j] = 0;
+#pragma unroll
+                    for (int i = 0; i < HeldV<DC>::kW; ++i) x.c[2 * e + j][i] = 0;
+                    if (there) {
+                        const uint8_t* src = vp + at.codes[e] + j * a.c.tok;
+                        if constexpr (DC == 128) {
+                            const uint2 w = __ldg(reinterpret_cast<const uint2*>(src));
+                            x.c[2 * e + j][0] = w.x;
+                            x.c[2 * e + j][HeldV<DC>::kW - 1] = w.y;
+                        } else
+                            x.c[2 * e + j][0] = __ldg(reinterpret_cast<const uint32_t*>(src));
+                        x.s[2 * e + j] = __ldg(vsp + at.scales[e] + j * z.tok) & v_mask;
+                    }
+                }
+        };
+
+        constexpr int kStep = kUnit * kWarps4;
+        int k0 = first + warp * kUnit;
+        HeldK<DC> kh;
+        HeldV<DC> vh;
+        Places at;
+        int pages = 0;
+        if (k0 < last) {
+            const int p = pages_of(k0);
+            pages = pages_of(k0 + kStep);
+            places_of(at, k0, p);
+            fetch_k(kh, at, k0);
+            fetch_v(vh, at, k0);
+        }
         // ---- queries: row 8 nt + g, the channels of quarter t, as halves
         uint32_t qf[NT][DC / 8];
         float row_sc[NT];
@@ -110,7 +220,7 @@ __global__ void __launch_bounds__(kThreads4, kPerSm4) few_rows_kernel(const Attn
             }
             const uint32_t* x = reinterpret_cast<const uint32_t*>(raw);
             row_sc[nt] = P.sc * ku;
-            if constexpr (sizeof(T) == 2 && Half<T>::kType == 0) {
+            if constexpr (Half<T>::kType == 0) {
 #pragma unroll
                 for (int i = 0; i < DC / 8; ++i) qf[nt][i] = x[i];
             } else {
@@ -132,19 +242,12 @@ __global__ void __launch_bounds__(kThreads4, kPerSm4) few_rows_kernel(const Attn
         }
         // of the lane's rows 8 nt + 2t, + 1 (an odd index: the second)
         float sc[2 * NT], m[2 * NT], l[2 * NT];
-        int vis[2 * NT];
-        const uint32_t* mask[2 * NT];
 #pragma unroll
         for (int r = 0; r < 2 * NT; ++r) {
             sc[r] = __shfl_sync(0xffffffffu, row_sc[r >> 1], 4 * (2 * t + (r & 1)));
-            const int row = 8 * (r >> 1) + 2 * t + (r & 1), tok = W.i0 + min(row / P.gs, W.ntok - 1);
-            mask[r] = a.mask ? a.mask + (int64_t)(W.q.off + tok) * a.mask_words : nullptr;
-            vis[r] = a.mask ? len : prefix + tok + 1;
             m[r] = -INFINITY;
             l[r] = 0.0f;
         }
-        const int plain = a.mask ? prefix : prefix + W.i0 + 1;  // keys below it are seen by every row
-        const int end = a.mask ? len : prefix + W.i0 + W.ntok;  // keys from it on by none
         float o[NT][DC / 16][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -153,64 +256,11 @@ __global__ void __launch_bounds__(kThreads4, kPerSm4) few_rows_kernel(const Attn
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.0f;
 
-        const int32_t* table = a.pages + (int64_t)W.s * a.pages_stride;
-        const int first = W.t0 * kTileKeys, last = min(W.t1 * kTileKeys, end);
-        auto page_of = [&](int k0) {  // lanes 0 to 3: of the eighths of the unit from key k0 on
-            const int k = k0 + 8 * (lane & 3);
-            int p = -1;
-            if (k < last && k < len) {
-                p = __ldg(table + (k >> P.page_log2));
-                if (p < 0 || p >= a.c.n_pages) {  // reads as zeros
-                    if (a.status && lane < 4) atomicOr(a.status, PPS_FLAG_INDEX);
-                    p = -1;
-                }
-            }
-            return p;
-        };
-        auto fetch = [&](H& x, int k0, int pages) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int p = __shfl_sync(0xffffffffu, pages, e), in_page = (k0 + 8 * e) & (a.c.page_size - 1);
-                const int64_t at = p * a.c.page + in_page * a.c.tok + kvh * a.c.head;
-                const int64_t st = p * z.page + in_page * z.tok + kvh * z.head;
-                const int left = p >= 0 ? last - k0 - 8 * e : 0;  // keys of the eighth that are there
-#pragma unroll
-                for (int i = 0; i < H::kW; ++i) x.k[e][i] = 0;
-                x.ks[e] = 0;
-                if (g < left && k_there) {
-                    const uint8_t* src = static_cast<const uint8_t*>(a.c.k) + at + g * a.c.tok + t * (DC / 8);
-#pragma unroll
-                    for (int i = 0; i < H::kW; i += 2)
-                        if (i == 0 || k_whole) {
-                            const uint2 w = __ldg(reinterpret_cast<const uint2*>(src) + i / 2);
-                            x.k[e][i] = w.x;
-                            x.k[e][i + 1] = w.y;
-                        }
-                    const uint8_t* sp = z.ks + st + g * z.tok + t * (DC / 64);
-                    if (DC == 128 && k_whole)
-                        x.ks[e] = __ldg(reinterpret_cast<const uint16_t*>(sp));
-                    else
-                        x.ks[e] = __ldg(sp);
-                }
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-#pragma unroll
-                    for (int i = 0; i < H::kVW; ++i) x.v[2 * e + j][i] = 0;
-                    x.vs[2 * e + j] = 0;
-                    if (2 * t + j < left && v_there) {
-                        const uint8_t* src = static_cast<const uint8_t*>(a.c.v) + at + (2 * t + j) * a.c.tok + g * (DC / 16);
-                        if constexpr (DC == 128) {
-                            const uint2 w = __ldg(reinterpret_cast<const uint2*>(src));
-                            x.v[2 * e + j][0] = w.x;
-                            x.v[2 * e + j][H::kVW - 1] = w.y;
-                        } else
-                            x.v[2 * e + j][0] = __ldg(reinterpret_cast<const uint32_t*>(src));
-                        x.vs[2 * e + j] = __ldg(z.vs + st + (2 * t + j) * z.tok + (DC == 128 ? g : g >> 1));
-                    }
-                }
-            }
-        };
-        auto work = [&](const H& x, int k0) {
+        while (k0 < last) {
+            const int key0 = k0;
+            k0 += kStep;
+            const int page_next = pages;
+            pages = pages_of(k0 + kStep);
             float s[NT][2][4];
 #pragma unroll
             for (int G = 0; G < 2; ++G) {
@@ -218,12 +268,12 @@ __global__ void __launch_bounds__(kThreads4, kPerSm4) few_rows_kernel(const Attn
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const int e = 2 * G + j;
-                    const uint32_t s2 = q4::scales2(x.ks[e]);
+                    const uint32_t s2 = q4::scales2(kh.s[e]);
                     const uint32_t lo = __byte_perm(s2, 0, 0x1010), hi = __byte_perm(s2, 0, 0x3232);
 #pragma unroll
-                    for (int i = 0; i < H::kW; ++i) {
+                    for (int i = 0; i < HeldK<DC>::kW; ++i) {
                         uint32_t w[4];
-                        q4::widen8(x.k[e][i], w);
+                        q4::widen8(kh.c[e][i], w);
 #pragma unroll
                         for (int c = 0; c < 4; ++c) h[j][4 * i + c] = q4::mul_halves(w[c], i < 2 ? lo : hi);
                     }
@@ -238,12 +288,18 @@ __global__ void __launch_bounds__(kThreads4, kPerSm4) few_rows_kernel(const Attn
                     }
                 }
             }
+            if (k0 < last) {  // the next unit's keys take the place of those that are used up
+                places_of(at, k0, page_next);
+                fetch_k(kh, at, k0);
+            }
             // scores of the lane: keys 16 G + 8 (e >> 1) + g, rows 8 nt + 2t + (e & 1)
             const bool odd_scale = P.s_xor != 0 || P.s_and == 0;
-            if (k0 + kUnit > plain || odd_scale) {
+            if (key0 + kUnit > plain || odd_scale) {
 #pragma unroll
                 for (int r = 0; r < 2 * NT; ++r) {
-                    const uint32_t bits = seen_bits(k0, vis[r], prefix, mask[r], a.mask_words) >> g;
+                    const int row = 8 * (r >> 1) + 2 * t + (r & 1), tok = W.i0 + min(row / P.gs, W.ntok - 1);
+                    const uint32_t* mask = a.mask ? a.mask + (int64_t)(W.q.off + tok) * a.mask_words : nullptr;
+                    const uint32_t bits = seen_bits(key0, mask ? len : prefix + tok + 1, prefix, mask, a.mask_words) >> g;
 #pragma unroll
                     for (int G = 0; G < 2; ++G)
 #pragma unroll
@@ -258,7 +314,7 @@ __global__ void __launch_bounds__(kThreads4, kPerSm4) few_rows_kernel(const Attn
 #pragma unroll
             for (int r = 0; r < 2 * NT; ++r) {
                 const float(&y)[2][4] = s[r >> 1];
-                top[r] = fmaxf(fmaxf(y[0][r & 1], y[0][2 + (r & 1)]), fmaxf(y[1][r & 1], y[1][2 + (r & 1)]));
+                top[r] = fmaxf(max3(y[0][r & 1], y[0][2 + (r & 1)], y[1][r & 1]), y[1][2 + (r & 1)]);
                 rises |= (top[r] - m[r]) * sc[r] > kLazy4;
             }
             if (__any_sync(0xffffffffu, rises)) {
@@ -295,13 +351,13 @@ __global__ void __launch_bounds__(kThreads4, kPerSm4) few_rows_kernel(const Attn
             for (int G = 0; G < 2; ++G) {
                 uint32_t s2[2];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) s2[j] = q4::scales2(x.vs[4 * G + 2 * j] | x.vs[4 * G + 2 * j + 1] << 8);
+                for (int j = 0; j < 2; ++j) s2[j] = q4::scales2(vh.s[4 * G + 2 * j] | vh.s[4 * G + 2 * j + 1] << 8);
 #pragma unroll
-                for (int w = 0; w < H::kVW; ++w) {
+                for (int w = 0; w < HeldV<DC>::kW; ++w) {
                     uint32_t lo[2][4], hi[2][4];  // the word's even and odd channels of two keys
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const uint32_t x0 = x.v[4 * G + 2 * j][w], x1 = x.v[4 * G + 2 * j + 1][w];
+                        const uint32_t x0 = vh.c[4 * G + 2 * j][w], x1 = vh.c[4 * G + 2 * j + 1][w];
                         q4::widen8((x0 & 0x0f0f0f0fu) | (x1 << 4 & 0xf0f0f0f0u), lo[j]);
                         q4::widen8((x0 >> 4 & 0x0f0f0f0fu) | (x1 & 0xf0f0f0f0u), hi[j]);
                     }
@@ -314,25 +370,7 @@ __global__ void __launch_bounds__(kThreads4, kPerSm4) few_rows_kernel(const Attn
                     }
                 }
             }
-        };
-        H even, odd;
-        constexpr int kStep = kUnit * kWarps4;
-        int k0 = first + warp * kUnit;
-        if (k0 < last) {
-            fetch(even, k0, page_of(k0));
-            int pages = page_of(k0 + kStep);
-            auto turn = [&](H& cur, H& nxt) {
-                const int k = k0;
-                k0 += kStep;
-                if (k0 < last) {
-                    fetch(nxt, k0, pages);
-                    pages = page_of(k0 + kStep);
-                }
-                work(cur, k);
-                return k0 < last;
-            };
-            while (turn(even, odd) && turn(odd, even)) {
-            }
+            if (k0 < last) fetch_v(vh, at, k0);
         }
 
         // ---- the segment's result: the warps' parts, joined
@@ -432,11 +470,14 @@ cudaError_t launch_few(const AttnArgs& a, const Q4View& z, const Rows4& rows, cu
     plan_common(P, a);
     carve(P, a.ws, kMaxCtas4);
     constexpr int kSmem = kWarps4 * 8 * NT * (DC + 4) * 4;
-    static std::atomic<uint64_t> ready{0};
-    cudaError_t e = allow_smem(ready, (const void*)few_rows_kernel<T, DC, NT>, kSmem);
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v) | (uintptr_t)a.c.page | (uintptr_t)a.c.tok | (uintptr_t)a.c.head;
+    const bool even = a.c.head_dim == DC && bits % 16 == 0 && a.c.page_size >= 16;
+    auto kernel = even ? few_rows_kernel<T, DC, NT, true> : few_rows_kernel<T, DC, NT, false>;
+    static std::atomic<uint64_t> ready[2] = {};
+    cudaError_t e = allow_smem(ready[even], (const void*)kernel, kSmem);
     if (e != cudaSuccess) return e;
-    const int ctas = std::min(device_sm_count() * kPerSm4, kMaxCtas4);
-    e = launch_pdl(few_rows_kernel<T, DC, NT>, dim3(ctas), dim3(kThreads4), kSmem, st, a, z, P);
+    const int ctas = std::min(device_sm_count() * few_ctas(NT), kMaxCtas4);
+    e = launch_pdl(kernel, dim3(ctas), dim3(kThreads4), kSmem, st, a, z, P);
     if (e != cudaSuccess) return e;
     return launch_pdl(join_kernel<T, DC>, dim3(ctas, join_blocks(a, P)), dim3(256), 0, st, a, P);
 }

@@ -44,10 +44,9 @@ struct Q4Rows {
     const float* row_scale;
 };
 
-// Global to shared memory, `valid` of `BYTES` bytes (zeros for the others).
 template <int BYTES>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool valid) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(valid ? BYTES : 0) : "memory");
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
 }
 // Where 16-byte unit c of row r of a packed tile lies: eight rows' units touch all banks.
 template <int DC>
@@ -143,100 +142,102 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
     if (warp >= kLoadWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (Q4 && warp < kMmaWarp) {
-            // ---- as below, of 4 bits
+            // ---- as below, of 4 bits.  A lane has keys lane, + 32, + 64, + 96 of every tile: it copies their codes (two tiles ahead, so
+            // that an address is formed once for a key, and no lane waits for another's) and widens them.
             const bool is_v = warp != kLoadWarp;
-            const int box = min(kTileKeys, a.c.page_size), box_keys_log2 = 31 - __clz(box), box_log2 = 7 - box_keys_log2;
-            const uint32_t packs = ring + C::kStages * C::kTile + (is_v ? C::kPacks * C::kPacked : 0);
+            const int page_mask = a.c.page_size - 1;
+            const uint32_t packs = C::kTile * (2 + C::kStages) + (is_v ? C::kPacks * C::kPacked : 0);
+            constexpr int kU = DC / 32, kRows = kTileKeys / 32, kScaleAt = kTileKeys * (DC / 2);
+            // 16-byte copies where every row starts on such a boundary
             const uint8_t* codes = static_cast<const uint8_t*>(is_v ? a.c.v : a.c.k);
             const uint8_t* scales = is_v ? R4.z.vs : R4.z.ks;
-            constexpr int kU = DC / 32, kScaleAt = kTileKeys * (DC / 2);
-            // 16-byte copies where every row starts on such a boundary
             const bool wide = ((reinterpret_cast<uintptr_t>(codes) | (uintptr_t)a.c.page | (uintptr_t)a.c.tok | (uintptr_t)a.c.head | (uintptr_t)(D / 2)) & 15) == 0;
             uint32_t ring0 = 0, issued = 0, used = 0;
             bool ok = true;
             while (ok && W.next(a, P)) {
                 const int n = W.t1 - W.t0, ahead = W.ntok <= P.tt ? 2 : 1, len = W.q.len, kvh = W.heads / P.nsub;
                 const int32_t* table = a.pages + (int64_t)W.s * a.pages_stride;
-                const int per = 32 >> box_log2;  // tiles of 32 boxes
-                auto pages_from = [&](int j) {
-                    const int64_t k = (int64_t)(W.t0 + j) * kTileKeys + lane * box;
-                    int page = -1;
-                    if (k < len && j < n) {
-                        page = __ldg(table + (k >> P.page_log2));
-                        if (page < 0 || page >= a.c.n_pages) {  // reads as zeros
-                            if (a.status) atomicOr(a.status, PPS_FLAG_INDEX);
-                            page = -1;
-                        }
+                const uint8_t* my_codes = codes + kvh * a.c.head;
+                const uint8_t* my_scales = scales + kvh * R4.z.head;
+                int page[kRows];  // of the next tile to copy
+                auto pages_of = [&](int j) {
+#pragma unroll
+                    for (int i = 0; i < kRows; ++i) {
+                        const int64_t k = (int64_t)(W.t0 + j) * kTileKeys + 32 * i + lane;
+                        page[i] = k < len && j < n ? __ldg(table + (k >> P.page_log2)) : 0;
                     }
-                    return page;
                 };
-                int cur = pages_from(0), nxt = pages_from(per);
                 auto issue = [&](int j) {
                     if (j < n) {
-                        if (j > 0 && (j & (per - 1)) == 0) {
-                            cur = nxt;
-                            nxt = pages_from(j + per);
-                        }
-                        const int k0 = (W.t0 + j) * kTileKeys, there = len - k0, box0 = (j & (per - 1)) << box_log2;
-                        const uint32_t dst = packs + (issued % C::kPacks) * C::kPacked;
-#pragma unroll 4
-                        for (int i = 0; i < kTileKeys * kU / 32; ++i) {
-                            const int r = i * (32 / kU) + lane / kU, c = lane % kU;
-                            const int page = __shfl_sync(0xffffffffu, cur, box0 + (r >> box_keys_log2));
-                            const bool row = r < there && page >= 0;
-                            const uint8_t* src = codes + (row ? page * a.c.page + ((k0 + r) & (a.c.page_size - 1)) * a.c.tok + kvh * a.c.head + 16 * c : 0);
-                            const uint32_t to = dst + packed_at<DC>(r, c);
-                            if (wide)
-                                copy_async<16>(to, src, row && 32 * c < D);
-                            else {
-                                copy_async<8>(to, src, row && 32 * c < D);
-                                copy_async<8>(to + 8, src + (row && 32 * c + 16 < D ? 8 : 0), row && 32 * c + 16 < D);
+                        const uint32_t dst = base + packs + (issued % C::kPacks) * C::kPacked;
+#pragma unroll
+                        for (int i = 0; i < kRows; ++i) {
+                            const int r = 32 * i + lane;
+                            const uint32_t st = dst + kScaleAt + 8 * r;
+                            const bool key = (W.t0 + j) * kTileKeys + r < len;
+                            if (!key || page[i] < 0 || page[i] >= a.c.n_pages) {  // no key, or no page: zeros, whatever the codes
+                                if (key && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
+                                asm volatile("st.shared.v2.b32 [%0], {%1, %1};" ::"r"(st), "r"(0) : "memory");
+                                continue;
                             }
-                        }
-#pragma unroll 4
-                        for (int i = 0; i < kTileKeys * (DC / 64) / 32; ++i) {
-                            const int r = i * (32 / (DC / 64)) + lane / (DC / 64), w = lane % (DC / 64);
-                            const int page = __shfl_sync(0xffffffffu, cur, box0 + (r >> box_keys_log2));
-                            const bool row = r < there && page >= 0 && 64 * w < D;
-                            const uint8_t* src = scales + (row ? page * R4.z.page + ((k0 + r) & (a.c.page_size - 1)) * R4.z.tok + kvh * R4.z.head + 4 * w : 0);
-                            copy_async<4>(dst + kScaleAt + r * 8 + 4 * w, src, row);
+                            const int in_page = (int)(((W.t0 + j) * kTileKeys + r) & page_mask);
+                            const uint8_t* src = my_codes + page[i] * a.c.page + in_page * a.c.tok;
+                            if (wide) {
+#pragma unroll
+                                for (int c = 0; c < kU; ++c)
+                                    if (32 * c < D) copy_async<16>(dst + packed_at<DC>(r, c), src + 16 * c);
+                            } else {
+#pragma unroll
+                                for (int c = 0; c < 2 * kU; ++c)
+                                    if (16 * c < D) copy_async<8>(dst + packed_at<DC>(r, c >> 1) + 8 * (c & 1), src + 8 * c);
+                            }
+                            const uint8_t* sp = my_scales + page[i] * R4.z.page + in_page * R4.z.tok;
+#pragma unroll
+                            for (int w = 0; w < DC / 64; ++w)
+                                if (64 * w < D) copy_async<4>(st + 4 * w, sp + 4 * w);
                         }
                         ++issued;
                     }
                     asm volatile("cp.async.commit_group;" ::: "memory");
                 };
+                pages_of(0);
 #pragma unroll 1
-                for (int j = 0; j < C::kPacks - 1; ++j) issue(j);
+                for (int j = 0; j < C::kPacks - 1; ++j) {
+                    issue(j);
+                    pages_of(j + 1);
+                }
 #pragma unroll 1
                 for (int j = 0; j < n; ++j) {
                     issue(j + C::kPacks - 1);
-                    asm volatile("cp.async.wait_group %0;" ::"n"(C::kPacks - 1) : "memory");
-                    __syncwarp();  // of all lanes
+                    pages_of(j + C::kPacks);
+                    asm volatile("cp.async.wait_group %0;" ::"n"(C::kPacks - 1) : "memory");  // of the lane's own keys
                     const uint32_t it = ring0 + (is_v ? (j + ahead < n ? ahead + 2 * j : n + j) : j < ahead ? j : 2 * j - ahead + 1);
                     const uint32_t s = it % C::kStages;
                     if (!(ok = wait_warp(empty(s), ((it / C::kStages) & 1u) ^ 1u, abort))) break;
-                    const uint32_t src = packs + (used++ % C::kPacks) * C::kPacked, dst = ring + s * C::kTile;
-#pragma unroll 1
-                    for (int r = lane; r < kTileKeys; r += 32) {
-                        uint32_t sb[2];
-                        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(sb[0]), "=r"(sb[1]) : "r"(src + kScaleAt + r * 8));
+                    const uint8_t* src = attn_smem + packs + (used++ % C::kPacks) * C::kPacked;
+                    uint8_t* dst = attn_smem + (2 + s) * C::kTile;
+#pragma unroll
+                    for (int i = 0; i < kRows; ++i) {
+                        const int r = 32 * i + lane;
+                        uint4 w[kU];
+                        const uint2 s8 = *reinterpret_cast<const uint2*>(src + kScaleAt + 8 * r);
+                        const uint32_t sb[2] = {s8.x, s8.y};
+#pragma unroll
+                        for (int c = 0; c < kU; ++c) w[c] = *reinterpret_cast<const uint4*>(src + packed_at<DC>(r, c));
 #pragma unroll
                         for (int c = 0; c < kU; ++c) {
-                            uint32_t w[4];
-                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src + packed_at<DC>(r, c)));
                             const uint32_t s2 = q4::scales2(c & 1 ? sb[c >> 1] >> 16 : sb[c >> 1]);
                             // (the bytes behind the last block's may be anything)
                             const uint32_t lo = 32 * c < D ? __byte_perm(s2, 0, 0x1010) : 0u, hi = 32 * c + 16 < D ? __byte_perm(s2, 0, 0x3232) : 0u;
-                            const uint32_t to = dst + (c >> 1) * C::kBlock + r * 128;
+                            uint8_t* to = dst + (c >> 1) * C::kBlock + r * 128;
+                            const uint32_t x[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
 #pragma unroll
                             for (int u = 0; u < 4; ++u) {
                                 uint32_t h[4];
-                                q4::widen8(w[u], h);
+                                q4::widen8(x[u], h);
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) h[e] = q4::mul_halves(h[e], u < 2 ? lo : hi);
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((((c & 1) * 4 + u) ^ (r & 7)) << 4)), "r"(h[0]),
-                                             "r"(h[1]), "r"(h[2]), "r"(h[3])
-                                             : "memory");
+                                *reinterpret_cast<uint4*>(to + ((((c & 1) * 4 + u) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
                             }
                         }
                     }
@@ -244,9 +245,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                     __syncwarp();
                     if (lane == 0) mbar_arrive(full(s));
                 }
+                asm volatile("cp.async.wait_all;" ::: "memory");
                 ring0 += 2 * n;
             }
-            asm volatile("cp.async.wait_all;" ::: "memory");
         } else if (warp < kMmaWarp) {
             // ---- one warp loads the keys' tiles, one the values'.  The ring holds them in the order of their use: K of
             // the first tile (or two, one per stream), then V_j and the next K in turn.
