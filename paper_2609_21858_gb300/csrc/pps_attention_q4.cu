@@ -33,8 +33,9 @@ namespace {
 
 constexpr int kWarps4 = 4, kThreads4 = 32 * kWarps4;
 constexpr int kUnit = 32;         // keys that a warp takes at a time
-constexpr int few_ctas(int nt) { return nt == 1 ? 3 : 2; }  // per SM: 168 or 255 registers
-constexpr int kMaxCtas4 = 480;
+constexpr int kStages4 = 3;       // units of a warp, on their way or in use
+constexpr int few_ctas(int nt) { return nt == 1 ? 4 : 2; }  // per SM: 128 or 255 registers
+constexpr int kMaxCtas4 = 640;
 constexpr int kFix4 = 2;          // key tiles that an item's start and end cost
 constexpr int kLeast4 = 1;
 constexpr float kLazy4 = 8.0f;    // log2 of the rise of a maximum that nothing is rescaled for
@@ -57,33 +58,33 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     return y;
 }
 
-// what a lane holds of 32 keys: eighth e has keys 8e .. 8e + 7
+// A warp's ring in shared memory: stages of 32 keys, each their codes, the values' codes, and the scales of both, row after row.
 template <int DC>
-struct HeldK {
-    static constexpr int kW = DC / 32;  // words of a quarter of a key's codes (4 or 2)
-    uint32_t c[4][kW], s[4];            // key 8e + g: codes, scale bytes
-};
-template <int DC>
-struct HeldV {
-    static constexpr int kW = DC / 64;  // words of an eighth (2 or 1)
-    uint32_t c[8][kW], s[8];            // keys 8e + 2t, 8e + 2t + 1
-};
-// where the four eighths of a unit's keys start (bytes from a head's first row), and whether all 32 keys are there
-struct Places {
-    int64_t codes[4], scales[4];
-    bool whole;
+struct Stage {
+    static constexpr int kRow = DC / 2, kScales = DC / 16;  // bytes of a key
+    static constexpr int kV = kUnit * kRow, kKs = 2 * kV, kVs = kKs + kUnit * kScales, kBytes = kVs + kUnit * kScales;
 };
 
-// EVEN: all DC channels are there, rows start on 16-byte boundaries, and 16 keys in a row share their page
-template <typename T, int DC, int NT, bool EVEN>
+// DENSE: all DC channels are there, 16 keys in a row share their page, and a page's rows of a head follow one another, from 16-byte
+// boundaries on (a page laid out head by head): a stage is eight bulk copies.  Otherwise a lane copies a key's rows.
+template <typename T, int DC, int NT, bool DENSE>
 __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const AttnArgs a, const Q4View z, const AttnPlan P) {
+    using S = Stage<DC>;
     constexpr int R = 8 * NT, RS = DC + 4;  // a row's floats in shared memory: 4 modulo 16, so that lanes (g, t) touch all banks
     __shared__ int64_t s_sum[kWarps4];
     __shared__ Start s_start;
     __shared__ float2 s_ml[kWarps4][R];
     __shared__ float2 s_tot[R];
-    extern __shared__ __align__(16) float s_o[];  // [kWarps4][R][RS]
+    __shared__ uint64_t s_bar[kWarps4][kStages4];
+    __shared__ int s_abort;
+    extern __shared__ __align__(128) uint8_t s_ring[];  // [kWarps4][kStages4] stages; between segments:
+    float* const s_o = reinterpret_cast<float*>(s_ring);  // [kWarps4][R][RS]
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x, g = lane >> 2, t = lane & 3;
+    if (DENSE && tid == 0) {
+        for (int i = 0; i < kWarps4 * kStages4; ++i) mbar_init(smem_u32(&s_bar[0][0] + i), 1);
+        s_abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     pdl_wait();
     pdl_launch_dependents();
     int64_t c0, c1;
@@ -92,12 +93,21 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
     if (c0 >= c1) return;
     const int least = (int)min(max(share / 8, (int64_t)1), (int64_t)kLeast4);
     Walk W(P, s_start, c0, c1, least);
-    const int D = EVEN ? DC : a.c.head_dim;
-    // the lane's place in a row of codes and of scales, for keys and for values; what of its scales' bytes counts
-    const bool k_there = EVEN || t * (DC / 4) < D, k_half = EVEN || t * (DC / 4) + 16 < D, v_there = EVEN || g * (DC / 8) < D;
-    const int64_t k_at = g * a.c.tok + (k_there ? t * (DC / 8) : 0), v_at = 2 * t * a.c.tok + (v_there ? g * (DC / 16) : 0);
-    const int64_t ks_at = g * z.tok + (k_there ? t * (DC / 64) : 0), vs_at = 2 * t * z.tok + (v_there ? (DC == 128 ? g : g >> 1) : 0);
+    const int D = DENSE ? DC : a.c.head_dim;
+    // what of the lane's scale bytes counts
+    const bool k_there = DENSE || t * (DC / 4) < D, k_half = DENSE || t * (DC / 4) + 16 < D, v_there = DENSE || g * (DC / 8) < D;
     const uint32_t k_mask = (k_there ? 0xffu : 0u) | (DC == 128 && k_half ? 0xff00u : 0u), v_mask = v_there ? 0xffu : 0u;
+    uint8_t* const my_ring = s_ring + warp * kStages4 * S::kBytes;
+    const uint32_t ring_at = smem_u32(my_ring), bar_at = smem_u32(&s_bar[warp][0]);
+    const bool wide = ((reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v) | (uintptr_t)a.c.page | (uintptr_t)a.c.tok |
+                        (uintptr_t)a.c.head | (uintptr_t)(D / 2)) & 15) == 0;
+    // of a bulk copy, lane 4 G + kind (keys, values, scales of keys, of values): 16 keys' rows
+    const int kind = lane & 3, G16 = lane >> 2 & 1;
+    const uint8_t* const part = kind == 0 ? static_cast<const uint8_t*>(a.c.k) : kind == 1 ? static_cast<const uint8_t*>(a.c.v) : kind == 2 ? z.ks : z.vs;
+    const int64_t part_page = kind < 2 ? a.c.page : z.page, part_head = kind < 2 ? a.c.head : z.head;
+    const int part_row = kind < 2 ? S::kRow : S::kScales;
+    const uint32_t part_at = (kind == 0 ? 0 : kind == 1 ? S::kV : kind == 2 ? S::kKs : S::kVs) + 16 * G16 * part_row;
+    uint32_t turn = 0;  // stages filled so far; used up: turn less those on their way
 
     while (W.next(a, P)) {
         const int kvh = W.heads / P.nsub, sub = W.heads - kvh * P.nsub;
@@ -109,100 +119,78 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
         const int end = a.mask ? len : prefix + W.i0 + W.ntok;  // keys from it on by none
         const int first = W.t0 * kTileKeys, last = min(W.t1 * kTileKeys, end);
         const int32_t* table = a.pages + (int64_t)W.s * a.pages_stride;
-        const uint8_t* const kp = static_cast<const uint8_t*>(a.c.k) + kvh * a.c.head + k_at;
-        const uint8_t* const vp = static_cast<const uint8_t*>(a.c.v) + kvh * a.c.head + v_at;
-        const uint8_t* const ksp = z.ks + kvh * z.head + ks_at;
-        const uint8_t* const vsp = z.vs + kvh * z.head + vs_at;
 
-        // pages of the eighths of the unit from key k0 on, in lanes 0 to 3 (and again in the others)
-        auto pages_of = [&](int k0) {
-            const int k = k0 + 8 * t;
+        // the lane's page of the unit from key k0 on: of half G16, or of key `lane`
+        auto page_of = [&](int k0) {
+            const int k = k0 + (DENSE ? 16 * G16 : lane);
             return k < last ? __ldg(table + (k >> P.page_log2)) : 0;
         };
-        auto places_of = [&](Places& x, int k0, int page) {
-            const bool key = k0 + 8 * t < last, good = !key || (page >= 0 && page < a.c.n_pages);
-            if (!good) {  // reads as zeros
-                if (a.status) atomicOr(a.status, PPS_FLAG_INDEX);
-                page = -1;
-            }
-            x.whole = __all_sync(0xffffffffu, good) && k0 + kUnit <= last;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (EVEN && (e & 1)) {
-                    x.codes[e] = x.codes[e - 1] + 8 * a.c.tok;
-                    x.scales[e] = x.scales[e - 1] + 8 * z.tok;
-                } else {
-                    const int p = __shfl_sync(0xffffffffu, page, e), in_page = (k0 + 8 * e) & (a.c.page_size - 1);
-                    x.codes[e] = p < 0 ? -1 : p * a.c.page + in_page * a.c.tok;
-                    x.scales[e] = p * z.page + in_page * z.tok;
-                }
-            }
-        };
-        // (keys past the last, and those of a missing page: codes of anything, scales of zero)
-        auto fetch_k = [&](HeldK<DC>& x, const Places& at, int k0) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const bool there = at.whole || (k0 + 8 * e + g < last && at.codes[EVEN ? e & 2 : e] >= 0);
-                x.s[e] = 0;
-#pragma unroll
-                for (int i = 0; i < HeldK<DC>::kW; ++i) x.c[e][i] = 0;
-                if (there) {
-                    const uint8_t* src = kp + at.codes[e];
-                    if constexpr (EVEN && DC == 128) {
-                        const uint4 w = __ldg(reinterpret_cast<const uint4*>(src));
-                        x.c[e][0] = w.x;
-                        x.c[e][1] = w.y;
-                        x.c[e][HeldK<DC>::kW - 2] = w.z;
-                        x.c[e][HeldK<DC>::kW - 1] = w.w;
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < HeldK<DC>::kW; i += 2) {
-                            const uint2 w = __ldg(reinterpret_cast<const uint2*>(src) + (k_half ? i / 2 : 0));
-                            x.c[e][i] = w.x;
-                            x.c[e][i + 1] = w.y;
-                        }
-                    }
-                    if constexpr (DC == 128)
-                        x.s[e] = __ldg(reinterpret_cast<const uint16_t*>(ksp + at.scales[e])) & k_mask;
+        uint32_t halves = 0;  // a bit per half of the units on their way, the newest lowest: its page is there
+        auto fill = [&](int k0, int page) {
+            const uint32_t st = turn % kStages4, to = ring_at + st * S::kBytes;
+            ++turn;
+            const int k = k0 + (DENSE ? 16 * G16 : lane), in_page = k & (a.c.page_size - 1);
+            const bool key = k < last, good = key && page >= 0 && page < a.c.n_pages;  // (a missing page reads as zeros)
+            if (key && !good && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
+            if constexpr (DENSE) {
+                const uint32_t who = __ballot_sync(0xffffffffu, good), two = (who & 1u) | (who >> 3 & 2u);
+                halves = halves << 2 | two;
+                if (lane == 0) {
+                    const uint32_t bytes = __popc(two) * 16 * 2 * (S::kRow + S::kScales);
+                    if (bytes)
+                        mbar_expect_tx(bar_at + 8 * st, bytes);
                     else
-                        x.s[e] = __ldg(ksp + at.scales[e]) & k_mask;
+                        mbar_arrive(bar_at + 8 * st);
+                }
+                __syncwarp();
+                if (lane < 8 && good)
+                    bulk_load(to + part_at, part + page * part_page + kvh * part_head + in_page * part_row, 16 * part_row, bar_at + 8 * st);
+            } else {
+                const uint32_t rows = to + lane * S::kRow, scales = to + S::kKs + lane * S::kScales;
+                if (good) {
+                    const int64_t at = page * a.c.page + in_page * a.c.tok + kvh * a.c.head, st4 = page * z.page + in_page * z.tok + kvh * z.head;
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) {
+                        const uint8_t* src = static_cast<const uint8_t*>(v ? a.c.v : a.c.k) + at;
+                        const uint8_t* sp = (v ? z.vs : z.ks) + st4;
+                        if (wide) {
+#pragma unroll
+                            for (int c = 0; c < DC / 32; ++c)
+                                if (32 * c < D) copy_async<16>(rows + v * S::kV + 16 * c, src + 16 * c);
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < DC / 16; ++c)
+                                if (16 * c < D) copy_async<8>(rows + v * S::kV + 8 * c, src + 8 * c);
+                        }
+#pragma unroll
+                        for (int c = 0; c < DC / 64; ++c)
+                            if (64 * c < D) copy_async<4>(scales + v * (S::kVs - S::kKs) + 4 * c, sp + 4 * c);
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < DC / 64; ++c) {  // scales of zero, whatever the codes
+                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(scales + 4 * c), "r"(0) : "memory");
+                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(scales + S::kVs - S::kKs + 4 * c), "r"(0) : "memory");
+                    }
                 }
             }
         };
-        auto fetch_v = [&](HeldV<DC>& x, const Places& at, int k0) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const bool there = at.whole || (k0 + 8 * e + 2 * t + j < last && at.codes[EVEN ? e & 2 : e] >= 0);
-                    x.s[2 * e + j] = 0;
-#pragma unroll
-                    for (int i = 0; i < HeldV<DC>::kW; ++i) x.c[2 * e + j][i] = 0;
-                    if (there) {
-                        const uint8_t* src = vp + at.codes[e] + j * a.c.tok;
-                        if constexpr (DC == 128) {
-                            const uint2 w = __ldg(reinterpret_cast<const uint2*>(src));
-                            x.c[2 * e + j][0] = w.x;
-                            x.c[2 * e + j][HeldV<DC>::kW - 1] = w.y;
-                        } else
-                            x.c[2 * e + j][0] = __ldg(reinterpret_cast<const uint32_t*>(src));
-                        x.s[2 * e + j] = __ldg(vsp + at.scales[e] + j * z.tok) & v_mask;
-                    }
-                }
+        auto close = [&]() {  // a group of copies per unit, with or without any
+            if constexpr (!DENSE) asm volatile("cp.async.commit_group;" ::: "memory");
         };
-
-        constexpr int kStep = kUnit * kWarps4;
+        constexpr int kStep = kUnit * kWarps4, kAhead4 = kStages4 - 1;
         int k0 = first + warp * kUnit;
-        HeldK<DC> kh;
-        HeldV<DC> vh;
-        Places at;
-        int pages = 0;
-        if (k0 < last) {
-            const int p = pages_of(k0);
-            pages = pages_of(k0 + kStep);
-            places_of(at, k0, p);
-            fetch_k(kh, at, k0);
-            fetch_v(vh, at, k0);
+        const int k_start = k0;
+        int pages = k0 < last ? page_of(k0) : 0;
+#pragma unroll
+        for (int i = 0; i < kAhead4; ++i) {
+            const int k = k_start + i * kStep, p = pages;
+            pages = page_of(k + kStep);
+            if (k < last)
+                fill(k, p);
+            else
+                halves <<= 2;
+            close();
         }
         // ---- queries: row 8 nt + g, the channels of quarter t, as halves
         uint32_t qf[NT][DC / 8];
@@ -256,26 +244,58 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.0f;
 
-        while (k0 < last) {
-            const int key0 = k0;
-            k0 += kStep;
-            const int page_next = pages;
-            pages = pages_of(k0 + kStep);
+        uint32_t used = turn - min(max((last - k_start + kStep - 1) / kStep, 0), kAhead4);
+#pragma unroll 1
+        for (; k0 < last; k0 += kStep) {
+            const int key0 = k0, ahead = k0 + kAhead4 * kStep, page = pages;
+            pages = page_of(ahead + kStep);
+            __syncwarp();  // the stage that is filled now has been read
+            if (ahead < last)
+                fill(ahead, page);
+            else
+                halves <<= 2;
+            close();
+            const uint32_t st = used % kStages4;
+            if constexpr (DENSE)
+                mbar_wait(bar_at + 8 * st, used / kStages4 & 1u, &s_abort);
+            else
+                asm volatile("cp.async.wait_group %0;" ::"n"(kAhead4) : "memory");
+            __syncwarp();
+            ++used;
+            const uint8_t* const unit = my_ring + st * S::kBytes;
+            // keys that are not there, or lie on a missing page, have scales of zero
+            uint32_t there = 0xffffffffu;
+            if constexpr (DENSE) {
+                const uint32_t two = halves >> (2 * kAhead4) & 3u;
+                if (k0 + kUnit > last || two != 3u) {
+                    const int n = last - k0;
+                    there = (n >= 32 ? 0xffffffffu : (1u << n) - 1u) & ((two & 1u ? 0xffffu : 0u) | (two & 2u ? 0xffff0000u : 0u));
+                }
+            }
             float s[NT][2][4];
 #pragma unroll
             for (int G = 0; G < 2; ++G) {
                 uint32_t h[2][DC / 8];  // the quarter of keys 16 G + g and 16 G + 8 + g
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const int e = 2 * G + j;
-                    const uint32_t s2 = q4::scales2(kh.s[e]);
+                    const int key = 16 * G + 8 * j + g;
+                    uint32_t c[DC / 32];
+                    if constexpr (DC == 128)
+                        *reinterpret_cast<uint4*>(c) = *reinterpret_cast<const uint4*>(unit + key * S::kRow + 16 * t);
+                    else
+                        *reinterpret_cast<uint2*>(c) = *reinterpret_cast<const uint2*>(unit + key * S::kRow + 8 * t);
+                    const uint8_t* sp = unit + S::kKs + key * S::kScales + t * (DC / 64);
+                    uint32_t sb = DC == 128 ? *reinterpret_cast<const uint16_t*>(sp) : *sp;
+                    if (!DENSE) sb &= k_mask;
+                    if (DENSE && there != 0xffffffffu) sb = there >> key & 1u ? sb : 0u;
+                    const uint32_t s2 = q4::scales2(sb);
                     const uint32_t lo = __byte_perm(s2, 0, 0x1010), hi = __byte_perm(s2, 0, 0x3232);
 #pragma unroll
-                    for (int i = 0; i < HeldK<DC>::kW; ++i) {
+                    for (int i = 0; i < DC / 32; ++i) {
                         uint32_t w[4];
-                        q4::widen8(kh.c[e][i], w);
+                        q4::widen8(c[i], w);
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) h[j][4 * i + c] = q4::mul_halves(w[c], i < 2 ? lo : hi);
+                        for (int e = 0; e < 4; ++e) h[j][4 * i + e] = q4::mul_halves(w[e], i < 2 ? lo : hi);
                     }
                 }
 #pragma unroll
@@ -287,10 +307,6 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                         mma16816(s[nt][G], A, qf[nt][2 * i], qf[nt][2 * i + 1]);
                     }
                 }
-            }
-            if (k0 < last) {  // the next unit's keys take the place of those that are used up
-                places_of(at, k0, page_next);
-                fetch_k(kh, at, k0);
             }
             // scores of the lane: keys 16 G + 8 (e >> 1) + g, rows 8 nt + 2t + (e & 1)
             const bool odd_scale = P.s_xor != 0 || P.s_and == 0;
@@ -349,28 +365,42 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
             }
 #pragma unroll
             for (int G = 0; G < 2; ++G) {
-                uint32_t s2[2];
+                uint32_t c[2][2][DC / 64], s2[2];  // of keys 16 G + 8 j + 2t, + 1
 #pragma unroll
-                for (int j = 0; j < 2; ++j) s2[j] = q4::scales2(vh.s[4 * G + 2 * j] | vh.s[4 * G + 2 * j + 1] << 8);
+                for (int j = 0; j < 2; ++j) {
+                    uint32_t sb[2];
 #pragma unroll
-                for (int w = 0; w < HeldV<DC>::kW; ++w) {
+                    for (int i = 0; i < 2; ++i) {
+                        const int key = 16 * G + 8 * j + 2 * t + i;
+                        const uint8_t* src = unit + S::kV + key * S::kRow + g * (DC / 16);
+                        if constexpr (DC == 128)
+                            *reinterpret_cast<uint2*>(c[j][i]) = *reinterpret_cast<const uint2*>(src);
+                        else
+                            c[j][i][0] = *reinterpret_cast<const uint32_t*>(src);
+                        sb[i] = unit[S::kVs + key * S::kScales + (DC == 128 ? g : g >> 1)];
+                        if (!DENSE) sb[i] &= v_mask;
+                        if (DENSE && there != 0xffffffffu) sb[i] = there >> key & 1u ? sb[i] : 0u;
+                    }
+                    s2[j] = q4::scales2(sb[0] | sb[1] << 8);
+                }
+#pragma unroll
+                for (int w = 0; w < DC / 64; ++w) {
                     uint32_t lo[2][4], hi[2][4];  // the word's even and odd channels of two keys
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const uint32_t x0 = vh.c[4 * G + 2 * j][w], x1 = vh.c[4 * G + 2 * j + 1][w];
+                        const uint32_t x0 = c[j][0][w], x1 = c[j][1][w];
                         q4::widen8((x0 & 0x0f0f0f0fu) | (x1 << 4 & 0xf0f0f0f0u), lo[j]);
                         q4::widen8((x0 >> 4 & 0x0f0f0f0fu) | (x1 & 0xf0f0f0f0u), hi[j]);
                     }
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const uint32_t A[4] = {q4::mul_halves(lo[0][c], s2[0]), q4::mul_halves(hi[0][c], s2[0]),
-                                               q4::mul_halves(lo[1][c], s2[1]), q4::mul_halves(hi[1][c], s2[1])};
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t A[4] = {q4::mul_halves(lo[0][e], s2[0]), q4::mul_halves(hi[0][e], s2[0]),
+                                               q4::mul_halves(lo[1][e], s2[1]), q4::mul_halves(hi[1][e], s2[1])};
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w + c], A, p[nt][2 * G], p[nt][2 * G + 1]);
+                        for (int nt = 0; nt < NT; ++nt) mma16816(o[nt][4 * w + e], A, p[nt][2 * G], p[nt][2 * G + 1]);
                     }
                 }
             }
-            if (k0 < last) fetch_v(vh, at, k0);
         }
 
         // ---- the segment's result: the warps' parts, joined
@@ -392,7 +422,7 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
             if (l[r] != l[r]) m[r] = INFINITY;  // a score that is not a number, or infinite: so is the row, whatever it is joined with
             if (g == 0) s_ml[warp][8 * (r >> 1) + 2 * t + (r & 1)] = make_float2(m[r], l[r]);
         }
-        __syncthreads();
+        __syncthreads();  // (the rings are read)
 #pragma unroll
         for (int r = 0; r < 2 * NT; ++r) {
             const int row = 8 * (r >> 1) + 2 * t + (r & 1);
@@ -440,8 +470,10 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                 if (at == 0) P.part_ml[to] = ml;
             }
         }
-        __syncthreads();  // s_ml, s_o and s_tot are free
+        fence_async_smem();
+        __syncthreads();  // s_ml, s_tot and the rings are free
     }
+    if (DENSE && tid == 0 && *static_cast<volatile int*>(&s_abort) && a.status) atomicOr(a.status, PPS_FLAG_TIMEOUT);
 }
 
 // the rows of a block, the heads taken at a time, the tokens of a block: by the mean number of tokens of a sequence
@@ -469,12 +501,13 @@ cudaError_t launch_few(const AttnArgs& a, const Q4View& z, const Rows4& rows, cu
     P.shift = kShift4;
     plan_common(P, a);
     carve(P, a.ws, kMaxCtas4);
-    constexpr int kSmem = kWarps4 * 8 * NT * (DC + 4) * 4;
-    const uintptr_t bits = reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v) | (uintptr_t)a.c.page | (uintptr_t)a.c.tok | (uintptr_t)a.c.head;
-    const bool even = a.c.head_dim == DC && bits % 16 == 0 && a.c.page_size >= 16;
-    auto kernel = even ? few_rows_kernel<T, DC, NT, true> : few_rows_kernel<T, DC, NT, false>;
+    constexpr int kSmem = std::max(kWarps4 * 8 * NT * (DC + 4) * 4, kWarps4 * kStages4 * Stage<DC>::kBytes);
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v) | reinterpret_cast<uintptr_t>(z.ks) |
+                           reinterpret_cast<uintptr_t>(z.vs) | (uintptr_t)a.c.page | (uintptr_t)a.c.head | (uintptr_t)z.page | (uintptr_t)z.head;
+    const bool dense = a.c.head_dim == DC && a.c.page_size >= 16 && a.c.tok == DC / 2 && z.tok == DC / 16 && bits % 16 == 0;
+    auto kernel = dense ? few_rows_kernel<T, DC, NT, true> : few_rows_kernel<T, DC, NT, false>;
     static std::atomic<uint64_t> ready[2] = {};
-    cudaError_t e = allow_smem(ready[even], (const void*)kernel, kSmem);
+    cudaError_t e = allow_smem(ready[dense], (const void*)kernel, kSmem);
     if (e != cudaSuccess) return e;
     const int ctas = std::min(device_sm_count() * few_ctas(NT), kMaxCtas4);
     e = launch_pdl(kernel, dim3(ctas), dim3(kThreads4), kSmem, st, a, z, P);
