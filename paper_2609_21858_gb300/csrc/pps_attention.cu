@@ -101,7 +101,7 @@ cudaError_t launch(const AttnArgs& a, int dtype, cudaStream_t st) {
     cudaError_t e = allow_smem(ready, (const void*)attention_kernel<T, DC, false>, Cfg<DC, false>::kSmem);
     if (e != cudaSuccess) return e;
     const int ctas = std::min(device_sm_count(), kMaxCtas);
-    e = launch_pdl(attention_kernel<T, DC, false>, dim3(ctas), dim3(kAttnThreads), Cfg<DC, false>::kSmem, st, tmQ, tmK, tmV, a, P, Q4Rows());
+    e = launch_pdl(attention_kernel<T, DC, false>, dim3(ctas), dim3(Cfg<DC, false>::kThreads), Cfg<DC, false>::kSmem, st, tmQ, tmK, tmV, a, P, Q4Rows());
     if (e != cudaSuccess) return e;
     return launch_pdl(join_kernel<T, DC>, dim3(ctas, join_blocks(a, P)), dim3(256), 0, st, a, P);
 }

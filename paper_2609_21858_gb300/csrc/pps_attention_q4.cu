@@ -52,6 +52,11 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma16816_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {  // c = a b
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     uint32_t y;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -229,12 +234,14 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
             }
         }
         // of the lane's rows 8 nt + 2t, + 1 (an odd index: the second)
-        float sc[2 * NT], m[2 * NT], l[2 * NT];
+        // m: maximum in use; limit: a score past it raises it; neg: what is added to a score times sc
+        float sc[2 * NT], m[2 * NT], l[2 * NT], limit[2 * NT], neg[2 * NT];
 #pragma unroll
         for (int r = 0; r < 2 * NT; ++r) {
             sc[r] = __shfl_sync(0xffffffffu, row_sc[r >> 1], 4 * (2 * t + (r & 1)));
-            m[r] = -INFINITY;
+            m[r] = limit[r] = -INFINITY;
             l[r] = 0.0f;
+            neg[r] = kShift4;
         }
         float o[NT][DC / 16][4];
 #pragma unroll
@@ -262,14 +269,19 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                 asm volatile("cp.async.wait_group %0;" ::"n"(kAhead4) : "memory");
             __syncwarp();
             ++used;
-            const uint8_t* const unit = my_ring + st * S::kBytes;
-            // keys that are not there, or lie on a missing page, have scales of zero
-            uint32_t there = 0xffffffffu;
-            if constexpr (DENSE) {
+            uint8_t* const unit = my_ring + st * S::kBytes;
+            if constexpr (DENSE) {  // keys that are not there, or lie on a missing page, get scales of zero
                 const uint32_t two = halves >> (2 * kAhead4) & 3u;
                 if (k0 + kUnit > last || two != 3u) {
-                    const int n = last - k0;
-                    there = (n >= 32 ? 0xffffffffu : (1u << n) - 1u) & ((two & 1u ? 0xffffu : 0u) | (two & 2u ? 0xffff0000u : 0u));
+                    if (k0 + lane >= last || !(two >> (lane >> 4) & 1u)) {
+#pragma unroll
+                        for (int i = 0; i < S::kScales; i += 4) {
+                            *reinterpret_cast<uint32_t*>(unit + S::kKs + lane * S::kScales + i) = 0;
+                            *reinterpret_cast<uint32_t*>(unit + S::kVs + lane * S::kScales + i) = 0;
+                        }
+                    }
+                    fence_async_smem();  // (before the stage's next copies)
+                    __syncwarp();
                 }
             }
             float s[NT][2][4];
@@ -287,7 +299,6 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                     const uint8_t* sp = unit + S::kKs + key * S::kScales + t * (DC / 64);
                     uint32_t sb = DC == 128 ? *reinterpret_cast<const uint16_t*>(sp) : *sp;
                     if (!DENSE) sb &= k_mask;
-                    if (DENSE && there != 0xffffffffu) sb = there >> key & 1u ? sb : 0u;
                     const uint32_t s2 = q4::scales2(sb);
                     const uint32_t lo = __byte_perm(s2, 0, 0x1010), hi = __byte_perm(s2, 0, 0x3232);
 #pragma unroll
@@ -300,11 +311,13 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    s[nt][G][0] = s[nt][G][1] = s[nt][G][2] = s[nt][G][3] = 0.0f;
 #pragma unroll
                     for (int i = 0; i < DC / 16; ++i) {
                         const uint32_t A[4] = {h[0][2 * i], h[1][2 * i], h[0][2 * i + 1], h[1][2 * i + 1]};
-                        mma16816(s[nt][G], A, qf[nt][2 * i], qf[nt][2 * i + 1]);
+                        if (i == 0)
+                            mma16816_first(s[nt][G], A, qf[nt][0], qf[nt][1]);
+                        else
+                            mma16816(s[nt][G], A, qf[nt][2 * i], qf[nt][2 * i + 1]);
                     }
                 }
             }
@@ -331,7 +344,7 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
             for (int r = 0; r < 2 * NT; ++r) {
                 const float(&y)[2][4] = s[r >> 1];
                 top[r] = fmaxf(max3(y[0][r & 1], y[0][2 + (r & 1)], y[1][r & 1]), y[1][2 + (r & 1)]);
-                rises |= (top[r] - m[r]) * sc[r] > kLazy4;
+                rises |= top[r] > limit[r];
             }
             if (__any_sync(0xffffffffu, rises)) {
 #pragma unroll
@@ -341,6 +354,8 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                     const float M = fmaxf(m[r], top[r]), f = m[r] == M ? 1.0f : ex2((m[r] - M) * sc[r]);
                     m[r] = M;
                     l[r] *= f;
+                    limit[r] = M + kLazy4 / sc[r];
+                    neg[r] = (M == -INFINITY ? 0.0f : -M * sc[r]) + kShift4;
 #pragma unroll
                     for (int i = 0; i < DC / 16; ++i) {
                         o[r >> 1][i][r & 1] *= f;
@@ -351,13 +366,10 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
             uint32_t p[NT][4];  // the operand P^T: rows 8 nt + g, keys 8 e + 2t, + 1
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                float neg[2];
-#pragma unroll
-                for (int r = 0; r < 2; ++r) neg[r] = (m[2 * nt + r] == -INFINITY ? 0.0f : -m[2 * nt + r] * sc[2 * nt + r]) + kShift4;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float x0 = ex2(fmaf(s[nt][e >> 1][2 * (e & 1)], sc[2 * nt], neg[0]));
-                    const float x1 = ex2(fmaf(s[nt][e >> 1][2 * (e & 1) + 1], sc[2 * nt + 1], neg[1]));
+                    const float x0 = ex2(fmaf(s[nt][e >> 1][2 * (e & 1)], sc[2 * nt], neg[2 * nt]));
+                    const float x1 = ex2(fmaf(s[nt][e >> 1][2 * (e & 1) + 1], sc[2 * nt + 1], neg[2 * nt + 1]));
                     l[2 * nt] += x0;
                     l[2 * nt + 1] += x1;
                     p[nt][e] = transpose8x8(Half<__half>::pack(x0, x1));
@@ -379,7 +391,6 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                             c[j][i][0] = *reinterpret_cast<const uint32_t*>(src);
                         sb[i] = unit[S::kVs + key * S::kScales + (DC == 128 ? g : g >> 1)];
                         if (!DENSE) sb[i] &= v_mask;
-                        if (DENSE && there != 0xffffffffu) sb[i] = there >> key & 1u ? sb[i] : 0u;
                     }
                     s2[j] = q4::scales2(sb[0] | sb[1] << 8);
                 }
@@ -476,6 +487,13 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
     if (DENSE && tid == 0 && *static_cast<volatile int*>(&s_abort) && a.status) atomicOr(a.status, PPS_FLAG_TIMEOUT);
 }
 
+// Whether a head's rows of a page follow one another, codes and scales, all of them of dc channels, from 16-byte boundaries on.
+bool is_dense(const AttnArgs& a, const Q4View& z, int dc) {
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v) | reinterpret_cast<uintptr_t>(z.ks) |
+                           reinterpret_cast<uintptr_t>(z.vs) | (uintptr_t)a.c.page | (uintptr_t)a.c.head | (uintptr_t)z.page | (uintptr_t)z.head;
+    return a.c.head_dim == dc && a.c.tok == dc / 2 && z.tok == dc / 16 && bits % 16 == 0;
+}
+
 // the rows of a block, the heads taken at a time, the tokens of a block: by the mean number of tokens of a sequence
 struct Rows4 {
     int nt, nsub, gs, tt;
@@ -502,9 +520,7 @@ cudaError_t launch_few(const AttnArgs& a, const Q4View& z, const Rows4& rows, cu
     plan_common(P, a);
     carve(P, a.ws, kMaxCtas4);
     constexpr int kSmem = std::max(kWarps4 * 8 * NT * (DC + 4) * 4, kWarps4 * kStages4 * Stage<DC>::kBytes);
-    const uintptr_t bits = reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v) | reinterpret_cast<uintptr_t>(z.ks) |
-                           reinterpret_cast<uintptr_t>(z.vs) | (uintptr_t)a.c.page | (uintptr_t)a.c.head | (uintptr_t)z.page | (uintptr_t)z.head;
-    const bool dense = a.c.head_dim == DC && a.c.page_size >= 16 && a.c.tok == DC / 2 && z.tok == DC / 16 && bits % 16 == 0;
+    const bool dense = is_dense(a, z, DC) && a.c.page_size >= 16;
     auto kernel = dense ? few_rows_kernel<T, DC, NT, true> : few_rows_kernel<T, DC, NT, false>;
     static std::atomic<uint64_t> ready[2] = {};
     cudaError_t e = allow_smem(ready[dense], (const void*)kernel, kSmem);
@@ -567,7 +583,7 @@ cudaError_t launch_tiles(const AttnArgs& given, const Q4View& z, cudaStream_t st
     plan_common(P, a);
     carve(P, a.ws, kMaxCtas);
     const int ctas = std::min(device_sm_count(), kMaxCtas);
-    Q4Rows r4 = {z, nullptr};
+    Q4Rows r4 = {z, nullptr, is_dense(a, z, DC)};
     if constexpr (std::is_same_v<T, __nv_bfloat16>) {
         char* w = static_cast<char*>(a.ws) + parts4_bytes(a.n_tok, P.group, a.c.head_dim);
         __half* halves = reinterpret_cast<__half*>(w);
@@ -584,7 +600,7 @@ cudaError_t launch_tiles(const AttnArgs& given, const Q4View& z, cudaStream_t st
     static std::atomic<uint64_t> ready{0};
     cudaError_t e = allow_smem(ready, (const void*)attention_kernel<T, DC, true>, kSmem);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(attention_kernel<T, DC, true>, dim3(ctas), dim3(kAttnThreads), kSmem, st, tmQ, tmQ, tmQ, a, P, r4);
+    e = launch_pdl(attention_kernel<T, DC, true>, dim3(ctas), dim3(Cfg<DC, true>::kThreads), kSmem, st, tmQ, tmQ, tmQ, a, P, r4);
     if (e != cudaSuccess) return e;
     return launch_pdl(join_kernel<T, DC>, dim3(ctas, join_blocks(a, P)), dim3(256), 0, st, a, P);
 }

@@ -13,9 +13,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kAttnThreads = 384;  // two softmax warpgroups; warps that load keys, values, issue products, load queries
-constexpr int kLoadWarp = 8, kMmaWarp = 10, kQueryWarp = 11;
-static_assert(32 * (kQueryWarp + 1) == kAttnThreads, "the last warp loads the queries");
+constexpr int kLoadWarp = 8;       // the first after two softmax warpgroups
 constexpr int kMaxCtas = 160;      // shares of the work (one per SM)
 // Key tiles that an item's start and end cost.  (2, 3, 4: decoding batches and ragged chunks 1 to 3 percent faster, trees 3 to 11
 // and one long sequence 4 to 6 percent slower.)
@@ -29,33 +27,31 @@ template <int DC, bool Q4>
 struct Cfg {
     static constexpr int kBlock = 128 * 128;                 // 128 rows of 64 channels, 128-byte swizzle
     static constexpr int kTile = kBlock * (DC / 64);         // 16 or 32 KB: a tile of Q, K or V
-    static constexpr int kPacked = Q4 ? 128 * (DC / 2) + 128 * 8 : 0;  // a tile of codes, and its scales (8 bytes a key)
-    static constexpr int kPacks = 3;                         // of keys, and of values, on their way
+    // warps that load keys, then as many that load values; one that issues products, one that loads queries
+    static constexpr int kLoaders = Q4 ? 2 : 1;
+    // (each quarter of the SM gets as many warps of a kind as the others: 14 become 16)
+    static constexpr int kMmaWarp = kLoadWarp + 2 * kLoaders, kQueryWarp = kMmaWarp + 1, kThreads = (32 * (kQueryWarp + 1) + 127) / 128 * 128;
+    static constexpr int kLoadRows = 128 / kLoaders;         // keys of a tile that a loading warp has
+    // of 4 bits: their codes, then their scales, as they come; how many such are on their way to a warp
+    static constexpr int kRow = DC / 2, kScales = DC / 16, kPack = kLoadRows * (kRow + kScales), kPacks = 3;
     // tiles of K and V in flight: 5 (or 12); of 4 bits 3 (or 6)
     static constexpr int kStages = Q4 ? 3 * 128 / DC : (224 * 1024 - 2 * kTile) / kTile;
-    static constexpr int kBars = (2 + kStages) * kTile + 2 * kPacks * kPacked;
+    static constexpr int kBars = (2 + kStages) * kTile + (Q4 ? 2 * kLoaders * kPacks * kPack : 0);
     static constexpr int kSmem = kBars + 320 /* barriers */ + 224 /* plan */ + 2048 /* maxima and sums */;
-    static_assert(8 * (2 * kStages + 13) <= 320 && kSmem <= 227 * 1024, "barriers and shared memory fit");
+    static_assert(8 * (2 * kStages + 13 + (Q4 ? 2 * kLoaders * kPacks : 0)) <= 320 && kSmem <= 227 * 1024, "barriers and shared memory fit");
 };
 
 // beside the cache, for 4 bits: scales and units; a factor per row (token, head) on its scores, null: ones
 struct Q4Rows {
     Q4View z;
     const float* row_scale;
+    bool dense;  // all DC channels, and a page's rows of a head follow one another, codes and scales, from 16-byte boundaries on
 };
 
 template <int BYTES>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
 }
-// Where 16-byte unit c of row r of a packed tile lies: eight rows' units touch all banks.
-template <int DC>
-__device__ __forceinline__ uint32_t packed_at(int r, int c) {
-    constexpr int kU = DC / 32;  // units per row
-    const int line = r / (8 / kU);
-    return (uint32_t)(line * 128 + ((((r % (8 / kU)) * kU + c) ^ (line & 7)) << 4));
-}
-
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort) {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort));
 }
@@ -63,11 +59,12 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatil
 // T: of the result, and but for Q4 of all operands.  Q4: queries are halves (with a factor per row), the cache has 4 bits: the loading
 // warps copy a tile's codes ahead, widen them and write the tile as TMA would have.
 template <typename T, int DC, bool Q4>
-__global__ void __launch_bounds__(kAttnThreads, 1)
+__global__ void __launch_bounds__(Cfg<DC, Q4>::kThreads, 1)
     attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                      const __grid_constant__ CUtensorMap tmV, const AttnArgs a, const AttnPlan P, const Q4Rows R4) {
     using C = Cfg<DC, Q4>;
     using H = Half<std::conditional_t<Q4, __half, T>>;
+    constexpr int kMmaWarp = C::kMmaWarp;
     extern __shared__ __align__(1024) uint8_t attn_smem[];
     const uint32_t base = smem_u32(attn_smem);
     const uint32_t ring = base + 2 * C::kTile;
@@ -81,18 +78,19 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
     auto qfull = [&](uint32_t t) { return bar(2 * C::kStages + 6 + t); };
     auto qfree = [&](uint32_t t) { return bar(2 * C::kStages + 8 + t); };
     const uint32_t segbar = bar(2 * C::kStages + 10);
+    auto packed = [&](uint32_t w, uint32_t p) { return bar(2 * C::kStages + 13 + w * C::kPacks + p); };  // of loading warp w
     uint8_t* tail = attn_smem + C::kBars + 320;
     volatile int* abort = reinterpret_cast<volatile int*>(tail);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 4);
-    int64_t* s_sum = reinterpret_cast<int64_t*>(tail + 16);          // [12] warp sums
-    Start* s_start = reinterpret_cast<Start*>(tail + 16 + 12 * 8);
+    int64_t* s_sum = reinterpret_cast<int64_t*>(tail + 16);          // a sum per warp
+    Start* s_start = reinterpret_cast<Start*>(tail + 16 + 16 * 8);
     float2* s_ml = reinterpret_cast<float2*>(tail + 224);            // [2][128]
-    static_assert(16 + 12 * 8 + sizeof(Start) <= 224, "plan fits");
+    static_assert(C::kThreads <= 16 * 32 && 16 + 16 * 8 + sizeof(Start) <= 224, "plan fits");
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
     if (tid == 0) {
         for (int s = 0; s < C::kStages; ++s) {
-            mbar_init(full(s), 1);
+            mbar_init(full(s), C::kLoaders);
             mbar_init(empty(s), 1);
         }
         for (int w = 0; w < 2; ++w) {
@@ -106,6 +104,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             mbar_init(qfree(t), 1);
         }
         mbar_init(segbar, 8);
+        if constexpr (Q4)
+            for (int i = 0; i < 2 * C::kLoaders * C::kPacks; ++i) mbar_init(packed(0, i), 1);
         *abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
     pdl_launch_dependents();
     // the share of the line of costs, and where on it the share starts
     int64_t c0, c1;
-    const int64_t share = find_share<kAttnThreads>(a, P, s_sum, s_start, c0, c1);
+    const int64_t share = find_share<C::kThreads>(a, P, s_sum, s_start, c0, c1);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -138,67 +138,97 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
     Walk W(P, *s_start, c0, c1, least);
     const int D = a.c.head_dim;
 
-    // registers: 384 x 168 at launch = 256 x 216 + 128 x 72
+    // registers: 384 x 168 at launch = 256 x 216 + 128 x 72; of 4 bits 512 x 128 = 256 x 192 + 256 x 64
     if (warp >= kLoadWarp) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if constexpr (Q4)
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        else
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (Q4 && warp < kMmaWarp) {
-            // ---- as below, of 4 bits.  A lane has keys lane, + 32, + 64, + 96 of every tile: it copies their codes (two tiles ahead, so
-            // that an address is formed once for a key, and no lane waits for another's) and widens them.
-            const bool is_v = warp != kLoadWarp;
-            const int page_mask = a.c.page_size - 1;
-            const uint32_t packs = C::kTile * (2 + C::kStages) + (is_v ? C::kPacks * C::kPacked : 0);
-            constexpr int kU = DC / 32, kRows = kTileKeys / 32, kScaleAt = kTileKeys * (DC / 2);
-            // 16-byte copies where every row starts on such a boundary
-            const uint8_t* codes = static_cast<const uint8_t*>(is_v ? a.c.v : a.c.k);
-            const uint8_t* scales = is_v ? R4.z.vs : R4.z.ks;
+            // ---- as below, of 4 bits: two warps for the keys, two for the values, each with half of a tile's.  Codes and scales come
+            // by bulk copies, a page's rows (or half a tile's) at a time where the cache is dense (R4.dense), else key by key.
+            const uint32_t me = warp - kLoadWarp;
+            const bool is_v = me >= C::kLoaders;
+            const int half0 = (int)(me % C::kLoaders) * C::kLoadRows;  // the tile's first key that is the warp's
+            uint8_t* const packs = attn_smem + (2 + C::kStages) * C::kTile + me * C::kPacks * C::kPack;
+            const uint8_t* const codes = static_cast<const uint8_t*>(is_v ? a.c.v : a.c.k);
+            const uint8_t* const scales = is_v ? R4.z.vs : R4.z.ks;
+            const int box = min(C::kLoadRows, a.c.page_size), boxes = C::kLoadRows / box;  // keys that lie together
+            const bool dense = R4.dense;
             const bool wide = ((reinterpret_cast<uintptr_t>(codes) | (uintptr_t)a.c.page | (uintptr_t)a.c.tok | (uintptr_t)a.c.head | (uintptr_t)(D / 2)) & 15) == 0;
+            // a bulk copy: lane 2 b + (codes, scales) of box b; else lane, + 32 of the warp's keys
+            const int first_key = half0 + (dense ? (lane >> 1) * box : lane);
+            constexpr int kOwn = C::kLoadRows / 32;
             uint32_t ring0 = 0, issued = 0, used = 0;
             bool ok = true;
             while (ok && W.next(a, P)) {
                 const int n = W.t1 - W.t0, ahead = W.ntok <= P.tt ? 2 : 1, len = W.q.len, kvh = W.heads / P.nsub;
                 const int32_t* table = a.pages + (int64_t)W.s * a.pages_stride;
-                const uint8_t* my_codes = codes + kvh * a.c.head;
-                const uint8_t* my_scales = scales + kvh * R4.z.head;
-                int page[kRows];  // of the next tile to copy
+                int page[kOwn];  // of the next tile to copy
                 auto pages_of = [&](int j) {
 #pragma unroll
-                    for (int i = 0; i < kRows; ++i) {
-                        const int64_t k = (int64_t)(W.t0 + j) * kTileKeys + 32 * i + lane;
-                        page[i] = k < len && j < n ? __ldg(table + (k >> P.page_log2)) : 0;
+                    for (int i = 0; i < kOwn; ++i) {
+                        const int64_t k = (int64_t)(W.t0 + j) * kTileKeys + first_key + 32 * i;
+                        if (i == 0 || !dense) page[i] = k < len && j < n && (!dense || lane < 2 * boxes) ? __ldg(table + (k >> P.page_log2)) : 0;
                     }
                 };
                 auto issue = [&](int j) {
                     if (j < n) {
-                        const uint32_t dst = base + packs + (issued % C::kPacks) * C::kPacked;
-#pragma unroll
-                        for (int i = 0; i < kRows; ++i) {
-                            const int r = 32 * i + lane;
-                            const uint32_t st = dst + kScaleAt + 8 * r;
-                            const bool key = (W.t0 + j) * kTileKeys + r < len;
-                            if (!key || page[i] < 0 || page[i] >= a.c.n_pages) {  // no key, or no page: zeros, whatever the codes
-                                if (key && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
-                                asm volatile("st.shared.v2.b32 [%0], {%1, %1};" ::"r"(st), "r"(0) : "memory");
-                                continue;
+                        const uint32_t st = issued % C::kPacks;
+                        uint8_t* const to = packs + st * C::kPack;
+                        if (dense) {
+                            const int k = (W.t0 + j) * kTileKeys + first_key;
+                            const bool key = lane < 2 * boxes && k < len, good = key && page[0] >= 0 && page[0] < a.c.n_pages;
+                            const uint32_t copied = __ballot_sync(0xffffffffu, good && !(lane & 1));
+                            if (lane == 0) {
+                                if (copied)
+                                    mbar_expect_tx(packed(me, st), __popc(copied) * box * (C::kRow + C::kScales));
+                                else
+                                    mbar_arrive(packed(me, st));
                             }
-                            const int in_page = (int)(((W.t0 + j) * kTileKeys + r) & page_mask);
-                            const uint8_t* src = my_codes + page[i] * a.c.page + in_page * a.c.tok;
-                            if (wide) {
-#pragma unroll
-                                for (int c = 0; c < kU; ++c)
-                                    if (32 * c < D) copy_async<16>(dst + packed_at<DC>(r, c), src + 16 * c);
-                            } else {
-#pragma unroll
-                                for (int c = 0; c < 2 * kU; ++c)
-                                    if (16 * c < D) copy_async<8>(dst + packed_at<DC>(r, c >> 1) + 8 * (c & 1), src + 8 * c);
+                            __syncwarp();
+                            const int b = lane >> 1, in_page = k & (a.c.page_size - 1);
+                            if (good && !(lane & 1))
+                                bulk_load(smem_u32(to + b * box * C::kRow), codes + page[0] * a.c.page + kvh * a.c.head + in_page * C::kRow, box * C::kRow, packed(me, st));
+                            if (good && (lane & 1))
+                                bulk_load(smem_u32(to + C::kLoadRows * C::kRow + b * box * C::kScales),
+                                          scales + page[0] * R4.z.page + kvh * R4.z.head + in_page * C::kScales, box * C::kScales, packed(me, st));
+                            if (key && !good) {  // a page that is missing: scales of zero, whatever the codes
+                                if (a.status) atomicOr(a.status, PPS_FLAG_INDEX);
+                                for (int i = 0; i < box * C::kScales; i += 4)
+                                    *reinterpret_cast<uint32_t*>(to + C::kLoadRows * C::kRow + b * box * C::kScales + i) = 0;
+                                fence_async_smem();  // (before the stage's next copies)
                             }
-                            const uint8_t* sp = my_scales + page[i] * R4.z.page + in_page * R4.z.tok;
+                        } else {
 #pragma unroll
-                            for (int w = 0; w < DC / 64; ++w)
-                                if (64 * w < D) copy_async<4>(st + 4 * w, sp + 4 * w);
+                            for (int i = 0; i < kOwn; ++i) {
+                                const int r = lane + 32 * i, k = (W.t0 + j) * kTileKeys + half0 + r, in_page = k & (a.c.page_size - 1);
+                                const uint32_t row = smem_u32(to + r * C::kRow), sc_at = smem_u32(to + C::kLoadRows * C::kRow + r * C::kScales);
+                                if (k >= len || page[i] < 0 || page[i] >= a.c.n_pages) {
+                                    if (k < len && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
+#pragma unroll
+                                    for (int c = 0; c < DC / 64; ++c) asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc_at + 4 * c), "r"(0) : "memory");
+                                    continue;
+                                }
+                                const uint8_t* src = codes + page[i] * a.c.page + in_page * a.c.tok + kvh * a.c.head;
+                                const uint8_t* sp = scales + page[i] * R4.z.page + in_page * R4.z.tok + kvh * R4.z.head;
+                                if (wide) {
+#pragma unroll
+                                    for (int c = 0; c < DC / 32; ++c)
+                                        if (32 * c < D) copy_async<16>(row + 16 * c, src + 16 * c);
+                                } else {
+#pragma unroll
+                                    for (int c = 0; c < DC / 16; ++c)
+                                        if (16 * c < D) copy_async<8>(row + 8 * c, src + 8 * c);
+                                }
+#pragma unroll
+                                for (int c = 0; c < DC / 64; ++c)
+                                    if (64 * c < D) copy_async<4>(sc_at + 4 * c, sp + 4 * c);
+                            }
                         }
                         ++issued;
                     }
-                    asm volatile("cp.async.commit_group;" ::: "memory");
+                    if (!dense) asm volatile("cp.async.commit_group;" ::: "memory");
                 };
                 pages_of(0);
 #pragma unroll 1
@@ -208,46 +238,59 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                 }
 #pragma unroll 1
                 for (int j = 0; j < n; ++j) {
+                    __syncwarp();  // the stage that is filled now has been read
                     issue(j + C::kPacks - 1);
                     pages_of(j + C::kPacks);
-                    asm volatile("cp.async.wait_group %0;" ::"n"(C::kPacks - 1) : "memory");  // of the lane's own keys
+                    const uint32_t st = used % C::kPacks;
+                    if (dense) {
+                        if (!(ok = wait_warp(packed(me, st), used / C::kPacks & 1u, abort))) break;
+                    } else {
+                        asm volatile("cp.async.wait_group %0;" ::"n"(C::kPacks - 1) : "memory");
+                        __syncwarp();
+                    }
+                    ++used;
                     const uint32_t it = ring0 + (is_v ? (j + ahead < n ? ahead + 2 * j : n + j) : j < ahead ? j : 2 * j - ahead + 1);
                     const uint32_t s = it % C::kStages;
                     if (!(ok = wait_warp(empty(s), ((it / C::kStages) & 1u) ^ 1u, abort))) break;
-                    const uint8_t* src = attn_smem + packs + (used++ % C::kPacks) * C::kPacked;
-                    uint8_t* dst = attn_smem + (2 + s) * C::kTile;
+                    // a lane widens 16 bytes of codes, 32 channels, of a key at a time; lanes of a key are neighbours
+                    constexpr int kU = DC / 32, kAt = 32 / kU;  // lanes of a key, keys of a turn
+                    const int c = lane % kU, r0 = lane / kU, there = len - (W.t0 + j) * kTileKeys - half0;
+                    const uint8_t* src = packs + st * C::kPack;
+                    uint8_t* dst = attn_smem + (2 + s) * C::kTile + (c >> 1) * C::kBlock + (half0 + r0) * 128;
+                    const bool lo_there = 32 * c < D, hi_there = 32 * c + 16 < D;  // (the bytes behind the last block's may be anything)
+#pragma unroll 2
+                    for (int i = 0; i < C::kLoadRows / kAt; ++i) {
+                        const int r = i * kAt + r0;
+                        const uint4 w = *reinterpret_cast<const uint4*>(src + r * C::kRow + 16 * c);
+                        const uint32_t s2 = q4::scales2(*reinterpret_cast<const uint16_t*>(src + C::kLoadRows * C::kRow + r * C::kScales + 2 * c));
+                        const bool key = r < there;
+                        const uint32_t lo = key && lo_there ? __byte_perm(s2, 0, 0x1010) : 0u, hi = key && hi_there ? __byte_perm(s2, 0, 0x3232) : 0u;
+                        // lanes of the second 64 channels begin with the other block of 16, so that eight lanes' stores touch all banks
+                        const bool swap = (c & 2) != 0;
+                        const uint32_t x[4] = {swap ? w.z : w.x, swap ? w.w : w.y, swap ? w.x : w.z, swap ? w.y : w.w};
+                        const uint32_t y[2] = {swap ? hi : lo, swap ? lo : hi};
+                        const uint32_t turn = (uint32_t)((c & 1) * 4 + (swap ? 2 : 0)) ^ (uint32_t)(r & 7);
+                        uint8_t* to = dst + i * kAt * 128;
 #pragma unroll
-                    for (int i = 0; i < kRows; ++i) {
-                        const int r = 32 * i + lane;
-                        uint4 w[kU];
-                        const uint2 s8 = *reinterpret_cast<const uint2*>(src + kScaleAt + 8 * r);
-                        const uint32_t sb[2] = {s8.x, s8.y};
+                        for (int u = 0; u < 4; ++u) {
+                            uint32_t h[4];
+                            q4::widen8(x[u], h);
 #pragma unroll
-                        for (int c = 0; c < kU; ++c) w[c] = *reinterpret_cast<const uint4*>(src + packed_at<DC>(r, c));
-#pragma unroll
-                        for (int c = 0; c < kU; ++c) {
-                            const uint32_t s2 = q4::scales2(c & 1 ? sb[c >> 1] >> 16 : sb[c >> 1]);
-                            // (the bytes behind the last block's may be anything)
-                            const uint32_t lo = 32 * c < D ? __byte_perm(s2, 0, 0x1010) : 0u, hi = 32 * c + 16 < D ? __byte_perm(s2, 0, 0x3232) : 0u;
-                            uint8_t* to = dst + (c >> 1) * C::kBlock + r * 128;
-                            const uint32_t x[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
-#pragma unroll
-                            for (int u = 0; u < 4; ++u) {
-                                uint32_t h[4];
-                                q4::widen8(x[u], h);
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) h[e] = q4::mul_halves(h[e], u < 2 ? lo : hi);
-                                *reinterpret_cast<uint4*>(to + ((((c & 1) * 4 + u) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-                            }
+                            for (int e = 0; e < 4; ++e) h[e] = q4::mul_halves(h[e], y[u >> 1]);
+                            *reinterpret_cast<uint4*>(to + ((turn ^ u) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
                         }
                     }
                     fence_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(full(s));
                 }
-                asm volatile("cp.async.wait_all;" ::: "memory");
+                if (!dense) asm volatile("cp.async.wait_all;" ::: "memory");
                 ring0 += 2 * n;
             }
+            // copies in flight when the CTA gives up: wait (bounded) for each
+            for (; dense && *abort && used < issued; ++used)
+                for (uint32_t i = 0; i < kWaitLimit && !mbar_try_wait(packed(me, used % C::kPacks), used / C::kPacks & 1u); ++i) {
+                }
         } else if (warp < kMmaWarp) {
             // ---- one warp loads the keys' tiles, one the values'.  The ring holds them in the order of their use: K of
             // the first tile (or two, one per stream), then V_j and the next K in turn.
@@ -393,7 +436,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
                 }
             }
             __syncwarp();
-        } else {
+        } else if (warp == C::kQueryWarp) {
             // ---- queries: both tiles of a block of two, or the tile that the last block of one did not use
             uint32_t n0 = 0, n1 = 0, turn = 0;
             bool ok = true;
@@ -425,7 +468,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        if constexpr (Q4)
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        else
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ---- softmax: warpgroup w drives stream w, thread = row r of its tile
         const uint32_t w = warp >> 2, q4 = warp & 3;
         const int r = (int)(q4 * 32) + lane;
