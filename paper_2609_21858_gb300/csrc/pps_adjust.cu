@@ -11,6 +11,7 @@
 // pieces of them).  Nearly all vectors have no such bit and are copied; tokens of a row's path, a handful, are looked up before
 // the row's piece is streamed (it may be written in place) and written after it.
 #include <algorithm>
+#include <climits>
 #include <cstdint>
 #include <cstring>
 
@@ -24,6 +25,7 @@ namespace {
 
 constexpr int kAdjustThreads = 256, kAdjustWarps = kAdjustThreads / 32;
 constexpr int kSlice = 4096;       // tokens
+constexpr int kPiece = 1024;       // tokens that a warp takes of a row at a time
 constexpr int kPath = 64;          // nodes of a path
 constexpr uint32_t kPrompt = 1u << 31;
 
@@ -51,15 +53,15 @@ struct Law {
     }
 };
 
-// 32 bits of a row's words from bit i on, of `n` bits in all (none past them)
-__device__ __forceinline__ uint32_t bits_at(const uint32_t* words, int n_words, int i) {
-    const int w = i >> 5;
-    const uint32_t lo = w < n_words ? words[w] : 0u, hi = w + 1 < n_words && (i & 31) ? words[w + 1] : 0u;
-    return __funnelshift_r(lo, hi, i & 31);
+// N bits of `words` from bit i on; a second word is read only where they reach into it
+template <int N>
+__device__ __forceinline__ uint32_t bits_at(const uint32_t* words, int i) {
+    const uint32_t lo = words[i >> 5], hi = (i & 31) > 32 - N ? words[(i >> 5) + 1] : 0u;
+    return __funnelshift_r(lo, hi, i & 31) & ((1u << N) - 1u);
 }
 
 template <typename T, bool COUNTS, bool BIAS>
-__global__ void __launch_bounds__(kAdjustThreads) adjust_kernel(const AdjustArgs a) {
+__global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustArgs a) {
     constexpr int VN = 16 / sizeof(T);
     __shared__ __align__(16) uint32_t s_count[COUNTS ? kSlice : 4];
     __shared__ __align__(16) int s_bias[BIAS ? kSlice : 4];   // 1 + the last entry for the token
@@ -93,15 +95,22 @@ __global__ void __launch_bounds__(kAdjustThreads) adjust_kernel(const AdjustArgs
                 const int prompt = a.prompt_len ? min(max(__ldg(a.prompt_len + seq), 0), len) : 0;
                 bad |= said != len;
                 const int32_t* text = a.text + seq * a.text_stride;
-                for (int i = tid; i < len; i += kAdjustThreads) {
-                    const int tok = __ldg(text + i), at = tok - t0;
-                    bad |= tok < 0 || tok >= a.V;
-                    if (tok < 0 || at < 0 || at >= tn) continue;
-                    if (i < prompt)
-                        atomicOr(&s_count[at], kPrompt);
-                    else
-                        atomicAdd(&s_count[at], 1u);
-                    atomicOr(&s_known[at >> 5], 1u << (at & 31));
+                for (int i0 = tid; i0 < len; i0 += 4 * kAdjustThreads) {
+                    int tok[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) tok[k] = i0 + k * kAdjustThreads < len ? __ldg(text + i0 + k * kAdjustThreads) : INT_MIN;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int i = i0 + k * kAdjustThreads, at = tok[k] - t0;
+                        if (i >= len) break;
+                        bad |= tok[k] < 0 || tok[k] >= a.V;
+                        if (tok[k] < 0 || at < 0 || at >= tn) continue;
+                        if (i < prompt)
+                            atomicOr(&s_count[at], kPrompt);
+                        else
+                            atomicAdd(&s_count[at], 1u);
+                        atomicOr(&s_known[at >> 5], 1u << (at & 31));
+                    }
                 }
             }
         }
@@ -129,16 +138,14 @@ __global__ void __launch_bounds__(kAdjustThreads) adjust_kernel(const AdjustArgs
         return law(x, (c & ~kPrompt) + more, (c & kPrompt) != 0, bias, allowed);
     };
 
-    // items: a row, or of few rows a piece of one
-    const int pieces = n_rows >= kAdjustWarps ? 1 : kAdjustWarps, piece = (tn + pieces - 1) / pieces;
+    // items: pieces of rows
+    const int pieces = (tn + kPiece - 1) / kPiece;
     for (int item = warp; item < n_rows * pieces; item += kAdjustWarps) {
-        const int i = item / pieces, p0 = (item - i * pieces) * piece, p1 = min(p0 + piece, tn);
-        if (p0 >= p1) continue;
+        const int i = item / pieces, p0 = (item - i * pieces) * kPiece, p1 = min(p0 + kPiece, tn);
         const int64_t row = first + i;
         const T* x = static_cast<const T*>(a.x) + row * a.x_stride + t0;
         T* out = static_cast<T*>(a.out) + row * a.out_stride + t0;
         const uint32_t* allowed = a.allowed ? a.allowed + row * a.allowed_stride : nullptr;
-        const int allowed_words = (int)((a.V + 31) >> 5);
         // the path's tokens: the row's own and its ancestors'
         int n_path = 0;
         float fixed[2];
@@ -192,28 +199,34 @@ __global__ void __launch_bounds__(kAdjustThreads) adjust_kernel(const AdjustArgs
         const int v0 = alike ? min(p0 + (lies ? VN - lies : 0), p1) : p1, nv = (p1 - v0) / VN;
         for (int at = p0 + lane; at < v0; at += 32) one(at);
         for (int at = v0 + nv * VN + lane; at < p1; at += 32) one(at);
-        for (int j = lane; j < nv; j += 32) {
-            const int at = v0 + j * VN;
-            uint4 raw = *reinterpret_cast<const uint4*>(x + at);
-            uint32_t ok = allowed ? bits_at(allowed, allowed_words, t0 + at) : 0xffffffffu;
-            uint32_t known = COUNTS || BIAS ? bits_at(s_known, kSlice / 32, at) : 0u;
-            constexpr uint32_t all = (1u << VN) - 1u;
-            ok &= all;
-            known &= all;
-            if (ok != all || known != 0) {
-                T v[VN];
-                memcpy(v, &raw, 16);
+        constexpr uint32_t all = (1u << VN) - 1u;
+        constexpr int kBatch = 4;  // vectors on their way
+        for (int j0 = lane; j0 < nv; j0 += 32 * kBatch) {
+            uint4 raw[kBatch];
+            uint32_t ok[kBatch];
 #pragma unroll
-                for (int e = 0; e < VN; ++e) {
-                    const bool yes = ok >> e & 1u;
-                    if (known >> e & 1u)
-                        v[e] = Logit<T>::put(adjusted(Logit<T>::get(v[e]), at + e, 0, yes));
-                    else if (!yes)
-                        v[e] = Logit<T>::put(-INFINITY);
+            for (int k = 0; k < kBatch; ++k) ok[k] = allowed && j0 + 32 * k < nv ? bits_at<VN>(allowed, t0 + v0 + (j0 + 32 * k) * VN) : all;
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k)  // what is not allowed need not be read
+                if (j0 + 32 * k < nv && ok[k] != 0) raw[k] = __ldcs(reinterpret_cast<const uint4*>(x + v0) + j0 + 32 * k);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int j = j0 + 32 * k, at = v0 + j * VN;
+                if (j >= nv) break;
+                const uint32_t known = COUNTS || BIAS ? bits_at<VN>(s_known, at) : 0u;
+                if (ok[k] != all || known != 0) {
+                    T v[VN];
+                    memcpy(v, &raw[k], 16);
+#pragma unroll
+                    for (int e = 0; e < VN; ++e)
+                        if (!(ok[k] >> e & 1u))
+                            v[e] = Logit<T>::put(-INFINITY);
+                        else if (known >> e & 1u)
+                            v[e] = Logit<T>::put(adjusted(Logit<T>::get(v[e]), at + e, 0, true));
+                    memcpy(&raw[k], v, 16);
                 }
-                memcpy(&raw, v, 16);
+                __stcs(reinterpret_cast<uint4*>(out + at), raw[k]);
             }
-            *reinterpret_cast<uint4*>(out + at) = raw;
         }
         if (COUNTS && a.node_tok) {
             __syncwarp();

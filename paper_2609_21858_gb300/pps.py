@@ -678,7 +678,8 @@ def _load_fast():
             spec.loader.exec_module(ext)
             ext.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
                 L.pps_kv_append, L.pps_paged_attention, L.pps_verify_chain, L.pps_attention_workspace_size,
-                L.pps_chain_workspace_size)))
+                L.pps_chain_workspace_size, L.pps_kv_append_q4, L.pps_kv_read_q4, L.pps_paged_attention_q4,
+                L.pps_attention_q4_workspace_size, L.pps_kv_reserve, L.pps_kv_trim, L.pps_adjust_logits)))
             _fast = ext
     return _fast
 
@@ -1025,6 +1026,11 @@ def _cache_q4(cache, di, d):
 def kv_append_q4(q, k, v, pos, slot, cache, rope, q_norm=None, k_norm=None, eps: float = 1e-6, interleaved: bool = False,
                  out=None, status=None, stream=None):
     """pps_kv_append_q4: kv_append into a cache in 4 bits (CacheQ4).  Returns the queries (`out`, which may be q)."""
+    if stream is None and cache.__class__ is CacheQ4:
+        done = (_fast or _load_fast()).kv_append_q4(q, k, v, pos, slot, *cache, rope, q_norm, k_norm, eps, interleaved, out,
+                                                    status)
+        if done is not None:
+            return _done("pps_kv_append_q4", done)
     di, dt, code = _half_rows(q)
     n, heads, d = shape = q.shape
     held = _cache_q4(cache, di, d)
@@ -1058,6 +1064,10 @@ def kv_append_q4(q, k, v, pos, slot, cache, rope, q_norm=None, k_norm=None, eps:
 def kv_read_q4(cache, slot, dtype=torch.bfloat16, out=None, status=None, stream=None):
     """pps_kv_read_q4: the values of cache slots (int64, < 0: zeros).  Returns (k, v) [n, kv heads, d] of dtype, written
     to the two tensors of `out` where it is given."""
+    if stream is None and out is None and cache.__class__ is CacheQ4 and dtype in _HALVES:
+        done = (_fast or _load_fast()).kv_read_q4(*cache, slot, dtype is torch.bfloat16, status)
+        if done is not None:
+            return _done("pps_kv_read_q4", done)
     if not isinstance(slot, torch.Tensor) or not slot.is_cuda:
         raise TypeError("slot must be a CUDA tensor")
     if dtype not in _HALVES:
@@ -1089,6 +1099,10 @@ def attention_q4_workspace(n_tok: int, n_heads: int, n_kv_heads: int, head_dim: 
 def paged_attention_q4(q, cache, pages, kv_len, q_off, mask=None, scale=None, out=None, lse=None, ws=None, status=None,
                        stream=None):
     """pps_paged_attention_q4: paged_attention over a cache in 4 bits (CacheQ4)."""
+    if stream is None and cache.__class__ is CacheQ4:
+        done = (_fast or _load_fast()).paged_attention_q4(q, *cache, pages, kv_len, q_off, mask, scale, out, lse, ws, status)
+        if done is not None:
+            return _done("pps_paged_attention_q4", done)
     di, dt, code = _half_rows(q)
     n, heads, d = shape = q.shape
     held = _cache_q4(cache, di, d)
@@ -1148,6 +1162,11 @@ def kv_reserve(pages, held, free_list, free_count, kv_len, n_new, page_size: int
     free_count[0] entries), and where the tokens go.  pages [n_seq, columns], held [n_seq], free_count [1] are updated in place,
     all int32.  n_tok: how many tokens the outputs are for (as many as n_new says, or a padded batch).  Returns dict(q_off [n_seq + 1],
     kv_len [n_seq], slot [n_tok] int64, pos [n_tok], seq [n_tok]); `out` may leave seq out."""
+    if stream is None and out is None:
+        done = (_fast or _load_fast()).kv_reserve(pages, held, free_list, free_count, kv_len, n_new, page_size, n_tok, pos_off,
+                                                  status)
+        if done is not None:
+            return _done("pps_kv_reserve", done)
     di, n_seq, columns, stride, at = _pool(pages, held, free_list, free_count)
     i32 = torch.int32
     lens, new = (_flat(name, _required(name, t, di), di, i32, n_seq) for name, t in (("kv_len", kv_len), ("n_new", n_new)))
@@ -1174,6 +1193,10 @@ def kv_reserve(pages, held, free_list, free_count, kv_len, n_new, page_size: int
 
 def kv_trim(pages, held, free_list, free_count, keep, page_size: int, status=None, stream=None):
     """pps_kv_trim: pages behind the first keep [n_seq] tokens of every sequence go back to the pool (0: all of them)."""
+    if stream is None:
+        done = (_fast or _load_fast()).kv_trim(pages, held, free_list, free_count, keep, page_size, status)
+        if done is not None:
+            return None if done is True else _done("pps_kv_trim", done)
     di, n_seq, columns, stride, at = _pool(pages, held, free_list, free_count)
     kept = _flat("keep", _required("keep", keep, di), di, torch.int32, n_seq)
     flags = _flat("status", status, di, torch.int32, 1)
@@ -1191,6 +1214,12 @@ def adjust_logits(logits, seq_off, text=None, text_len=None, prompt_len=None, no
     of the rows' paths (node_tok [n_rows], node_mask [n_rows, words] or None: chains), biases (bias_tok, bias_val [entries],
     those of sequence s from bias_off[s] to bias_off[s + 1]) and masks (allowed [n_rows, words] int32).  repetition, frequency,
     presence [n_seq] float32.  Returns out (which may be logits)."""
+    if stream is None:
+        done = (_fast or _load_fast()).adjust_logits(logits, seq_off, text, text_len, prompt_len, node_tok, node_mask,
+                                                     repetition, frequency, presence, bias_off, bias_tok, bias_val, allowed, out,
+                                                     status)
+        if done is not None:
+            return _done("pps_adjust_logits", done)
     if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
         raise TypeError("logits must be a CUDA tensor")
     di, dt, code, i32, f32 = logits.get_device(), logits.dtype, _dtype_code(logits), torch.int32, torch.float32
