@@ -7,9 +7,10 @@
 //
 // Every logit is read and written once, whatever the texts are, so the pass is bound by HBM.  A CTA has a slice of the vocabulary
 // of one sequence: it counts the text's tokens that fall into the slice in shared memory (and which entry of the bias list is
-// a token's last), with a bit per token that anything is known of; its warps then take the sequence's rows (or, of few rows,
-// pieces of them).  Nearly all vectors have no such bit and are copied; tokens of a row's path, a handful, are looked up before
-// the row's piece is streamed (it may be written in place) and written after it.
+// a token's last) and lists the tokens that anything is known of, in order.  Its warps then take pieces of the sequence's rows: a piece
+// is copied, but for the mask; then its listed tokens are formed from their logits, which the copy has left as they were (also in
+// place); last the tokens of the row's path, a handful, whose values were formed before.  (Formed within the copy, with a look at each vector, they
+// cost 400 us where this takes 250: of 32 vectors nearly always one has such a token, and all wait for it.)
 #include <algorithm>
 #include <climits>
 #include <cstdint>
@@ -66,6 +67,9 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
     __shared__ __align__(16) uint32_t s_count[COUNTS ? kSlice : 4];
     __shared__ __align__(16) int s_bias[BIAS ? kSlice : 4];   // 1 + the last entry for the token
     __shared__ uint32_t s_known[kSlice / 32];
+    __shared__ uint16_t s_list[COUNTS || BIAS ? kSlice : 2];  // the slice's known tokens, in order
+    __shared__ int s_from[kSlice / kPiece + 1];               // where those of a piece begin
+    __shared__ int s_warp[kAdjustWarps];
     __shared__ int s_path[kAdjustWarps][kPath];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int seq = blockIdx.y;
@@ -128,6 +132,22 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
                 }
         }
         __syncthreads();
+        static_assert(kSlice / 32 <= kAdjustThreads && kPiece % 32 == 0, "a thread per word, whole words in a piece");
+        uint32_t word = tid < kSlice / 32 ? s_known[tid] : 0u;
+        int before = __popc(word);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, before, o);
+            if (lane >= o) before += y;
+        }
+        if (lane == 31) s_warp[warp] = before;
+        __syncthreads();
+        before -= __popc(word);
+        for (int w = 0; w < warp; ++w) before += s_warp[w];
+        if (tid < kSlice / 32 && tid % (kPiece / 32) == 0) s_from[tid / (kPiece / 32)] = before;
+        if (tid == kSlice / 32 - 1) s_from[kSlice / kPiece] = before + __popc(word);
+        for (; word != 0; word &= word - 1) s_list[before++] = (uint16_t)(32 * tid + __ffs(word) - 1);
+        __syncthreads();
     }
     auto adjusted = [&](float x, int at, uint32_t more, bool allowed) {
         uint32_t c = 0;
@@ -186,12 +206,7 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
         auto one = [&](int at) {
             const int tok = t0 + at;
             const bool ok = !allowed || (__ldg(allowed + (tok >> 5)) >> (tok & 31) & 1u);
-            const bool known = (COUNTS || BIAS) && (s_known[at >> 5] >> (at & 31) & 1u);
-            const T v = x[at];
-            if (known || !ok)
-                out[at] = Logit<T>::put(known ? adjusted(Logit<T>::get(v), at, 0, ok) : -INFINITY);
-            else
-                out[at] = v;
+            out[at] = ok ? x[at] : Logit<T>::put(-INFINITY);
         };
         // whole vectors where input and output lie alike, what is before and behind them one by one
         const int lies = (int)((reinterpret_cast<uintptr_t>(x + p0) & 15) / sizeof(T));
@@ -213,19 +228,34 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
             for (int k = 0; k < kBatch; ++k) {
                 const int j = j0 + 32 * k, at = v0 + j * VN;
                 if (j >= nv) break;
-                const uint32_t known = COUNTS || BIAS ? bits_at<VN>(s_known, at) : 0u;
-                if (ok[k] != all || known != 0) {
+                if (ok[k] != all) {
                     T v[VN];
                     memcpy(v, &raw[k], 16);
 #pragma unroll
                     for (int e = 0; e < VN; ++e)
-                        if (!(ok[k] >> e & 1u))
-                            v[e] = Logit<T>::put(-INFINITY);
-                        else if (known >> e & 1u)
-                            v[e] = Logit<T>::put(adjusted(Logit<T>::get(v[e]), at + e, 0, true));
+                        if (!(ok[k] >> e & 1u)) v[e] = Logit<T>::put(-INFINITY);
                     memcpy(&raw[k], v, 16);
                 }
                 __stcs(reinterpret_cast<uint4*>(out + at), raw[k]);
+            }
+        }
+        if constexpr (COUNTS || BIAS) {
+            __syncwarp();
+            const int from = s_from[p0 / kPiece], to = s_from[p0 / kPiece + 1];
+            for (int e0 = from + lane; e0 < to; e0 += 64) {  // two on their way
+                int at[2];
+                T v[2];
+                bool ok[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int e = e0 + 32 * k;
+                    at[k] = e < to ? s_list[e] : -1;
+                    ok[k] = at[k] >= 0 && (!allowed || (allowed[(t0 + at[k]) >> 5] >> ((t0 + at[k]) & 31) & 1u));
+                    if (ok[k]) v[k] = x[at[k]];
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    if (ok[k]) out[at[k]] = Logit<T>::put(adjusted(Logit<T>::get(v[k]), at[k], 0, true));
             }
         }
         if (COUNTS && a.node_tok) {
