@@ -7,10 +7,11 @@
 //
 // Every logit is read and written once, whatever the texts are, so the pass is bound by HBM.  A CTA has a slice of the vocabulary
 // of one sequence: it counts the text's tokens that fall into the slice in shared memory (and which entry of the bias list is
-// a token's last) and lists the tokens that anything is known of, in order.  Its warps then take pieces of the sequence's rows: a piece
-// is copied, but for the mask; then its listed tokens are formed from their logits, which the copy has left as they were (also in
-// place); last the tokens of the row's path, a handful, whose values were formed before.  (Formed within the copy, with a look at each vector, they
-// cost 400 us where this takes 250: of 32 vectors nearly always one has such a token, and all wait for it.)
+// a token's last), with a bit per token that anything is known of.  Its warps take pieces of the sequence's rows: vectors are copied
+// through registers, and a vector's known tokens, by their bits, formed there one at a time.  (All elements of such a vector at once:
+// 423 us for 64 x 41 rows of 128256 where this takes 249; listed and formed in memory after the copy, 295 to 320: a read and a write of 32 bytes for each, of what
+// has left L2 in part.)  Tokens of a row's path, a handful, are formed before its piece (which may be written in place) and written
+// after it.
 #include <algorithm>
 #include <climits>
 #include <cstdint>
@@ -26,7 +27,7 @@ namespace {
 
 constexpr int kAdjustThreads = 256, kAdjustWarps = kAdjustThreads / 32;
 constexpr int kSlice = 4096;       // tokens
-constexpr int kPiece = 1024;       // tokens that a warp takes of a row at a time
+constexpr int kBatch = 4;          // vectors of a lane on their way
 constexpr int kPath = 64;          // nodes of a path
 constexpr uint32_t kPrompt = 1u << 31;
 
@@ -43,14 +44,42 @@ struct Logit<__nv_bfloat16> {
     static __device__ __forceinline__ __nv_bfloat16 put(float x) { return __float2bfloat16_rn(x); }
 };
 
+// element e of a 16-byte vector that stays in registers
+template <typename T>
+struct Pick;
+template <>
+struct Pick<float> {
+    static __device__ __forceinline__ float get(const uint4& v, int e) { return __uint_as_float(e & 2 ? (e & 1 ? v.w : v.z) : (e & 1 ? v.y : v.x)); }
+    static __device__ __forceinline__ void set(uint4& v, int e, float f) {
+        const uint32_t x = __float_as_uint(f);
+        v.x = e == 0 ? x : v.x;
+        v.y = e == 1 ? x : v.y;
+        v.z = e == 2 ? x : v.z;
+        v.w = e == 3 ? x : v.w;
+    }
+};
+template <>
+struct Pick<__nv_bfloat16> {
+    static __device__ __forceinline__ float get(const uint4& v, int e) {
+        const uint32_t w = e & 4 ? (e & 2 ? v.w : v.z) : (e & 2 ? v.y : v.x);
+        return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+    }
+    static __device__ __forceinline__ void set(uint4& v, int e, float f) {
+        const uint32_t x = __bfloat16_as_ushort(__float2bfloat16_rn(f)), how = e & 1 ? 0x5410u : 0x3254u;  // (of x, w: w's low half and x; x and w's high half)
+        v.x = e >> 1 == 0 ? __byte_perm(v.x, x, how) : v.x;
+        v.y = e >> 1 == 1 ? __byte_perm(v.y, x, how) : v.y;
+        v.z = e >> 1 == 2 ? __byte_perm(v.z, x, how) : v.z;
+        v.w = e >> 1 == 3 ? __byte_perm(v.w, x, how) : v.w;
+    }
+};
+
 struct Law {
     float rep, freq, pres;
-    __device__ __forceinline__ float operator()(float x, uint32_t count, bool prompt, float bias, bool allowed) const {
+    __device__ __forceinline__ float operator()(float x, uint32_t count, bool prompt, float bias) const {
         if (count > 0 || prompt) x = x > 0.0f ? __fdiv_rn(x, rep) : __fmul_rn(x, rep);
         x = __fsub_rn(x, __fmul_rn(freq, (float)count));
         if (count > 0) x = __fsub_rn(x, pres);
-        x = __fadd_rn(x, bias);
-        return allowed ? x : -INFINITY;
+        return __fadd_rn(x, bias);
     }
 };
 
@@ -67,9 +96,6 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
     __shared__ __align__(16) uint32_t s_count[COUNTS ? kSlice : 4];
     __shared__ __align__(16) int s_bias[BIAS ? kSlice : 4];   // 1 + the last entry for the token
     __shared__ uint32_t s_known[kSlice / 32];
-    __shared__ uint16_t s_list[COUNTS || BIAS ? kSlice : 2];  // the slice's known tokens, in order
-    __shared__ int s_from[kSlice / kPiece + 1];               // where those of a piece begin
-    __shared__ int s_warp[kAdjustWarps];
     __shared__ int s_path[kAdjustWarps][kPath];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int seq = blockIdx.y;
@@ -132,45 +158,31 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
                 }
         }
         __syncthreads();
-        static_assert(kSlice / 32 <= kAdjustThreads && kPiece % 32 == 0, "a thread per word, whole words in a piece");
-        uint32_t word = tid < kSlice / 32 ? s_known[tid] : 0u;
-        int before = __popc(word);
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, before, o);
-            if (lane >= o) before += y;
-        }
-        if (lane == 31) s_warp[warp] = before;
-        __syncthreads();
-        before -= __popc(word);
-        for (int w = 0; w < warp; ++w) before += s_warp[w];
-        if (tid < kSlice / 32 && tid % (kPiece / 32) == 0) s_from[tid / (kPiece / 32)] = before;
-        if (tid == kSlice / 32 - 1) s_from[kSlice / kPiece] = before + __popc(word);
-        for (; word != 0; word &= word - 1) s_list[before++] = (uint16_t)(32 * tid + __ffs(word) - 1);
-        __syncthreads();
     }
-    auto adjusted = [&](float x, int at, uint32_t more, bool allowed) {
+    auto adjusted = [&](float x, int at, uint32_t more) {
         uint32_t c = 0;
         if constexpr (COUNTS) c = s_count[at];
         float bias = 0.0f;
         if constexpr (BIAS)
             if (const int e = s_bias[at]) bias = __ldg(a.bias_val + e - 1);
-        return law(x, (c & ~kPrompt) + more, (c & kPrompt) != 0, bias, allowed);
+        return law(x, (c & ~kPrompt) + more, (c & kPrompt) != 0, bias);
     };
 
     // items: pieces of rows
-    const int pieces = (tn + kPiece - 1) / kPiece;
+    // 2048 tokens, or 1024 of a few rows (64 x 41 rows 249 and 276 us, 16 x 9 rows 46 and 44, one row 7.1 and 6.1)
+    const int piece = n_rows >= 16 ? 2048 : 1024, pieces = (tn + piece - 1) / piece;
     for (int item = warp; item < n_rows * pieces; item += kAdjustWarps) {
-        const int i = item / pieces, p0 = (item - i * pieces) * kPiece, p1 = min(p0 + kPiece, tn);
+        const int i = item / pieces, p0 = (item - i * pieces) * piece, p1 = min(p0 + piece, tn);
         const int64_t row = first + i;
         const T* x = static_cast<const T*>(a.x) + row * a.x_stride + t0;
         T* out = static_cast<T*>(a.out) + row * a.out_stride + t0;
-        const uint32_t* allowed = a.allowed ? a.allowed + row * a.allowed_stride : nullptr;
+        const uint32_t* allowed = a.allowed ? a.allowed + row * a.allowed_stride + (t0 >> 5) : nullptr;
+        auto may = [&](int at) { return !allowed || (__ldg(allowed + (at >> 5)) >> (at & 31) & 1u); };
         // the path's tokens: the row's own and its ancestors'
-        int n_path = 0;
         float fixed[2];
         int fixed_at[2] = {-1, -1};
         if (COUNTS && a.node_tok) {
+            int n_path = 0;
             const int words = a.node_mask ? min(a.mask_words, (n_rows + 31) >> 5) : (i >> 5) + 1;
             for (int w = 0; w < words; ++w) {
                 const int node = 32 * w + lane;
@@ -197,38 +209,49 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
                         ++n;
                         again |= j < me;
                     }
-                if (again) continue;
+                if (again || !may(at)) continue;
                 fixed_at[k] = at;
-                fixed[k] = adjusted(Logit<T>::get(x[at]), at, n, !allowed || (allowed[tok >> 5] >> (tok & 31) & 1u));
+                fixed[k] = adjusted(Logit<T>::get(x[at]), at, n);
             }
             __syncwarp();  // (in place: the logits are read)
         }
-        auto one = [&](int at) {
-            const int tok = t0 + at;
-            const bool ok = !allowed || (__ldg(allowed + (tok >> 5)) >> (tok & 31) & 1u);
-            out[at] = ok ? x[at] : Logit<T>::put(-INFINITY);
-        };
         // whole vectors where input and output lie alike, what is before and behind them one by one
         const int lies = (int)((reinterpret_cast<uintptr_t>(x + p0) & 15) / sizeof(T));
         const bool alike = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
         const int v0 = alike ? min(p0 + (lies ? VN - lies : 0), p1) : p1, nv = (p1 - v0) / VN;
+        auto one = [&](int at) {
+            const bool known = (COUNTS || BIAS) && (s_known[at >> 5] >> (at & 31) & 1u);
+            const T v = x[at];
+            out[at] = !may(at) ? Logit<T>::put(-INFINITY) : known ? Logit<T>::put(adjusted(Logit<T>::get(v), at, 0)) : v;
+        };
         for (int at = p0 + lane; at < v0; at += 32) one(at);
         for (int at = v0 + nv * VN + lane; at < p1; at += 32) one(at);
+        const uint4* from = reinterpret_cast<const uint4*>(x + v0);
+        uint4* to = reinterpret_cast<uint4*>(out + v0);
         constexpr uint32_t all = (1u << VN) - 1u;
-        constexpr int kBatch = 4;  // vectors on their way
         for (int j0 = lane; j0 < nv; j0 += 32 * kBatch) {
             uint4 raw[kBatch];
             uint32_t ok[kBatch];
 #pragma unroll
-            for (int k = 0; k < kBatch; ++k) ok[k] = allowed && j0 + 32 * k < nv ? bits_at<VN>(allowed, t0 + v0 + (j0 + 32 * k) * VN) : all;
+            for (int k = 0; k < kBatch; ++k) {
+                ok[k] = j0 + 32 * k < nv ? all : 0u;
+                if (allowed && ok[k]) ok[k] = bits_at<VN>(allowed, v0 + (j0 + 32 * k) * VN);
+            }
 #pragma unroll
             for (int k = 0; k < kBatch; ++k)  // what is not allowed need not be read
-                if (j0 + 32 * k < nv && ok[k] != 0) raw[k] = __ldcs(reinterpret_cast<const uint4*>(x + v0) + j0 + 32 * k);
+                if (ok[k] != 0) raw[k] = __ldcs(from + j0 + 32 * k);
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
-                const int j = j0 + 32 * k, at = v0 + j * VN;
-                if (j >= nv) break;
-                if (ok[k] != all) {
+                if (j0 + 32 * k >= nv) break;
+                const int at = v0 + (j0 + 32 * k) * VN;
+                if constexpr (COUNTS || BIAS) {
+                    // a known token at a time: of 32 vectors nearly always one has one, rarely one has two
+                    for (uint32_t known = bits_at<VN>(s_known, at) & ok[k]; known != 0; known &= known - 1) {
+                        const int e = __ffs(known) - 1;
+                        Pick<T>::set(raw[k], e, adjusted(Pick<T>::get(raw[k], e), at + e, 0));
+                    }
+                }
+                if (allowed && ok[k] != all) {
                     T v[VN];
                     memcpy(v, &raw[k], 16);
 #pragma unroll
@@ -236,26 +259,7 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
                         if (!(ok[k] >> e & 1u)) v[e] = Logit<T>::put(-INFINITY);
                     memcpy(&raw[k], v, 16);
                 }
-                __stcs(reinterpret_cast<uint4*>(out + at), raw[k]);
-            }
-        }
-        if constexpr (COUNTS || BIAS) {
-            __syncwarp();
-            const int from = s_from[p0 / kPiece], to = s_from[p0 / kPiece + 1];
-            for (int e0 = from + lane; e0 < to; e0 += 64) {  // two on their way
-                int at[2];
-                T v[2];
-                bool ok[2];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int e = e0 + 32 * k;
-                    at[k] = e < to ? s_list[e] : -1;
-                    ok[k] = at[k] >= 0 && (!allowed || (allowed[(t0 + at[k]) >> 5] >> ((t0 + at[k]) & 31) & 1u));
-                    if (ok[k]) v[k] = x[at[k]];
-                }
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    if (ok[k]) out[at[k]] = Logit<T>::put(adjusted(Logit<T>::get(v[k]), at[k], 0, true));
+                __stcs(to + j0 + 32 * k, raw[k]);
             }
         }
         if (COUNTS && a.node_tok) {
