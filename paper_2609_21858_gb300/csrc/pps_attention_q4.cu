@@ -32,9 +32,10 @@ namespace pps {
 namespace {
 
 constexpr int kWarps4 = 4, kThreads4 = 32 * kWarps4;
-constexpr int kUnit = 32;         // keys that a warp takes at a time
-constexpr int kStages4 = 3;       // units of a warp, on their way or in use
-constexpr int few_ctas(int nt) { return nt == 1 ? 4 : 2; }  // per SM: 128 or 255 registers
+constexpr int kUnit = 64;         // keys that a warp takes at a time
+constexpr int kGroups = kUnit / 16;
+constexpr int kStages4 = 2;       // units of a warp, on their way or in use
+constexpr int few_ctas(int nt) { return nt == 1 ? 3 : 2; }  // per SM: 168 or 255 registers
 constexpr int kMaxCtas4 = 640;
 constexpr int kFix4 = 2;          // key tiles that an item's start and end cost
 constexpr int kLeast4 = 1;
@@ -48,18 +49,18 @@ __device__ __forceinline__ int halving(uint32_t top) { return top == 0 ? 0 : min
 __device__ __forceinline__ float power_of_two(int k) { return __uint_as_float((uint32_t)(127 + k) << 23); }
 
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma16816_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {  // c = a b
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
                  : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
 
@@ -106,13 +107,16 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
     const uint32_t ring_at = smem_u32(my_ring), bar_at = smem_u32(&s_bar[warp][0]);
     const bool wide = ((reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v) | (uintptr_t)a.c.page | (uintptr_t)a.c.tok |
                         (uintptr_t)a.c.head | (uintptr_t)(D / 2)) & 15) == 0;
-    // of a bulk copy, lane 4 G + kind (keys, values, scales of keys, of values): 16 keys' rows
-    const int kind = lane & 3, G16 = lane >> 2 & 1;
+    // of a bulk copy, lane 4 G + kind (keys, values, scales of keys, of values): the G-th 16 keys' rows
+    const int kind = lane & 3, G16 = lane >> 2 & (kGroups - 1);
     const uint8_t* const part = kind == 0 ? static_cast<const uint8_t*>(a.c.k) : kind == 1 ? static_cast<const uint8_t*>(a.c.v) : kind == 2 ? z.ks : z.vs;
-    const int64_t part_page = kind < 2 ? a.c.page : z.page, part_head = kind < 2 ? a.c.head : z.head;
+    const int64_t part_page = kind < 2 ? a.c.page : z.page;
     const int part_row = kind < 2 ? S::kRow : S::kScales;
     const uint32_t part_at = (kind == 0 ? 0 : kind == 1 ? S::kV : kind == 2 ? S::kKs : S::kVs) + 16 * G16 * part_row;
-    uint32_t turn = 0;  // stages filled so far; used up: turn less those on their way
+    // key by key: four lanes copy a row of codes; a lane has the scales of keys lane, + 32
+    const int64_t quarter = (lane >> 2) * a.c.tok + (lane & 3) * (DC / 8);
+    const bool q_there = (lane & 3) * (DC / 4) < D, q_half = (lane & 3) * (DC / 4) + 16 < D;
+    uint32_t to_fill = 0, to_use = 0, phase = 0;  // the stage that is filled next, used next, and the phase of the latter's barrier
 
     while (W.next(a, P)) {
         const int kvh = W.heads / P.nsub, sub = W.heads - kvh * P.nsub;
@@ -125,57 +129,70 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
         const int first = W.t0 * kTileKeys, last = min(W.t1 * kTileKeys, end);
         const int32_t* table = a.pages + (int64_t)W.s * a.pages_stride;
 
-        // the lane's page of the unit from key k0 on: of half G16, or of key `lane`
+        // the lane's page of the unit from key k0 on: of 16 keys G16, or of eight keys, lane modulo 8
         auto page_of = [&](int k0) {
-            const int k = k0 + (DENSE ? 16 * G16 : lane);
+            const int k = k0 + (DENSE ? 16 * G16 : 8 * (lane & 7));
             return k < last ? __ldg(table + (k >> P.page_log2)) : 0;
         };
-        uint32_t halves = 0;  // a bit per half of the units on their way, the newest lowest: its page is there
+        const uint8_t* const my_part = part + kvh * (kind < 2 ? a.c.head : z.head);
+        uint32_t paged = 0;  // a bit per 16 keys of the units on their way, the newest lowest: their page is there
         auto fill = [&](int k0, int page) {
-            const uint32_t st = turn % kStages4, to = ring_at + st * S::kBytes;
-            ++turn;
-            const int k = k0 + (DENSE ? 16 * G16 : lane), in_page = k & (a.c.page_size - 1);
-            const bool key = k < last, good = key && page >= 0 && page < a.c.n_pages;  // (a missing page reads as zeros)
-            if (key && !good && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
+            const uint32_t to = ring_at + to_fill * S::kBytes, full = bar_at + 8 * to_fill;
+            to_fill = to_fill + 1 == kStages4 ? 0 : to_fill + 1;
             if constexpr (DENSE) {
-                const uint32_t who = __ballot_sync(0xffffffffu, good), two = (who & 1u) | (who >> 3 & 2u);
-                halves = halves << 2 | two;
+                const int k = k0 + 16 * G16, in_page = k & (a.c.page_size - 1);
+                const bool key = k < last, good = key && (uint32_t)page < (uint32_t)a.c.n_pages;  // (a missing page reads as zeros)
+                if (key && !good && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
+                const uint32_t who = __ballot_sync(0xffffffffu, good && kind == 0) & ((1u << 4 * kGroups) - 1u);
+                paged = paged << 4 * kGroups | who;
                 if (lane == 0) {
-                    const uint32_t bytes = __popc(two) * 16 * 2 * (S::kRow + S::kScales);
-                    if (bytes)
-                        mbar_expect_tx(bar_at + 8 * st, bytes);
+                    if (who)
+                        mbar_expect_tx(full, __popc(who) * (16 * 2 * (S::kRow + S::kScales)));
                     else
-                        mbar_arrive(bar_at + 8 * st);
+                        mbar_arrive(full);
                 }
                 __syncwarp();
-                if (lane < 8 && good)
-                    bulk_load(to + part_at, part + page * part_page + kvh * part_head + in_page * part_row, 16 * part_row, bar_at + 8 * st);
+                if (lane < 4 * kGroups && good) bulk_load(to + part_at, my_part + page * part_page + in_page * part_row, 16 * part_row, full);
             } else {
-                const uint32_t rows = to + lane * S::kRow, scales = to + S::kKs + lane * S::kScales;
-                if (good) {
-                    const int64_t at = page * a.c.page + in_page * a.c.tok + kvh * a.c.head, st4 = page * z.page + in_page * z.tok + kvh * z.head;
+                if (k0 + 8 * (lane & 7) < last && (uint32_t)page >= (uint32_t)a.c.n_pages) {  // reads as zeros
+                    if (a.status) atomicOr(a.status, PPS_FLAG_INDEX);
+                    page = -1;
+                }
+#pragma unroll
+                for (int i = 0; i < kUnit / 8; ++i) {  // codes
+                    const int p = __shfl_sync(0xffffffffu, page, i), k = k0 + 8 * i, in_page = k & (a.c.page_size - 1);
+                    if (p < 0 || k + (lane >> 2) >= last || !q_there) continue;
+                    const int64_t at = p * a.c.page + in_page * a.c.tok + kvh * a.c.head + quarter;
+                    const uint32_t row = to + (8 * i + (lane >> 2)) * S::kRow + (lane & 3) * (DC / 8);
 #pragma unroll
                     for (int v = 0; v < 2; ++v) {
                         const uint8_t* src = static_cast<const uint8_t*>(v ? a.c.v : a.c.k) + at;
-                        const uint8_t* sp = (v ? z.vs : z.ks) + st4;
-                        if (wide) {
-#pragma unroll
-                            for (int c = 0; c < DC / 32; ++c)
-                                if (32 * c < D) copy_async<16>(rows + v * S::kV + 16 * c, src + 16 * c);
-                        } else {
-#pragma unroll
-                            for (int c = 0; c < DC / 16; ++c)
-                                if (16 * c < D) copy_async<8>(rows + v * S::kV + 8 * c, src + 8 * c);
+                        if (DC == 128 && wide)
+                            copy_async<16>(row + v * S::kV, src);
+                        else {
+                            copy_async<8>(row + v * S::kV, src);
+                            if (DC == 128 && q_half) copy_async<8>(row + v * S::kV + 8, src + 8);
                         }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kUnit / 32; ++i) {
+                    const int key = lane + 32 * i, k = k0 + key, p = __shfl_sync(0xffffffffu, page, key >> 3);
+                    const uint32_t scales = to + S::kKs + key * S::kScales;
+                    if (k < last && p >= 0) {
+                        const int64_t at = p * z.page + (k & (a.c.page_size - 1)) * z.tok + kvh * z.head;
 #pragma unroll
                         for (int c = 0; c < DC / 64; ++c)
-                            if (64 * c < D) copy_async<4>(scales + v * (S::kVs - S::kKs) + 4 * c, sp + 4 * c);
-                    }
-                } else {
+                            if (64 * c < D) {
+                                copy_async<4>(scales + 4 * c, z.ks + at + 4 * c);
+                                copy_async<4>(scales + S::kVs - S::kKs + 4 * c, z.vs + at + 4 * c);
+                            }
+                    } else {
 #pragma unroll
-                    for (int c = 0; c < DC / 64; ++c) {  // scales of zero, whatever the codes
-                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(scales + 4 * c), "r"(0) : "memory");
-                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(scales + S::kVs - S::kKs + 4 * c), "r"(0) : "memory");
+                        for (int c = 0; c < DC / 64; ++c) {  // scales of zero, whatever the codes
+                            asm volatile("st.shared.b32 [%0], %1;" ::"r"(scales + 4 * c), "r"(0) : "memory");
+                            asm volatile("st.shared.b32 [%0], %1;" ::"r"(scales + S::kVs - S::kKs + 4 * c), "r"(0) : "memory");
+                        }
                     }
                 }
             }
@@ -194,7 +211,7 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
             if (k < last)
                 fill(k, p);
             else
-                halves <<= 2;
+                paged <<= 4 * kGroups;
             close();
         }
         // ---- queries: row 8 nt + g, the channels of quarter t, as halves
@@ -251,7 +268,6 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.0f;
 
-        uint32_t used = turn - min(max((last - k_start + kStep - 1) / kStep, 0), kAhead4);
 #pragma unroll 1
         for (; k0 < last; k0 += kStep) {
             const int key0 = k0, ahead = k0 + kAhead4 * kStep, page = pages;
@@ -260,33 +276,37 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
             if (ahead < last)
                 fill(ahead, page);
             else
-                halves <<= 2;
+                paged <<= 4 * kGroups;
             close();
-            const uint32_t st = used % kStages4;
             if constexpr (DENSE)
-                mbar_wait(bar_at + 8 * st, used / kStages4 & 1u, &s_abort);
+                mbar_wait(bar_at + 8 * to_use, phase, &s_abort);
             else
                 asm volatile("cp.async.wait_group %0;" ::"n"(kAhead4) : "memory");
             __syncwarp();
-            ++used;
-            uint8_t* const unit = my_ring + st * S::kBytes;
+            uint8_t* const unit = my_ring + to_use * S::kBytes;
+            if (++to_use == kStages4) {
+                to_use = 0;
+                phase ^= 1u;
+            }
             if constexpr (DENSE) {  // keys that are not there, or lie on a missing page, get scales of zero
-                const uint32_t two = halves >> (2 * kAhead4) & 3u;
-                if (k0 + kUnit > last || two != 3u) {
-                    if (k0 + lane >= last || !(two >> (lane >> 4) & 1u)) {
+                const uint32_t who = paged >> (4 * kGroups * kAhead4) & ((1u << 4 * kGroups) - 1u);
+                if (k0 + kUnit > last || who != (0x1111u & ((1u << 4 * kGroups) - 1u))) {
 #pragma unroll
-                        for (int i = 0; i < S::kScales; i += 4) {
-                            *reinterpret_cast<uint32_t*>(unit + S::kKs + lane * S::kScales + i) = 0;
-                            *reinterpret_cast<uint32_t*>(unit + S::kVs + lane * S::kScales + i) = 0;
+                    for (int key = lane; key < kUnit; key += 32)
+                        if (k0 + key >= last || !(who >> (4 * (key >> 4)) & 1u)) {
+#pragma unroll
+                            for (int i = 0; i < S::kScales; i += 4) {
+                                *reinterpret_cast<uint32_t*>(unit + S::kKs + key * S::kScales + i) = 0;
+                                *reinterpret_cast<uint32_t*>(unit + S::kVs + key * S::kScales + i) = 0;
+                            }
                         }
-                    }
                     fence_async_smem();  // (before the stage's next copies)
                     __syncwarp();
                 }
             }
-            float s[NT][2][4];
+            float s[NT][kGroups][4];
 #pragma unroll
-            for (int G = 0; G < 2; ++G) {
+            for (int G = 0; G < kGroups; ++G) {
                 uint32_t h[2][DC / 8];  // the quarter of keys 16 G + g and 16 G + 8 + g
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
@@ -328,22 +348,25 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                 for (int r = 0; r < 2 * NT; ++r) {
                     const int row = 8 * (r >> 1) + 2 * t + (r & 1), tok = W.i0 + min(row / P.gs, W.ntok - 1);
                     const uint32_t* mask = a.mask ? a.mask + (int64_t)(W.q.off + tok) * a.mask_words : nullptr;
-                    const uint32_t bits = seen_bits(key0, mask ? len : prefix + tok + 1, prefix, mask, a.mask_words) >> g;
 #pragma unroll
-                    for (int G = 0; G < 2; ++G)
+                    for (int h = 0; h < kUnit / 32; ++h) {
+                        const uint32_t bits = seen_bits(key0 + 32 * h, mask ? len : prefix + tok + 1, prefix, mask, a.mask_words) >> g;
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            float& y = s[r >> 1][G][2 * j + (r & 1)];
-                            y = bits >> (16 * G + 8 * j) & 1u ? __uint_as_float((__float_as_uint(y) & P.s_and) ^ P.s_xor) : -INFINITY;
+                        for (int e = 0; e < 4; ++e) {
+                            float& y = s[r >> 1][2 * h + (e >> 1)][2 * (e & 1) + (r & 1)];
+                            y = bits >> (8 * e) & 1u ? __uint_as_float((__float_as_uint(y) & P.s_and) ^ P.s_xor) : -INFINITY;
                         }
+                    }
                 }
             }
             float top[2 * NT];
             bool rises = false;
 #pragma unroll
             for (int r = 0; r < 2 * NT; ++r) {
-                const float(&y)[2][4] = s[r >> 1];
-                top[r] = fmaxf(max3(y[0][r & 1], y[0][2 + (r & 1)], y[1][r & 1]), y[1][2 + (r & 1)]);
+                const float(&y)[kGroups][4] = s[r >> 1];
+                top[r] = fmaxf(y[0][r & 1], y[0][2 + (r & 1)]);
+#pragma unroll
+                for (int G = 1; G < kGroups; ++G) top[r] = max3(top[r], y[G][r & 1], y[G][2 + (r & 1)]);
                 rises |= top[r] > limit[r];
             }
             if (__any_sync(0xffffffffu, rises)) {
@@ -363,11 +386,11 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                     }
                 }
             }
-            uint32_t p[NT][4];  // the operand P^T: rows 8 nt + g, keys 8 e + 2t, + 1
+            uint32_t p[NT][2 * kGroups];  // the operand P^T: rows 8 nt + g, keys 8 e + 2t, + 1
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                for (int e = 0; e < 2 * kGroups; ++e) {
                     const float x0 = ex2(fmaf(s[nt][e >> 1][2 * (e & 1)], sc[2 * nt], neg[2 * nt]));
                     const float x1 = ex2(fmaf(s[nt][e >> 1][2 * (e & 1) + 1], sc[2 * nt + 1], neg[2 * nt + 1]));
                     l[2 * nt] += x0;
@@ -376,7 +399,7 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                 }
             }
 #pragma unroll
-            for (int G = 0; G < 2; ++G) {
+            for (int G = 0; G < kGroups; ++G) {
                 uint32_t c[2][2][DC / 64], s2[2];  // of keys 16 G + 8 j + 2t, + 1
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
