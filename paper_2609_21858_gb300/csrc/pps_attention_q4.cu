@@ -510,11 +510,11 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
     if (DENSE && tid == 0 && *static_cast<volatile int*>(&s_abort) && a.status) atomicOr(a.status, PPS_FLAG_TIMEOUT);
 }
 
-// Whether a head's rows of a page follow one another, codes and scales, all of them of dc channels, from 16-byte boundaries on.
+// Whether a cache lies as Copy64 wants it dense.
 bool is_dense(const AttnArgs& a, const Q4View& z, int dc) {
     const uintptr_t bits = reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v) | reinterpret_cast<uintptr_t>(z.ks) |
                            reinterpret_cast<uintptr_t>(z.vs) | (uintptr_t)a.c.page | (uintptr_t)a.c.head | (uintptr_t)z.page | (uintptr_t)z.head;
-    return a.c.head_dim == dc && a.c.tok == dc / 2 && z.tok == dc / 16 && bits % 16 == 0;
+    return a.c.head_dim == dc && a.c.page_size >= 16 && a.c.tok == dc / 2 && z.tok == dc / 16 && bits % 16 == 0;
 }
 
 // the rows of a block, the heads taken at a time, the tokens of a block: by the mean number of tokens of a sequence
@@ -543,7 +543,7 @@ cudaError_t launch_few(const AttnArgs& a, const Q4View& z, const Rows4& rows, cu
     plan_common(P, a);
     carve(P, a.ws, kMaxCtas4);
     constexpr int kSmem = std::max(kWarps4 * 8 * NT * (DC + 4) * 4, kWarps4 * kStages4 * Stage<DC>::kBytes);
-    const bool dense = is_dense(a, z, DC) && a.c.page_size >= 16;
+    const bool dense = is_dense(a, z, DC);
     auto kernel = dense ? few_rows_kernel<T, DC, NT, true> : few_rows_kernel<T, DC, NT, false>;
     static std::atomic<uint64_t> ready[2] = {};
     cudaError_t e = allow_smem(ready[dense], (const void*)kernel, kSmem);
@@ -554,32 +554,42 @@ cudaError_t launch_few(const AttnArgs& a, const Q4View& z, const Rows4& rows, cu
     return launch_pdl(join_kernel<T, DC>, dim3(ctas, join_blocks(a, P)), dim3(256), 0, st, a, P);
 }
 
-// Queries in bf16 as halves, rows side by side, and the factor that a row's scores get for it.  A warp has a row; four channels a lane.
+// Queries in bf16 as halves, rows side by side, and the factor that a row's scores get for it.  Half a warp has a row, eight channels
+// a lane; four rows of it are on their way.
 __global__ void __launch_bounds__(256) halve_kernel(const AttnArgs a, __half* out, float* row_scale) {
     pdl_wait();
     pdl_launch_dependents();
-    const int64_t rows = a.n_tok * a.n_heads;
-    const int lane = threadIdx.x & 31, D = a.c.head_dim;
-    for (int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); i < rows; i += (int64_t)gridDim.x * 8) {
-        const int64_t tok = i / a.n_heads;
-        const int head = (int)(i - tok * a.n_heads);
-        uint2 x = make_uint2(0, 0);
-        if (4 * lane < D) x = __ldg(reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(a.q.p) + tok * a.q.tok + head * a.q.head) + lane);
-        uint32_t top = 0;
+    constexpr int kAtOnce = 4;
+    const int64_t rows = a.n_tok * a.n_heads, step = (int64_t)gridDim.x * 16;
+    const int at = 8 * (threadIdx.x & 15), D = a.c.head_dim;
+    for (int64_t i0 = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); i0 < (rows + 1) / 2 * 2; i0 += kAtOnce * step) {  // (both halves of a warp)
+        uint4 x[kAtOnce];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t v = ((e & 2) ? x.y : x.x) >> (16 * (e & 1)) & 0x7fffu;
-            top = max(top, v < 0x7f80u ? v : 0u);
+        for (int e = 0; e < kAtOnce; ++e) {
+            const int64_t i = i0 + e * step, tok = i / a.n_heads;
+            x[e] = make_uint4(0, 0, 0, 0);
+            if (i < rows && at < D)
+                x[e] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q.p) + tok * a.q.tok + (i - tok * a.n_heads) * a.q.head + at));
         }
-        top = __reduce_max_sync(0xffffffffu, top);
-        const int k = halving(top);
-        const float f = power_of_two(k);
-        if (4 * lane < D) {
-            const uint2 y = make_uint2(Half<__half>::pack(__uint_as_float(x.x << 16) * f, __uint_as_float(x.x & 0xffff0000u) * f),
-                                       Half<__half>::pack(__uint_as_float(x.y << 16) * f, __uint_as_float(x.y & 0xffff0000u) * f));
-            *reinterpret_cast<uint2*>(out + i * D + 4 * lane) = y;
+#pragma unroll
+        for (int e = 0; e < kAtOnce; ++e) {
+            const int64_t i = i0 + e * step;
+            const uint32_t w[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
+            uint32_t top = 0, h[4];  // the largest finite magnitude
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const uint32_t lo = w[c] & 0x7fffu, hi = w[c] >> 16 & 0x7fffu;
+                top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+            }
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const int k = halving(top);
+            const float f = power_of_two(k);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) h[c] = Half<__half>::pack(__uint_as_float(w[c] << 16) * f, __uint_as_float(w[c] & 0xffff0000u) * f);
+            if (i < rows && at < D) *reinterpret_cast<uint4*>(out + i * D + at) = make_uint4(h[0], h[1], h[2], h[3]);
+            if (i < rows && at == 0) row_scale[i] = power_of_two(-k);
         }
-        if (lane == 0) row_scale[i] = power_of_two(-k);
     }
 }
 
@@ -611,7 +621,7 @@ cudaError_t launch_tiles(const AttnArgs& given, const Q4View& z, cudaStream_t st
         char* w = static_cast<char*>(a.ws) + parts4_bytes(a.n_tok, P.group, a.c.head_dim);
         __half* halves = reinterpret_cast<__half*>(w);
         float* factors = reinterpret_cast<float*>(w + halves_bytes(a.n_tok, a.n_heads, a.c.head_dim));
-        const int64_t blocks = std::min<int64_t>((a.n_tok * a.n_heads + 7) / 8, (int64_t)ctas * 8);
+        const int64_t blocks = std::min<int64_t>((a.n_tok * a.n_heads + 15) / 16, (int64_t)ctas * 8);
         const cudaError_t e = launch_pdl(halve_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a, halves, factors);
         if (e != cudaSuccess) return e;
         a.q = {halves, (int64_t)a.n_heads * a.c.head_dim, a.c.head_dim};

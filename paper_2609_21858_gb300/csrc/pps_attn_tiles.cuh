@@ -33,25 +33,102 @@ struct Cfg {
     static constexpr int kMmaWarp = kLoadWarp + 2 * kLoaders, kQueryWarp = kMmaWarp + 1, kThreads = (32 * (kQueryWarp + 1) + 127) / 128 * 128;
     static constexpr int kLoadRows = 128 / kLoaders;         // keys of a tile that a loading warp has
     // of 4 bits: their codes, then their scales, as they come; how many such are on their way to a warp
-    static constexpr int kRow = DC / 2, kScales = DC / 16, kPack = kLoadRows * (kRow + kScales), kPacks = 3;
+    static constexpr int kRow = DC / 2, kScales = DC / 16, kPack = 64 * (kRow + kScales), kPacks = 3;
     // tiles of K and V in flight: 5 (or 12); of 4 bits 3 (or 6)
     static constexpr int kStages = Q4 ? 3 * 128 / DC : (224 * 1024 - 2 * kTile) / kTile;
     static constexpr int kBars = (2 + kStages) * kTile + (Q4 ? 2 * kLoaders * kPacks * kPack : 0);
     static constexpr int kSmem = kBars + 320 /* barriers */ + 224 /* plan */ + 2048 /* maxima and sums */;
-    static_assert(8 * (2 * kStages + 13 + (Q4 ? 2 * kLoaders * kPacks : 0)) <= 320 && kSmem <= 227 * 1024, "barriers and shared memory fit");
+    static_assert(8 * (2 * kStages + 13) <= 320 && (!Q4 || kLoadRows == 64) && kSmem <= 227 * 1024, "barriers and shared memory fit");
 };
 
 // beside the cache, for 4 bits: scales and units; a factor per row (token, head) on its scores, null: ones
 struct Q4Rows {
     Q4View z;
     const float* row_scale;
-    bool dense;  // all DC channels, and a page's rows of a head follow one another, codes and scales, from 16-byte boundaries on
+    bool dense;  // as Copy64 has it
 };
 
 template <int BYTES>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
 }
+
+// A warp copies 64 keys, codes and scales of one half of the cache, from a head's rows (`codes`, `scales`: of page 0) into shared
+// memory, row after row.  Keys of a missing page, and those from `last` on in blocks without any key, get scales of zero, whatever
+// their codes.  Sixteen bytes a lane and instruction throughout: bulk copies of a page's rows take a warp longer, as each of its
+// lanes' is issued by itself (16 rows at a time: 64 keys of one half 1500 clocks, 64 trees of 41 nodes 246 us instead of FIGT).
+// DENSE: all DC channels are there, 16 keys in a row share their page, and a page's rows of a head follow one another, from
+// 16-byte boundaries on (a page laid out head by head).
+template <int DC, bool DENSE>
+struct Copy64 {
+    static constexpr int kRow = DC / 2, kScales = DC / 16, kBytes = 64 * (kRow + kScales);
+    static constexpr int kKeys = DENSE ? 16 : 8;  // with a page to themselves
+    int page, k0;                                 // of keys k0 + kKeys (lane modulo 64 / kKeys) on
+    // of the 64 keys from key k0_ on
+    __device__ __forceinline__ void find(const int32_t* table, int page_log2, int k0_, int last) {
+        const int k = k0_ + kKeys * (threadIdx.x & (64 / kKeys - 1));
+        k0 = k0_;
+        page = k < last ? __ldg(table + (k >> page_log2)) : 0;
+    }
+    __device__ __forceinline__ void go(uint8_t* to, const uint8_t* codes, const uint8_t* scales, const CacheView& c, const Q4View& z, int last, int D,
+                                       bool wide, uint32_t* status) const {
+        const int lane = threadIdx.x & 31;
+        const bool key = k0 + kKeys * (lane & (64 / kKeys - 1)) < last, good = key && (uint32_t)page < (uint32_t)c.n_pages;
+        if (key && !good && status) atomicOr(status, PPS_FLAG_INDEX);
+        const uint32_t who = __ballot_sync(0xffffffffu, good), dst = tc::smem_u32(to);
+        if constexpr (DENSE) {
+            constexpr int kTurns = 16 * kRow / 512;  // of 16 keys' codes
+#pragma unroll
+            for (int G = 0; G < 4; ++G) {
+                const int p = __shfl_sync(0xffffffffu, page, G);
+                if (!(who >> G & 1u)) continue;  // (warp-uniform)
+                const uint8_t* src = codes + p * c.page + ((k0 + 16 * G) & (c.page_size - 1)) * kRow + 16 * lane;
+#pragma unroll
+                for (int i = 0; i < kTurns; ++i) copy_async<16>(dst + 16 * G * kRow + 512 * i + 16 * lane, src + 512 * i);
+            }
+            constexpr int kLanes = 16 * kScales / 16;  // of 16 keys' scales
+            const int G = lane / kLanes & 3, p = __shfl_sync(0xffffffffu, page, G);
+            if (lane < 4 * kLanes) {
+                const uint32_t at = dst + 64 * kRow + 16 * lane;
+                if (who >> G & 1u)
+                    copy_async<16>(at, scales + p * z.page + ((k0 + 16 * G) & (c.page_size - 1)) * kScales + 16 * (lane % kLanes));
+                else
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
+            }
+        } else {
+            const int part = lane & 3;  // four lanes copy a row of codes
+            const int64_t mine = (lane >> 2) * c.tok + part * (DC / 8);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int p = __shfl_sync(0xffffffffu, page, i), k = k0 + 8 * i;
+                if (!(who >> i & 1u) || k + (lane >> 2) >= last || part * (DC / 4) >= D) continue;
+                const uint8_t* src = codes + p * c.page + (k & (c.page_size - 1)) * c.tok + mine;
+                const uint32_t at = dst + (8 * i + (lane >> 2)) * kRow + part * (DC / 8);
+                if (DC == 128 && wide)
+                    copy_async<16>(at, src);
+                else {
+                    copy_async<8>(at, src);
+                    if (DC == 128 && part * (DC / 4) + 16 < D) copy_async<8>(at + 8, src + 8);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = lane + 32 * i, p = __shfl_sync(0xffffffffu, page, r >> 3);
+                const uint32_t at = dst + 64 * kRow + r * kScales;
+                const bool there = (who >> (r >> 3) & 1u) && k0 + r < last;
+                const uint8_t* src = scales + p * z.page + ((k0 + r) & (c.page_size - 1)) * z.tok;
+#pragma unroll
+                for (int w = 0; w < DC / 64; ++w) {
+                    if (there && 64 * w < D)
+                        copy_async<4>(at + 4 * w, src + 4 * w);
+                    else
+                        asm volatile("st.shared.b32 [%0], %1;" ::"r"(at + 4 * w), "r"(0) : "memory");
+                }
+            }
+        }
+    }
+};
+
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort) {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort));
 }
@@ -78,7 +155,6 @@ __global__ void __launch_bounds__(Cfg<DC, Q4>::kThreads, 1)
     auto qfull = [&](uint32_t t) { return bar(2 * C::kStages + 6 + t); };
     auto qfree = [&](uint32_t t) { return bar(2 * C::kStages + 8 + t); };
     const uint32_t segbar = bar(2 * C::kStages + 10);
-    auto packed = [&](uint32_t w, uint32_t p) { return bar(2 * C::kStages + 13 + w * C::kPacks + p); };  // of loading warp w
     uint8_t* tail = attn_smem + C::kBars + 320;
     volatile int* abort = reinterpret_cast<volatile int*>(tail);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(tail + 4);
@@ -104,8 +180,6 @@ __global__ void __launch_bounds__(Cfg<DC, Q4>::kThreads, 1)
             mbar_init(qfree(t), 1);
         }
         mbar_init(segbar, 8);
-        if constexpr (Q4)
-            for (int i = 0; i < 2 * C::kLoaders * C::kPacks; ++i) mbar_init(packed(0, i), 1);
         *abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -145,152 +219,90 @@ __global__ void __launch_bounds__(Cfg<DC, Q4>::kThreads, 1)
         else
             asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (Q4 && warp < kMmaWarp) {
-            // ---- as below, of 4 bits: two warps for the keys, two for the values, each with half of a tile's.  Codes and scales come
-            // by bulk copies, a page's rows (or half a tile's) at a time where the cache is dense (R4.dense), else key by key.
-            const uint32_t me = warp - kLoadWarp;
-            const bool is_v = me >= C::kLoaders;
-            const int half0 = (int)(me % C::kLoaders) * C::kLoadRows;  // the tile's first key that is the warp's
-            uint8_t* const packs = attn_smem + (2 + C::kStages) * C::kTile + me * C::kPacks * C::kPack;
-            const uint8_t* const codes = static_cast<const uint8_t*>(is_v ? a.c.v : a.c.k);
-            const uint8_t* const scales = is_v ? R4.z.vs : R4.z.ks;
-            const int box = min(C::kLoadRows, a.c.page_size), boxes = C::kLoadRows / box;  // keys that lie together
-            const bool dense = R4.dense;
-            const bool wide = ((reinterpret_cast<uintptr_t>(codes) | (uintptr_t)a.c.page | (uintptr_t)a.c.tok | (uintptr_t)a.c.head | (uintptr_t)(D / 2)) & 15) == 0;
-            // a bulk copy: lane 2 b + (codes, scales) of box b; else lane, + 32 of the warp's keys
-            const int first_key = half0 + (dense ? (lane >> 1) * box : lane);
-            constexpr int kOwn = C::kLoadRows / 32;
-            uint32_t ring0 = 0, issued = 0, used = 0;
-            bool ok = true;
-            while (ok && W.next(a, P)) {
-                const int n = W.t1 - W.t0, ahead = W.ntok <= P.tt ? 2 : 1, len = W.q.len, kvh = W.heads / P.nsub;
-                const int32_t* table = a.pages + (int64_t)W.s * a.pages_stride;
-                int page[kOwn];  // of the next tile to copy
-                auto pages_of = [&](int j) {
-#pragma unroll
-                    for (int i = 0; i < kOwn; ++i) {
-                        const int64_t k = (int64_t)(W.t0 + j) * kTileKeys + first_key + 32 * i;
-                        if (i == 0 || !dense) page[i] = k < len && j < n && (!dense || lane < 2 * boxes) ? __ldg(table + (k >> P.page_log2)) : 0;
-                    }
-                };
-                auto issue = [&](int j) {
-                    if (j < n) {
-                        const uint32_t st = issued % C::kPacks;
-                        uint8_t* const to = packs + st * C::kPack;
-                        if (dense) {
-                            const int k = (W.t0 + j) * kTileKeys + first_key;
-                            const bool key = lane < 2 * boxes && k < len, good = key && page[0] >= 0 && page[0] < a.c.n_pages;
-                            const uint32_t copied = __ballot_sync(0xffffffffu, good && !(lane & 1));
-                            if (lane == 0) {
-                                if (copied)
-                                    mbar_expect_tx(packed(me, st), __popc(copied) * box * (C::kRow + C::kScales));
-                                else
-                                    mbar_arrive(packed(me, st));
-                            }
-                            __syncwarp();
-                            const int b = lane >> 1, in_page = k & (a.c.page_size - 1);
-                            if (good && !(lane & 1))
-                                bulk_load(smem_u32(to + b * box * C::kRow), codes + page[0] * a.c.page + kvh * a.c.head + in_page * C::kRow, box * C::kRow, packed(me, st));
-                            if (good && (lane & 1))
-                                bulk_load(smem_u32(to + C::kLoadRows * C::kRow + b * box * C::kScales),
-                                          scales + page[0] * R4.z.page + kvh * R4.z.head + in_page * C::kScales, box * C::kScales, packed(me, st));
-                            if (key && !good) {  // a page that is missing: scales of zero, whatever the codes
-                                if (a.status) atomicOr(a.status, PPS_FLAG_INDEX);
-                                for (int i = 0; i < box * C::kScales; i += 4)
-                                    *reinterpret_cast<uint32_t*>(to + C::kLoadRows * C::kRow + b * box * C::kScales + i) = 0;
-                                fence_async_smem();  // (before the stage's next copies)
-                            }
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < kOwn; ++i) {
-                                const int r = lane + 32 * i, k = (W.t0 + j) * kTileKeys + half0 + r, in_page = k & (a.c.page_size - 1);
-                                const uint32_t row = smem_u32(to + r * C::kRow), sc_at = smem_u32(to + C::kLoadRows * C::kRow + r * C::kScales);
-                                if (k >= len || page[i] < 0 || page[i] >= a.c.n_pages) {
-                                    if (k < len && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
-#pragma unroll
-                                    for (int c = 0; c < DC / 64; ++c) asm volatile("st.shared.b32 [%0], %1;" ::"r"(sc_at + 4 * c), "r"(0) : "memory");
-                                    continue;
-                                }
-                                const uint8_t* src = codes + page[i] * a.c.page + in_page * a.c.tok + kvh * a.c.head;
-                                const uint8_t* sp = scales + page[i] * R4.z.page + in_page * R4.z.tok + kvh * R4.z.head;
-                                if (wide) {
-#pragma unroll
-                                    for (int c = 0; c < DC / 32; ++c)
-                                        if (32 * c < D) copy_async<16>(row + 16 * c, src + 16 * c);
-                                } else {
-#pragma unroll
-                                    for (int c = 0; c < DC / 16; ++c)
-                                        if (16 * c < D) copy_async<8>(row + 8 * c, src + 8 * c);
-                                }
-#pragma unroll
-                                for (int c = 0; c < DC / 64; ++c)
-                                    if (64 * c < D) copy_async<4>(sc_at + 4 * c, sp + 4 * c);
-                            }
-                        }
-                        ++issued;
-                    }
-                    if (!dense) asm volatile("cp.async.commit_group;" ::: "memory");
-                };
-                pages_of(0);
+            // ---- as below, of 4 bits: two warps for the keys, two for the values, each with half of a tile's
+            auto load = [&](auto is_dense) {
+                using Copy = Copy64<DC, decltype(is_dense)::value>;
+                const uint32_t me = warp - kLoadWarp;
+                const bool is_v = me >= C::kLoaders;
+                const int half0 = (int)(me % C::kLoaders) * C::kLoadRows;  // the tile's first key that is the warp's
+                uint8_t* const packs = attn_smem + (2 + C::kStages) * C::kTile + me * C::kPacks * C::kPack;
+                const uint8_t* const codes = static_cast<const uint8_t*>(is_v ? a.c.v : a.c.k);
+                const uint8_t* const scales = is_v ? R4.z.vs : R4.z.ks;
+                const bool wide = ((reinterpret_cast<uintptr_t>(codes) | (uintptr_t)a.c.page | (uintptr_t)a.c.tok | (uintptr_t)a.c.head | (uintptr_t)(D / 2)) & 15) == 0;
+                uint32_t ring0 = 0;
+                bool ok = true;
+                while (ok && W.next(a, P)) {
+                    const int n = W.t1 - W.t0, ahead = W.ntok <= P.tt ? 2 : 1, len = W.q.len, kvh = W.heads / P.nsub;
+                    const int32_t* table = a.pages + (int64_t)W.s * a.pages_stride;
+                    const uint8_t* const my_codes = codes + kvh * a.c.head;
+                    const uint8_t* const my_scales = scales + kvh * R4.z.head;
+                    const int last = min(len, W.t1 * kTileKeys);
+                    Copy copy;
+                    uint32_t to_fill = 0, to_use = 0;
+                    auto find = [&](int j) { copy.find(table, P.page_log2, (W.t0 + j) * kTileKeys + half0, last); };
+                    auto issue = [&](int j) {
+                        if (j < n) copy.go(packs + to_fill * C::kPack, my_codes, my_scales, a.c, R4.z, last, D, wide, a.status);
+                        to_fill = to_fill + 1 == C::kPacks ? 0 : to_fill + 1;
+                        asm volatile("cp.async.commit_group;" ::: "memory");
+                    };
+                    find(0);
 #pragma unroll 1
-                for (int j = 0; j < C::kPacks - 1; ++j) {
-                    issue(j);
-                    pages_of(j + 1);
-                }
+                    for (int j = 0; j < C::kPacks - 1; ++j) {
+                        issue(j);
+                        find(j + 1);
+                    }
 #pragma unroll 1
-                for (int j = 0; j < n; ++j) {
-                    __syncwarp();  // the stage that is filled now has been read
-                    issue(j + C::kPacks - 1);
-                    pages_of(j + C::kPacks);
-                    const uint32_t st = used % C::kPacks;
-                    if (dense) {
-                        if (!(ok = wait_warp(packed(me, st), used / C::kPacks & 1u, abort))) break;
-                    } else {
+                    for (int j = 0; j < n; ++j) {
+                        __syncwarp();  // what is filled now has been read
+                        issue(j + C::kPacks - 1);
+                        find(j + C::kPacks);
                         asm volatile("cp.async.wait_group %0;" ::"n"(C::kPacks - 1) : "memory");
                         __syncwarp();
-                    }
-                    ++used;
-                    const uint32_t it = ring0 + (is_v ? (j + ahead < n ? ahead + 2 * j : n + j) : j < ahead ? j : 2 * j - ahead + 1);
-                    const uint32_t s = it % C::kStages;
-                    if (!(ok = wait_warp(empty(s), ((it / C::kStages) & 1u) ^ 1u, abort))) break;
-                    // a lane widens 16 bytes of codes, 32 channels, of a key at a time; lanes of a key are neighbours
-                    constexpr int kU = DC / 32, kAt = 32 / kU;  // lanes of a key, keys of a turn
-                    const int c = lane % kU, r0 = lane / kU, there = len - (W.t0 + j) * kTileKeys - half0;
-                    const uint8_t* src = packs + st * C::kPack;
-                    uint8_t* dst = attn_smem + (2 + s) * C::kTile + (c >> 1) * C::kBlock + (half0 + r0) * 128;
-                    const bool lo_there = 32 * c < D, hi_there = 32 * c + 16 < D;  // (the bytes behind the last block's may be anything)
+                        const uint8_t* const src = packs + to_use * C::kPack;
+                        to_use = to_use + 1 == C::kPacks ? 0 : to_use + 1;
+                        const uint32_t it = ring0 + (is_v ? (j + ahead < n ? ahead + 2 * j : n + j) : j < ahead ? j : 2 * j - ahead + 1);
+                        const uint32_t s = it % C::kStages;
+                        if (!(ok = wait_warp(empty(s), ((it / C::kStages) & 1u) ^ 1u, abort))) break;
+                        // a lane widens 16 bytes of codes, 32 channels, of a key at a time; lanes of a key are neighbours
+                        constexpr int kU = DC / 32, kAt = 32 / kU;  // lanes of a key, keys of a turn
+                        const int c = lane % kU, r0 = lane / kU, there = len - (W.t0 + j) * kTileKeys - half0;
+                        uint8_t* dst = attn_smem + (2 + s) * C::kTile + (c >> 1) * C::kBlock + (half0 + r0) * 128;
+                        const bool lo_there = 32 * c < D, hi_there = 32 * c + 16 < D;  // (the bytes behind the last block's may be anything)
 #pragma unroll 2
-                    for (int i = 0; i < C::kLoadRows / kAt; ++i) {
-                        const int r = i * kAt + r0;
-                        const uint4 w = *reinterpret_cast<const uint4*>(src + r * C::kRow + 16 * c);
-                        const uint32_t s2 = q4::scales2(*reinterpret_cast<const uint16_t*>(src + C::kLoadRows * C::kRow + r * C::kScales + 2 * c));
-                        const bool key = r < there;
-                        const uint32_t lo = key && lo_there ? __byte_perm(s2, 0, 0x1010) : 0u, hi = key && hi_there ? __byte_perm(s2, 0, 0x3232) : 0u;
-                        // lanes of the second 64 channels begin with the other block of 16, so that eight lanes' stores touch all banks
-                        const bool swap = (c & 2) != 0;
-                        const uint32_t x[4] = {swap ? w.z : w.x, swap ? w.w : w.y, swap ? w.x : w.z, swap ? w.y : w.w};
-                        const uint32_t y[2] = {swap ? hi : lo, swap ? lo : hi};
-                        const uint32_t turn = (uint32_t)((c & 1) * 4 + (swap ? 2 : 0)) ^ (uint32_t)(r & 7);
-                        uint8_t* to = dst + i * kAt * 128;
+                        for (int i = 0; i < C::kLoadRows / kAt; ++i) {
+                            const int r = i * kAt + r0;
+                            const uint4 w = *reinterpret_cast<const uint4*>(src + r * C::kRow + 16 * c);
+                            const uint32_t s2 = q4::scales2(*reinterpret_cast<const uint16_t*>(src + C::kLoadRows * C::kRow + r * C::kScales + 2 * c));
+                            const bool key = r < there;
+                            const uint32_t lo = key && lo_there ? __byte_perm(s2, 0, 0x1010) : 0u, hi = key && hi_there ? __byte_perm(s2, 0, 0x3232) : 0u;
+                            // lanes of the second 64 channels begin with the other block of 16, so that eight lanes' stores touch all banks
+                            const bool swap = (c & 2) != 0;
+                            const uint32_t x[4] = {swap ? w.z : w.x, swap ? w.w : w.y, swap ? w.x : w.z, swap ? w.y : w.w};
+                            const uint32_t y[2] = {swap ? hi : lo, swap ? lo : hi};
+                            const uint32_t turn = (uint32_t)((c & 1) * 4 + (swap ? 2 : 0)) ^ (uint32_t)(r & 7);
+                            uint8_t* to = dst + i * kAt * 128;
 #pragma unroll
-                        for (int u = 0; u < 4; ++u) {
-                            uint32_t h[4];
-                            q4::widen8(x[u], h);
+                            for (int u = 0; u < 4; ++u) {
+                                uint32_t h[4];
+                                q4::widen8(x[u], h);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) h[e] = q4::mul_halves(h[e], y[u >> 1]);
-                            *reinterpret_cast<uint4*>(to + ((turn ^ u) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                                for (int e = 0; e < 4; ++e) h[e] = q4::mul_halves(h[e], y[u >> 1]);
+                                *reinterpret_cast<uint4*>(to + ((turn ^ u) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                            }
                         }
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(full(s));
                     }
-                    fence_async_smem();
+                    asm volatile("cp.async.wait_all;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(full(s));
+                    ring0 += 2 * n;
                 }
-                if (!dense) asm volatile("cp.async.wait_all;" ::: "memory");
-                ring0 += 2 * n;
-            }
-            // copies in flight when the CTA gives up: wait (bounded) for each
-            for (; dense && *abort && used < issued; ++used)
-                for (uint32_t i = 0; i < kWaitLimit && !mbar_try_wait(packed(me, used % C::kPacks), used / C::kPacks & 1u); ++i) {
-                }
+            };
+            if (R4.dense)
+                load(std::true_type());
+            else
+                load(std::false_type());
         } else if (warp < kMmaWarp) {
             // ---- one warp loads the keys' tiles, one the values'.  The ring holds them in the order of their use: K of
             // the first tile (or two, one per stream), then V_j and the next K in turn.
