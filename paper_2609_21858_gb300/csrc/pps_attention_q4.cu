@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
     if (DENSE && tid == 0 && *static_cast<volatile int*>(&s_abort) && a.status) atomicOr(a.status, PPS_FLAG_TIMEOUT);
 }
 
-// Whether a cache lies as Copy64 wants it dense.
+// Whether a cache lies as CopyKeys wants it dense.
 bool is_dense(const AttnArgs& a, const Q4View& z, int dc) {
     const uintptr_t bits = reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v) | reinterpret_cast<uintptr_t>(z.ks) |
                            reinterpret_cast<uintptr_t>(z.vs) | (uintptr_t)a.c.page | (uintptr_t)a.c.head | (uintptr_t)z.page | (uintptr_t)z.head;

@@ -27,25 +27,25 @@ template <int DC, bool Q4>
 struct Cfg {
     static constexpr int kBlock = 128 * 128;                 // 128 rows of 64 channels, 128-byte swizzle
     static constexpr int kTile = kBlock * (DC / 64);         // 16 or 32 KB: a tile of Q, K or V
-    // warps that load keys, then as many that load values; one that issues products, one that loads queries
-    static constexpr int kLoaders = Q4 ? 2 : 1;
-    // (each quarter of the SM gets as many warps of a kind as the others: 14 become 16)
-    static constexpr int kMmaWarp = kLoadWarp + 2 * kLoaders, kQueryWarp = kMmaWarp + 1, kThreads = (32 * (kQueryWarp + 1) + 127) / 128 * 128;
-    static constexpr int kLoadRows = 128 / kLoaders;         // keys of a tile that a loading warp has
-    // of 4 bits: their codes, then their scales, as they come; how many such are on their way to a warp
-    static constexpr int kRow = DC / 2, kScales = DC / 16, kPack = 64 * (kRow + kScales), kPacks = 3;
+    // Warps that load, one that issues products, one that loads queries: the same number of warps on each quarter of the SM.  Of 16
+    // bits one loads keys, one values; of 4 bits six take the halves of the tiles of keys and of values in turn.
+    static constexpr int kLoaders = Q4 ? 6 : 2;
+    static constexpr int kMmaWarp = kLoadWarp + kLoaders, kQueryWarp = kMmaWarp + 1, kThreads = 32 * (kQueryWarp + 1);
+    static constexpr int kHalves = Q4 ? 2 : 1;               // loads that fill a tile
+    // of 4 bits: codes, then scales of half a tile, as they come; how many such a warp has, on their way or in use
+    static constexpr int kHalf = 64, kRow = DC / 2, kScales = DC / 16, kPack = kHalf * (kRow + kScales), kPacks = 2;
     // tiles of K and V in flight: 5 (or 12); of 4 bits 3 (or 6)
     static constexpr int kStages = Q4 ? 3 * 128 / DC : (224 * 1024 - 2 * kTile) / kTile;
-    static constexpr int kBars = (2 + kStages) * kTile + (Q4 ? 2 * kLoaders * kPacks * kPack : 0);
+    static constexpr int kBars = (2 + kStages) * kTile + (Q4 ? kLoaders * kPacks * kPack : 0);
     static constexpr int kSmem = kBars + 320 /* barriers */ + 224 /* plan */ + 2048 /* maxima and sums */;
-    static_assert(8 * (2 * kStages + 13) <= 320 && (!Q4 || kLoadRows == 64) && kSmem <= 227 * 1024, "barriers and shared memory fit");
+    static_assert(8 * (2 * kStages + 13) <= 320 && kThreads % 128 == 0 && kSmem <= 227 * 1024, "barriers and shared memory fit");
 };
 
 // beside the cache, for 4 bits: scales and units; a factor per row (token, head) on its scores, null: ones
 struct Q4Rows {
     Q4View z;
     const float* row_scale;
-    bool dense;  // as Copy64 has it
+    bool dense;  // as CopyKeys has it
 };
 
 template <int BYTES>
@@ -53,33 +53,33 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
 }
 
-// A warp copies 64 keys, codes and scales of one half of the cache, from a head's rows (`codes`, `scales`: of page 0) into shared
+// A warp copies 32 or 64 keys, codes and scales of one half of the cache, from a head's rows (`codes`, `scales`: of page 0) into shared
 // memory, row after row.  Keys of a missing page, and those from `last` on in blocks without any key, get scales of zero, whatever
 // their codes.  Sixteen bytes a lane and instruction throughout: bulk copies of a page's rows take a warp longer, as each of its
 // lanes' is issued by itself (16 rows at a time: 64 keys of one half 1500 clocks, 64 trees of 41 nodes 246 us instead of FIGT).
 // DENSE: all DC channels are there, 16 keys in a row share their page, and a page's rows of a head follow one another, from
 // 16-byte boundaries on (a page laid out head by head).
-template <int DC, bool DENSE>
-struct Copy64 {
-    static constexpr int kRow = DC / 2, kScales = DC / 16, kBytes = 64 * (kRow + kScales);
+template <int DC, bool DENSE, int KEYS>
+struct CopyKeys {
+    static constexpr int kRow = DC / 2, kScales = DC / 16, kBytes = KEYS * (kRow + kScales);
     static constexpr int kKeys = DENSE ? 16 : 8;  // with a page to themselves
-    int page, k0;                                 // of keys k0 + kKeys (lane modulo 64 / kKeys) on
-    // of the 64 keys from key k0_ on
+    int page, k0;                                 // of keys k0 + kKeys (lane modulo KEYS / kKeys) on
+    // of the keys from key k0_ on
     __device__ __forceinline__ void find(const int32_t* table, int page_log2, int k0_, int last) {
-        const int k = k0_ + kKeys * (threadIdx.x & (64 / kKeys - 1));
+        const int k = k0_ + kKeys * (threadIdx.x & (KEYS / kKeys - 1));
         k0 = k0_;
         page = k < last ? __ldg(table + (k >> page_log2)) : 0;
     }
     __device__ __forceinline__ void go(uint8_t* to, const uint8_t* codes, const uint8_t* scales, const CacheView& c, const Q4View& z, int last, int D,
                                        bool wide, uint32_t* status) const {
         const int lane = threadIdx.x & 31;
-        const bool key = k0 + kKeys * (lane & (64 / kKeys - 1)) < last, good = key && (uint32_t)page < (uint32_t)c.n_pages;
+        const bool key = k0 + kKeys * (lane & (KEYS / kKeys - 1)) < last, good = key && (uint32_t)page < (uint32_t)c.n_pages;
         if (key && !good && status) atomicOr(status, PPS_FLAG_INDEX);
         const uint32_t who = __ballot_sync(0xffffffffu, good), dst = tc::smem_u32(to);
         if constexpr (DENSE) {
             constexpr int kTurns = 16 * kRow / 512;  // of 16 keys' codes
 #pragma unroll
-            for (int G = 0; G < 4; ++G) {
+            for (int G = 0; G < KEYS / 16; ++G) {
                 const int p = __shfl_sync(0xffffffffu, page, G);
                 if (!(who >> G & 1u)) continue;  // (warp-uniform)
                 const uint8_t* src = codes + p * c.page + ((k0 + 16 * G) & (c.page_size - 1)) * kRow + 16 * lane;
@@ -87,9 +87,9 @@ struct Copy64 {
                 for (int i = 0; i < kTurns; ++i) copy_async<16>(dst + 16 * G * kRow + 512 * i + 16 * lane, src + 512 * i);
             }
             constexpr int kLanes = 16 * kScales / 16;  // of 16 keys' scales
-            const int G = lane / kLanes & 3, p = __shfl_sync(0xffffffffu, page, G);
-            if (lane < 4 * kLanes) {
-                const uint32_t at = dst + 64 * kRow + 16 * lane;
+            const int G = lane / kLanes & (KEYS / 16 - 1), p = __shfl_sync(0xffffffffu, page, G);
+            if (lane < KEYS / 16 * kLanes) {
+                const uint32_t at = dst + KEYS * kRow + 16 * lane;
                 if (who >> G & 1u)
                     copy_async<16>(at, scales + p * z.page + ((k0 + 16 * G) & (c.page_size - 1)) * kScales + 16 * (lane % kLanes));
                 else
@@ -99,7 +99,7 @@ struct Copy64 {
             const int part = lane & 3;  // four lanes copy a row of codes
             const int64_t mine = (lane >> 2) * c.tok + part * (DC / 8);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < KEYS / 8; ++i) {
                 const int p = __shfl_sync(0xffffffffu, page, i), k = k0 + 8 * i;
                 if (!(who >> i & 1u) || k + (lane >> 2) >= last || part * (DC / 4) >= D) continue;
                 const uint8_t* src = codes + p * c.page + (k & (c.page_size - 1)) * c.tok + mine;
@@ -112,9 +112,9 @@ struct Copy64 {
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < KEYS / 32; ++i) {
                 const int r = lane + 32 * i, p = __shfl_sync(0xffffffffu, page, r >> 3);
-                const uint32_t at = dst + 64 * kRow + r * kScales;
+                const uint32_t at = dst + KEYS * kRow + r * kScales;
                 const bool there = (who >> (r >> 3) & 1u) && k0 + r < last;
                 const uint8_t* src = scales + p * z.page + ((k0 + r) & (c.page_size - 1)) * z.tok;
 #pragma unroll
@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(Cfg<DC, Q4>::kThreads, 1)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = blockIdx.x;
     if (tid == 0) {
         for (int s = 0; s < C::kStages; ++s) {
-            mbar_init(full(s), C::kLoaders);
+            mbar_init(full(s), C::kHalves);
             mbar_init(empty(s), 1);
         }
         for (int w = 0; w < 2; ++w) {
@@ -219,60 +219,65 @@ __global__ void __launch_bounds__(Cfg<DC, Q4>::kThreads, 1)
         else
             asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (Q4 && warp < kMmaWarp) {
-            // ---- as below, of 4 bits: two warps for the keys, two for the values, each with half of a tile's
+            // ---- as below, of 4 bits: half a tile of keys or of values at a time
             auto load = [&](auto is_dense) {
-                using Copy = Copy64<DC, decltype(is_dense)::value>;
-                const uint32_t me = warp - kLoadWarp;
-                const bool is_v = me >= C::kLoaders;
-                const int half0 = (int)(me % C::kLoaders) * C::kLoadRows;  // the tile's first key that is the warp's
+                using Copy = CopyKeys<DC, decltype(is_dense)::value, C::kHalf>;
+                const int me = warp - kLoadWarp;
                 uint8_t* const packs = attn_smem + (2 + C::kStages) * C::kTile + me * C::kPacks * C::kPack;
-                const uint8_t* const codes = static_cast<const uint8_t*>(is_v ? a.c.v : a.c.k);
-                const uint8_t* const scales = is_v ? R4.z.vs : R4.z.ks;
-                const bool wide = ((reinterpret_cast<uintptr_t>(codes) | (uintptr_t)a.c.page | (uintptr_t)a.c.tok | (uintptr_t)a.c.head | (uintptr_t)(D / 2)) & 15) == 0;
+                const bool wide = ((reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v) | (uintptr_t)a.c.page | (uintptr_t)a.c.tok |
+                                    (uintptr_t)a.c.head | (uintptr_t)(D / 2)) & 15) == 0;
                 uint32_t ring0 = 0;
                 bool ok = true;
                 while (ok && W.next(a, P)) {
-                    const int n = W.t1 - W.t0, ahead = W.ntok <= P.tt ? 2 : 1, len = W.q.len, kvh = W.heads / P.nsub;
+                    const int n = W.t1 - W.t0, ahead = min(W.ntok <= P.tt ? 2 : 1, n), len = W.q.len, kvh = W.heads / P.nsub;
                     const int32_t* table = a.pages + (int64_t)W.s * a.pages_stride;
-                    const uint8_t* const my_codes = codes + kvh * a.c.head;
-                    const uint8_t* const my_scales = scales + kvh * R4.z.head;
                     const int last = min(len, W.t1 * kTileKeys);
                     Copy copy;
                     uint32_t to_fill = 0, to_use = 0;
-                    auto find = [&](int j) { copy.find(table, P.page_log2, (W.t0 + j) * kTileKeys + half0, last); };
-                    auto issue = [&](int j) {
-                        if (j < n) copy.go(packs + to_fill * C::kPack, my_codes, my_scales, a.c, R4.z, last, D, wide, a.status);
-                        to_fill = to_fill + 1 == C::kPacks ? 0 : to_fill + 1;
-                        asm volatile("cp.async.commit_group;" ::: "memory");
+                    // load u: the half u % 2 of the tile at place u / 2 of the segment's in the ring (below); twice the tile's number, + 1: values.
+                    // A warp takes every sixth load of all segments, so that its places in the ring are 3 apart: a wait for a
+                    // place's last use, told by its parity, would not tell it from the use before that if they were over kStages apart.
+                    auto tile_of = [&](int u) {
+                        const int x = u / 2, y = x - ahead;
+                        return x < ahead ? 2 * x : y < 2 * (n - ahead) ? (y & 1 ? 2 * (ahead + y / 2) : 2 * (y / 2) + 1) : 2 * (y - (n - ahead)) + 1;
                     };
-                    find(0);
+                    auto key_of = [&](int u) { return (W.t0 + tile_of(u) / 2) * kTileKeys + C::kHalf * (u & 1); };
+                    const int first = (int)((me + 2 * C::kLoaders - 2 * ring0 % C::kLoaders) % C::kLoaders);
+                    auto issue = [&](int u) {
+                        if (u < 4 * n) {
+                            const bool is_v = tile_of(u) & 1;
+                            copy.go(packs + to_fill * C::kPack, static_cast<const uint8_t*>(is_v ? a.c.v : a.c.k) + kvh * a.c.head,
+                                    (is_v ? R4.z.vs : R4.z.ks) + kvh * R4.z.head, a.c, R4.z, last, D, wide, a.status);
+                        }
+                        to_fill ^= 1u;
+                        asm volatile("cp.async.commit_group;" ::: "memory");
+                        copy.find(table, P.page_log2, key_of(u + C::kLoaders), last);
+                    };
+                    static_assert(C::kPacks == 2, "one on its way, one in use");
+                    copy.find(table, P.page_log2, key_of(first), last);
+                    issue(first);
 #pragma unroll 1
-                    for (int j = 0; j < C::kPacks - 1; ++j) {
-                        issue(j);
-                        find(j + 1);
-                    }
-#pragma unroll 1
-                    for (int j = 0; j < n; ++j) {
+                    for (int u = first; u < 4 * n; u += C::kLoaders) {
                         __syncwarp();  // what is filled now has been read
-                        issue(j + C::kPacks - 1);
-                        find(j + C::kPacks);
-                        asm volatile("cp.async.wait_group %0;" ::"n"(C::kPacks - 1) : "memory");
+                        issue(u + C::kLoaders);
+                        asm volatile("cp.async.wait_group 1;" ::: "memory");
                         __syncwarp();
                         const uint8_t* const src = packs + to_use * C::kPack;
-                        to_use = to_use + 1 == C::kPacks ? 0 : to_use + 1;
-                        const uint32_t it = ring0 + (is_v ? (j + ahead < n ? ahead + 2 * j : n + j) : j < ahead ? j : 2 * j - ahead + 1);
+                        to_use ^= 1u;
+                        const int half0 = C::kHalf * (u & 1);
+                        const uint32_t it = ring0 + u / 2;
                         const uint32_t s = it % C::kStages;
                         if (!(ok = wait_warp(empty(s), ((it / C::kStages) & 1u) ^ 1u, abort))) break;
                         // a lane widens 16 bytes of codes, 32 channels, of a key at a time; lanes of a key are neighbours
                         constexpr int kU = DC / 32, kAt = 32 / kU;  // lanes of a key, keys of a turn
-                        const int c = lane % kU, r0 = lane / kU, there = len - (W.t0 + j) * kTileKeys - half0;
+                        const int c = lane % kU, r0 = lane / kU, there = len - key_of(u);
                         uint8_t* dst = attn_smem + (2 + s) * C::kTile + (c >> 1) * C::kBlock + (half0 + r0) * 128;
                         const bool lo_there = 32 * c < D, hi_there = 32 * c + 16 < D;  // (the bytes behind the last block's may be anything)
 #pragma unroll 2
-                        for (int i = 0; i < C::kLoadRows / kAt; ++i) {
+                        for (int i = 0; i < C::kHalf / kAt; ++i) {
                             const int r = i * kAt + r0;
                             const uint4 w = *reinterpret_cast<const uint4*>(src + r * C::kRow + 16 * c);
-                            const uint32_t s2 = q4::scales2(*reinterpret_cast<const uint16_t*>(src + C::kLoadRows * C::kRow + r * C::kScales + 2 * c));
+                            const uint32_t s2 = q4::scales2(*reinterpret_cast<const uint16_t*>(src + C::kHalf * C::kRow + r * C::kScales + 2 * c));
                             const bool key = r < there;
                             const uint32_t lo = key && lo_there ? __byte_perm(s2, 0, 0x1010) : 0u, hi = key && hi_there ? __byte_perm(s2, 0, 0x3232) : 0u;
                             // lanes of the second 64 channels begin with the other block of 16, so that eight lanes' stores touch all banks
@@ -282,12 +287,12 @@ __global__ void __launch_bounds__(Cfg<DC, Q4>::kThreads, 1)
                             const uint32_t turn = (uint32_t)((c & 1) * 4 + (swap ? 2 : 0)) ^ (uint32_t)(r & 7);
                             uint8_t* to = dst + i * kAt * 128;
 #pragma unroll
-                            for (int u = 0; u < 4; ++u) {
+                            for (int b = 0; b < 4; ++b) {
                                 uint32_t h[4];
-                                q4::widen8(x[u], h);
+                                q4::widen8(x[b], h);
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) h[e] = q4::mul_halves(h[e], y[u >> 1]);
-                                *reinterpret_cast<uint4*>(to + ((turn ^ u) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                                for (int e = 0; e < 4; ++e) h[e] = q4::mul_halves(h[e], y[b >> 1]);
+                                *reinterpret_cast<uint4*>(to + ((turn ^ b) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
                             }
                         }
                         fence_async_smem();
