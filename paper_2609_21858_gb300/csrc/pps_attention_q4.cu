@@ -107,12 +107,12 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
     const uint32_t ring_at = smem_u32(my_ring), bar_at = smem_u32(&s_bar[warp][0]);
     const bool wide = ((reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v) | (uintptr_t)a.c.page | (uintptr_t)a.c.tok |
                         (uintptr_t)a.c.head | (uintptr_t)(D / 2)) & 15) == 0;
-    // of a bulk copy, lane 4 G + kind (keys, values, scales of keys, of values): the G-th 16 keys' rows
-    const int kind = lane & 3, G16 = lane >> 2 & (kGroups - 1);
-    const uint8_t* const part = kind == 0 ? static_cast<const uint8_t*>(a.c.k) : kind == 1 ? static_cast<const uint8_t*>(a.c.v) : kind == 2 ? z.ks : z.vs;
-    const int64_t part_page = kind < 2 ? a.c.page : z.page;
-    const int part_row = kind < 2 ? S::kRow : S::kScales;
-    const uint32_t part_at = (kind == 0 ? 0 : kind == 1 ? S::kV : kind == 2 ? S::kKs : S::kVs) + 16 * G16 * part_row;
+    // of a bulk copy, lane 2 G + kind (keys, values): the codes of the G-th 16 keys; scales come sixteen bytes a lane
+    const int kind = lane & 1, G16 = lane >> 1 & (kGroups - 1);
+    const uint8_t* const part = static_cast<const uint8_t*>(kind ? a.c.v : a.c.k);
+    const uint32_t part_at = (kind ? S::kV : 0) + 16 * G16 * S::kRow;
+    constexpr int kScaleLanes = 16 * S::kScales / 16;  // of 16 keys
+    const int Gs = lane / kScaleLanes & (kGroups - 1);
     // key by key: four lanes copy a row of codes; a lane has the scales of keys lane, + 32
     const int64_t quarter = (lane >> 2) * a.c.tok + (lane & 3) * (DC / 8);
     const bool q_there = (lane & 3) * (DC / 4) < D, q_half = (lane & 3) * (DC / 4) + 16 < D;
@@ -134,7 +134,8 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
             const int k = k0 + (DENSE ? 16 * G16 : 8 * (lane & 7));
             return k < last ? __ldg(table + (k >> P.page_log2)) : 0;
         };
-        const uint8_t* const my_part = part + kvh * (kind < 2 ? a.c.head : z.head);
+        const uint8_t* const my_part = part + kvh * a.c.head;
+        const int64_t my_scales = kvh * z.head + 16 * (lane % kScaleLanes);
         uint32_t paged = 0;  // a bit per 16 keys of the units on their way, the newest lowest: their page is there
         auto fill = [&](int k0, int page) {
             const uint32_t to = ring_at + to_fill * S::kBytes, full = bar_at + 8 * to_fill;
@@ -143,16 +144,22 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                 const int k = k0 + 16 * G16, in_page = k & (a.c.page_size - 1);
                 const bool key = k < last, good = key && (uint32_t)page < (uint32_t)a.c.n_pages;  // (a missing page reads as zeros)
                 if (key && !good && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
-                const uint32_t who = __ballot_sync(0xffffffffu, good && kind == 0) & ((1u << 4 * kGroups) - 1u);
-                paged = paged << 4 * kGroups | who;
+                const uint32_t who = __ballot_sync(0xffffffffu, good && kind == 0) & ((1u << 2 * kGroups) - 1u);
+                paged = paged << 2 * kGroups | who;
                 if (lane == 0) {
                     if (who)
-                        mbar_expect_tx(full, __popc(who) * (16 * 2 * (S::kRow + S::kScales)));
+                        mbar_expect_tx(full, __popc(who) * (16 * 2 * S::kRow));
                     else
                         mbar_arrive(full);
                 }
                 __syncwarp();
-                if (lane < 4 * kGroups && good) bulk_load(to + part_at, my_part + page * part_page + in_page * part_row, 16 * part_row, full);
+                if (lane < 2 * kGroups && good) bulk_load(to + part_at, my_part + page * a.c.page + in_page * S::kRow, 16 * S::kRow, full);
+                const int p = __shfl_sync(0xffffffffu, page, 2 * Gs);
+                if (lane < kGroups * kScaleLanes && (who >> 2 * Gs & 1u)) {
+                    const int64_t at = p * z.page + ((k0 + 16 * Gs) & (a.c.page_size - 1)) * S::kScales + my_scales;
+                    copy_async<16>(to + S::kKs + 16 * lane, z.ks + at);
+                    copy_async<16>(to + S::kVs + 16 * lane, z.vs + at);
+                }
             } else {
                 if (k0 + 8 * (lane & 7) < last && (uint32_t)page >= (uint32_t)a.c.n_pages) {  // reads as zeros
                     if (a.status) atomicOr(a.status, PPS_FLAG_INDEX);
@@ -198,7 +205,7 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
             }
         };
         auto close = [&]() {  // a group of copies per unit, with or without any
-            if constexpr (!DENSE) asm volatile("cp.async.commit_group;" ::: "memory");
+            asm volatile("cp.async.commit_group;" ::: "memory");
         };
         constexpr int kStep = kUnit * kWarps4, kAhead4 = kStages4 - 1;
         int k0 = first + warp * kUnit;
@@ -211,7 +218,7 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
             if (k < last)
                 fill(k, p);
             else
-                paged <<= 4 * kGroups;
+                paged <<= 2 * kGroups;
             close();
         }
         // ---- queries: row 8 nt + g, the channels of quarter t, as halves
@@ -276,12 +283,11 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
             if (ahead < last)
                 fill(ahead, page);
             else
-                paged <<= 4 * kGroups;
+                paged <<= 2 * kGroups;
             close();
             if constexpr (DENSE)
                 mbar_wait(bar_at + 8 * to_use, phase, &s_abort);
-            else
-                asm volatile("cp.async.wait_group %0;" ::"n"(kAhead4) : "memory");
+            asm volatile("cp.async.wait_group %0;" ::"n"(kAhead4) : "memory");
             __syncwarp();
             uint8_t* const unit = my_ring + to_use * S::kBytes;
             if (++to_use == kStages4) {
@@ -289,11 +295,11 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                 phase ^= 1u;
             }
             if constexpr (DENSE) {  // keys that are not there, or lie on a missing page, get scales of zero
-                const uint32_t who = paged >> (4 * kGroups * kAhead4) & ((1u << 4 * kGroups) - 1u);
-                if (k0 + kUnit > last || who != (0x1111u & ((1u << 4 * kGroups) - 1u))) {
+                const uint32_t who = paged >> (2 * kGroups * kAhead4) & ((1u << 2 * kGroups) - 1u);
+                if (k0 + kUnit > last || who != (0x5555u & ((1u << 2 * kGroups) - 1u))) {
 #pragma unroll
                     for (int key = lane; key < kUnit; key += 32)
-                        if (k0 + key >= last || !(who >> (4 * (key >> 4)) & 1u)) {
+                        if (k0 + key >= last || !(who >> (2 * (key >> 4)) & 1u)) {
 #pragma unroll
                             for (int i = 0; i < S::kScales; i += 4) {
                                 *reinterpret_cast<uint32_t*>(unit + S::kKs + key * S::kScales + i) = 0;
