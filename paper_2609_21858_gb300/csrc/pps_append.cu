@@ -39,6 +39,9 @@ namespace {
 constexpr int kAppendWarps = 4;  // per CTA
 constexpr int kAhead = 2;        // heads of a lane group in an item
 constexpr int kAppendCtas = 4;   // per SM
+// What an item with keys or values takes where they become 4 bits, to one of queries alone.  16384 tokens of (28 + 2 x 4) heads of 128
+// channels: 77.5 us at 1, 68.4 at 1.3, 71.8 at 1.6, 80.3 at 2 (52.6 into a cache of 16 bits).
+constexpr double kHeavy = 1.3;
 // a block's 16 channels in shared memory, 80 bytes apart: eight lanes' 16-byte reads touch all banks
 constexpr int kBlockFloats = 20;
 
@@ -46,6 +49,7 @@ struct AppendPlan {
     int lg;          // log2 of the lanes per head
     int parts;       // items per token
     int tok_step;    // tokens in work at a time: tok_step x parts warps
+    int light, light_step;  // of 4 bits: the first parts, of queries alone, and their tokens in work at a time (else 0)
     int page_log2;   // -1: not a power of two
     int units;       // units per head
     int pair_units;  // of which rotated
@@ -260,9 +264,12 @@ __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(
     const int D = a.c.head_dim, half = a.rot >> 1;
     const int l = lane & ((1 << P.lg) - 1), hp = 32 >> P.lg, group = lane >> P.lg;
     const int n_kv = a.c.n_kv_heads, n_qk = a.n_heads + n_kv, H = n_qk + n_kv;
-    const uint32_t me = blockIdx.x * kAppendWarps + (threadIdx.x >> 5), n = (uint32_t)a.n_tok, step = (uint32_t)P.tok_step;
-    uint32_t tok = me / (uint32_t)P.parts;
-    const int part = (int)(me - tok * P.parts);
+    const uint32_t me = blockIdx.x * kAppendWarps + (threadIdx.x >> 5), n = (uint32_t)a.n_tok;
+    // the warp's first token, how many tokens further its next one is, and its part of all of them
+    const uint32_t light = Q4 ? (uint32_t)(P.light * P.light_step) : 0u, of = Q4 && me < light ? (uint32_t)P.light : (uint32_t)(P.parts - P.light);
+    const uint32_t step = Q4 && me < light ? (uint32_t)P.light_step : (uint32_t)P.tok_step, mine = Q4 && me >= light ? me - light : me;
+    uint32_t tok = mine / of;
+    const int part = (int)(mine - tok * of) + (Q4 && me >= light ? P.light : 0);
     if (tok >= min(n, step)) return;  // warp-uniform
 
     // the lane's units: channel starts of their two vectors
@@ -300,7 +307,7 @@ __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(
     const int n_blk = Q4 ? D / 16 : 0;
     uint8_t *codes[2] = {}, *scales[2] = {};
     float inv[2] = {};
-    float* const mine = s_x[Q4 ? threadIdx.x >> 5 : 0];
+    float* const spread_at = s_x[Q4 ? threadIdx.x >> 5 : 0];
     const bool holds = Q4 && (part + 1) * kAhead * hp > a.n_heads;  // warp-uniform: keys or values among the item's heads
     if constexpr (Q4) {
 #pragma unroll
@@ -406,7 +413,7 @@ __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(
                 for (int k = 0; k < NU; ++k)
                     if (goes && c0[k] < D) {
                         if constexpr (Q4)
-                            Wide<T, VW>(cur.x[j][k]).spread(mine + (j * hp + group) * n_blk * kBlockFloats, c0[k], c1[k], c1[k] < D);
+                            Wide<T, VW>(cur.x[j][k]).spread(spread_at + (j * hp + group) * n_blk * kBlockFloats, c0[k], c1[k], c1[k] < D);
                         else
                             put(k);
                     }
@@ -438,9 +445,9 @@ __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(
                     if (!Q4 || is_q[j])
                         f.round(cur.x[j][k]);
                     else
-                        f.spread(mine + (j * hp + group) * n_blk * kBlockFloats, c0[k], c1[k], c1[k] < D);
+                        f.spread(spread_at + (j * hp + group) * n_blk * kBlockFloats, c0[k], c1[k], c1[k] < D);
                 } else if constexpr (Q4)
-                    Wide<T, VW>(cur.x[j][k]).spread(mine + (j * hp + group) * n_blk * kBlockFloats, c0[k], c1[k], c1[k] < D);
+                    Wide<T, VW>(cur.x[j][k]).spread(spread_at + (j * hp + group) * n_blk * kBlockFloats, c0[k], c1[k], c1[k] < D);
                 if (!Q4 || is_q[j]) put(k);
                 // A vector that is never read (only one of 8 channels can be) stays zero: a norm that is not finite, or a weight,
                 // would make it NaN, and with it the sums of all heads that these lanes take later.
@@ -454,14 +461,12 @@ __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     if (kept && codes[i] != nullptr) {
-                        const float* x = mine + (lane + 32 * i) * kBlockFloats;
-                        float z[16];
+                        const float* x = spread_at + (lane + 32 * i) * kBlockFloats;
+                        uint64_t z[8];
 #pragma unroll
-                        for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(z + e) = *reinterpret_cast<const float4*>(x + e);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) z[e] *= inv[i];
+                        for (int e = 0; e < 8; e += 2) *reinterpret_cast<ulonglong2*>(z + e) = *reinterpret_cast<const ulonglong2*>(x + 2 * e);
                         uint32_t scale;
-                        const uint2 c = q4::quantise(z, scale);
+                        const uint2 c = q4::quantise(z, inv[i], scale);
                         *reinterpret_cast<uint2*>(codes[i] + in_cache) = c;
                         scales[i][in_scales] = (uint8_t)scale;
                     }
@@ -496,8 +501,15 @@ cudaError_t launch(const AppendArgs& a, cudaStream_t st) {
     const int64_t items = a.n_tok * P.parts, most = (int64_t)device_sm_count() * kAppendCtas * kAppendWarps;
     if (items > INT32_MAX) return cudaErrorInvalidValue;
     P.tok_step = (int)std::max<int64_t>(std::min(items, most) / P.parts, 1);
-    const int64_t blocks = ((int64_t)P.tok_step * P.parts + kAppendWarps - 1) / kAppendWarps;
+    P.light = P.light_step = 0;
     const bool norm = a.q_norm != nullptr || a.k_norm != nullptr, bits4 = a.q4.ks != nullptr;
+    if (bits4) {  // parts with keys or values take longer than those of queries alone: more warps have them
+        P.light = a.n_heads / per_item;
+        const double heavy = kHeavy * (P.parts - P.light);
+        P.light_step = (int)std::min<int64_t>(std::max<int64_t>((int64_t)((double)most / (P.light + heavy)), 1), a.n_tok);
+        P.tok_step = (int)std::min<int64_t>(std::max<int64_t>((int64_t)(kHeavy * (double)most / (P.light + heavy)), 1), a.n_tok);
+    }
+    const int64_t blocks = ((int64_t)P.tok_step * (P.parts - P.light) + (int64_t)P.light * P.light_step + kAppendWarps - 1) / kAppendWarps;
     auto kernel = bits4 ? (norm ? append_kernel<T, VW, NU, true, true> : append_kernel<T, VW, NU, false, true>)
                         : (norm ? append_kernel<T, VW, NU, true, false> : append_kernel<T, VW, NU, false, false>);
     kernel<<<(unsigned)blocks, 32 * kAppendWarps, 0, st>>>(a, P);

@@ -18,8 +18,7 @@
 namespace pps {
 namespace {
 
-constexpr int kPageThreads = 512;
-constexpr int kPageWarps = kPageThreads / 32;
+constexpr int kPageThreads = 1024;  // at most
 constexpr int kPageCluster = 8;
 
 __device__ __forceinline__ void cluster_sync() {
@@ -44,8 +43,7 @@ __device__ __forceinline__ void scan2(int64_t& x, int64_t& y, int64_t& all_x, in
     x = a - x;
     y = b - y;
     all_x = all_y = 0;
-#pragma unroll
-    for (int w = 0; w < kPageWarps; ++w) {
+    for (int w = 0; w < (int)blockDim.x / 32; ++w) {
         const longlong2 v = s[w];
         if (w < warp) {
             x += v.x;
@@ -73,15 +71,17 @@ __device__ __forceinline__ int pages_of(int64_t tokens, int page_size) { return 
 
 __global__ void __launch_bounds__(kPageThreads) reserve_kernel(const ReserveArgs a) {
     extern __shared__ int s_seq[];  // [n_seq] each: tokens before it, pages before it, its length, its pages (~: not served)
-    __shared__ longlong2 s_sum[kPageWarps];
+    __shared__ longlong2 s_sum[kPageThreads / 32];
     const int n = a.n_seq, tid = threadIdx.x;
     int *s_tok = s_seq, *s_page = s_tok + n, *s_len = s_page + n, *s_held = s_len + n;
     const int rank = blockIdx.x, ranks = gridDim.x;  // one cluster
     const int avail = max(min(a.free_count[0], a.free_cap), 0);
     const int64_t most = INT32_MAX;
-    int64_t tok0 = 0, page0 = 0, granted = 0;
+    __shared__ int s_granted;  // pages: the demands before the first one that the pool cannot meet
+    if (tid == 0) s_granted = 0;
+    int64_t tok0 = 0, page0 = 0;
     bool bad = false, out_of = false;
-    for (int s0 = 0; s0 < n; s0 += kPageThreads) {
+    for (int s0 = 0; s0 < n; s0 += blockDim.x) {
         const int s = s0 + tid;
         int64_t n_new = 0, need = 0;
         int len = 0, held = 0;
@@ -105,6 +105,7 @@ __global__ void __launch_bounds__(kPageThreads) reserve_kernel(const ReserveArgs
             const bool served = fits && (need == 0 || y + need <= avail);
             if (!fits) bad = true;
             if (fits && !served) out_of = true;
+            if (served && need > 0) atomicMax(&s_granted, (int)(y + need));
             s_tok[s] = (int)min(x, most);
             s_page[s] = (int)min(y, most);
             s_len[s] = len;
@@ -113,19 +114,10 @@ __global__ void __launch_bounds__(kPageThreads) reserve_kernel(const ReserveArgs
         tok0 += all_x;
         page0 += all_y;
     }
-    // what is granted: the demands before the first one that the pool cannot meet
     __syncthreads();
-    {
-        int64_t g = 0, unused = 0, all, none;
-        for (int s = tid; s < n; s += kPageThreads) {
-            const int next = s + 1 < n ? s_page[s + 1] : (int)min(page0, most);
-            if (s_held[s] >= 0) g += next - s_page[s];
-        }
-        scan2(g, unused, all, none, s_sum);
-        granted = all;
-    }
+    const int granted = s_granted;
     cluster_sync();  // every CTA has read the state
-    const int stride = kPageThreads * ranks, me = rank * kPageThreads + tid;
+    const int stride = blockDim.x * ranks, me = rank * blockDim.x + tid;
     // sequences
     for (int s = me; s < n; s += stride) {
         const int next_t = s + 1 < n ? s_tok[s + 1] : (int)min(tok0, most), next_p = s + 1 < n ? s_page[s + 1] : (int)min(page0, most);
@@ -136,34 +128,44 @@ __global__ void __launch_bounds__(kPageThreads) reserve_kernel(const ReserveArgs
     }
     if (me == 0) {
         a.out_q_off[n] = (int)min(tok0, most);
-        a.free_count[0] = avail - (int)granted;
+        a.free_count[0] = avail - granted;
     }
     // pages
-    for (int p = me; p < (int)granted; p += stride) {
+    for (int p = me; p < granted; p += stride) {
         const int s = find(s_page, n, p);
         a.pages[s * a.pages_stride + s_held[s] + (p - s_page[s])] = __ldg(a.free_list + (avail - 1 - p));
     }
     // tokens
     const int64_t tokens = min(tok0, a.n_tok);
-    for (int64_t i = me; i < a.n_tok; i += stride) {
-        int64_t slot = -1;
-        int pos = 0, seq = -1;
-        if (i < tokens) {
-            seq = find(s_tok, n, (int)i);
-            const int at = (int)i - s_tok[seq], len = s_len[seq];
-            pos = len + (a.pos_off ? __ldg(a.pos_off + i) : at);
-            const int held = s_held[seq];
-            if (held >= 0) {
-                const int64_t place = (int64_t)len + at;
-                const int col = (int)(place / a.page_size);
-                const int page = col < held ? a.pages[seq * a.pages_stride + col] : __ldg(a.free_list + (avail - 1 - (s_page[seq] + col - held)));
-                slot = page < 0 ? -1 : (int64_t)page * a.page_size + place % a.page_size;
-                bad |= page < 0;
-            }
+    constexpr int kAtOnce = 4;
+    for (int64_t i0 = me; i0 < a.n_tok; i0 += (int64_t)kAtOnce * stride) {
+        int seq[kAtOnce], off[kAtOnce], page[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {  // what has to be loaded, on its way together
+            const int64_t i = i0 + (int64_t)k * stride;
+            seq[k] = -1;
+            if (i >= tokens) continue;
+            seq[k] = find(s_tok, n, (int)i);
+            const int at = (int)i - s_tok[seq[k]], held = s_held[seq[k]], col = (int)(((int64_t)s_len[seq[k]] + at) / a.page_size);
+            off[k] = a.pos_off ? __ldg(a.pos_off + i) : at;
+            page[k] = held < 0 ? INT32_MIN : col < held ? a.pages[seq[k] * a.pages_stride + col] : __ldg(a.free_list + (avail - 1 - (s_page[seq[k]] + col - held)));
         }
-        a.out_slot[i] = slot;
-        a.out_pos[i] = pos;
-        if (a.out_seq) a.out_seq[i] = seq;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int64_t i = i0 + (int64_t)k * stride;
+            if (i >= a.n_tok) break;
+            int64_t slot = -1;
+            int pos = 0;
+            if (seq[k] >= 0) {
+                const int len = s_len[seq[k]], at = (int)i - s_tok[seq[k]];
+                pos = len + off[k];
+                if (page[k] >= 0) slot = (int64_t)page[k] * a.page_size + ((int64_t)len + at) % a.page_size;
+                bad |= page[k] < 0 && s_held[seq[k]] >= 0;
+            }
+            a.out_slot[i] = slot;
+            a.out_pos[i] = pos;
+            if (a.out_seq) a.out_seq[i] = seq[k];
+        }
     }
     if (a.status && (bad || (tok0 > a.n_tok && me == 0))) atomicOr(a.status, PPS_FLAG_INDEX);
     if (a.status && out_of) atomicOr(a.status, PPS_FLAG_POOL);
@@ -171,14 +173,14 @@ __global__ void __launch_bounds__(kPageThreads) reserve_kernel(const ReserveArgs
 
 __global__ void __launch_bounds__(kPageThreads) trim_kernel(const ReserveArgs a) {
     extern __shared__ int s_seq[];  // [n_seq] each: pages that sequences before it give back, the pages it keeps
-    __shared__ longlong2 s_sum[kPageWarps];
+    __shared__ longlong2 s_sum[kPageThreads / 32];
     const int n = a.n_seq, tid = threadIdx.x;
     int *s_back = s_seq, *s_keep = s_back + n;
     const int rank = blockIdx.x, ranks = gridDim.x;
     const int have = max(min(a.free_count[0], a.free_cap), 0);
     int64_t back0 = 0;
     bool bad = false;
-    for (int s0 = 0; s0 < n; s0 += kPageThreads) {
+    for (int s0 = 0; s0 < n; s0 += blockDim.x) {
         const int s = s0 + tid;
         int64_t back = 0;
         int keep = 0;
@@ -200,7 +202,7 @@ __global__ void __launch_bounds__(kPageThreads) trim_kernel(const ReserveArgs a)
     __syncthreads();
     cluster_sync();  // every CTA has read the state
     const int64_t total = min(back0, (int64_t)INT32_MAX);
-    const int stride = kPageThreads * ranks, me = rank * kPageThreads + tid;
+    const int stride = blockDim.x * ranks, me = rank * blockDim.x + tid;
     for (int s = me; s < n; s += stride) a.held[s] = s_keep[s];
     const bool over = have + total > a.free_cap;  // more pages than there are: what passes the list's end is lost
     if (me == 0) a.free_count[0] = (int)min(have + total, (int64_t)a.free_cap);
@@ -214,12 +216,14 @@ __global__ void __launch_bounds__(kPageThreads) trim_kernel(const ReserveArgs a)
     if (a.status && (bad || over)) atomicOr(a.status, PPS_FLAG_INDEX);
 }
 
-cudaError_t launch_cluster(void (*kernel)(const ReserveArgs), const ReserveArgs& a, int ctas, int smem, std::atomic<uint64_t>& ready, cudaStream_t st) {
+cudaError_t launch_cluster(void (*kernel)(const ReserveArgs), const ReserveArgs& a, int64_t items, int smem, std::atomic<uint64_t>& ready, cudaStream_t st) {
     cudaError_t e = allow_smem(ready, (const void*)kernel, 4 * (int)sizeof(int) * kMaxPageSeqs);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
+    // one CTA where its threads have a turn or two, else a cluster
+    const int ctas = items <= kPageThreads ? 1 : kPageCluster;
     cfg.gridDim = dim3(ctas);
-    cfg.blockDim = dim3(kPageThreads);
+    cfg.blockDim = dim3(ctas > 1 ? kPageThreads : (int)std::max<int64_t>((items + 31) / 32 * 32, 128));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -231,19 +235,16 @@ cudaError_t launch_cluster(void (*kernel)(const ReserveArgs), const ReserveArgs&
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
-// CTAs: one where its threads have a turn or two, else a cluster
-int cluster_for(int64_t items) { return items <= 2 * kPageThreads ? 1 : kPageCluster; }
-
 }  // namespace
 
 cudaError_t launch_kv_reserve(const ReserveArgs& a, cudaStream_t stream) {
     static std::atomic<uint64_t> ready{0};
-    return launch_cluster(reserve_kernel, a, cluster_for(std::max<int64_t>(a.n_tok, a.n_seq)), 4 * (int)sizeof(int) * a.n_seq, ready, stream);
+    return launch_cluster(reserve_kernel, a, std::max<int64_t>(a.n_tok, a.n_seq), 4 * (int)sizeof(int) * a.n_seq, ready, stream);
 }
 
 cudaError_t launch_kv_trim(const ReserveArgs& a, cudaStream_t stream) {
     static std::atomic<uint64_t> ready{0};
-    return launch_cluster(trim_kernel, a, cluster_for(a.n_seq), 2 * (int)sizeof(int) * a.n_seq, ready, stream);
+    return launch_cluster(trim_kernel, a, a.n_seq, 2 * (int)sizeof(int) * a.n_seq, ready, stream);
 }
 
 }  // namespace pps

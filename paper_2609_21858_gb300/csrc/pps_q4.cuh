@@ -43,30 +43,55 @@ __device__ __forceinline__ float scale_float(uint32_t byte) {
     return __low2float(h);
 }
 
-// Codes (x: channels 0 to 7, y: 8 to 15) and scale byte of a block.  One that is not finite throughout has the scale NaN.
-// z / s is rounded correctly, as a remainder corrects the product with 1 / s (Markstein, IBM J. Res. Dev. 34, 1990): next to the
-// middle between two codes its last bit decides.
-__device__ __forceinline__ uint2 quantise(const float (&z)[16], uint32_t& scale) {
-    uint32_t top = 0;
+__device__ __forceinline__ float max3_abs(float a, float b, float c) {  // NaN if one is
+    float y;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(fabsf(a)), "f"(fabsf(b)), "f"(fabsf(c)));
+    return y;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t both(float x) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(x));
+    return r;
+}
+
+// Codes (x: channels 0 to 7, y: 8 to 15) and scale byte of a block of z = x inv, x in pairs of neighbours.  One that is not finite
+// throughout has the scale NaN.  z / s is rounded correctly, as a remainder corrects the product with 1 / s (Markstein, IBM J. Res.
+// Dev. 34, 1990): next to the middle between two codes its last bit decides.
+__device__ __forceinline__ uint2 quantise(const uint64_t (&x)[8], float inv, uint32_t& scale) {
+    uint64_t z[8];
+    float f[16], top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(z[i]) & 0x7fffffffu);  // NaN above infinity above all others
+    for (int i = 0; i < 8; ++i) {
+        z[i] = mul2(x[i], both(inv));
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(f[2 * i]), "=f"(f[2 * i + 1]) : "l"(z[i]));
+        top = max3_abs(top, f[2 * i], f[2 * i + 1]);
+    }
     scale = 0x7fu;
-    if (top >= 0x7f800000u) return make_uint2(0u, 0u);
-    const float want = __fdiv_rn(__uint_as_float(top), 6.0f);
+    if (!(top < INFINITY)) return make_uint2(0u, 0u);
     uint16_t two;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.0f), "f"(want));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(0.0f), "f"(__fdiv_rn(top, 6.0f)));
     scale = two & 0xffu;
     if (scale == 0) return make_uint2(0u, 0u);
     const float s = scale_float(scale), r = __frcp_rn(s);
+    const uint64_t r2 = both(r), s2 = both(-s);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint64_t p = mul2(z[i], r2), q = fma2(fma2(p, s2, z[i]), r2, p);
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(f[2 * i]), "=f"(f[2 * i + 1]) : "l"(q));
+    }
     uint32_t w[2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        float q[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float x = z[8 * k + i], p = x * r;
-            q[i] = fmaf(fmaf(-p, s, x), r, p);
-        }
+    for (int k = 0; k < 2; ++k)
         asm("{\n\t.reg .b8 a, b, c, d;\n\t"
             "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
             "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
@@ -74,8 +99,8 @@ __device__ __forceinline__ uint2 quantise(const float (&z)[16], uint32_t& scale)
             "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
             "mov.b32 %0, {a, b, c, d};\n\t}"
             : "=r"(w[k])
-            : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[4]), "f"(q[5]), "f"(q[6]), "f"(q[7]));
-    }
+            : "f"(f[8 * k]), "f"(f[8 * k + 1]), "f"(f[8 * k + 2]), "f"(f[8 * k + 3]), "f"(f[8 * k + 4]), "f"(f[8 * k + 5]), "f"(f[8 * k + 6]),
+              "f"(f[8 * k + 7]));
     return make_uint2(w[0], w[1]);
 }
 
