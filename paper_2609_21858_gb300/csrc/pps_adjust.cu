@@ -90,7 +90,8 @@ __device__ __forceinline__ uint32_t bits_at(const uint32_t* words, int i) {
     return __funnelshift_r(lo, hi, i & 31) & ((1u << N) - 1u);
 }
 
-template <typename T, bool COUNTS, bool BIAS>
+// PIECE: tokens that a warp takes of a row at a time
+template <typename T, bool COUNTS, bool BIAS, int PIECE>
 __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustArgs a) {
     constexpr int VN = 16 / sizeof(T);
     __shared__ __align__(16) uint32_t s_count[COUNTS ? kSlice : 4];
@@ -169,10 +170,9 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
     };
 
     // items: pieces of rows
-    // 2048 tokens, or 1024 of a few rows (64 x 41 rows 249 and 276 us, 16 x 9 rows 46 and 44, one row 7.1 and 6.1)
-    const int piece = n_rows >= 16 ? 2048 : 1024, pieces = (tn + piece - 1) / piece;
+    const int pieces = (tn + PIECE - 1) / PIECE;
     for (int item = warp; item < n_rows * pieces; item += kAdjustWarps) {
-        const int i = item / pieces, p0 = (item - i * pieces) * piece, p1 = min(p0 + piece, tn);
+        const int i = item / pieces, p0 = (item - i * pieces) * PIECE, p1 = min(p0 + PIECE, tn);
         const int64_t row = first + i;
         const T* x = static_cast<const T*>(a.x) + row * a.x_stride + t0;
         T* out = static_cast<T*>(a.out) + row * a.out_stride + t0;
@@ -275,8 +275,13 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
 template <typename T>
 cudaError_t by_parts(const AdjustArgs& a, cudaStream_t st) {
     const bool counts = a.text != nullptr || a.node_tok != nullptr, bias = a.bias_tok != nullptr;
-    auto kernel = counts ? (bias ? adjust_kernel<T, true, true> : adjust_kernel<T, true, false>)
-                         : (bias ? adjust_kernel<T, false, true> : adjust_kernel<T, false, false>);
+    // Pieces of 2048 tokens, or of 1024 where a sequence has few rows (64 x 41 rows 249 and 276 us, 16 x 9 rows 46 and 44, one row 7.1
+    // and 6.1).  They are a compile-time choice: 249 us became 290 with a variable.
+    const bool many = a.n_rows / 16 >= a.n_seq;
+    auto kernel = counts ? (bias ? (many ? adjust_kernel<T, true, true, 2048> : adjust_kernel<T, true, true, 1024>)
+                                 : (many ? adjust_kernel<T, true, false, 2048> : adjust_kernel<T, true, false, 1024>))
+                         : (bias ? (many ? adjust_kernel<T, false, true, 2048> : adjust_kernel<T, false, true, 1024>)
+                                 : (many ? adjust_kernel<T, false, false, 2048> : adjust_kernel<T, false, false, 1024>));
     const int64_t slices = (a.V + kSlice - 1) / kSlice;
     for (int s0 = 0; s0 < a.n_seq; s0 += 65535) {  // (a grid's second dimension)
         AdjustArgs part = a;
