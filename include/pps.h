@@ -842,7 +842,7 @@ pps_status pps_kv_trim(const pps_trim_args* args, pps_stream_t stream);
  * bias_off     nullable [n_seq + 1]: entries bias_off[s] .. bias_off[s+1]-1 of
  *              bias_tok, bias_val [n_bias] are added in sequence s; of several for a token the last counts
  * allowed      nullable [n_rows, allowed_stride] words, bit i % 32 of word i / 32:
- *              token i may follow (allowed_stride >= ceil(vocab / 32))
+ *              token i may follow (allowed_stride >= ceil(vocab / 32), or 0: one row for all)
  * Tokens outside the vocabulary are left out (PPS_FLAG_INDEX).
  */
 typedef struct {

@@ -1014,7 +1014,7 @@ pps_status pps_adjust_logits(const pps_adjust_args* args, pps_stream_t stream) {
     if (node_mask && (!node_tok || mask_words < 1)) return PPS_ERR_INVALID_ARG;
     if ((repetition || frequency || presence) && !text && !node_tok) return PPS_ERR_INVALID_ARG;
     if (bias_off && n_bias > 0 && (!bias_tok || !bias_val)) return PPS_ERR_INVALID_ARG;
-    if (allowed && (allowed_stride < (vocab + 31) / 32 || !strides_ok(allowed_stride, n_rows, 0, 0))) return PPS_ERR_INVALID_ARG;
+    if (allowed && ((allowed_stride != 0 && allowed_stride < (vocab + 31) / 32) || !strides_ok(allowed_stride, n_rows, 0, 0))) return PPS_ERR_INVALID_ARG;
     if (n_rows == 0 || n_seq == 0) return PPS_OK;
     if (!logits || !out || !seq_off) return PPS_ERR_INVALID_ARG;
     AdjustArgs a;

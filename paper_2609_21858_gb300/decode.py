@@ -10,6 +10,11 @@ One step of `Session`, for all its sequences at once and without waiting for the
   keep       the accepted nodes' keys and values move up behind the prefix: pps_kv_append once more, with
              slot -1 for the others (a chain's nodes already lie there)
 
+A cache of 4 bits takes pps_kv_append_q4 and pps_paged_attention_q4 in their place.  Pages either belong to a sequence for good, or
+come from a pool: then pps_kv_reserve gives a step's nodes their pages, slots and positions, and pps_kv_trim takes
+back what the accepted ones do not need.  With `laws` (penalties, biases, a grammar), pps_adjust_logits shapes the target's law on
+pps_lmhead_logits, and pps_verify_tree takes the fused call's place.
+
 `Decoder` is a small stand-in for a model: attention layers with random weights, whose projections are torch
 matmuls.  `python -m paper_2609_21858_gb300.decode` runs it.
 """
@@ -24,21 +29,55 @@ from . import pps, synth
 
 
 class Cache:
-    """Paged keys and values of every layer, and each sequence's page table (its pages in no order)."""
+    """Paged keys and values of every layer, of 16 bits or of 4, and each sequence's page table (its pages in no order).
+    pool: how many pages there are for all sequences together, handed out as they are needed (None: every sequence has pages for
+    its whole capacity)."""
 
     def __init__(self, n_seq: int, capacity: int, layers: int, kv_heads: int, head_dim: int, page_size: int = 16,
-                 dtype=torch.bfloat16, device="cuda"):
+                 dtype=torch.bfloat16, device="cuda", bits: int = 16, pool: int = None):
+        if bits not in (4, 16):
+            raise ValueError(f"a cache has 4 or 16 bits, not {bits}")
         columns = -(-capacity // page_size)
-        self.page_size, self.capacity = page_size, columns * page_size
-        shape = (layers, n_seq * columns, page_size, kv_heads, head_dim)
-        self.k = torch.zeros(shape, dtype=dtype, device=device)
-        self.v = torch.zeros(shape, dtype=dtype, device=device)
-        gen = torch.Generator().manual_seed(n_seq * columns)
-        self.pages = torch.randperm(n_seq * columns, generator=gen).to(torch.int32).view(n_seq, columns).to(device)
+        n_pages = n_seq * columns if pool is None else pool
+        self.page_size, self.capacity, self.bits, self.pooled = page_size, columns * page_size, bits, pool is not None
+        if bits == 4:
+            self.layers = [pps.cache_q4(n_pages, page_size, kv_heads, head_dim, device=device) for _ in range(layers)]
+        else:
+            shape = (layers, n_pages, page_size, kv_heads, head_dim)
+            self.k = torch.zeros(shape, dtype=dtype, device=device)
+            self.v = torch.zeros(shape, dtype=dtype, device=device)
+        order = torch.randperm(n_pages, generator=torch.Generator().manual_seed(n_seq * columns)).to(torch.int32)
+        if self.pooled:
+            self.pages = torch.full((n_seq, columns), -1, dtype=torch.int32, device=device)
+            self.held = torch.zeros(n_seq, dtype=torch.int32, device=device)
+            self.free_list, self.free_count = order.to(device), torch.full((1,), n_pages, dtype=torch.int32, device=device)
+        else:
+            self.pages = order.view(n_seq, columns).to(device)
 
     def slots(self, seq: torch.Tensor, pos: torch.Tensor) -> torch.Tensor:
         """The cache slots of positions `pos` of sequences `seq` (int64)."""
         return self.pages[seq, pos // self.page_size].long() * self.page_size + pos % self.page_size
+
+    def reserve(self, length, n_new, n_tok: int, pos_off=None, status=None):
+        """Of a pool: pages, slots and positions for n_new more tokens of every sequence (pps.kv_reserve)."""
+        return pps.kv_reserve(self.pages, self.held, self.free_list, self.free_count, length.int(), n_new, self.page_size, n_tok,
+                              pos_off=pos_off, status=status)
+
+    def trim(self, length, status=None):
+        """Of a pool: gives back the pages behind `length` tokens of every sequence."""
+        pps.kv_trim(self.pages, self.held, self.free_list, self.free_count, length.int(), self.page_size, status=status)
+
+    def append(self, l: int, q, k, v, pos, slot, rope, q_norm, k_norm, status=None):
+        """Norm and rotation of queries and keys, keys and values to layer l's slots; returns the queries."""
+        if self.bits == 4:
+            return pps.kv_append_q4(q, k, v, pos, slot, self.layers[l], rope, q_norm, k_norm, status=status)
+        return pps.kv_append(q, k, v, pos, slot, self.k[l], self.v[l], rope, q_norm, k_norm, status=status)
+
+    def attend(self, l: int, q, kv_len, q_off, mask=None, status=None):
+        """Attention of the newest tokens over layer l."""
+        if self.bits == 4:
+            return pps.paged_attention_q4(q, self.layers[l], self.pages, kv_len, q_off, mask=mask, status=status)
+        return pps.paged_attention(q, self.k[l], self.v[l], self.pages, kv_len, q_off, mask=mask, status=status)
 
 
 class Decoder:
@@ -71,8 +110,8 @@ class Decoder:
         for l, (wqkv, wo, (qn, kn)) in enumerate(zip(self.wqkv, self.wo, self.qk)):
             y = (self.norm(x) @ wqkv.T).view(n, -1, hd)
             q, k, v = y.split([self.heads, self.kv_heads, self.kv_heads], dim=1)
-            q = pps.kv_append(q, k, v, pos, slot, cache.k[l], cache.v[l], self.rope, qn, kn, status=status)
-            a = pps.paged_attention(q, cache.k[l], cache.v[l], cache.pages, kv_len, q_off, mask=mask, status=status)
+            q = cache.append(l, q, k, v, pos, slot, self.rope, qn, kn, status)
+            a = cache.attend(l, q, kv_len, q_off, mask, status)
             x = x + a.view(n, -1) @ wo.T
             kept.append((k, v))
         return self.norm(x), kept
@@ -80,23 +119,25 @@ class Decoder:
     def keep(self, kept, pos, slot, cache: Cache, status=None):
         """Write tokens' keys and values, as `forward` returned them, to other slots (< 0: not written)."""
         for l, (k, v) in enumerate(kept):
-            kn = self.qk[l][1]
-            pps.kv_append(k, k, v, pos, slot, cache.k[l], cache.v[l], self.rope, None, kn, status=status)
+            cache.append(l, k, k, v, pos, slot, self.rope, None, self.qk[l][1], status)
 
 
 class Session:
     """Sequences that decode together.  `branching[d]`: children of a node of depth d; all ones: chains.
     `text` [n_seq, ...] holds the tokens, `length` [n_seq] how many of them the cache holds (the next one,
-    text[s, length[s]], is known and not cached yet)."""
+    text[s, length[s]], is known and not cached yet).  bits, pool: the cache's.  laws: what shapes the target's law, by
+    pps.adjust_logits' names: repetition, frequency, presence [n_seq], bias_off, bias_tok, bias_val, and `allowed`, a mask
+    [nodes of all sequences, words] or a function that gives one for the nodes' tokens."""
 
     def __init__(self, model: Decoder, branching, n_seq: int, capacity: int, key: int = 1, temperature: float = 1.0,
-                 page_size: int = 16):
+                 page_size: int = 16, bits: int = 16, pool: int = None, laws: dict = None):
         dev, i32 = model.embed.device, torch.int32
         self.model, self.temperature, self.device = model, temperature, dev
         self.tree = t = synth.make_tree(branching, n_seq)
         self.nodes, self.width = t.nodes_per_seq, t.gamma + 1
         self.cache = Cache(n_seq, capacity, len(model.wo), model.kv_heads, model.head_dim, page_size,
-                           model.embed.dtype, dev)
+                           model.embed.dtype, dev, bits, pool)
+        self.laws = laws
         put = lambda x: torch.as_tensor(x).to(dev)
         self.seq_off, self.node_draft_row, self.child_node = put(t.seq_off), put(t.node_draft_row), put(t.child_node)
         self.depth, self.row_k = put(t.node_depth).long(), put(t.row_k)
@@ -115,6 +156,10 @@ class Session:
             bits[b] = 1 << b | (bits[parent[b]] if b else 0)
         mask = torch.tensor([[(x >> 32 * w) & 0xffffffff for w in range(words)] for x in bits], dtype=torch.int64)
         self.mask = mask.to(i32).repeat(n_seq, 1).to(dev)  # modulo 2^32: the same bits
+        self.path = self.mask.clone()  # the tokens behind a node's root, which the text holds
+        self.path[:, 0] &= -2
+        self.new = torch.full((n_seq,), self.nodes, dtype=i32, device=dev)
+        self.node_depth = self.depth.int()
         # nodes of a depth are neighbours, and so are the draft lists of those with children
         count, self.levels, first = 1, [], 0
         for b in t.branching:
@@ -140,6 +185,7 @@ class Session:
         for s, p in enumerate(prompts):
             self.text[s, :len(p)] = put(p, torch.int32)
         self.length = put(n, torch.int64)
+        self.prompt = put(n, torch.int32) + 1
         if sum(n) == 0:
             return
         tok = put([x for p in prompts for x in p[:-1]], torch.int64)
@@ -148,8 +194,12 @@ class Session:
         off = [0]
         for m in n:
             off.append(off[-1] + m)
-        self.model.forward(tok, pos.int(), self.cache.slots(seq, pos), self.cache, self.length.int(),
-                           put(off, torch.int32), status=self.status)
+        if self.cache.pooled:
+            p = self.cache.reserve(torch.zeros_like(self.length), self.length.int(), len(tok), status=self.status)
+            pos, slot, kv_len, q_off = p["pos"], p["slot"], p["kv_len"], p["q_off"]
+        else:
+            pos, slot, kv_len, q_off = pos.int(), self.cache.slots(seq, pos), self.length.int(), put(off, torch.int32)
+        self.model.forward(tok, pos, slot, self.cache, kv_len, q_off, status=self.status)
 
     def _room(self, more: int):
         if self.most + more > self.cache.capacity:
@@ -186,17 +236,23 @@ class Session:
         tok, lists, counts = self._draft()
         start = self.length[self.node_seq]
         pos = (start + self.depth).int()
-        slot = self.cache.slots(self.node_seq, start + self.node_index)
         mask = self.mask if t.K > 1 else None  # a chain's nodes lie in their order: causal
-        hidden, kept = model.forward(tok, pos, slot, self.cache, (self.length + self.nodes).int(), self.seq_off, mask,
-                                     self.status)
+        if self.cache.pooled:
+            p = self.cache.reserve(self.length, self.new, t.n_nodes, self.node_depth, self.status)
+            slot, kv_len = p["slot"], p["kv_len"]
+        else:
+            slot, kv_len = self.cache.slots(self.node_seq, start + self.node_index), (self.length + self.nodes).int()
+        hidden, kept = model.forward(tok, pos, slot, self.cache, kv_len, self.seq_off, mask, self.status)
         if coupling:
             drafter = model.norm(model.embed[tok.view(-1, self.nodes)[:, :-1].reshape(-1)])
             u = torch.rand(t.n_draft, generator=self.gen, device=self.device)
             noise = torch.empty(t.n_seq, model.vocab, device=self.device).exponential_(generator=self.gen)
-            v = pps.verify_chain(pps.lmhead_logits(hidden, model.head), pps.lmhead_logits(drafter, model.head), t.gamma,
+            v = pps.verify_chain(self._logits(hidden, tok), pps.lmhead_logits(drafter, model.head), t.gamma,
                                  self.seq_off, self.node_draft_row, lists.view(-1), u, noise, self.temperature,
                                  status=self.status)
+        elif self.laws:
+            v = pps.verify_tree(self._logits(hidden, tok), self.node_key, self.zero, pos + 1, t.gamma, self.seq_off,
+                                self.node_draft_row, lists, counts, self.child_node, self.temperature, status=self.status)
         else:
             v = pps.lmhead_verify_tree(hidden, model.head, self.node_key, self.zero, pos + 1, t.gamma, self.seq_off,
                                        self.node_draft_row, lists, counts, self.child_node, self.temperature,
@@ -207,7 +263,20 @@ class Session:
         self.text.scatter_(1, at, v["emitted"])
         self.length = self.length + v["n_emitted"]
         self.most += self.width
+        if self.cache.pooled:
+            self.cache.trim(self.length, self.status)
         return v
+
+    def _logits(self, hidden, tok):
+        """The target's logits of all nodes, as `laws` shape them."""
+        logits = pps.lmhead_logits(hidden, self.model.head)
+        if not self.laws:
+            return logits
+        laws = dict(self.laws)
+        if callable(laws.get("allowed")):
+            laws["allowed"] = laws["allowed"](tok)
+        return pps.adjust_logits(logits, self.seq_off, text=self.text, text_len=(self.length + 1).int(), prompt_len=self.prompt,
+                                 node_tok=tok.int(), node_mask=self.path, out=logits, status=self.status, **laws)
 
     def _kept_slots(self, lists, v):
         """Where the accepted nodes go: the node of depth d to the d-th slot after the root's; -1 for the others."""
@@ -226,7 +295,7 @@ class Session:
         """The tokens so far, a list per sequence (waits for the device)."""
         flags = int(self.status)
         if flags:
-            raise pps.PPSError(f"status flags {flags:#x}")
+            raise RuntimeError(f"the calls raised status flags {flags:#x}")
         return [row[:n + 1] for row, n in zip(self.text.tolist(), self.length.tolist())]
 
 
@@ -234,12 +303,16 @@ def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--branching", default="4,1,1,1", help="children per depth; all ones: chains")
     ap.add_argument("--coupling", action="store_true", help="chains: the token-level coupling, not the keyed race")
+    ap.add_argument("--bits", type=int, default=16, choices=(4, 16), help="of the cache")
+    ap.add_argument("--pool", type=int, help="pages for all sequences, handed out as they are needed")
+    ap.add_argument("--repetition", type=float, help="penalty for tokens that the text holds already")
     ap.add_argument("--sequences", type=int, default=8)
     ap.add_argument("--steps", type=int, default=16)
     a = ap.parse_args(argv)
     branching = [int(x) for x in a.branching.split(",")]
     model = Decoder(vocab=8000, width=1024, layers=4, heads=16, kv_heads=4, head_dim=64)
-    s = Session(model, branching, a.sequences, 64 + a.steps * (len(branching) + 1) + 256)
+    laws = None if a.repetition is None else dict(repetition=torch.full((a.sequences,), a.repetition, device="cuda"))
+    s = Session(model, branching, a.sequences, 64 + a.steps * (len(branching) + 1) + 256, bits=a.bits, pool=a.pool, laws=laws)
     s.prefill([[(7 * i + j) % 8000 for j in range(1 + 5 * i % 60)] for i in range(a.sequences)])
     accepted = torch.zeros((), dtype=torch.float64, device=s.device)
     for _ in range(a.steps):

@@ -172,6 +172,8 @@ def test_strides_alignments_and_in_place():
     # wider rows of masks, text columns past the longest
     c = Case([3, 2], 2000, BF, [10, 20], grammar=True, seed=9)
     want = c.check()
+    one = c.args["allowed"][3:4].expand(5, -1)  # the same mask for all rows
+    assert torch.equal(c.call(allowed=one), c.call(allowed=one.contiguous()))
     wide = torch.full((5, 70), -1, dtype=torch.int32, device="cuda")
     wide[:, :63] = c.args["allowed"]
     text = torch.full((2, 90), -3, dtype=torch.int32, device="cuda")
