@@ -1,0 +1,116 @@
+"""The 4-bit cache's calls where offsets pass 32 bits, where one kernel hands over to the other, from several threads and from two graphs."""
+import threading
+
+import pytest
+import torch
+
+from paper_2609_21858_gb300 import pps
+from test_gpu_q4_attention import BF, F16, Case, _cuda  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# rows of a sequence and key head around 32, on average and by sequence
+@pytest.mark.parametrize("heads,kv_heads", [(32, 1), (33, 1), (31, 1), (8, 2), (6, 6)])
+@pytest.mark.parametrize("q_len", [[1, 1], [8, 8], [8, 9], [9, 9], [1, 15], [2, 130, 0, 0, 0, 0, 0, 0], [32, 32], [33, 33]])
+def test_where_the_kernels_meet(heads, kv_heads, q_len):
+    Case(q_len, [n + 3 * i + 200 for i, n in enumerate(q_len)], heads, kv_heads, 64, 16, BF, seed=heads + len(q_len)).check()
+    Case(q_len, [n + 3 * i + 70 for i, n in enumerate(q_len)], heads, kv_heads, 128, 8, F16, tree=True, seed=heads + len(q_len)).check()
+
+
+def _i32(*x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def far(cache, pages, layout):
+    """The cache's pages behind so many others that their bytes lie past 2^32, and the table that says so."""
+    n, page, heads, d2 = cache.k.shape
+    first = 2 ** 32 // (page * heads * d2) + 5
+
+    def moved(t):
+        shape = (first + n, heads, page, t.shape[3]) if layout == "head" else (first + n, page, heads, t.shape[3])
+        x = torch.zeros(shape, dtype=torch.uint8, device="cuda")
+        x = x.transpose(1, 2) if layout == "head" else x
+        x[first:] = t
+        return x
+
+    return cache._replace(**{k: moved(getattr(cache, k)) for k in ("k", "v", "k_scale", "v_scale")}), torch.where(pages >= 0, pages + first, pages)
+
+
+@pytest.mark.parametrize("layout", ["token", "head"])
+def test_caches_past_32_bits(layout):
+    for q_len in ([1, 1, 1], [40, 33, 70]):
+        c = Case(q_len, [500, 333, 70], 8, 8, 128, 64, BF, layout=layout, seed=3)
+        c.cache, c.pages = far(c.cache, c.pages, layout)
+        c.check()
+    # what is appended there is what is appended near, it reads back, and the pages before it are left as they were
+    n, rows = 9, torch.randn(3, 9, 8, 128, device="cuda").to(BF)
+    near, near_at = pps.cache_q4(2, 64, 8, 128), torch.arange(3, 3 + n, device="cuda")
+    first = c.cache.k.shape[0] - 2
+    slot = first * 64 + near_at
+    for cache, at in ((near, near_at), (c.cache, slot)):
+        pps.kv_append_q4(rows[0], rows[1], rows[2], None, at, cache, None)
+    for a, b in zip(near[:4], c.cache[:4]):
+        assert torch.equal(a[0, 3:3 + n], b[first, 3:3 + n])
+    for a, b in zip(pps.kv_read_q4(near, near_at), pps.kv_read_q4(c.cache, slot)):
+        assert torch.equal(a, b) and bool(a.any())
+    assert not any(bool(t[:20].any()) for t in c.cache[:4])
+
+
+@pytest.mark.parametrize("named", [False, True])
+def test_threads(named):
+    """Several threads, each on a stream of its own and without a workspace."""
+    jobs = []
+    for i in range(6):
+        attend = Case([1, 1, 1] if i % 2 else [1, 30 + i, 40], [3000 + 500 * i, 200, 900], 8, 2, 128 if i % 3 else 64, 16, BF if i % 2 else F16, seed=i)
+        x = torch.randn(9 + i, 30001 + 16 * i, device="cuda").to(BF)
+        text = torch.randint(0, x.shape[1], (3, 50), device="cuda", dtype=torch.int32)
+        off, lens, laws = _i32(0, 2, 3, 9 + i), _i32(50, 7, 33), torch.tensor([1.3, 1.0, 2.0], device="cuda")
+        shape = lambda x=x, off=off, text=text, lens=lens, laws=laws, **kw: pps.adjust_logits(
+            x, off, text=text, text_len=lens, repetition=laws, presence=laws, **kw)
+        jobs.append((attend, shape, attend.call(), shape()))
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(attend, shape, out, shaped):
+        try:
+            stream = torch.cuda.Stream()
+            kw = dict(stream=stream) if named else {}
+            with torch.cuda.stream(stream):
+                for _ in range(30):
+                    a, b = attend.call(**kw), shape(**kw)
+                    if not torch.equal(a, out) or not torch.equal(b, shaped):
+                        wrong.append("differs")
+                stream.synchronize()
+        except Exception as e:  # a thread's exception would be lost
+            wrong.append(repr(e))
+
+    threads = [threading.Thread(target=work, args=job) for job in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong
+
+
+def test_two_graphs_at_the_same_time_with_a_workspace_each():
+    cases = [Case([1] * 5, [4000, 900, 20, 7000, 3], 8, 2, 128, 16, BF, seed=1), Case([41, 9], [5000, 600], 8, 2, 128, 16, BF, seed=2)]
+    graphs, outs, wants, streams = [], [], [], []
+    for c in cases:
+        ws, out = pps.attention_q4_workspace(sum(c.q_len), 8, 2, 128), torch.empty_like(c.q)
+        wants.append(c.call(ws=ws, out=out).clone())
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for _ in range(20):
+                c.call(ws=ws, out=out)
+        graphs.append((graph, ws))
+        outs.append(out.fill_(3.0))
+        streams.append(torch.cuda.Stream())
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (graph, _ws), stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, wants))
