@@ -9,13 +9,14 @@
 // of one sequence: it counts the text's tokens that fall into the slice in shared memory (and which entry of the bias list is
 // a token's last), with a bit per token that anything is known of.  Its warps take pieces of the sequence's rows: vectors are copied
 // through registers, and a vector's known tokens, by their bits, formed there one at a time.  (All elements of such a vector at once:
-// 423 us for 64 x 41 rows of 128256 where this takes 249; listed and formed in memory after the copy, 295 to 320: a read and a write of 32 bytes for each, of what
+// 423 us for 64 x 41 rows of 128256 where this took 249, and takes 231 now; listed and formed in memory after the copy, 295 to 320: a read and a write of 32 bytes for each, of what
 // has left L2 in part.)  Tokens of a row's path, a handful, are formed before its piece (which may be written in place) and written
 // after it.
 #include <algorithm>
 #include <climits>
 #include <cstdint>
 #include <cstring>
+#include <type_traits>
 
 #include <cuda_bf16.h>
 
@@ -27,7 +28,6 @@ namespace {
 
 constexpr int kAdjustThreads = 256, kAdjustWarps = kAdjustThreads / 32;
 constexpr int kSlice = 4096;       // tokens
-constexpr int kBatch = 4;          // vectors of a lane on their way
 constexpr int kPath = 64;          // nodes of a path
 constexpr uint32_t kPrompt = 1u << 31;
 
@@ -91,13 +91,17 @@ __device__ __forceinline__ uint32_t bits_at(const uint32_t* words, int i) {
 }
 
 // PIECE: tokens that a warp takes of a row at a time
-template <typename T, bool COUNTS, bool BIAS, int PIECE>
+template <typename T, bool COUNTS, bool BIAS, bool MASK, int PIECE>
 __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustArgs a) {
     constexpr int VN = 16 / sizeof(T);
+    // vectors of a lane on their way (64 x 41 rows: eight 231 us, four 238; beside biases or masks eight do not fit in the 64 registers)
+    constexpr int kBatch = PIECE == 2048 && !BIAS && !MASK ? 8 : 4;
     __shared__ __align__(16) uint32_t s_count[COUNTS ? kSlice : 4];
     __shared__ __align__(16) int s_bias[BIAS ? kSlice : 4];   // 1 + the last entry for the token
     __shared__ uint32_t s_known[kSlice / 32];
     __shared__ int s_path[kAdjustWarps][kPath];
+    constexpr int kWords = PIECE / 32;
+    __shared__ uint32_t s_may[MASK ? kAdjustWarps : 1][kWords];  // a piece's part of the mask
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int seq = blockIdx.y;
     const int t0 = blockIdx.x * kSlice, tn = (int)min((int64_t)kSlice, a.V - t0);
@@ -171,13 +175,29 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
 
     // items: pieces of rows
     const int pieces = (tn + PIECE - 1) / PIECE;
+    // the next piece's part of the mask, on its way while this piece's logits are: read when it is needed, it is one more latency before
+    // theirs (16 x 9 rows of 152063 in fp32: 41 us, 44 without)
+    uint32_t next[kWords / 32];
+    auto mask_of = [&](int item) {
+        const int i = item / pieces, p0 = (item - i * pieces) * PIECE, words = item < n_rows * pieces ? (tn - p0 + 31) >> 5 : 0;
+        const uint32_t* from = a.allowed + (first + i) * a.allowed_stride + ((t0 + p0) >> 5);
+#pragma unroll
+        for (int j = 0; j < kWords / 32; ++j) next[j] = 32 * j + lane < words ? __ldg(from + 32 * j + lane) : 0u;
+    };
+    if constexpr (MASK) mask_of(warp);
     for (int item = warp; item < n_rows * pieces; item += kAdjustWarps) {
         const int i = item / pieces, p0 = (item - i * pieces) * PIECE, p1 = min(p0 + PIECE, tn);
         const int64_t row = first + i;
         const T* x = static_cast<const T*>(a.x) + row * a.x_stride + t0;
         T* out = static_cast<T*>(a.out) + row * a.out_stride + t0;
-        const uint32_t* allowed = a.allowed ? a.allowed + row * a.allowed_stride + (t0 >> 5) : nullptr;
-        auto may = [&](int at) { return !allowed || (__ldg(allowed + (at >> 5)) >> (at & 31) & 1u); };
+        if constexpr (MASK) {
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < kWords / 32; ++j) s_may[warp][32 * j + lane] = next[j];
+            __syncwarp();
+            mask_of(item + kAdjustWarps);
+        }
+        auto may = [&](int at) { return !MASK || (s_may[warp][(at - p0) >> 5] >> (at & 31) & 1u); };
         // the path's tokens: the row's own and its ancestors'
         float fixed[2];
         int fixed_at[2] = {-1, -1};
@@ -235,7 +255,7 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
                 ok[k] = j0 + 32 * k < nv ? all : 0u;
-                if (allowed && ok[k]) ok[k] = bits_at<VN>(allowed, v0 + (j0 + 32 * k) * VN);
+                if (MASK && ok[k]) ok[k] = bits_at<VN>(s_may[warp], v0 - p0 + (j0 + 32 * k) * VN);
             }
 #pragma unroll
             for (int k = 0; k < kBatch; ++k)  // what is not allowed need not be read
@@ -251,7 +271,7 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
                         Pick<T>::set(raw[k], e, adjusted(Pick<T>::get(raw[k], e), at + e, 0));
                     }
                 }
-                if (allowed && ok[k] != all) {
+                if (MASK && ok[k] != all) {
                     T v[VN];
                     memcpy(v, &raw[k], 16);
 #pragma unroll
@@ -275,13 +295,16 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
 template <typename T>
 cudaError_t by_parts(const AdjustArgs& a, cudaStream_t st) {
     const bool counts = a.text != nullptr || a.node_tok != nullptr, bias = a.bias_tok != nullptr;
-    // Pieces of 2048 tokens, or of 1024 where a sequence has few rows (64 x 41 rows 249 and 276 us, 16 x 9 rows 46 and 44, one row 7.1
-    // and 6.1).  They are a compile-time choice: 249 us became 290 with a variable.
+    // Pieces of 2048 tokens, or of 1024 where a sequence has few rows (measured on an earlier form: 64 x 41 rows 249 and 276 us, 16 x 9
+    // rows 46 and 44, one row 7.1 and 6.1).  What a piece is, and whether there is a mask, are compile-time choices: each as a variable
+    // made the call of 64 x 41 rows, which has no mask, 16 to 25 percent slower.
     const bool many = a.n_rows / 16 >= a.n_seq;
-    auto kernel = counts ? (bias ? (many ? adjust_kernel<T, true, true, 2048> : adjust_kernel<T, true, true, 1024>)
-                                 : (many ? adjust_kernel<T, true, false, 2048> : adjust_kernel<T, true, false, 1024>))
-                         : (bias ? (many ? adjust_kernel<T, false, true, 2048> : adjust_kernel<T, false, true, 1024>)
-                                 : (many ? adjust_kernel<T, false, false, 2048> : adjust_kernel<T, false, false, 1024>));
+    auto sized = [&](auto c, auto b, auto m) {
+        return many ? adjust_kernel<T, c.value, b.value, m.value, 2048> : adjust_kernel<T, c.value, b.value, m.value, 1024>;
+    };
+    auto masked = [&](auto c, auto b) { return a.allowed ? sized(c, b, std::true_type()) : sized(c, b, std::false_type()); };
+    auto biased = [&](auto c) { return bias ? masked(c, std::true_type()) : masked(c, std::false_type()); };
+    auto kernel = counts ? biased(std::true_type()) : biased(std::false_type());
     const int64_t slices = (a.V + kSlice - 1) / kSlice;
     for (int s0 = 0; s0 < a.n_seq; s0 += 65535) {  // (a grid's second dimension)
         AdjustArgs part = a;
