@@ -3,24 +3,29 @@
 //   out[i] = v_unit sum_j w_j v_j / sum_j w_j,   w_j = exp(scale k_unit q_i . k_j)   over the keys j that row i sees
 //
 // Rows.  The tokens of a sequence and the heads that share a key head are packed into rows, token after token; a row block has
-// R = 8 NT of them.
+// R = 8 NT of them (NT 1 or 2).
 //
 // Few rows.  A key's 128 channels are 72 bytes, and what a decoding step has to do per byte of them is to widen it: both
-// products run on registers, without a way through shared memory.  A warp takes 32 keys at a time, keys of a quad side by side:
-//   S^T = K Q^T  (m16n8k16, m: keys, n: rows).  Lane (g, t) of the warp loads a quarter of key g's codes, t-th from the left, and
+// products run on registers, without a way through shared memory for what was widened.  A warp takes 64 keys at a time, 16 by 16:
+//   S^T = K Q^T  (m16n8k16, m: keys, n: rows).  Lane (g, t) of the warp reads a quarter of key g's codes, t-th from the left, and
 //                takes them as the operand's elements whatever channels these are: the queries are read in the same order;
-//   O^T += V^T P^T (m: channels, n: rows, k: keys).  Lane (g, t) loads the g-th eighth of the codes of keys 2t, 2t + 1; nibbles of
+//   O^T += V^T P^T (m: channels, n: rows, k: keys).  Lane (g, t) reads the g-th eighth of the codes of keys 2t, 2t + 1; nibbles of
 //                two keys are put together into bytes, which become pairs of halves along the keys; a transposing move turns S^T into
 //                the operand P^T.
 // Codes times scales are exact halves.  Queries in bf16 are brought to halves by a power of two per row, exactly but for
 // channels below 2^-31 of the row's largest.  Weights are rounded to halves (2^-11 of each); sums are formed before rounding,
-// in 32 bits, and the softmax is the running one with the rescaling left out while a maximum rises by less than 2^kLazy.
+// in 32 bits, and the softmax is the running one with the rescaling left out while a maximum rises by less than 2^kLazy4.
+// The warps of a CTA take the units of a segment in turn, each through a ring of its own (a unit on its way while one is in use),
+// and join at its end.
+// What bounds it: with many keys the issue of those conversions and products beside HBM (64 sequences of 2000 to 8000 keys: 80 us, 4.7
+// TB/s, 2.1 instructions a clock of 4; the first form, 32 keys at a time with codes by lanes' copies, took 98), with few the start,
+// the plan and the join's launch (one sequence of 900 keys: 9.3 us).  Three CTAs of four warps to an SM leave 168 registers.
 //
-// A CTA's warps take the 32-key units of a segment in turn and join at its end.
-//
-// Many rows (trees, chunks).  The 128-row tiles of pps_attn_tiles.cuh on the 5th-generation tensor cores: the warps that load keys and
-// values copy a tile's codes and scales into shared memory two tiles ahead, widen them (64 conversions and as many multiplications
-// a lane for 32 keys of 128 channels) and write the halves where TMA would have put them.  Queries in bf16 become halves in a launch before it.
+// Many rows (trees, chunks).  The 128-row tiles of pps_attn_tiles.cuh on the 5th-generation tensor cores: six warps copy a tile's codes
+// and scales into shared memory ahead of the products, widen them (64 conversions and as many multiplications a lane for 32 keys of
+// 128 channels) and write the halves where TMA would have put them.  Queries in bf16 become halves in a launch before it, at the same
+// power of two per row.  64 trees of 41 nodes: 227 us, of which that launch is some 8; a cache of 16 bits takes 180, as the softmax
+// has the issue slots to itself there.
 //
 // Work split.  The line of pps_attn.cuh.
 #include <atomic>
@@ -66,7 +71,7 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     return y;
 }
 
-// A warp's ring in shared memory: stages of 32 keys, each their codes, the values' codes, and the scales of both, row after row.
+// A warp's ring in shared memory: stages of kUnit keys, each their codes, the values' codes, and the scales of both, row after row.
 template <int DC>
 struct Stage {
     static constexpr int kRow = DC / 2, kScales = DC / 16;  // bytes of a key
@@ -74,7 +79,9 @@ struct Stage {
 };
 
 // DENSE: all DC channels are there, 16 keys in a row share their page, and a page's rows of a head follow one another, from 16-byte
-// boundaries on (a page laid out head by head): a stage is eight bulk copies.  Otherwise a lane copies a key's rows.
+// boundaries on (a page laid out head by head): a stage's codes are eight bulk copies, its scales sixteen bytes a lane.  Otherwise
+// four lanes copy a row of codes and a lane a row's scales: what a page laid out token by token has of a head are pieces of 64 and 8
+// bytes, as many requests as keys (one sequence of 130001 keys over 4 heads: 33 us against 25 head by head, back to back in a graph).
 template <typename T, int DC, int NT, bool DENSE>
 __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const AttnArgs a, const Q4View z, const AttnPlan P) {
     using S = Stage<DC>;
