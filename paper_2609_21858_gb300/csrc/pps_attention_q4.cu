@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                 if (valid && t * (DC / 4) + 8 * i < D) raw[i] = __ldg(reinterpret_cast<const uint4*>(src) + i);
             }
             const uint32_t* x = reinterpret_cast<const uint32_t*>(raw);
-            row_sc[nt] = P.sc * ku;
+            row_sc[nt] = P.sc * ku;  // (kept from zero: scores of zero, equal weights, are what the smallest normal number gives too)
             if constexpr (Half<T>::kType == 0) {
 #pragma unroll
                 for (int i = 0; i < DC / 8; ++i) qf[nt][i] = x[i];
@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
         float sc[2 * NT], m[2 * NT], l[2 * NT], limit[2 * NT], neg[2 * NT];
 #pragma unroll
         for (int r = 0; r < 2 * NT; ++r) {
-            sc[r] = __shfl_sync(0xffffffffu, row_sc[r >> 1], 4 * (2 * t + (r & 1)));
+            sc[r] = fmaxf(__shfl_sync(0xffffffffu, row_sc[r >> 1], 4 * (2 * t + (r & 1))), FLT_MIN);
             m[r] = limit[r] = -INFINITY;
             l[r] = 0.0f;
             neg[r] = kShift4;
@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                     const float M = fmaxf(m[r], top[r]), f = m[r] == M ? 1.0f : ex2((m[r] - M) * sc[r]);
                     m[r] = M;
                     l[r] *= f;
-                    limit[r] = M + kLazy4 / sc[r];
+                    limit[r] = M == -INFINITY ? M : M + kLazy4 / sc[r];
                     neg[r] = (M == -INFINITY ? 0.0f : -M * sc[r]) + kShift4;
 #pragma unroll
                     for (int i = 0; i < DC / 16; ++i) {

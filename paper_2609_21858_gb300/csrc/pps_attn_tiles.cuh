@@ -522,6 +522,7 @@ __global__ void __launch_bounds__(Cfg<DC, Q4>::kThreads, 1)
                 if (R4.z.k_unit) sc *= __ldg(R4.z.k_unit + kvh);
                 if (R4.z.v_unit) vu = __ldg(R4.z.v_unit + kvh);
                 if (R4.row_scale && valid) sc = fminf(sc * __ldg(R4.row_scale + (int64_t)(W.q.off + tok) * a.n_heads + head), FLT_MAX);
+                sc = fmaxf(sc, FLT_MIN);  // (a factor of zero would make scores that are not seen NaN)
             }
             float m = -INFINITY, l = 0.0f;
             int i = 0;  // tiles of the stream in this segment

@@ -18,6 +18,30 @@ def test_where_the_kernels_meet(heads, kv_heads, q_len):
     Case(q_len, [n + 3 * i + 70 for i, n in enumerate(q_len)], heads, kv_heads, 128, 8, F16, tree=True, seed=heads + len(q_len)).check()
 
 
+@pytest.mark.parametrize("q_len", [[1, 1], [2, 3], [50, 60]])
+@pytest.mark.parametrize("dt", [BF, F16])
+def test_factors_on_scores_that_vanish(q_len, dt):
+    """Units and queries whose product with the scale has no number in 32 bits: equal weights."""
+    c = Case(q_len, [300, 90], 8, 2, 64, 16, dt, seed=14)
+    c.cache = c.cache._replace(k_unit=torch.full((2,), 1e-30, device="cuda"))
+    c.keys = [k.double() * 1e-30 for k in c.keys]
+    if dt is BF:
+        c.q = (c.q.double() * 2.0 ** -110).to(dt)
+    c.check()
+    c.check(scale=1e-38)
+
+
+def test_a_tree_whose_first_nodes_are_not_seen():
+    """Seven rows of a key head, whose first keys no row sees, at scales down to the smallest."""
+    c = Case([200, 1, 1, 1, 1, 1, 1, 1], [200, 3, 3, 3, 3, 3, 3, 3], 1, 1, 64, 16, BF, tree=True, seed=15)
+    c.mask[:200, :5] = 0
+    c.bits[:200, :160] = False
+    for scale in (None, 1e-20, 1e-38, 0.0):
+        c.check(**({} if scale is None else dict(scale=scale)))
+    c.q = (c.q.double() * 2.0 ** -120).to(BF)
+    c.check()
+
+
 def _i32(*x):
     return torch.tensor(x, dtype=torch.int32, device="cuda")
 
