@@ -42,6 +42,7 @@ constexpr int kGroups = kUnit / 16;
 constexpr int kStages4 = 2;       // units of a warp, on their way or in use
 constexpr int few_ctas(int nt) { return nt == 1 ? 3 : 2; }  // per SM: 168 or 255 registers
 constexpr int kMaxCtas4 = 640;
+constexpr auto kFetch4 = CU_TENSOR_MAP_L2_PROMOTION_L2_64B;  // what a miss brings into L2: a row (520000 keys: 68 us, 128 bytes 70, 256 71)
 constexpr int kFix4 = 2;          // key tiles that an item's start and end cost
 constexpr int kLeast4 = 1;
 constexpr float kLazy4 = 8.0f;    // log2 of the rise of a maximum that nothing is rescaled for
@@ -78,12 +79,18 @@ struct Stage {
     static constexpr int kV = kUnit * kRow, kKs = 2 * kV, kVs = kKs + kUnit * kScales, kBytes = kVs + kUnit * kScales;
 };
 
-// DENSE: all DC channels are there, 16 keys in a row share their page, and a page's rows of a head follow one another, from 16-byte
-// boundaries on (a page laid out head by head): a stage's codes are eight bulk copies, its scales sixteen bytes a lane.  Otherwise
-// four lanes copy a row of codes and a lane a row's scales: what a page laid out token by token has of a head are pieces of 64 and 8
-// bytes, as many requests as keys (one sequence of 130001 keys over 4 heads: 33 us against 25 head by head, back to back in a graph).
-template <typename T, int DC, int NT, bool DENSE>
-__global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const AttnArgs a, const Q4View z, const AttnPlan P) {
+// How a cache lies.  kByHead: all DC channels are there, 16 keys in a row share their page, and a page's rows of a head follow one
+// another, from 16-byte boundaries on (a page laid out head by head): a stage's codes are eight bulk copies, its scales sixteen bytes a
+// lane.  kByToken: the same, but rows are apart: the copies are boxes of 16 rows, scales a row a lane.  kAnyHow: anything else; four
+// lanes copy a row of codes and a lane a row's scales, each with a look at the key's page and length.  (One sequence of 130001 and 520000
+// keys over 4 heads of 128, back to back in a graph: 25 and 65 us head by head, 27 and 68 token by token, which kAnyHow reads in 34 and 104.)
+enum Lie { kAnyHow, kByToken, kByHead };
+
+template <typename T, int DC, int NT, Lie LIE>
+__global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const __grid_constant__ CUtensorMap tmK,
+                                                                           const __grid_constant__ CUtensorMap tmV, const AttnArgs a, const Q4View z,
+                                                                           const AttnPlan P) {
+    constexpr bool DENSE = LIE != kAnyHow;
     using S = Stage<DC>;
     constexpr int R = 8 * NT, RS = DC + 4;  // a row's floats in shared memory: 4 modulo 16, so that lanes (g, t) touch all banks
     __shared__ int64_t s_sum[kWarps4];
@@ -162,12 +169,25 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                         mbar_arrive(full);
                 }
                 __syncwarp();
-                if (lane < 2 * kGroups && good) bulk_load(to + part_at, my_part + page * a.c.page + in_page * S::kRow, 16 * S::kRow, full);
-                const int p = __shfl_sync(0xffffffffu, page, 2 * Gs);
-                if (lane < kGroups * kScaleLanes && (who >> 2 * Gs & 1u)) {
-                    const int64_t at = p * z.page + ((k0 + 16 * Gs) & (a.c.page_size - 1)) * S::kScales + my_scales;
-                    copy_async<16>(to + S::kKs + 16 * lane, z.ks + at);
-                    copy_async<16>(to + S::kVs + 16 * lane, z.vs + at);
+                if constexpr (LIE == kByHead) {
+                    if (lane < 2 * kGroups && good) bulk_load(to + part_at, my_part + page * a.c.page + in_page * S::kRow, 16 * S::kRow, full);
+                    const int p = __shfl_sync(0xffffffffu, page, 2 * Gs);
+                    if (lane < kGroups * kScaleLanes && (who >> 2 * Gs & 1u)) {
+                        const int64_t at = p * z.page + ((k0 + 16 * Gs) & (a.c.page_size - 1)) * S::kScales + my_scales;
+                        copy_async<16>(to + S::kKs + 16 * lane, z.ks + at);
+                        copy_async<16>(to + S::kVs + 16 * lane, z.vs + at);
+                    }
+                } else {
+                    if (lane < 2 * kGroups && good) tma_load_4d(to + part_at, kind ? &tmV : &tmK, full, 0, in_page, kvh, page);
+#pragma unroll
+                    for (int i = 0; i < kUnit / 32; ++i) {
+                        const int G = 2 * i + (lane >> 4), p = __shfl_sync(0xffffffffu, page, 2 * G);
+                        if (!(who >> 2 * G & 1u)) continue;
+                        const int64_t at = p * z.page + ((k0 + 32 * i + lane) & (a.c.page_size - 1)) * z.tok + kvh * z.head;
+                        const uint32_t scales = to + S::kKs + (32 * i + lane) * S::kScales;
+                        copy_async<S::kScales>(scales, z.ks + at);
+                        copy_async<S::kScales>(scales + S::kVs - S::kKs, z.vs + at);
+                    }
                 }
             } else {
                 if (k0 + 8 * (lane & 7) < last && (uint32_t)page >= (uint32_t)a.c.n_pages) {  // reads as zeros
@@ -525,8 +545,26 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
     if (DENSE && tid == 0 && *static_cast<volatile int*>(&s_abort) && a.status) atomicOr(a.status, PPS_FLAG_TIMEOUT);
 }
 
-// Whether a cache lies as CopyKeys wants it dense.
-bool is_dense(const AttnArgs& a, const Q4View& z, int dc) {
+// Whether a cache lies as kByToken has it; its maps in boxes of 16 rows, [page, head, token, byte].
+bool by_token_maps(CUtensorMap (&m)[2], const AttnArgs& a, const Q4View& z, int dc) {
+    const CacheView& c = a.c;
+    const uintptr_t codes = reinterpret_cast<uintptr_t>(c.k) | reinterpret_cast<uintptr_t>(c.v) | (uintptr_t)c.page | (uintptr_t)c.tok | (uintptr_t)c.head;
+    const uintptr_t scales = reinterpret_cast<uintptr_t>(z.ks) | reinterpret_cast<uintptr_t>(z.vs) | (uintptr_t)z.page | (uintptr_t)z.tok | (uintptr_t)z.head;
+    if (c.head_dim != dc || c.page_size < 16 || c.n_pages < 1 || codes % 16 != 0 || scales % (dc / 16) != 0) return false;
+    EncodeTiledFn f = encode_fn();
+    if (f == nullptr) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)dc / 2, (cuuint64_t)c.page_size, (cuuint64_t)c.n_kv_heads, (cuuint64_t)c.n_pages};
+    // the stride of a dimension of one is never used, but has to be a multiple of 16 bytes
+    const cuuint64_t strides[3] = {(cuuint64_t)c.tok, c.n_kv_heads > 1 ? (cuuint64_t)c.head : 256, c.n_pages > 1 ? (cuuint64_t)c.page : 256};
+    const cuuint32_t box[4] = {(cuuint32_t)dc / 2, 16, 1, 1}, es[4] = {1, 1, 1, 1};
+    for (int i = 0; i < 2; ++i)
+        if (f(&m[i], CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, i ? c.v : c.k, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+              kFetch4, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return false;
+    return true;
+}
+// Whether it lies as kByHead has it, and CopyKeys dense.
+bool is_by_head(const AttnArgs& a, const Q4View& z, int dc) {
     const uintptr_t bits = reinterpret_cast<uintptr_t>(a.c.k) | reinterpret_cast<uintptr_t>(a.c.v) | reinterpret_cast<uintptr_t>(z.ks) |
                            reinterpret_cast<uintptr_t>(z.vs) | (uintptr_t)a.c.page | (uintptr_t)a.c.head | (uintptr_t)z.page | (uintptr_t)z.head;
     return a.c.head_dim == dc && a.c.page_size >= 16 && a.c.tok == dc / 2 && z.tok == dc / 16 && bits % 16 == 0;
@@ -558,13 +596,15 @@ cudaError_t launch_few(const AttnArgs& a, const Q4View& z, const Rows4& rows, cu
     plan_common(P, a);
     carve(P, a.ws, kMaxCtas4);
     constexpr int kSmem = std::max(kWarps4 * 8 * NT * (DC + 4) * 4, kWarps4 * kStages4 * Stage<DC>::kBytes);
-    const bool dense = is_dense(a, z, DC);
-    auto kernel = dense ? few_rows_kernel<T, DC, NT, true> : few_rows_kernel<T, DC, NT, false>;
-    static std::atomic<uint64_t> ready[2] = {};
-    cudaError_t e = allow_smem(ready[dense], (const void*)kernel, kSmem);
+    CUtensorMap maps[2] = {};
+    const Lie lie = is_by_head(a, z, DC) ? kByHead : by_token_maps(maps, a, z, DC) ? kByToken : kAnyHow;
+    auto kernel = lie == kByHead ? few_rows_kernel<T, DC, NT, kByHead>
+                                 : lie == kByToken ? few_rows_kernel<T, DC, NT, kByToken> : few_rows_kernel<T, DC, NT, kAnyHow>;
+    static std::atomic<uint64_t> ready[3] = {};
+    cudaError_t e = allow_smem(ready[lie], (const void*)kernel, kSmem);
     if (e != cudaSuccess) return e;
     const int ctas = std::min(device_sm_count() * few_ctas(NT), kMaxCtas4);
-    e = launch_pdl(kernel, dim3(ctas), dim3(kThreads4), kSmem, st, a, z, P);
+    e = launch_pdl(kernel, dim3(ctas), dim3(kThreads4), kSmem, st, maps[0], maps[1], a, z, P);
     if (e != cudaSuccess) return e;
     return launch_pdl(join_kernel<T, DC>, dim3(ctas, join_blocks(a, P)), dim3(256), 0, st, a, P);
 }
@@ -631,7 +671,7 @@ cudaError_t launch_tiles(const AttnArgs& given, const Q4View& z, cudaStream_t st
     plan_common(P, a);
     carve(P, a.ws, kMaxCtas);
     const int ctas = std::min(device_sm_count(), kMaxCtas);
-    Q4Rows r4 = {z, nullptr, is_dense(a, z, DC)};
+    Q4Rows r4 = {z, nullptr, is_by_head(a, z, DC)};
     if constexpr (std::is_same_v<T, __nv_bfloat16>) {
         char* w = static_cast<char*>(a.ws) + parts4_bytes(a.n_tok, P.group, a.c.head_dim);
         __half* halves = reinterpret_cast<__half*>(w);

@@ -18,6 +18,38 @@ def test_where_the_kernels_meet(heads, kv_heads, q_len):
     Case(q_len, [n + 3 * i + 70 for i, n in enumerate(q_len)], heads, kv_heads, 128, 8, F16, tree=True, seed=heads + len(q_len)).check()
 
 
+@pytest.mark.parametrize("heads,kv_heads,d", [(8, 2, 128), (4, 4, 64), (6, 1, 128), (3, 1, 64)])
+@pytest.mark.parametrize("page", [16, 32, 128])
+@pytest.mark.parametrize("more", [(0, 0), (16, 8), (48, 4), (8, 8)])
+def test_rows_that_lie_apart(heads, kv_heads, d, page, more):
+    """Pages token by token, rows of codes and of scales with something between them, a page that is missing."""
+    c = Case([1, 2, 1], [700, 131, 2 * page + 1], heads, kv_heads, d, page, BF, layout="token", seed=page + d, unit=True)
+
+    def apart(t, n):
+        x = torch.full(t.shape[:3] + (t.shape[3] + n,), 0x7f, dtype=torch.uint8, device="cuda")
+        x[..., :t.shape[3]] = t
+        return x[..., :t.shape[3]]
+
+    k = c.cache
+    c.cache = k._replace(k=apart(k.k, more[0]), v=apart(k.v, more[0]), k_scale=apart(k.k_scale, more[1]), v_scale=apart(k.v_scale, more[1]))
+    good = c.check()
+    pages, status = c.pages.clone(), torch.zeros(1, dtype=torch.int32, device="cuda")
+    pages[1, 0] = c.cache.k.shape[0]
+    got = c.call(pages=pages, status=status)
+    assert int(status.item()) == pps.FLAG_INDEX and torch.equal(got[:1], good[:1]) and torch.equal(got[3:], good[3:])
+    assert bool(torch.isfinite(got).all())
+
+
+def test_a_cache_of_one_page():
+    for layout in ("token", "head"):
+        for d in (64, 128):
+            c = Case([1], [61], 8, 2, d, 64, F16, layout=layout, seed=d)
+            at = int(c.pages[0, 0])
+            c.cache = pps.CacheQ4(*(t[at:at + 1] for t in c.cache[:4]))
+            c.pages.fill_(0)
+            c.check()
+
+
 @pytest.mark.parametrize("q_len", [[1, 1], [2, 3], [50, 60]])
 @pytest.mark.parametrize("dt", [BF, F16])
 def test_factors_on_scores_that_vanish(q_len, dt):
