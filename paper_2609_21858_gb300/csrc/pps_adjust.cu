@@ -105,6 +105,8 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int seq = blockIdx.y;
     const int t0 = blockIdx.x * kSlice, tn = (int)min((int64_t)kSlice, a.V - t0);
+    pdl_wait();
+    pdl_launch_dependents();
     int first = __ldg(a.seq_off + seq), end = __ldg(a.seq_off + seq + 1);
     if (first < 0 || end < first || end > a.n_rows) {
         if (tid == 0 && a.status) atomicOr(a.status, PPS_FLAG_INDEX);
@@ -318,8 +320,7 @@ cudaError_t by_parts(const AdjustArgs& a, cudaStream_t st) {
         if (part.freq) part.freq += s0;
         if (part.pres) part.pres += s0;
         if (part.bias_off) part.bias_off += s0;
-        kernel<<<dim3((unsigned)slices, (unsigned)n), kAdjustThreads, 0, st>>>(part);
-        const cudaError_t e = cudaGetLastError();
+        const cudaError_t e = launch_pdl(kernel, dim3((unsigned)slices, (unsigned)n), dim3(kAdjustThreads), 0, st, part);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;

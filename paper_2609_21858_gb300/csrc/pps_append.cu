@@ -276,6 +276,10 @@ __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(
     const uint32_t step = Q4 && me < light ? (uint32_t)P.light_step : (uint32_t)P.tok_step, mine = Q4 && me >= light ? me - light : me;
     uint32_t tok = mine / of;
     const int part = (int)(mine - tok * of) + (Q4 && me >= light ? P.light : 0);
+    if constexpr (Q4) {
+        pdl_wait();
+        pdl_launch_dependents();
+    }
     if (tok >= min(n, step)) return;  // warp-uniform
 
     // the lane's units: channel starts of their two vectors
@@ -518,6 +522,7 @@ cudaError_t launch(const AppendArgs& a, cudaStream_t st) {
     const int64_t blocks = ((int64_t)P.tok_step * (P.parts - P.light) + (int64_t)P.light * P.light_step + kAppendWarps - 1) / kAppendWarps;
     auto kernel = bits4 ? (norm ? append_kernel<T, VW, NU, true, true> : append_kernel<T, VW, NU, false, true>)
                         : (norm ? append_kernel<T, VW, NU, true, false> : append_kernel<T, VW, NU, false, false>);
+    if (bits4) return launch_pdl(kernel, dim3((unsigned)blocks), dim3(32 * kAppendWarps), 0, st, a, P);
     kernel<<<(unsigned)blocks, 32 * kAppendWarps, 0, st>>>(a, P);
     return cudaGetLastError();
 }
@@ -546,6 +551,8 @@ __global__ void __launch_bounds__(256) read_kernel(const ReadArgs a, int per_slo
     const int in_cta = 256 / per_slot, sl = threadIdx.x / per_slot, task = threadIdx.x - sl * per_slot;
     // per_slot: blocks of a slot that a CTA takes at a time; blockIdx.y: which of them
     const int b = blockIdx.y * per_slot + task, head = b / n_blk, blk = b - head * n_blk;
+    pdl_wait();
+    pdl_launch_dependents();
     if (sl >= in_cta || head >= a.c.n_kv_heads) return;
     const float ku = a.q4.k_unit ? __ldg(a.q4.k_unit + head) : 1.0f, vu = a.q4.v_unit ? __ldg(a.q4.v_unit + head) : 1.0f;
     for (int64_t i = (int64_t)blockIdx.x * in_cta + sl; i < a.n; i += step) {
@@ -592,11 +599,7 @@ cudaError_t launch_kv_read(const ReadArgs& a, int dtype, cudaStream_t stream) {
     const int64_t ctas = std::min<int64_t>((a.n + in_cta - 1) / in_cta, std::max<int64_t>((int64_t)device_sm_count() * 8 / rounds, 1));
     const dim3 grid((unsigned)ctas, (unsigned)rounds);
     const int step = (int)(ctas * in_cta);
-    if (dtype == PPS_BF16)
-        read_kernel<__nv_bfloat16><<<grid, 256, 0, stream>>>(a, per_slot, step);
-    else
-        read_kernel<__half><<<grid, 256, 0, stream>>>(a, per_slot, step);
-    return cudaGetLastError();
+    return launch_pdl(dtype == PPS_BF16 ? read_kernel<__nv_bfloat16> : read_kernel<__half>, grid, dim3(256), 0, stream, a, per_slot, step);
 }
 
 cudaError_t launch_kv_append(const AppendArgs& a, int dtype, cudaStream_t stream) {

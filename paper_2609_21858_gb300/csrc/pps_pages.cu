@@ -77,6 +77,8 @@ __global__ void __launch_bounds__(kPageThreads) reserve_kernel(const ReserveArgs
     const int n = a.n_seq, tid = threadIdx.x;
     int *s_tok = s_seq, *s_page = s_tok + n, *s_len = s_page + n, *s_held = s_len + n;
     const int rank = blockIdx.x, ranks = gridDim.x;  // one cluster
+    pdl_wait();
+    pdl_launch_dependents();
     const int avail = max(min(a.free_count[0], a.free_cap), 0);
     const int64_t most = INT32_MAX;
     __shared__ int s_granted;  // pages: the demands before the first one that the pool cannot meet
@@ -182,6 +184,8 @@ __global__ void __launch_bounds__(kPageThreads) trim_kernel(const ReserveArgs a)
     const int n = a.n_seq, tid = threadIdx.x;
     int *s_back = s_seq, *s_keep = s_back + n;
     const int rank = blockIdx.x, ranks = gridDim.x;
+    pdl_wait();
+    pdl_launch_dependents();
     const int have = max(min(a.free_count[0], a.free_cap), 0);
     int64_t back0 = 0;
     bool bad = false;
@@ -231,12 +235,14 @@ cudaError_t launch_cluster(void (*kernel)(const ReserveArgs), const ReserveArgs&
     cfg.blockDim = dim3(ctas > 1 ? kPageThreads : (int)std::min<int64_t>(std::max<int64_t>((items + 31) / 32 * 32, 128), kPageThreads));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = ctas;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // as launch_pdl
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 

@@ -128,6 +128,14 @@ PyObject* common(PyObject* const* a, Py_ssize_t n, Py_ssize_t want, F f) {
 }
 
 // a dict of tensors
+// n elements of type st in the memory of `all`, from the element `from` of its own on, as a tensor that owns that memory too
+at::Tensor piece(const at::Tensor& all, at::ScalarType st, int64_t from, int64_t n) {
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), c10::scalarTypeToTypeMeta(st));
+    const int64_t size[1] = {n}, stride[1] = {1};
+    t.unsafeGetTensorImpl()->set_sizes_and_strides(c10::IntArrayRef(size), c10::IntArrayRef(stride),
+                                                   from * (int64_t)all.element_size() / (int64_t)c10::elementSize(st));
+    return t;
+}
 PyObject* dict_of(std::initializer_list<std::pair<const char*, at::Tensor*>> outs) {
     PyObject* d = PyDict_New();
     if (d == nullptr) return nullptr;
@@ -491,8 +499,12 @@ PyObject* kv_reserve(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
         x.pos_off = flat<int32_t>(a[8], di, at::kInt, x.n_tok);
         x.status = flat<uint32_t>(a[9], di, at::kInt, 1);
         const auto ints = tensor(a[0]).options();
-        at::Tensor off = at::empty({x.n_seq + (int64_t)1}, ints), len = at::empty({x.n_seq}, ints), slot = at::empty({x.n_tok}, ints.dtype(at::kLong)),
-                   pos = at::empty({x.n_tok}, ints), seq = at::empty({x.n_tok}, ints);
+        // the outputs share one allocation, each from a 16-byte boundary on: five take longer than the rest of the call
+        const int64_t seqs = (x.n_seq + (int64_t)4) / 4 * 4, toks = (x.n_tok + 3) / 4 * 4;
+        const at::Tensor all = at::empty({2 * toks + 2 * seqs + 2 * toks}, ints);
+        at::Tensor slot = piece(all, at::kLong, 0, x.n_tok), off = piece(all, at::kInt, 2 * toks, x.n_seq + (int64_t)1),
+                   len = piece(all, at::kInt, 2 * toks + seqs, x.n_seq), pos = piece(all, at::kInt, 2 * toks + 2 * seqs, x.n_tok),
+                   seq = piece(all, at::kInt, 3 * toks + 2 * seqs, x.n_tok);
         x.out_q_off = static_cast<int32_t*>(off.data_ptr());
         x.out_kv_len = static_cast<int32_t*>(len.data_ptr());
         x.out_slot = static_cast<int64_t*>(slot.data_ptr());
