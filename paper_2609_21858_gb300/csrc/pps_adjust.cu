@@ -9,7 +9,7 @@
 // of one sequence: it counts the text's tokens that fall into the slice in shared memory (and which entry of the bias list is
 // a token's last), with a bit per token that anything is known of.  Its warps take pieces of the sequence's rows: vectors are copied
 // through registers, and a vector's known tokens, by their bits, formed there one at a time.  (All elements of such a vector at once:
-// 423 us for 64 x 41 rows of 128256 where this took 249, and takes 231 now; listed and formed in memory after the copy, 295 to 320: a read and a write of 32 bytes for each, of what
+// 423 us for 64 x 41 rows of 128256 where this took 249, and takes 229 now; listed and formed in memory after the copy, 295 to 320: a read and a write of 32 bytes for each, of what
 // has left L2 in part.)  Tokens of a row's path, a handful, are formed before its piece (which may be written in place) and written
 // after it.
 #include <algorithm>

@@ -27,7 +27,7 @@
 // through shared memory as floats: lanes spread their channels there, then each lane takes a block or two, finds the scale, forms the
 // codes and writes 8 bytes and 1.  A warp whose heads are all queries has none of that.  16384 tokens of (28 + 2 x 4) heads of 128: 68.4 us
 // (its bytes: 42; 16 bits 52.6), bound by the issue and latency of 16 warps an SM (1.6 instructions a clock, DRAM at 45 percent).  Eight
-// tokens with a norm: 4.1 us in a graph, a chain of loads and the division.  The codes' way back (read_kernel) takes 10.8 us for 16 thousand slots.
+// tokens with a norm: 3.8 us in a graph, a chain of loads and the division.  The codes' way back (read_kernel) takes 10.8 us for 16 thousand slots.
 #include <algorithm>
 #include <cstdint>
 #include <cstring>

@@ -18,7 +18,7 @@
 namespace pps {
 namespace {
 
-// At most (512 trees of 41 nodes: 8.4 us; with 1024 9.0, with 256 11.4).
+// At most (512 trees of 41 nodes, launched after the end of what is before: 8.4 us; with 1024 9.0, with 256 11.4; on its drain 7.6).
 constexpr int kPageThreads = 512;
 constexpr int kPageCluster = 8;
 
