@@ -127,7 +127,6 @@ PyObject* common(PyObject* const* a, Py_ssize_t n, Py_ssize_t want, F f) {
     END_HANDLE_TH_ERRORS
 }
 
-// a dict of tensors
 // n elements of type st in the memory of `all`, from the element `from` of its own on, as a tensor that owns that memory too
 at::Tensor piece(const at::Tensor& all, at::ScalarType st, int64_t from, int64_t n) {
     at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), c10::scalarTypeToTypeMeta(st));
@@ -136,6 +135,7 @@ at::Tensor piece(const at::Tensor& all, at::ScalarType st, int64_t from, int64_t
                                                    from * (int64_t)all.element_size() / (int64_t)c10::elementSize(st));
     return t;
 }
+// a dict of tensors
 PyObject* dict_of(std::initializer_list<std::pair<const char*, at::Tensor*>> outs) {
     PyObject* d = PyDict_New();
     if (d == nullptr) return nullptr;
