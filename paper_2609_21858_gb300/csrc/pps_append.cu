@@ -25,9 +25,10 @@
 //
 // Into 4 bits (pps_q4.cuh).  A block's scale needs all its 16 channels, which lie in two to sixteen lanes, so a warp's keys and values go
 // through shared memory as floats: lanes spread their channels there, then each lane takes a block or two, finds the scale, forms the
-// codes and writes 8 bytes and 1.  A warp whose heads are all queries has none of that.  16384 tokens of (28 + 2 x 4) heads of 128: 68.4 us
-// (its bytes: 42; 16 bits 52.6), bound by the issue and latency of 16 warps an SM (1.6 instructions a clock, DRAM at 45 percent).  Eight
-// tokens with a norm: 3.8 us in a graph, a chain of loads and the division.  The codes' way back (read_kernel) takes 10.8 us for 16 thousand slots.
+// codes and writes 8 bytes and 1.  A warp whose heads are all queries has none of that.  The next item's channels come through
+// shared memory too (16-byte vectors): in registers they made the compiler spill, 68.8 us where this takes 59.7 (20 warps an SM at 96
+// registers: 99).  16384 tokens of (28 + 2 x 4) heads of 128: 57.9 us (its bytes: 42; 16 bits 52.3), bound by the issue and latency of
+// 16 warps an SM.  Eight tokens with a norm: 3.7 us in a graph, a chain of loads and the division.  The codes' way back (read_kernel) takes 10.8 us for 16 thousand slots.
 #include <algorithm>
 #include <cstdint>
 #include <cstring>
@@ -45,9 +46,10 @@ namespace {
 constexpr int kAppendWarps = 4;  // per CTA
 constexpr int kAhead = 2;        // heads of a lane group in an item
 constexpr int kAppendCtas = 4;   // per SM
+constexpr int kRing = 2;         // items of a warp in shared memory (below; 3: 61.9 us where 2 take 59.6)
 // What an item with keys or values takes where they become 4 bits, to one of queries alone.  16384 tokens of (28 + 2 x 4) heads of 128
-// channels: 77.5 us at 1, 68.4 at 1.3, 71.8 at 1.6, 80.3 at 2 (52.6 into a cache of 16 bits).
-constexpr double kHeavy = 1.3;
+// channels: 59.0 us at 1.1, 57.9 at 1.2, 59.7 at 1.3, 60.9 at 1.4 (52.3 into a cache of 16 bits).
+constexpr double kHeavy = 1.2;
 // a block's 16 channels in shared memory, 80 bytes apart: eight lanes' 16-byte reads touch all banks
 constexpr int kBlockFloats = 20;
 
@@ -266,6 +268,9 @@ template <typename T, int VW, int NU, bool NORM, bool Q4>
 __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(const AppendArgs a, const AppendPlan P) {
     constexpr int kBlocks = 64;  // of an item: 32 lanes x 16 channels x kAhead
     __shared__ __align__(16) float s_x[Q4 ? kAppendWarps : 1][Q4 ? kBlocks * kBlockFloats : 4];
+    // of 4 bits, channels come through shared memory, a lane's own sixteen bytes at a time: an item in use and kRing - 1 on their way
+    constexpr bool RING = Q4 && VW == 8;
+    __shared__ uint4 s_ring[RING ? kAppendWarps : 1][RING ? kRing : 1][2 * kAhead][RING ? 32 : 1];
     const int lane = threadIdx.x & 31;
     const int D = a.c.head_dim, half = a.rot >> 1;
     const int l = lane & ((1 << P.lg) - 1), hp = 32 >> P.lg, group = lane >> P.lg;
@@ -332,6 +337,36 @@ __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(
             inv[i] = unit ? __frcp_rn(__ldg(unit + in_kind)) : 1.0f;
         }
     }
+    uint4(*const ring)[2 * kAhead][RING ? 32 : 1] = s_ring[RING ? threadIdx.x >> 5 : 0];
+    uint32_t to_fill = 0, to_use = 0;
+    auto fetch_ring = [&](bool more) {  // the channels of the next item that is not on its way; a group of copies in any case
+        if (more) {
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                if (there[j])
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) {
+                        const int c = v ? c1[0] : c0[0];
+                        if (c < D)
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(&ring[to_fill][2 * j + v][lane])),
+                                         "l"(src[j] + c)
+                                         : "memory");
+                    }
+                src[j] += src_step[j];
+            }
+            to_fill = to_fill + 1 == kRing ? 0 : to_fill + 1;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto take_ring = [&](Item<T, VW, NU>& y) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 2) : "memory");
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+            for (int v = 0; v < 2; ++v)
+                *reinterpret_cast<uint4*>(&y.x[j][0][v]) = there[j] && (v ? c1[0] : c0[0]) < D ? ring[to_use][2 * j + v][lane] : make_uint4(0, 0, 0, 0);
+        to_use = to_use + 1 == kRing ? 0 : to_use + 1;
+    };
     auto fetch_x = [&](Item<T, VW, NU>& y) {
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
@@ -372,7 +407,11 @@ __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(
 #pragma unroll
             for (int v = 0; v < 2; ++v)  // channels that are never read count as zeros in a norm
                 even.x[j][k][v].raw = odd.x[j][k][v].raw = typename RawVec<VW>::type{};
-    fetch_x(even);
+    if constexpr (RING) {
+#pragma unroll
+        for (int i = 0; i < kRing - 1; ++i) fetch_ring(n - tok > i * step);
+    } else
+        fetch_x(even);
     int64_t slot = __ldg(a.slot + tok), slot1 = -1;
     int pos = half > 0 ? __ldg(a.pos + tok) : 0, pos1 = 0;
     if (n - tok > step) {
@@ -384,8 +423,12 @@ __global__ void __launch_bounds__(32 * kAppendWarps, kAppendCtas) append_kernel(
         const bool more = n - tok > step;
         int64_t slot2 = -1;
         int pos2 = 0;
+        if constexpr (RING) {
+            take_ring(cur);
+            fetch_ring(n - tok > (kRing - 1) * step);
+        }
         if (more) {
-            fetch_x(nxt);
+            if constexpr (!RING) fetch_x(nxt);
             if (n - tok > 2 * step) {
                 slot2 = __ldg(a.slot + tok + 2 * step);
                 if (half > 0) pos2 = __ldg(a.pos + tok + 2 * step);
@@ -522,7 +565,9 @@ cudaError_t launch(const AppendArgs& a, cudaStream_t st) {
     const int64_t blocks = ((int64_t)P.tok_step * (P.parts - P.light) + (int64_t)P.light * P.light_step + kAppendWarps - 1) / kAppendWarps;
     auto kernel = bits4 ? (norm ? append_kernel<T, VW, NU, true, true> : append_kernel<T, VW, NU, false, true>)
                         : (norm ? append_kernel<T, VW, NU, true, false> : append_kernel<T, VW, NU, false, false>);
-    if (bits4) return launch_pdl(kernel, dim3((unsigned)blocks), dim3(32 * kAppendWarps), 0, st, a, P);
+    // A few CTAs may come while what is before them ends.  Many may not: they would find SMs whose shared memory is divided for that
+    // other kernel, and the one wave that they are would become two (append, then read of 16384 tokens: 72 us, 80 to 91 that way).
+    if (bits4 && blocks <= device_sm_count()) return launch_pdl(kernel, dim3((unsigned)blocks), dim3(32 * kAppendWarps), 0, st, a, P);
     kernel<<<(unsigned)blocks, 32 * kAppendWarps, 0, st>>>(a, P);
     return cudaGetLastError();
 }
