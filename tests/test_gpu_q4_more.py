@@ -4,6 +4,7 @@ import threading
 import pytest
 import torch
 
+import test_gpu_q4_append as appends
 from paper_2609_21858_gb300 import pps
 from test_gpu_q4_attention import BF, F16, Case, _cuda  # noqa: F401
 
@@ -170,3 +171,61 @@ def test_two_graphs_at_the_same_time_with_a_workspace_each():
                 graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(outs, wants))
+
+
+@pytest.mark.parametrize("n,hq,hk,d,rot,page,dt", [(9001, 28, 4, 128, 128, 16, F16), (7777, 6, 2, 64, 48, 32, BF), (20011, 1, 1, 32, 32, 64, BF)])
+@pytest.mark.parametrize("norm,offset", [(False, 0), (True, 0), (True, 4)])
+def test_appends_whose_warps_take_many_tokens(n, hq, hk, d, rot, page, dt, norm, offset):
+    appends.test_against_the_formulas(n, hq, hk, d, rot, page, dt, norm, False, "head", offset, True)
+
+
+class Server:
+    """Three sequences, pages from a pool, five tokens a step of which two are kept."""
+
+    def __init__(self):
+        g = torch.Generator(device="cuda").manual_seed(5)
+        rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").to(BF)
+        self.q, self.k, self.v, self.logits = rnd(17, 8, 64), rnd(17, 2, 64), rnd(17, 2, 64), rnd(17, 5003)
+        self.cache, self.rope = pps.cache_q4(64, 16, 2, 64), pps.rope_table(512, 64)
+        self.pages, self.held = torch.full((3, 20), -1, dtype=torch.int32, device="cuda"), _i32(0, 0, 0)
+        self.free_list, self.free_count = torch.randperm(64, generator=g, device="cuda").int(), _i32(64)
+        self.kv_len, self.new, self.laws = _i32(30, 0, 100), _i32(5, 5, 5), torch.tensor([1.3, 2.0, 0.5], device="cuda")
+        self.text = torch.randint(0, 5003, (3, 200), generator=g, device="cuda", dtype=torch.int32)
+        self.status = _i32(0)
+        # what the sequences hold already
+        pool = (self.pages, self.held, self.free_list, self.free_count)
+        at = pps.kv_reserve(*pool, _i32(0, 0, 0), self.kv_len, 16, 130)
+        pps.kv_append_q4(rnd(130, 8, 64), rnd(130, 2, 64), rnd(130, 2, 64), at["pos"], at["slot"], self.cache, self.rope)
+
+    def step(self):
+        pool = (self.pages, self.held, self.free_list, self.free_count)
+        at = pps.kv_reserve(*pool, self.kv_len, self.new, 16, 17, status=self.status)  # a batch padded by two
+        q = pps.kv_append_q4(self.q, self.k, self.v, at["pos"], at["slot"], self.cache, self.rope, status=self.status)
+        a = pps.paged_attention_q4(q, self.cache, self.pages, at["kv_len"], at["q_off"], out=torch.zeros_like(q), status=self.status)
+        x = pps.adjust_logits(self.logits, at["q_off"], text=self.text, text_len=self.kv_len, repetition=self.laws, frequency=self.laws,
+                              out=torch.zeros_like(self.logits), status=self.status)
+        self.kv_len.add_(2)
+        pps.kv_trim(*pool, self.kv_len, 16, status=self.status)
+        k, v = pps.kv_read_q4(self.cache, at["slot"])
+        return a, x, k, v, at["slot"], at["pos"], at["seq"]
+
+
+def test_a_step_of_all_calls_captured_and_replayed():
+    eager, server = Server(), Server()
+    want = [[t.clone() for t in eager.step()] for _ in range(12)]
+    assert int(eager.status) == 0 and bool((want[0][4][15:] == -1).all()) and not bool(want[0][0][15:].any())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = server.step()
+    for w in want:
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(got, w))
+    assert int(server.status) == 0 and torch.equal(server.held, eager.held) and torch.equal(server.free_count, eager.free_count)
+    assert torch.equal(server.kv_len, _i32(54, 24, 124)) and torch.equal(server.held, _i32(4, 2, 8))
+    # the two tokens that each step kept are in the cache, in the pages that the table says
+    k, _ = pps.kv_read_q4(server.cache, server.pages[1, 0].long() * 16 + torch.arange(16, device="cuda"))
+    last = pps.cache_q4(1, 16, 2, 64)
+    at = torch.tensor([14, 15], device="cuda")
+    pps.kv_append_q4(server.q[5:7], server.k[5:7], server.v[5:7], at.int(), at, last, server.rope)
+    assert torch.equal(k[14:], pps.kv_read_q4(last, at)[0])
