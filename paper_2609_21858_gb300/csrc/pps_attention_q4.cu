@@ -24,7 +24,7 @@
 // Many rows (trees, chunks).  The 128-row tiles of pps_attn_tiles.cuh on the 5th-generation tensor cores: six warps copy a tile's codes
 // and scales into shared memory ahead of the products, widen them (64 conversions and as many multiplications a lane for 32 keys of
 // 128 channels) and write the halves where TMA would have put them.  Queries in bf16 become halves in a launch before it, at the same
-// power of two per row.  64 trees of 41 nodes: 227 us, of which that launch is some 8; a cache of 16 bits takes 180, as the softmax
+// power of two per row.  64 trees of 41 nodes: 220 us, of which that launch is some 8; a cache of 16 bits takes 180, as the softmax
 // has the issue slots to itself there.
 //
 // Work split.  The line of pps_attn.cuh.
@@ -43,7 +43,10 @@ constexpr int kStages4 = 2;       // units of a warp, on their way or in use
 constexpr int few_ctas(int nt) { return nt == 1 ? 3 : 2; }  // per SM: 168 or 255 registers
 constexpr int kMaxCtas4 = 640;
 constexpr auto kFetch4 = CU_TENSOR_MAP_L2_PROMOTION_L2_64B;  // what a miss brings into L2: a row (520000 keys: 68 us, 128 bytes 70, 256 71)
-constexpr int kFix4 = 2;          // key tiles that an item's start and end cost
+// Key tiles that an item's start and end cost: few rows (seven batches of 8 to 256 sequences, 1500 to 30000 keys: 4 is 1 to 5 percent
+// faster than 2, and equal to 3, 5 and 6 within 3), and tiles, which take longer each than those of 16 bits (six of trees, four of chunks: 3
+// is 3 to 5 percent faster than 6, within 1 of 4; 64 trees 220 us, 2: 238).
+constexpr int kFix4 = 4, kFixTiles4 = 3;
 constexpr int kLeast4 = 1;
 constexpr float kLazy4 = 8.0f;    // log2 of the rise of a maximum that nothing is rescaled for
 constexpr float kShift4 = 6.0f;   // log2 of a factor on all weights: 2^(8 + 6) is below fp16's largest number
@@ -665,7 +668,7 @@ cudaError_t launch_tiles(const AttnArgs& given, const Q4View& z, cudaStream_t st
     P.gs = rows.gs;
     P.tt = rows.tt;
     P.bt = 2 * rows.tt;
-    P.fix = kFix;
+    P.fix = kFixTiles4;
     P.cap_rows = rows.cap;
     P.shift = Half<__half>::kShift;
     plan_common(P, a);
