@@ -202,8 +202,9 @@ struct Wide {
 #pragma unroll
             for (int i = 0; i < kN; ++i) f[v][i] = mul2(f[v][i], mul2(rr, y.f[v][i]));
     }
-    // FUSED: a product's rounding is left out of each second sum (never of what becomes 4 bits: there the values are those of
-    // the formula's own operations in 32 bits, whatever computes them)
+    // FUSED: a product's rounding may be left out of a sum.  Never of what becomes 4 bits, where a last bit can decide a code: the
+    // values are those of products and sums rounded one by one, and so operations of one channel, as the compiler joins packed products
+    // and sums of the same rounding (16384 tokens of (28 + 2 x 4) heads of 128 channels in fp16: one query's channel in 8500 was a bit off).
     template <bool FUSED>
     __device__ __forceinline__ void rotate(bool interleaved, const float (&cs)[VW], const float (&sn)[VW]) {
         if (VW > 1 && interleaved) {
@@ -222,8 +223,23 @@ struct Wide {
             for (int i = 0; i < kN; ++i) {
                 const uint64_t c = pack2(cs[2 * i], cs[(2 * i + 1) % VW]), s = pack2(sn[2 * i], sn[(2 * i + 1) % VW]);
                 const uint64_t p = f[0][i], q = f[1][i];
-                f[0][i] = sub2(mul2(p, c), mul2(q, s));
-                f[1][i] = FUSED ? fma2(p, s, mul2(q, c)) : add2(mul2(p, s), mul2(q, c));
+                if constexpr (FUSED) {
+                    f[0][i] = sub2(mul2(p, c), mul2(q, s));
+                    f[1][i] = fma2(p, s, mul2(q, c));
+                } else {
+                    float x[2], y[2], cc[2], ss[2], a[2], b[2];
+                    unpack2(p, x[0], x[1]);
+                    unpack2(q, y[0], y[1]);
+                    unpack2(c, cc[0], cc[1]);
+                    unpack2(s, ss[0], ss[1]);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        a[e] = __fsub_rn(__fmul_rn(x[e], cc[e]), __fmul_rn(y[e], ss[e]));
+                        b[e] = __fadd_rn(__fmul_rn(x[e], ss[e]), __fmul_rn(y[e], cc[e]));
+                    }
+                    f[0][i] = pack2(a[0], a[1]);
+                    f[1][i] = pack2(b[0], b[1]);
+                }
             }
         }
     }
