@@ -307,6 +307,7 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.0f;
 
+        bool ok = true;
 #pragma unroll 1
         for (; k0 < last; k0 += kStep) {
             const int key0 = k0, ahead = k0 + kAhead4 * kStep, page = pages;
@@ -318,7 +319,7 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
                 paged <<= 2 * kGroups;
             close();
             if constexpr (DENSE)
-                mbar_wait(bar_at + 8 * to_use, phase, &s_abort);
+                if (!(ok = wait_warp(bar_at + 8 * to_use, phase, &s_abort))) break;
             asm volatile("cp.async.wait_group %0;" ::"n"(kAhead4) : "memory");
             __syncwarp();
             uint8_t* const unit = my_ring + to_use * S::kBytes;
@@ -475,7 +476,25 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
             }
         }
 
+        if (DENSE && !ok) {  // the warp gave up: its copies on their way are waited for (bounded)
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            for (int i = 0; i <= kAhead4 && k0 + i * kStep < last; ++i) {
+                const uint32_t at = to_use + i, bar = bar_at + 8 * (at % kStages4), parity = phase ^ (at / kStages4 & 1u);
+                for (uint32_t n = 0; n < kDrainLimit && !mbar_try_wait(bar, parity); ++n) {
+                }
+            }
+        }
+
         // ---- the segment's result: the warps' parts, joined
+#pragma unroll
+        for (int r = 0; r < 2 * NT; ++r) {
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
+            m[r] = m[r] == -INFINITY ? -INFINITY : m[r] * sc[r];  // log2 of the largest weight
+            if (l[r] != l[r]) m[r] = INFINITY;  // a score that is not a number, or infinite: so is the row, whatever it is joined with
+            if (g == 0) s_ml[warp][8 * (r >> 1) + 2 * t + (r & 1)] = make_float2(m[r], l[r]);
+        }
+        if (__syncthreads_or(!ok)) break;  // (the rings are read; or a warp gave up: nothing of this segment or a later one is written)
         const bool whole = W.t0 == 0 && W.t1 == W.T;
         const int slot = 2 * cta + (W.t0 == 0 ? 1 : 0);
         if (tid == 0 && W.t0 == 0 && !whole) {
@@ -486,15 +505,6 @@ __global__ void __launch_bounds__(kThreads4, few_ctas(NT)) few_rows_kernel(const
             c.vh = W.heads;
             P.cuts[cta] = c;
         }
-#pragma unroll
-        for (int r = 0; r < 2 * NT; ++r) {
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], d);
-            m[r] = m[r] == -INFINITY ? -INFINITY : m[r] * sc[r];  // log2 of the largest weight
-            if (l[r] != l[r]) m[r] = INFINITY;  // a score that is not a number, or infinite: so is the row, whatever it is joined with
-            if (g == 0) s_ml[warp][8 * (r >> 1) + 2 * t + (r & 1)] = make_float2(m[r], l[r]);
-        }
-        __syncthreads();  // (the rings are read)
 #pragma unroll
         for (int r = 0; r < 2 * NT; ++r) {
             const int row = 8 * (r >> 1) + 2 * t + (r & 1);

@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(Cfg<DC, Q4>::kThreads, 1)
             // copies in flight when the CTA gives up: wait (bounded) for each
             for (uint32_t j = 0; j < (uint32_t)C::kStages && *abort; ++j)
                 if (filled >> j & 1u)
-                    for (uint32_t n = 0, i = last - 1 - j; n < kWaitLimit && !mbar_try_wait(full(i % C::kStages), (i / C::kStages) & 1u); ++n) {
+                    for (uint32_t n = 0, i = last - 1 - j; n < kDrainLimit && !mbar_try_wait(full(i % C::kStages), (i / C::kStages) & 1u); ++n) {
                     }
         } else if (warp == kMmaWarp) {
             // ---- products (one thread): per stream S = Q K^T, then O += P V as its weights arrive
@@ -480,7 +480,7 @@ __global__ void __launch_bounds__(Cfg<DC, Q4>::kThreads, 1)
             // copies in flight when the CTA gives up: wait (bounded) for each
             for (uint32_t tile = 0; tile < 2 && *abort; ++tile) {
                 const uint32_t u = tile ? n1 : n0;
-                for (uint32_t n = 0; u > 0 && n < kWaitLimit && !mbar_try_wait(qfull(tile), (u - 1) & 1u); ++n) {
+                for (uint32_t n = 0; u > 0 && n < kDrainLimit && !mbar_try_wait(qfull(tile), (u - 1) & 1u); ++n) {
                 }
             }
         }

@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(kThreads + 32, kStatCtas + 1) stats_kernel(con
             }
             // copies in flight when the CTA gives up: wait (bounded) for each
             for (uint32_t i = it > (uint32_t)kStatStages ? it - kStatStages : 0u; i < it && s_abort; ++i)
-                for (uint32_t n = 0; n < kWaitLimit && !mbar_try_wait(full(i % kStatStages), (i / kStatStages) & 1u); ++n) {
+                for (uint32_t n = 0; n < kDrainLimit && !mbar_try_wait(full(i % kStatStages), (i / kStatStages) & 1u); ++n) {
                 }
         }
     } else {
@@ -488,7 +488,7 @@ __global__ void __launch_bounds__(kThreads + 32) finish_kernel(const ChainArgs a
             }
             // copies in flight when the CTA gives up: wait (bounded) for each
             for (uint32_t i = rows > (uint32_t)kRaceStages ? rows - kRaceStages : 0u; i < rows && s_abort; ++i)
-                for (uint32_t n = 0; n < kWaitLimit && !mbar_try_wait(full(i % kRaceStages), (i / kRaceStages) & 1u); ++n) {
+                for (uint32_t n = 0; n < kDrainLimit && !mbar_try_wait(full(i % kRaceStages), (i / kRaceStages) & 1u); ++n) {
                 }
         }
     } else {

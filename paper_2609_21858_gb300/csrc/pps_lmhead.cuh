@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(kLmThreads, 1)
             // wait (bounded) for each of them before the CTA leaves
             const uint32_t from = it > (uint32_t)kStages ? it - kStages : 0u;
             for (uint32_t j = from; j < it && *abort; ++j)
-                for (uint32_t n = 0; n < kWaitLimit && !mbar_try_wait(full(j % kStages), (j / kStages) & 1u); ++n) {
+                for (uint32_t n = 0; n < kDrainLimit && !mbar_try_wait(full(j % kStages), (j / kStages) & 1u); ++n) {
                 }
         }
     } else if (warp == 1) {

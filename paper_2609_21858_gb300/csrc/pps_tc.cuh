@@ -1,6 +1,7 @@
 // pps_tc.cuh -- mbarriers, TMA, tensor memory and tcgen05 for the kernels that use them (sm_103a).
 //
-// Every wait on an mbarrier gives up after kWaitLimit polls and raises the CTA's abort flag.
+// Every wait on an mbarrier gives up after kWaitLimit polls and raises the CTA's abort flag; what a CTA that gives up has on its way
+// to shared memory is waited for, at most kDrainLimit polls a copy, before the CTA ends.
 #pragma once
 #include <atomic>
 #include <cstdint>
@@ -9,7 +10,10 @@
 
 namespace tc {
 
-constexpr uint32_t kWaitLimit = 1u << 22;
+#ifndef PPS_WAIT_LIMIT  // (0: every wait gives up at once, which tests build)
+#define PPS_WAIT_LIMIT (1u << 22)
+#endif
+constexpr uint32_t kWaitLimit = PPS_WAIT_LIMIT, kDrainLimit = 1u << 22;
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
