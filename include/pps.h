@@ -757,7 +757,8 @@ pps_status pps_paged_attention_q4(const pps_attention_q4_args* args, pps_stream_
  * column, is free_list[free_count - 1 - k].
  * A sequence whose demand, with the demands of those before it, passes the pool
  * gets nothing (PPS_FLAG_POOL), and neither does any later one that lacks a page;
- * one that would pass its row's columns gets nothing either and demands nothing
+ * one that would pass its row's columns, or holds fewer pages than its kv_len
+ * tokens take, gets nothing either and demands nothing
  * (PPS_FLAG_INDEX).  Such a sequence's tokens have slot -1 and out_kv_len 0, so that nothing is
  * written for them and they attend to nothing.
  *

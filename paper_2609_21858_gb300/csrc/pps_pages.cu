@@ -97,9 +97,9 @@ __global__ void __launch_bounds__(kPageThreads) reserve_kernel(const ReserveArgs
             held = min(max(hh, 0), a.columns);
             bad |= nn < 0 || ll < 0 || hh != held;
             const int64_t want = pages_of((uint32_t)len + (uint32_t)n_new, a.page_size);
-            fits = want <= a.columns;
-            if (n_new > 0 && fits) need = max(want - held, (int64_t)0);
-            if (n_new == 0 && want > held) bad = true;  // holds fewer pages than it has tokens
+            // (one that holds fewer pages than its tokens take is not served: pages from the pool would stand for tokens that nothing wrote)
+            fits = want <= a.columns && pages_of(len, a.page_size) <= (uint32_t)held;
+            if (fits) need = max(want - held, (int64_t)0);
         }
         int64_t x = n_new, y = need, all_x, all_y;
         scan2(x, y, all_x, all_y, s_sum);
