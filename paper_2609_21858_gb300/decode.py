@@ -125,7 +125,8 @@ class Decoder:
 class Session:
     """Sequences that decode together.  `branching[d]`: children of a node of depth d; all ones: chains.
     `text` [n_seq, ...] holds the tokens, `length` [n_seq] how many of them the cache holds (the next one,
-    text[s, length[s]], is known and not cached yet).  bits, pool: the cache's.  laws: what shapes the target's law, by
+    text[s, length[s]], is known and not cached yet).  bits, pool: the cache's; a step in which the pool has no pages left for a sequence
+    emits nothing for it (n_emitted 0, tokens -1) and raises the flag.  laws: what shapes the target's law, by
     pps.adjust_logits' names: repetition, frequency, presence [n_seq], bias_off, bias_tok, bias_val, and `allowed`, a mask
     [nodes of all sequences, words] or a function that gives one for the nodes' tokens."""
 
@@ -257,6 +258,11 @@ class Session:
             v = pps.lmhead_verify_tree(hidden, model.head, self.node_key, self.zero, pos + 1, t.gamma, self.seq_off,
                                        self.node_draft_row, lists, counts, self.child_node, self.temperature,
                                        status=self.status)
+        if self.cache.pooled:  # a sequence that got no pages stands still
+            served = kv_len > 0
+            v["accept_len"] = torch.where(served, v["accept_len"], 0)
+            v["n_emitted"] = torch.where(served, v["n_emitted"], 0)
+            v["emitted"] = torch.where(served[:, None], v["emitted"], -1)
         if t.K > 1:
             model.keep(kept, pos, self._kept_slots(lists, v), self.cache, self.status)
         at = self.length[:, None] + 1 + torch.arange(self.width, device=self.device)
