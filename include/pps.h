@@ -831,7 +831,7 @@ pps_status pps_kv_trim(const pps_trim_args* args, pps_stream_t stream);
  * seq_off      [n_seq + 1] sequence s owns rows seq_off[s] .. seq_off[s+1]-1 (as
  *              pps_verify_tree).  Rows of no sequence are not written; a sequence whose rows
  *              lie outside them is left out (PPS_FLAG_INDEX)
- * text         nullable [n_seq, text_stride], text_len [n_seq] its tokens (at
+ * text         nullable [n_seq, text_stride] (NULL, too, where text_cap is 0), text_len nullable [n_seq] its tokens (at
  *              most text_cap <= text_stride), prompt_len nullable [n_seq] (NULL: none of them is prompt)
  * node_tok     nullable [n_rows]: the token that each row's node stands for; the
  *              row's path is its own and its ancestors' (they count as output):
@@ -839,7 +839,7 @@ pps_status pps_kv_trim(const pps_trim_args* args, pps_stream_t stream);
  *              (the tree mask of pps_paged_attention); NULL: the rows of a
  *              sequence are a chain.  A path of more than 64 counts its first 64
  *              (PPS_FLAG_INDEX)
- * repetition (> 0), frequency, presence  nullable [n_seq], finite; they need text or node_tok
+ * repetition (> 0), frequency, presence  nullable [n_seq], finite; they need text_len or node_tok
  * bias_off     nullable [n_seq + 1]: entries bias_off[s] .. bias_off[s+1]-1 of
  *              bias_tok, bias_val [n_bias] are added in sequence s; of several for a token the last counts
  * allowed      nullable [n_rows, allowed_stride] words, bit i % 32 of word i / 32:

@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
             if (a.rep) law.rep = __ldg(a.rep + seq);
             if (a.freq) law.freq = __ldg(a.freq + seq);
             if (a.pres) law.pres = __ldg(a.pres + seq);
-            if (a.text) {
+            if (a.text_len) {
                 const int said = __ldg(a.text_len + seq), len = min(max(said, 0), a.text_cap);
                 const int prompt = a.prompt_len ? min(max(__ldg(a.prompt_len + seq), 0), len) : 0;
                 bad |= said != len;
@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
 
 template <typename T>
 cudaError_t by_parts(const AdjustArgs& a, cudaStream_t st) {
-    const bool counts = a.text != nullptr || a.node_tok != nullptr, bias = a.bias_tok != nullptr;
+    const bool counts = a.text_len != nullptr || a.node_tok != nullptr, bias = a.bias_tok != nullptr;
     // Pieces of 2048 tokens, or of 1024 where a sequence has few rows (measured on an earlier form: 64 x 41 rows 249 and 276 us, 16 x 9
     // rows 46 and 44, one row 7.1 and 6.1).  What a piece is, and whether there is a mask, are compile-time choices: each as a variable
     // made the call of 64 x 41 rows, which has no mask, 16 to 25 percent slower.

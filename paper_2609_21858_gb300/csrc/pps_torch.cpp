@@ -559,6 +559,7 @@ PyObject* adjust_logits(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
         }
         x.prompt_len = flat<int32_t>(a[4], di, at::kInt, n_seq);
         x.node_tok = flat<int32_t>(a[5], di, at::kInt, n);
+        if (a[5] != Py_None && n == 0) x.node_tok = x.seq_off;  // (an empty tensor has no address: any other, of which nothing is read)
         if (a[6] != Py_None) {
             const at::Tensor& m = on(a[6], di, at::kInt);
             if (m.dim() != 2 || m.size(0) != n || m.size(1) < 1 || !m.is_contiguous()) throw NotCommon();

@@ -1236,6 +1236,8 @@ def adjust_logits(logits, seq_off, text=None, text_len=None, prompt_len=None, no
         lens = _flat("text_len", _required("text_len", text_len, di), di, i32, n_seq)
     prompt = _flat("prompt_len", prompt_len, di, i32, n_seq)
     toks = _flat("node_tok", node_tok, di, i32, n)
+    if node_tok is not None and n == 0:
+        toks = offs  # empty tensors have no address; any other says that there are tokens, and none is read
     if node_mask is not None:
         if _required("node_mask", node_mask, di).dim() != 2 or node_mask.shape[0] != n or node_mask.shape[1] < 1:
             raise ValueError(f"node_mask must be [{n}, words]")
