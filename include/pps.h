@@ -844,7 +844,8 @@ pps_status pps_kv_trim(const pps_trim_args* args, pps_stream_t stream);
  *              bias_tok, bias_val [n_bias] are added in sequence s; of several for a token the last counts
  * allowed      nullable [n_rows, allowed_stride] words, bit i % 32 of word i / 32:
  *              token i may follow (allowed_stride >= ceil(vocab / 32), or 0: one row for all)
- * Tokens outside the vocabulary are left out (PPS_FLAG_INDEX).
+ * Tokens outside the vocabulary are left out (PPS_FLAG_INDEX).  What says something about an argument that is missing
+ * (prompt_len without text_len, bias_tok or bias_val without bias_off, node_mask without node_tok) is refused.
  */
 typedef struct {
     size_t size; /* sizeof(pps_adjust_args) */

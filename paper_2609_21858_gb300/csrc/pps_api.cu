@@ -1010,11 +1010,11 @@ pps_status pps_adjust_logits(const pps_adjust_args* args, pps_stream_t stream) {
     if (in_stride < vocab || out_stride < vocab || !strides_ok(in_stride, n_rows, out_stride, n_rows)) return PPS_ERR_INVALID_ARG;
     if (logits == out && in_stride != out_stride && n_rows > 1) return PPS_ERR_INVALID_ARG;
     if (!multiple(logits, dtype == PPS_F32 ? 4 : 2) || !multiple(out, dtype == PPS_F32 ? 4 : 2)) return PPS_ERR_INVALID_ARG;
-    if (text && !text_len) return PPS_ERR_INVALID_ARG;
+    if ((text || prompt_len) && !text_len) return PPS_ERR_INVALID_ARG;
     if (text_len && ((!text && text_cap > 0 && n_seq > 0) || text_stride < text_cap || !strides_ok(text_stride, n_seq, 0, 0))) return PPS_ERR_INVALID_ARG;
     if (node_mask && (!node_tok || mask_words < 1)) return PPS_ERR_INVALID_ARG;
     if ((repetition || frequency || presence) && !text_len && !node_tok) return PPS_ERR_INVALID_ARG;
-    if (bias_off && n_bias > 0 && (!bias_tok || !bias_val)) return PPS_ERR_INVALID_ARG;
+    if (bias_off ? n_bias > 0 && (!bias_tok || !bias_val) : bias_tok || bias_val || n_bias > 0) return PPS_ERR_INVALID_ARG;
     if (allowed && ((allowed_stride != 0 && allowed_stride < (vocab + 31) / 32) || !strides_ok(allowed_stride, n_rows, 0, 0))) return PPS_ERR_INVALID_ARG;
     if (n_rows == 0 || n_seq == 0) return PPS_OK;
     if (!logits || !out || !seq_off) return PPS_ERR_INVALID_ARG;

@@ -549,7 +549,7 @@ PyObject* adjust_logits(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
         x.n_rows = n;
         x.vocab = V;
         x.in_stride = n > 1 ? l.stride(0) : V;
-        if (a[2] != Py_None) {
+        if (a[2] != Py_None || a[3] != Py_None) {
             const at::Tensor& t = on(a[2], di, at::kInt);
             if (t.dim() != 2 || t.size(0) != n_seq || (t.size(1) > 1 && t.stride(1) != 1) || a[3] == Py_None) throw NotCommon();
             x.text = static_cast<const int32_t*>(t.data_ptr());
@@ -569,8 +569,8 @@ PyObject* adjust_logits(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
         x.repetition = flat<float>(a[7], di, at::kFloat, n_seq);
         x.frequency = flat<float>(a[8], di, at::kFloat, n_seq);
         x.presence = flat<float>(a[9], di, at::kFloat, n_seq);
-        if (a[10] != Py_None) {
-            if (a[11] == Py_None || a[12] == Py_None) throw NotCommon();
+        if (a[10] != Py_None || a[11] != Py_None || a[12] != Py_None) {
+            if (a[10] == Py_None || a[11] == Py_None || a[12] == Py_None) throw NotCommon();
             x.n_bias = small(tensor(a[11]).numel());
             x.bias_off = flat<int32_t>(a[10], di, at::kInt, n_seq + 1);
             x.bias_tok = flat<int32_t>(a[11], di, at::kInt, 0);

@@ -1229,7 +1229,7 @@ def adjust_logits(logits, seq_off, text=None, text_len=None, prompt_len=None, no
     offs = _flat("seq_off", _required("seq_off", seq_off, di), di, i32, 1)
     n_seq = seq_off.numel() - 1
     texts = lens = text_stride = cap = words = nodes = 0
-    if text is not None:
+    if text is not None or text_len is not None:
         text_stride = _strided("text", text, di, i32, (n_seq, None), "[n_seq, tokens]")[0]
         texts, cap = text.data_ptr(), text.shape[1]
         text_stride = text_stride if n_seq > 1 else cap
@@ -1246,9 +1246,9 @@ def adjust_logits(logits, seq_off, text=None, text_len=None, prompt_len=None, no
                                                            ("presence", presence))]
     entries = [0, 0, 0]
     n_bias = 0
-    if bias_off is not None:
+    if bias_off is not None or bias_tok is not None or bias_val is not None:
         n_bias = _required("bias_tok", bias_tok, di).numel()
-        entries = [_flat("bias_off", bias_off, di, i32, n_seq + 1), _flat("bias_tok", bias_tok, di, i32, 0),
+        entries = [_flat("bias_off", _required("bias_off", bias_off, di), di, i32, n_seq + 1), _flat("bias_tok", bias_tok, di, i32, 0),
                    _flat("bias_val", _required("bias_val", bias_val, di), di, f32, n_bias)]
     bits = bits_stride = 0
     if allowed is not None:
