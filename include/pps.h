@@ -832,7 +832,8 @@ pps_status pps_kv_trim(const pps_trim_args* args, pps_stream_t stream);
  *              pps_verify_tree).  Rows of no sequence are not written; a sequence whose rows
  *              lie outside them is left out (PPS_FLAG_INDEX)
  * text         nullable [n_seq, text_stride] (NULL, too, where text_cap is 0), text_len nullable [n_seq] its tokens (at
- *              most text_cap <= text_stride), prompt_len nullable [n_seq] (NULL: none of them is prompt)
+ *              most text_cap <= text_stride), prompt_len nullable [n_seq] (NULL: none of them is prompt; at most
+ *              text_len).  Lengths outside these are cut (PPS_FLAG_INDEX)
  * node_tok     nullable [n_rows]: the token that each row's node stands for; the
  *              row's path is its own and its ancestors' (they count as output):
  * node_mask    nullable [n_rows, mask_words] bit b: the b-th row of the sequence lies on the path

@@ -129,8 +129,8 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
             if (a.pres) law.pres = __ldg(a.pres + seq);
             if (a.text_len) {
                 const int said = __ldg(a.text_len + seq), len = min(max(said, 0), a.text_cap);
-                const int prompt = a.prompt_len ? min(max(__ldg(a.prompt_len + seq), 0), len) : 0;
-                bad |= said != len;
+                const int given = a.prompt_len ? __ldg(a.prompt_len + seq) : 0, prompt = min(max(given, 0), len);
+                bad |= said != len || given != prompt;
                 const int32_t* text = a.text + seq * a.text_stride;
                 for (int i0 = tid; i0 < len; i0 += 4 * kAdjustThreads) {
                     int tok[4];
