@@ -838,8 +838,8 @@ pps_status pps_kv_trim(const pps_trim_args* args, pps_stream_t stream);
  *              row's path is its own and its ancestors' (they count as output):
  * node_mask    nullable [n_rows, mask_words] bit b: the b-th row of the sequence lies on the path
  *              (the tree mask of pps_paged_attention); NULL: the rows of a
- *              sequence are a chain.  A path of more than 64 counts its first 64
- *              (PPS_FLAG_INDEX)
+ *              sequence are a chain.  A path of more than 64 counts its first 64, rows from the
+ *              32 * mask_words-th of a sequence on lie on no path (both PPS_FLAG_INDEX)
  * repetition (> 0), frequency, presence  nullable [n_seq], finite; they need text_len or node_tok
  * bias_off     nullable [n_seq + 1]: entries bias_off[s] .. bias_off[s+1]-1 of
  *              bias_tok, bias_val [n_bias] are added in sequence s; of several for a token the last counts

@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(kAdjustThreads, 4) adjust_kernel(const AdjustA
     }
     if (first == end) return;
     const int n_rows = end - first;
-    bool bad = false;
+    bool bad = COUNTS && a.node_mask && n_rows > 32ll * a.mask_words;  // rows that no mask has a bit for
     Law law = {1.0f, 0.0f, 0.0f};
     if constexpr (COUNTS || BIAS) {
         for (int i = tid; i < kSlice / 32; i += kAdjustThreads) s_known[i] = 0;

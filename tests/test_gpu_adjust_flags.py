@@ -27,3 +27,21 @@ def test_prompts_longer_than_their_text(lens, prompt, cut, dt):
     status.zero_()
     c.call(prompt_len=i32(lens), status=status)  # all of it is prompt
     assert int(status) == 0
+
+
+@pytest.mark.parametrize("rows,words", [([33, 2], 1), ([1, 65], 2), ([40, 40, 3], 1)])
+def test_masks_without_a_bit_for_every_row(rows, words):
+    c = Case(rows, 3000, BF, near=20, seed=2)
+    have = c.args["node_mask"].shape[1]
+    assert have == words + 1
+    for s in range(len(rows)):
+        c.sees[s][:, 32 * words:] = False  # what a mask of `words` words can say
+    want, size = c.exact()
+    status = i32([0])
+    got = c.call(node_mask=c.args["node_mask"][:, :words].contiguous(), status=status)
+    assert int(status) == pps.FLAG_INDEX
+    # five operations in fp32, 2^-24 of the terms each, and the result's rounding (2^-8, half a step of bf16)
+    assert bool(((got.double() - want).abs() <= 6 * 2.0 ** -24 * size + 2.0 ** -8 * want.abs()).all())
+    status.zero_()
+    c.call(status=status)
+    assert int(status) == 0
