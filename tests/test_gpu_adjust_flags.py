@@ -45,3 +45,31 @@ def test_masks_without_a_bit_for_every_row(rows, words):
     status.zero_()
     c.call(status=status)
     assert int(status) == 0
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("wrong", [-1, 3000, -2 ** 31, 2 ** 31 - 1])
+@pytest.mark.parametrize("key,at", [("text", (1, 2)), ("text", (0, 0)), ("node_tok", (1,)), ("node_tok", (4,)), ("bias_tok", (0,)), ("bias_tok", (7,))])
+def test_a_wrong_token_counts_as_left_out(key, at, wrong, dt):
+    c = Case([3, 2], 3000, dt, [20, 30], near=25, bias=30, seed=12)
+    off = c.args["bias_off"].tolist()
+    assert off[-1] > 7
+    c.args[key] = c.args[key].clone()
+    c.args[key][at] = wrong
+    seen = True
+    if key == "text":
+        c.text[at[0]] = torch.cat([c.text[at[0]][:at[1]], c.text[at[0]][at[1] + 1:]])
+    elif key == "node_tok":
+        s = 0 if at[0] < 3 else 1
+        seen = bool(c.sees[s][:, at[0] - c.off[s]].any())
+        c.sees[s][:, at[0] - c.off[s]] = False
+    else:
+        entries = list(zip(c.args["bias_tok"].tolist(), c.args["bias_val"].tolist()))
+        c.bias = [{t: v for t, v in entries[a:b] if t != wrong} for a, b in zip(off, off[1:])]
+    status = i32([0])
+    got = c.call(status=status)
+    assert int(status) == (pps.FLAG_INDEX if seen else 0)
+    if key == "node_tok":
+        c.args["node_tok"][at] = 0  # (of no path: any token will do)
+    want, size = c.exact()
+    assert bool(((got.double() - want).abs() <= 6 * 2.0 ** -24 * size + (2.0 ** -8 if dt is BF else 0) * want.abs()).all())
