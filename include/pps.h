@@ -650,10 +650,13 @@ pps_status pps_verify_chain(const pps_chain_args* args, pps_stream_t stream);
  * held from a block x as  z = x * (1 / unit),  scale = e4m3(min(max |z| / 6, 448)),
  * code = e2m1(z / scale), in fp32, to nearest with ties to even, at most 6; a
  * scale that rounds to zero makes the block zeros (of either sign), and a block
- * with a channel that is not finite is held as NaN throughout.  So a block's channel is off by a
- * sixth of the block's largest at most (half the step from 4 to 6; a scale's
- * rounding adds up to 2^-4 of the largest's), and a block whose largest is below
- * 6 * 2^-10 units is zeros: units (nullable: ones) keep heads of small values in range.
+ * with a channel that is not finite is held as NaN throughout.  So a block whose
+ * largest magnitude lies between 6 * 2^-6 and 2688 units has channels that are off by
+ * at most 3/17 of that largest (half the step from 4 to 6, of a scale rounded up by a
+ * 17th).  Below, where scales are 2^-9 apart, it is up to a third of the largest; from
+ * 6 * 2^-10 units down the block is zeros; and channels past 2688 units are cut there,
+ * however far.  Units (nullable: ones) bring a head's blocks into the range: a 2688th of
+ * the largest magnitude of a head leaves the most room below.
  * Codes of (page, token, head) are head_dim / 2 bytes at k + page * page_stride +
  * token * tok_stride + head * head_stride, scales 4 * ceil(head_dim / 64) bytes of which
  * head_dim / 16 count, at k_scale with strides of their own (all strides in
