@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(kPageThreads) reserve_kernel(const ReserveArgs
             bad |= nn < 0 || ll < 0 || hh != held;
             const int64_t want = pages_of((uint32_t)len + (uint32_t)n_new, a.page_size);
             // (one that holds fewer pages than its tokens take is not served: pages from the pool would stand for tokens that nothing wrote)
-            fits = want <= a.columns && pages_of(len, a.page_size) <= (uint32_t)held;
+            fits = want <= a.columns && len <= (int64_t)held * a.page_size;
             if (fits) need = max(want - held, (int64_t)0);
         }
         int64_t x = n_new, y = need, all_x, all_y;
