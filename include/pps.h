@@ -655,8 +655,8 @@ pps_status pps_verify_chain(const pps_chain_args* args, pps_stream_t stream);
  * at most 3/17 of that largest (half the step from 4 to 6, of a scale rounded up by a
  * 17th).  Below, where scales are 2^-9 apart, it is up to a third of the largest; from
  * 6 * 2^-10 units down the block is zeros; and channels past 2688 units are cut there,
- * however far.  Units (nullable: ones) bring a head's blocks into the range: a 2688th of
- * the largest magnitude of a head leaves the most room below.
+ * however far.  Units (nullable: ones; from 2^-126 to 2^126) bring a head's blocks into the range:
+ * a 2688th of the largest magnitude of a head leaves the most room below.
  * Codes of (page, token, head) are head_dim / 2 bytes at k + page * page_stride +
  * token * tok_stride + head * head_stride, scales 4 * ceil(head_dim / 64) bytes of which
  * head_dim / 16 count, at k_scale with strides of their own (all strides in
@@ -670,7 +670,7 @@ typedef struct {
     void* v;
     void* k_scale;
     void* v_scale;
-    const float* k_unit; /* nullable [n_kv_heads], positive and finite */
+    const float* k_unit; /* nullable [n_kv_heads], 2^-126 .. 2^126 */
     const float* v_unit;
     int64_t n_pages;
     int32_t page_size, n_kv_heads, head_dim;
@@ -726,8 +726,12 @@ pps_status pps_kv_read_q4(const pps_read_q4_args* args, pps_stream_t stream);
  * done about numbers that are not finite.  Codes times scales are exact in fp16, in which both products run
  * on the tensor cores with fp32 accumulation: queries in bf16 are brought there by a
  * power of two per row (channels below 2^-31 of a row's largest lose bits), the softmax is in fp32,
- * its weights are rounded to fp16 for the second product (2^-11 of each).
+ * its weights are rounded to fp16 for the second product (2^-11 of each).  scale * log2(e) * k_unit
+ * is finite in fp32 for every head (else its rows are NaN or wrong).
  * head_dim is a multiple of 16 up to 128, page_size a power of two >= 8.
+ * Which of two kernels takes a call, and how many rows it takes at a time, follows ceil(n_tok / n_seq), as lengths are on the
+ * device.  A batch of single tokens and long chunks, or one padded with many empty sequences, gets right results but takes longer
+ * than a call for each kind, of the sequences of that kind (measured: 1.6 to 1.9 times).
  * ws, ws_bytes pps_attention_q4_workspace_size(n_tok, n_heads, n_kv_heads,
  *              head_dim) bytes; need not be cleared
  */

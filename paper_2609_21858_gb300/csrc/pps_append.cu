@@ -26,9 +26,10 @@
 // Into 4 bits (pps_q4.cuh).  A block's scale needs all its 16 channels, which lie in two to sixteen lanes, so a warp's keys and values go
 // through shared memory as floats: lanes spread their channels there, then each lane takes a block or two, finds the scale, forms the
 // codes and writes 8 bytes and 1.  A warp whose heads are all queries has none of that.  The next item's channels come through
-// shared memory too (16-byte vectors): in registers they made the compiler spill, 68.8 us where this takes 59.7 (20 warps an SM at 96
-// registers: 99).  16384 tokens of (28 + 2 x 4) heads of 128: 57.9 us (its bytes: 42; 16 bits 52.3), bound by the issue and latency of
-// 16 warps an SM.  Eight tokens with a norm: 3.7 us in a graph, a chain of loads and the division.  The codes' way back (read_kernel) takes 10.8 us for 16 thousand slots.
+// shared memory too (16-byte vectors): in registers they made the compiler spill, 68.8 us where an earlier form of this took 59.7 (20 warps an SM
+// at 96 registers: 99).  16384 tokens of (28 + 2 x 4) heads of 128: 59.2 us (its bytes: 42; 16 bits 52.7), bound by the latency of
+// 16 warps an SM (1.9 of 4 issue slots, DRAM at 52 percent).  Eight tokens with a norm: 3.7 us in a graph, a chain of loads and the division.
+// The codes' way back (read_kernel) takes 10.7 us for 16 thousand slots, of 6: the slot's division, its codes and its stores stand one behind the other.
 #include <algorithm>
 #include <cstdint>
 #include <cstring>
@@ -46,9 +47,9 @@ namespace {
 constexpr int kAppendWarps = 4;  // per CTA
 constexpr int kAhead = 2;        // heads of a lane group in an item
 constexpr int kAppendCtas = 4;   // per SM
-constexpr int kRing = 2;         // items of a warp in shared memory (below; 3: 61.9 us where 2 take 59.6)
+constexpr int kRing = 2;         // items of a warp in shared memory (below; 3: 62.1 us where 2 take 59.3)
 // What an item with keys or values takes where they become 4 bits, to one of queries alone.  16384 tokens of (28 + 2 x 4) heads of 128
-// channels: 59.0 us at 1.1, 57.9 at 1.2, 59.7 at 1.3, 60.9 at 1.4 (52.3 into a cache of 16 bits).
+// channels: 62.0 us at 1.1, 59.3 at 1.2, 60.4 at 1.3, 62.5 at 1.4 (52.7 into a cache of 16 bits).  No other shape was measured.
 constexpr double kHeavy = 1.2;
 // a block's 16 channels in shared memory, 80 bytes apart: eight lanes' 16-byte reads touch all banks
 constexpr int kBlockFloats = 20;
@@ -582,7 +583,7 @@ cudaError_t launch(const AppendArgs& a, cudaStream_t st) {
     auto kernel = bits4 ? (norm ? append_kernel<T, VW, NU, true, true> : append_kernel<T, VW, NU, false, true>)
                         : (norm ? append_kernel<T, VW, NU, true, false> : append_kernel<T, VW, NU, false, false>);
     // A few CTAs may come while what is before them ends.  Many may not: they would find SMs whose shared memory is divided for that
-    // other kernel, and the one wave that they are would become two (append, then read of 16384 tokens: 72 us, 80 to 91 that way).
+    // other kernel, and the one wave that they are would become two (append, then read of 16384 tokens, on an earlier form: 72 us, 80 to 91 that way).
     if (bits4 && blocks <= device_sm_count()) return launch_pdl(kernel, dim3((unsigned)blocks), dim3(32 * kAppendWarps), 0, st, a, P);
     kernel<<<(unsigned)blocks, 32 * kAppendWarps, 0, st>>>(a, P);
     return cudaGetLastError();

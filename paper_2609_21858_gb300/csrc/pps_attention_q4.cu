@@ -17,15 +17,18 @@
 // in 32 bits, and the softmax is the running one with the rescaling left out while a maximum rises by less than 2^kLazy4.
 // The warps of a CTA take the units of a segment in turn, each through a ring of its own (a unit on its way while one is in use),
 // and join at its end.
-// What bounds it: with many keys the issue of those conversions and products beside HBM (64 sequences of 2000 to 8000 keys: 80 us, 4.7
-// TB/s, 2.1 instructions a clock of 4; the first form, 32 keys at a time with codes by lanes' copies, took 98), with few the start,
-// the plan and the join's launch (one sequence of 900 keys: 9.3 us).  Three CTAs of four warps to an SM leave 168 registers.
+// What bounds it: with many keys the latency of those conversions and products in 12 warps an SM (64 sequences of 2000 to 8000 keys: 80 us, 4.7
+// TB/s, 61 percent of DRAM's time and 2.1 instructions a clock of 4; the first form, 32 keys at a time with codes by lanes' copies, took 98), with few the start,
+// the plan and the join's launch (one sequence of 900 keys: 9.6 us).  Three CTAs of four warps to an SM leave 168 registers.
+// A wait that gives up ends its CTA: its warps' copies on their way are waited for, and nothing more is written.
 //
 // Many rows (trees, chunks).  The 128-row tiles of pps_attn_tiles.cuh on the 5th-generation tensor cores: six warps copy a tile's codes
 // and scales into shared memory ahead of the products, widen them (64 conversions and as many multiplications a lane for 32 keys of
 // 128 channels) and write the halves where TMA would have put them.  Queries in bf16 become halves in a launch before it, at the same
-// power of two per row.  64 trees of 41 nodes: 220 us, of which that launch is some 8; a cache of 16 bits takes 180, as the softmax
-// has the issue slots to itself there.
+// power of two per row.  64 trees of 41 nodes: 220 us, of which that launch is some 8; a cache of 16 bits takes 180.  As there, what bounds it is
+// the softmax's latency: two warps a scheduler, each with whole rows, whose steps (wait, load, maximum, exponentials, store) stand one
+// behind the other.  The tensor cores are busy 37 percent of the time and 1.4 instructions issue a clock of 4; which part of the
+// difference the widening warps make has not been measured.
 //
 // Work split.  The line of pps_attn.cuh.
 #include <atomic>
@@ -52,7 +55,9 @@ constexpr float kLazy4 = 8.0f;    // log2 of the rise of a maximum that nothing 
 constexpr float kShift4 = 6.0f;   // log2 of a factor on all weights: 2^(8 + 6) is below fp16's largest number
 constexpr int kQBits = 14;        // a bf16 row's largest channel lies in [2^14, 2^15) as a half
 // Rows of a sequence and key head, on average, up to which the kernel of few rows takes a call (64 sequences of 1000 to 4000 keys, 32
-// over 8 heads: 8 rows 54 us against 149 on tiles, 16 rows 78 against 150, 32 rows 138 against 152, 48 rows 197 against 157).
+// over 8 heads: 8 rows 54 us against 149 on tiles, 16 rows 78 against 150, 32 rows 138 against 152, 48 rows 197 against 157).  All of these are batches
+// of one kind.  Of a batch of both kinds one gets the wrong kernel, whatever the mean says: 63 single tokens (63 us alone) with a chunk
+// of 300 (48 alone) take 183 us here, with a chunk of 2048 (139 alone) 381 on tiles; two calls take the sum.
 constexpr int kFewRows = 32;
 
 // The power of two that brings a row in bf16 whose largest finite magnitude has the bits `top` to halves.

@@ -987,7 +987,8 @@ def q4_scale_bytes(head_dim: int) -> int:
 
 
 def cache_q4(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, k_unit=None, v_unit=None, device=None) -> CacheQ4:
-    """An empty (zero) cache in 4 bits, each page laid out head by head in memory."""
+    """An empty (zero) cache in 4 bits, each page laid out head by head in memory.  (paged_attention_q4 takes heads of up to 128
+    channels; wider ones can be appended and read back.)"""
     if head_dim % 16 or not 16 <= head_dim <= 256:
         raise ValueError(f"head_dim must be a multiple of 16 up to 256, got {head_dim}")
     made = [torch.zeros(n_pages, n_kv_heads, page_size, n, dtype=torch.uint8, device=device or "cuda").transpose(1, 2)
@@ -1098,7 +1099,8 @@ def attention_q4_workspace(n_tok: int, n_heads: int, n_kv_heads: int, head_dim: 
 
 def paged_attention_q4(q, cache, pages, kv_len, q_off, mask=None, scale=None, out=None, lse=None, ws=None, status=None,
                        stream=None):
-    """pps_paged_attention_q4: paged_attention over a cache in 4 bits (CacheQ4)."""
+    """pps_paged_attention_q4: paged_attention over a cache in 4 bits (CacheQ4).  Single tokens and long chunks are faster in a call
+    each than together."""
     if stream is None and cache.__class__ is CacheQ4:
         done = (_fast or _load_fast()).paged_attention_q4(q, *cache, pages, kv_len, q_off, mask, scale, out, lse, ws, status)
         if done is not None:
@@ -1161,7 +1163,8 @@ def kv_reserve(pages, held, free_list, free_count, kv_len, n_new, page_size: int
     """pps_kv_reserve: pages for n_new [n_seq] more tokens of every sequence from the pool (free_list, its first
     free_count[0] entries), and where the tokens go.  pages [n_seq, columns], held [n_seq], free_count [1] are updated in place,
     all int32.  n_tok: how many tokens the outputs are for (as many as n_new says, or a padded batch).  Returns dict(q_off [n_seq + 1],
-    kv_len [n_seq], slot [n_tok] int64, pos [n_tok], seq [n_tok]); `out` may leave seq out."""
+    kv_len [n_seq], slot [n_tok] int64, pos [n_tok], seq [n_tok]); `out` may leave seq out.  Tensors that the call makes may lie side
+    by side in one allocation, which any of them keeps alive: clone what is to be resized, or kept without the others."""
     if stream is None and out is None:
         done = (_fast or _load_fast()).kv_reserve(pages, held, free_list, free_count, kv_len, n_new, page_size, n_tok, pos_off,
                                                   status)
